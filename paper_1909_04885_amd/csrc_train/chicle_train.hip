@@ -1,0 +1,652 @@
+// Entry points of include/chicle_train.h: checks of arguments, workspace layout, launches.
+#include <hip/hip_runtime.h>
+#include <stdarg.h>
+#include <stdio.h>
+#include <string.h>
+#include "../../include/chicle_train.h"
+#include "clip.hpp"
+#include "elements.hpp"
+#include "embedding.hpp"
+#include "layer_norm.hpp"
+#include "softmax_loss.hpp"
+
+using namespace chicle_train;
+
+namespace {
+
+constexpr int64_t CLIP_PIECE = 8192;                     // values of a tensor that a workgroup takes at a time
+
+thread_local char last_error[256] = "";
+
+int fail(int code, const char *format, ...)
+{
+    va_list args;
+    va_start(args, format);
+    vsnprintf(last_error, sizeof last_error, format, args);
+    va_end(args);
+    return code;
+}
+
+int launched(const char *what)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? CHICLE_OK : fail(CHICLE_EDEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+#define TRY(expr)                              \
+    do {                                       \
+        const int rc_ = (expr);                \
+        if (rc_ != CHICLE_OK) return rc_;      \
+    } while (0)
+
+constexpr size_t ALIGN = 256;
+
+// Hands out parts of the workspace; without one it only adds up.
+struct Carver {
+    char *base;
+    size_t used = 0;
+    explicit Carver(void *p) : base((char *)p) {}
+    template <typename T> T *take(int64_t count)
+    {
+        used = (used + ALIGN - 1) / ALIGN * ALIGN;
+        T *p = base ? (T *)(base + used) : nullptr;
+        used += sizeof(T) * (size_t)count;
+        return p;
+    }
+    size_t total() const { return used + ALIGN; }        // (the workspace itself may begin at any sixteen bytes)
+};
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+int size_of(int32_t type) { return type == CHICLE_F32 ? 4 : 2; }
+bool type_ok(int32_t type) { return type == CHICLE_F32 || type == CHICLE_BF16 || type == CHICLE_F16; }
+bool placed(const void *p, int size) { return p && (uintptr_t)p % (uintptr_t)size == 0; }
+
+int check_workspace(const void *workspace, size_t have, size_t need)
+{
+    if (have < need) return fail(CHICLE_ENOMEM, "workspace of %zu bytes where %zu are needed", have, need);
+    if (need > 0 && !placed(workspace, 16)) return fail(CHICLE_EINVAL, "workspace must be 16-byte aligned");
+    return CHICLE_OK;
+}
+
+// f(T()) with the element type
+template <typename F>
+int with_type(int32_t type, F f)
+{
+    return type == CHICLE_F32 ? f(float()) : type == CHICLE_BF16 ? f(bf16()) : f(f16());
+}
+
+int pow2_at_least(int64_t x, int most)
+{
+    int p = 1;
+    while (p < x && p < most) p <<= 1;
+    return p;
+}
+
+// ---- layer norm -----------------------------------------------------------------------------------------------------
+
+struct RowShape { int lanes, vectors, threads; };        // vectors 0: the row is not held
+
+// Threads of a row and vectors of each: up to `most_values` values to a thread.
+RowShape row_shape(int64_t d, int vec, int most_values)
+{
+    const int64_t v = ceil_div(d, vec);
+    const int most = most_values / vec;
+    RowShape s;
+    s.vectors = 1;
+    s.lanes = pow2_at_least(v, 256);
+    while ((int64_t)s.lanes * s.vectors < v && s.vectors < most) s.vectors *= 2;
+    while ((int64_t)s.lanes * s.vectors < v && s.lanes < LN_MOST_THREADS) s.lanes *= 2;
+    if ((int64_t)s.lanes * s.vectors < v) s.vectors = 0;
+    s.threads = s.lanes > 256 ? s.lanes : 256;
+    return s;
+}
+
+constexpr int LN_FORWARD_VALUES = 32, LN_GRAD_VALUES = 8;
+constexpr int LN_GRAD_GRID = 1024;
+
+int64_t layer_norm_parts(int64_t n, int64_t d, int32_t type)
+{
+    const RowShape s = row_shape(d, 16 / size_of(type), LN_GRAD_VALUES);
+    const int64_t g = ceil_div(n, s.threads / s.lanes);
+    return g < LN_GRAD_GRID ? g : LN_GRAD_GRID;
+}
+
+template <typename F>
+int with_vectors(int vectors, F f)
+{
+    switch (vectors) {
+    case 1: return f(std::integral_constant<int, 1>());
+    case 2: return f(std::integral_constant<int, 2>());
+    case 4: return f(std::integral_constant<int, 4>());
+    case 8: return f(std::integral_constant<int, 8>());
+    default: return f(std::integral_constant<int, 0>());
+    }
+}
+
+// ---- products -------------------------------------------------------------------------------------------------------
+
+typedef MmConfig<256, 256, 2, 4> MmWide;
+typedef MmConfig<128, 128, 2, 2> MmMiddle;
+typedef MmConfig<256, 64, 4, 1> MmThin;
+
+enum { WIDE, MIDDLE, THIN };
+
+int mm_tile_i(int c) { return c == MIDDLE ? 128 : 256; }
+int mm_tile_j(int c) { return c == WIDE ? 256 : c == MIDDLE ? 128 : 64; }
+
+int mm_choose(int64_t rows_i, int64_t rows_j)
+{
+    if (rows_j <= 64) return THIN;
+    return ceil_div(rows_i, 256) * ceil_div(rows_j, 256) >= 192 ? WIDE : MIDDLE;
+}
+
+template <typename F>
+int with_config(int c, F f)
+{
+    return c == WIDE ? f(MmWide()) : c == MIDDLE ? f(MmMiddle()) : f(MmThin());
+}
+
+template <typename K>
+int allow_lds(K kernel, int bytes)
+{
+    const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e == hipSuccess ? CHICLE_OK : fail(CHICLE_EDEVICE, "shared memory: %s", hipGetErrorString(e));
+}
+
+// ---- softmax loss: where everything lies ------------------------------------------------------------------------------
+
+struct LossPlan {
+    int64_t n, d, classes, ldk;          // ldk: length of laid-out rows along d
+    int planes, config;
+    bool lay_x, lay_w;
+    // gradient
+    int64_t piece, ldg, ldt, ldp;        // classes of a piece; lengths of rows along the classes, along the rows, of dx's parts
+    int pieces, splits, config_dx, config_dw;
+    void *x, *w, *xt, *wt, *g, *gt;
+    float *parts, *lse, *picked, *power;
+    float2 *tile_sums;
+    size_t bytes;
+};
+
+constexpr int64_t LOSS_PIECE_BYTES = (int64_t)1 << 30;   // G of a piece, both layouts
+constexpr int64_t LOSS_MOST = (int64_t)1 << 22;
+
+LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t n, int64_t d, int64_t classes, int32_t type, bool grad, void *workspace)
+{
+    LossPlan p = {};
+    p.bytes = ALIGN;
+    if (n == 0) return p;                                // (nothing to lay out)
+    p.n = n; p.d = d; p.classes = classes;
+    p.planes = type == CHICLE_F32 ? 3 : 1;
+    p.ldk = round_up(d, MM_K);
+    // rows that are whole slices of aligned chunks are read where they are
+    auto as_is = [&](const void *q, int64_t ld) { return p.planes == 1 && d % MM_K == 0 && ld % 8 == 0 && (uintptr_t)q % 16 == 0 && ld < LOSS_MOST; };
+    p.lay_x = !as_is(x, ldx);
+    p.lay_w = !as_is(w, ldw);
+    p.config = mm_choose(classes, n);
+    Carver c(workspace);
+    p.x = p.lay_x ? c.take<uint16_t>(n * p.ldk * p.planes) : (uint16_t *)x;
+    p.w = p.lay_w ? c.take<uint16_t>(classes * p.ldk * p.planes) : (uint16_t *)w;
+    p.tile_sums = c.take<float2>(n * ceil_div(classes, mm_tile_i(p.config)));
+    p.picked = c.take<float>(n);
+    if (grad) {
+        p.lse = c.take<float>(n);
+        p.power = c.take<float>(2);
+        p.ldt = round_up(n, MM_K);
+        const int64_t per_class = 2 * 2 * p.planes * p.ldt;
+        int64_t most = LOSS_PIECE_BYTES / per_class / 256 * 256;
+        most = most < 256 ? 256 : most;
+        p.pieces = (int)ceil_div(classes, most);
+        p.piece = round_up(ceil_div(classes, p.pieces), 256);
+        p.pieces = (int)ceil_div(classes, p.piece);
+        if (p.piece > classes) p.piece = classes;
+        p.ldg = round_up(p.piece, MM_K);
+        p.ldp = round_up(d, 4);
+        p.config_dx = mm_choose(d, n);
+        const int64_t tiles = ceil_div(d, mm_tile_i(p.config_dx)) * ceil_div(n, mm_tile_j(p.config_dx));
+        const int64_t slices = p.ldg / MM_K * (p.planes == 3 ? 6 : 1);
+        int64_t splits = tiles >= 256 ? 1 : ceil_div(512, tiles);
+        if (splits > slices / 8) splits = slices / 8;
+        p.splits = splits < 1 ? 1 : (int)splits;
+        p.config_dw = mm_choose(d, p.piece);
+        p.xt = c.take<uint16_t>(d * p.ldt * p.planes);
+        p.wt = c.take<uint16_t>(d * p.ldg * p.planes);
+        p.g = c.take<uint16_t>(n * p.ldg * p.planes);
+        p.gt = c.take<uint16_t>(p.piece * p.ldt * p.planes);
+        p.parts = c.take<float>(n * p.ldp * p.splits * p.pieces);
+    }
+    p.bytes = c.total();
+    return p;
+}
+
+int loss_check(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *labels, int32_t wide, int64_t n, int64_t d, int64_t classes,
+               int32_t type)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (n < 0 || d < 1 || classes < 1 || n >= LOSS_MOST || d >= LOSS_MOST || classes >= ((int64_t)1 << 30))
+        return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, classes %lld", (long long)n, (long long)d, (long long)classes);
+    if (ceil_div(classes, 128) * ceil_div(n, 64) > INT32_MAX / 2) return fail(CHICLE_EINVAL, "too many rows times classes");
+    if (ldx < d || ldw < d) return fail(CHICLE_EINVAL, "a row distance is shorter than a row");
+    const int s = size_of(type);
+    if (!placed(w, s) || (n > 0 && (!placed(x, s) || !placed(labels, wide ? 8 : 4)))) return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    return CHICLE_OK;
+}
+
+int64_t grid_of(int64_t items, int threads, int64_t most)
+{
+    const int64_t g = ceil_div(items, threads);
+    return g < 1 ? 1 : g < most ? g : most;
+}
+
+template <typename T>
+int loss_lay_rows(const T *in, int64_t ldi, void *out, int64_t ld, int64_t rows, int64_t cols, hipStream_t stream)
+{
+    if (rows == 0) return CHICLE_OK;
+    typedef typename Product<T>::type P;
+    lay_rows<T><<<(unsigned)grid_of(rows * (ld / 8), 256, 16384), 256, 0, stream>>>(in, ldi, (P *)out, ld, rows * ld, rows, cols);
+    return launched("lay_rows");
+}
+
+template <typename T>
+int loss_lay_columns(const T *in, int64_t ldi, void *out, int64_t ld, int64_t plane, int64_t rows, int64_t cols, const void *labels, int wide,
+                     int64_t classes, hipStream_t stream)
+{
+    typedef typename Product<T>::type P;
+    const dim3 grid((unsigned)ceil_div(cols, 64), (unsigned)(ld / 64));
+    lay_columns<T><<<grid, 256, 0, stream>>>(in, ldi, (P *)out, ld, plane, rows, cols, labels, wide, classes);
+    return launched("lay_columns");
+}
+
+MmShape mm_shape(const MmOperand &a, const MmOperand &b, int64_t k, int planes, int config, int splits)
+{
+    MmShape s;
+    s.a = a; s.b = b;
+    s.k_slices = (int)(k / MM_K);
+    s.planes = planes;
+    s.tiles_i = (int)ceil_div(a.rows, mm_tile_i(config));
+    s.tiles_j = (int)ceil_div(b.rows, mm_tile_j(config));
+    s.splits = splits;
+    return s;
+}
+
+// lse and loss of all rows
+template <typename T>
+int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw, LossRows &rows, float *loss, float *lse, int32_t *flags, hipStream_t stream)
+{
+    typedef typename Product<T>::type P;
+    if (p.lay_x) TRY(loss_lay_rows<T>(x, ldx, p.x, p.ldk, p.n, p.d, stream));
+    if (p.lay_w) TRY(loss_lay_rows<T>(w, ldw, p.w, p.ldk, p.classes, p.d, stream));
+    const MmOperand a = {p.w, p.lay_w ? p.ldk : ldw, p.classes * p.ldk, (int)p.classes}, b = {p.x, p.lay_x ? p.ldk : ldx, p.n * p.ldk, (int)p.n};
+    const MmShape s = mm_shape(a, b, p.ldk, p.planes, p.config, 1);
+    TRY(with_config(p.config, [&](auto c) {
+        typedef decltype(c) C;
+        auto kernel = loss_tiles<P, C, sizeof(T) == 4>;
+        TRY(allow_lds(kernel, C::LDS));
+        kernel<<<(unsigned)(s.tiles_i * s.tiles_j), C::THREADS, C::LDS, stream>>>(s, rows);
+        return launched("loss_tiles");
+    }));
+    loss_rows<<<(unsigned)ceil_div(p.n, 4), 256, 0, stream>>>(rows, s.tiles_i, loss, lse, flags);
+    return launched("loss_rows");
+}
+
+template <typename T>
+int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw, LossRows &rows, float *loss, T *dx, int64_t lddx, T *dw,
+                  int64_t lddw, int32_t *flags, hipStream_t stream)
+{
+    typedef typename Product<T>::type P;
+    constexpr int PLANES = Product<T>::PLANES;
+    TRY(run_loss<T>(p, x, ldx, w, ldw, rows, loss, p.lse, flags, stream));
+    rows.lse = p.lse;
+    const bool scaled = sizeof(T) == 2 && std::is_same<T, f16>::value;
+    if (scaled) {
+        loss_power<<<1, 1024, 0, stream>>>(rows.weight, (int)p.n, p.power);
+        TRY(launched("loss_power"));
+        rows.power = p.power;
+    }
+    const float *inverse = scaled ? p.power + 1 : nullptr;
+    TRY(loss_lay_columns<T>(x, ldx, p.xt, p.ldt, p.d * p.ldt, p.n, p.d, rows.labels, rows.wide, p.classes, stream));
+    const MmOperand xr = {p.x, p.lay_x ? p.ldk : ldx, p.n * p.ldk, (int)p.n}, xc = {p.xt, p.ldt, p.d * p.ldt, (int)p.d};
+    for (int k = 0; k < p.pieces; ++k) {
+        const int64_t first = k * p.piece, many = p.classes - first < p.piece ? p.classes - first : p.piece;
+        const int64_t ldg = round_up(many, MM_K), plane_g = p.n * ldg, plane_t = many * p.ldt, plane_w = p.d * ldg;
+        const MmOperand wr = {(const uint16_t *)p.w + first * (p.lay_w ? p.ldk : ldw), p.lay_w ? p.ldk : ldw, p.classes * p.ldk, (int)many};
+        TRY(loss_lay_columns<T>(w + first * ldw, ldw, p.wt, ldg, plane_w, many, p.d, nullptr, 0, 0, stream));
+        const int config_g = mm_choose(many, p.n);
+        TRY(with_config(config_g, [&](auto c) {
+            typedef decltype(c) C;
+            const MmShape s = mm_shape(wr, xr, p.ldk, p.planes, config_g, 1);
+            auto kernel = loss_grad_tiles<P, C, sizeof(T) == 4, PLANES>;
+            TRY(allow_lds(kernel, C::LDS));
+            kernel<<<(unsigned)(s.tiles_i * s.tiles_j), C::THREADS, C::LDS, stream>>>(s, rows, (int)first, (int)many, (P *)p.g, ldg, plane_g, (P *)p.gt,
+                                                                                     p.ldt, plane_t);
+            return launched("loss_grad_tiles");
+        }));
+        const MmOperand gr = {p.g, ldg, plane_g, (int)p.n}, gc = {p.gt, p.ldt, plane_t, (int)many}, wc = {p.wt, ldg, plane_w, (int)p.d};
+        TRY(with_config(p.config_dx, [&](auto c) {
+            typedef decltype(c) C;
+            const MmShape s = mm_shape(wc, gr, ldg, p.planes, p.config_dx, p.splits);
+            auto kernel = product_parts<P, C>;
+            TRY(allow_lds(kernel, C::LDS));
+            kernel<<<(unsigned)(s.tiles_i * s.tiles_j * s.splits), C::THREADS, C::LDS, stream>>>(s, p.parts + (int64_t)k * p.splits * p.n * p.ldp, p.ldp,
+                                                                                                p.n * p.ldp);
+            return launched("product_parts");
+        }));
+        TRY(with_config(p.config_dw, [&](auto c) {
+            typedef decltype(c) C;
+            const MmShape s = mm_shape(xc, gc, p.ldt, p.planes, p.config_dw, 1);
+            auto kernel = product_out<P, C, T>;
+            TRY(allow_lds(kernel, C::LDS));
+            kernel<<<(unsigned)(s.tiles_i * s.tiles_j), C::THREADS, C::LDS, stream>>>(s, dw + first * lddw, lddw, inverse);
+            return launched("product_out");
+        }));
+    }
+    sum_parts<T><<<(unsigned)grid_of(p.n * (p.ldp / 4), 256, 16384), 256, 0, stream>>>(p.parts, p.ldp, p.n * p.ldp, p.splits * p.pieces, dx, lddx, p.n,
+                                                                                      p.d, inverse);
+    return launched("sum_parts");
+}
+
+// ---- embedding gradient -----------------------------------------------------------------------------------------------
+
+constexpr int64_t EMBED_MOST_D = (1 << 23) - 1;          // blocks of columns are a grid's second dimension
+
+struct EmbedPlan {
+    int64_t pieces, tiles, seen_words;
+    int piece, lanes, bits, passes, digit;
+    unsigned *keys[2], *places[2], *count, *seen;
+    float *head, *tail;
+    size_t bytes;
+};
+
+EmbedPlan embed_plan(int64_t n, int64_t d, int64_t n_rows, void *workspace)
+{
+    EmbedPlan p = {};
+    p.piece = 32;
+    p.pieces = ceil_div(n, p.piece);
+    p.bits = 1;
+    while (((int64_t)1 << p.bits) <= n_rows) ++p.bits;   // keys are 0 .. n_rows
+    p.passes = n <= SORT_ONE ? 0 : (int)ceil_div(p.bits, SORT_BITS);
+    p.digit = p.passes ? (int)ceil_div(p.bits, p.passes) : 0;
+    p.tiles = ceil_div(n, SORT_TILE);
+    p.seen_words = ceil_div(n_rows, 32);
+    Carver c(workspace);
+    for (int k = 0; k < (p.passes ? 2 : 1); ++k) { p.keys[k] = c.take<unsigned>(n); p.places[k] = c.take<unsigned>(n); }
+    if (p.passes) p.count = c.take<unsigned>(p.tiles << p.digit);
+    p.seen = c.take<unsigned>(p.seen_words);
+    p.head = c.take<float>(p.pieces * d);
+    p.tail = c.take<float>(p.pieces * d);
+    p.bytes = c.total();
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+const char *chicle_train_last_error(void) { return last_error; }
+
+size_t chicle_softmax_loss_bytes(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t n, int64_t d, int64_t classes, int32_t type,
+                                 int32_t with_grad)
+{
+    if (!type_ok(type) || n < 0 || d < 1 || classes < 1 || n >= LOSS_MOST || d >= LOSS_MOST || classes >= ((int64_t)1 << 30)) return 0;
+    return loss_plan(x, ldx, w, ldw, n, d, classes, type, with_grad != 0, nullptr).bytes;
+}
+
+int chicle_softmax_loss(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *labels, int32_t wide, int64_t n, int64_t d,
+                        int64_t classes, int32_t type, float *loss, float *lse, void *workspace, size_t workspace_bytes, int32_t *flags,
+                        void *hip_stream)
+{
+    TRY(loss_check(x, ldx, w, ldw, labels, wide, n, d, classes, type));
+    if (n == 0) return CHICLE_OK;
+    if (!placed(loss, 4) || !placed(lse, 4)) return fail(CHICLE_EINVAL, "a null or misplaced output");
+    TRY(check_workspace(workspace, workspace_bytes, loss_plan(x, ldx, w, ldw, n, d, classes, type, false, nullptr).bytes));
+    const LossPlan p = loss_plan(x, ldx, w, ldw, n, d, classes, type, false, workspace);
+    LossRows rows = {labels, wide, (int)n, (int)classes, nullptr, nullptr, nullptr, p.tile_sums, p.picked};
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        return run_loss<T>(p, (const T *)x, ldx, (const T *)w, ldw, rows, loss, lse, flags, (hipStream_t)hip_stream);
+    });
+}
+
+int chicle_softmax_loss_grad(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *labels, int32_t wide, const float *row_weight,
+                             int64_t n, int64_t d, int64_t classes, int32_t type, float *loss, void *dx, int64_t lddx, void *dw, int64_t lddw,
+                             void *workspace, size_t workspace_bytes, int32_t *flags, void *hip_stream)
+{
+    TRY(loss_check(x, ldx, w, ldw, labels, wide, n, d, classes, type));
+    const int s = size_of(type);
+    if (lddx < d || lddw < d) return fail(CHICLE_EINVAL, "a row distance is shorter than a row");
+    if (!placed(dw, s) || (n > 0 && (!placed(dx, s) || !placed(loss, 4) || !placed(row_weight, 4)))) return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    hipStream_t stream = (hipStream_t)hip_stream;
+    if (n == 0)                                          // no row: the classes' gradient is zero
+        return with_type(type, [&](auto t) {
+            typedef decltype(t) T;
+            sum_parts<T><<<(unsigned)grid_of(classes * ceil_div(d, 4), 256, 16384), 256, 0, stream>>>(nullptr, round_up(d, 4), 0, 0, (T *)dw, lddw, classes, d,
+                                                                                                     nullptr);
+            return launched("sum_parts");
+        });
+    TRY(check_workspace(workspace, workspace_bytes, loss_plan(x, ldx, w, ldw, n, d, classes, type, true, nullptr).bytes));
+    const LossPlan p = loss_plan(x, ldx, w, ldw, n, d, classes, type, true, workspace);
+    LossRows rows = {labels, wide, (int)n, (int)classes, nullptr, row_weight, nullptr, p.tile_sums, p.picked};
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        return run_loss_grad<T>(p, (const T *)x, ldx, (const T *)w, ldw, rows, loss, (T *)dx, lddx, (T *)dw, lddw, flags, stream);
+    });
+}
+
+int chicle_embed(const void *table, int64_t ld, int64_t n_rows, const void *ids, int32_t wide, int64_t n, int64_t d, int32_t type, float scale,
+                 void *out, int64_t ldo, int32_t *flags, void *hip_stream)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (n < 0 || d < 1 || n_rows < 1 || n > INT32_MAX || n_rows > INT32_MAX || d > EMBED_MOST_D || ld < d || ldo < d)
+        return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, n_rows %lld, or a row distance", (long long)n, (long long)d, (long long)n_rows);
+    if (n == 0) return CHICLE_OK;
+    const int s = size_of(type);
+    if (!placed(table, s) || !placed(out, s) || !placed(ids, wide ? 8 : 4)) return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    const int lanes = pow2_at_least(ceil_div(d, 16 / s), EMBED_THREADS);
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        embed_rows<T><<<(unsigned)ceil_div(n, EMBED_THREADS / lanes), EMBED_THREADS, 0, (hipStream_t)hip_stream>>>(
+            (const T *)table, ld, n_rows, ids, wide, (T *)out, ldo, n, d, lanes, scale, flags);
+        return launched("embed_rows");
+    });
+}
+
+size_t chicle_embed_grad_bytes(int64_t n, int64_t d, int64_t n_rows)
+{
+    if (n < 0 || d < 1 || n_rows < 1 || n > INT32_MAX || n_rows >= INT32_MAX || d > EMBED_MOST_D) return 0;
+    return embed_plan(n, d, n_rows, nullptr).bytes;
+}
+
+int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t ldd, int64_t n, int64_t d, int64_t n_rows, int32_t type, float scale,
+                      int32_t accumulate, void *dtable, int64_t ldo, void *workspace, size_t workspace_bytes, int32_t *flags, void *hip_stream)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (n < 0 || d < 1 || n_rows < 1 || n > INT32_MAX || n_rows >= INT32_MAX || d > EMBED_MOST_D || ldd < d || ldo < d)
+        return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, n_rows %lld, or a row distance", (long long)n, (long long)d, (long long)n_rows);
+    const int s = size_of(type);
+    if (!placed(dtable, s) || (n > 0 && (!placed(dout, s) || !placed(ids, wide ? 8 : 4)))) return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    hipStream_t stream = (hipStream_t)hip_stream;
+    if (n == 0 && accumulate) return CHICLE_OK;
+    if (n == 0)
+        return with_type(type, [&](auto t) {
+            typedef decltype(t) T;
+            sum_parts<T><<<(unsigned)grid_of(n_rows * ceil_div(d, 4), 256, 16384), 256, 0, stream>>>(nullptr, round_up(d, 4), 0, 0, (T *)dtable, ldo, n_rows, d,
+                                                                                                    nullptr);
+            return launched("sum_parts");
+        });
+    TRY(check_workspace(workspace, workspace_bytes, embed_plan(n, d, n_rows, nullptr).bytes));
+    const EmbedPlan p = embed_plan(n, d, n_rows, workspace);
+    unsigned *seen = accumulate ? nullptr : p.seen;
+    int last = 0;
+    if (!p.passes) {
+        sort_tokens_one<<<1, 1024, 0, stream>>>(ids, wide, (int)n, n_rows, p.keys[0], p.places[0], seen, p.seen_words, flags);
+        TRY(launched("sort_tokens_one"));
+    } else
+        for (int k = 0; k < p.passes; ++k) {
+            SortPass q = {ids, p.keys[(k + 1) & 1], p.places[(k + 1) & 1], p.keys[k & 1], p.places[k & 1], p.count, seen, n, n_rows, p.seen_words,
+                          wide, k * p.digit, 1 << p.digit, (int)p.tiles, k == 0, k == p.passes - 1, flags};
+            sort_count<<<(unsigned)p.tiles, SORT_THREADS, 0, stream>>>(q);
+            TRY(launched("sort_count"));
+            sort_offsets<<<1, 1024, 0, stream>>>(p.count, p.tiles << p.digit);
+            TRY(launched("sort_offsets"));
+            sort_scatter<<<(unsigned)p.tiles, SORT_THREADS, 0, stream>>>(q, p.digit);
+            TRY(launched("sort_scatter"));
+            last = k & 1;
+        }
+    const int vec = 16 / s;
+    EmbedGrad g;
+    g.keys = p.keys[last]; g.places = p.places[last]; g.seen = seen;
+    g.head = p.head; g.tail = p.tail;
+    g.n = n; g.d = d; g.n_rows = n_rows; g.ldo = ldo; g.ldd = ldd;
+    g.piece = p.piece;
+    g.lanes = pow2_at_least(ceil_div(d, vec), EMBED_THREADS);
+    g.run_blocks = (int)ceil_div(p.pieces, EMBED_THREADS / g.lanes);
+    g.scale = scale;
+    const int64_t zero_blocks = accumulate ? 0 : p.seen_words < 2048 ? p.seen_words : 2048;
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        embed_grad_runs<T><<<dim3((unsigned)(g.run_blocks + zero_blocks), (unsigned)ceil_div(d, (int64_t)g.lanes * vec)), EMBED_THREADS, 0, stream>>>(
+            g, (const T *)dout, (T *)dtable);
+        TRY(launched("embed_grad_runs"));
+        if (p.pieces > 1) {
+            embed_grad_join<T><<<dim3((unsigned)(p.pieces - 1), (unsigned)ceil_div(d, 64 * vec)), 64 * JOIN_WAVES, 0, stream>>>(g, (T *)dtable);
+            TRY(launched("embed_grad_join"));
+        }
+        return (int)CHICLE_OK;
+    });
+}
+
+int chicle_layer_norm(const void *x, int64_t ldx, const void *gamma, const void *beta, int64_t n, int64_t d, int32_t type, float eps,
+                      void *y, int64_t ldy, float *mean, float *rstd, void *hip_stream)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (n < 0 || d < 1 || n > INT32_MAX || d > INT32_MAX || ldx < d || ldy < d || !(eps >= 0.f))
+        return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, a row distance or eps", (long long)n, (long long)d);
+    if (n == 0) return CHICLE_OK;
+    const int s = size_of(type);
+    if (!placed(x, s) || !placed(y, s) || !placed(gamma, s) || !placed(beta, s) || !placed(mean, 4) || !placed(rstd, 4))
+        return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    const RowShape r = row_shape(d, 16 / s, LN_FORWARD_VALUES);
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        return with_vectors(r.vectors, [&](auto v) {
+            constexpr int NV = decltype(v)::value;
+            if constexpr (NV * Elem<T>::VEC <= LN_FORWARD_VALUES) {
+                auto kernel = r.threads > 256 ? layer_norm_rows<T, NV, LN_MOST_THREADS> : layer_norm_rows<T, NV, 256>;
+                kernel<<<(unsigned)ceil_div(n, r.threads / r.lanes), r.threads, 0, (hipStream_t)hip_stream>>>(
+                    (const T *)x, ldx, (const T *)gamma, (const T *)beta, (T *)y, ldy, mean, rstd, n, d, r.lanes, eps);
+            }
+            return launched("layer_norm_rows");
+        });
+    });
+}
+
+size_t chicle_layer_norm_grad_bytes(int64_t n, int64_t d, int32_t type)
+{
+    if (!type_ok(type) || n < 0 || d < 1 || n > INT32_MAX || d > INT32_MAX) return 0;
+    Carver c(nullptr);
+    c.take<float>(layer_norm_parts(n, d, type) * 2 * d);
+    return c.total();
+}
+
+int chicle_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *gamma, const float *mean, const float *rstd,
+                           int64_t n, int64_t d, int32_t type, void *dx, int64_t lddx, void *dgamma, void *dbeta, void *workspace,
+                           size_t workspace_bytes, void *hip_stream)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (n < 0 || d < 1 || n > INT32_MAX || d > INT32_MAX || ldx < d || lddy < d || lddx < d)
+        return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, or a row distance", (long long)n, (long long)d);
+    const int s = size_of(type);
+    if (!placed(gamma, s) || !placed(dgamma, s) || !placed(dbeta, s) ||
+        (n > 0 && (!placed(dy, s) || !placed(x, s) || !placed(dx, s) || !placed(mean, 4) || !placed(rstd, 4))))
+        return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    const int64_t parts = layer_norm_parts(n, d, type);
+    TRY(check_workspace(workspace, workspace_bytes, chicle_layer_norm_grad_bytes(n, d, type)));
+    Carver c(workspace);
+    float *part = c.take<float>(parts * 2 * d);
+    const RowShape r = row_shape(d, 16 / s, LN_GRAD_VALUES);
+    hipStream_t stream = (hipStream_t)hip_stream;
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        if (parts > 0)
+            TRY(with_vectors(r.vectors, [&](auto v) {
+                constexpr int NV = decltype(v)::value;
+                if constexpr (NV * Elem<T>::VEC <= LN_GRAD_VALUES) {
+                    auto kernel = r.threads > 256 ? layer_norm_grad_rows<T, NV, LN_MOST_THREADS> : layer_norm_grad_rows<T, NV, 256>;
+                    kernel<<<(unsigned)parts, r.threads, (size_t)r.threads * Elem<T>::VEC * sizeof(float), stream>>>(
+                        (const T *)dy, lddy, (const T *)x, ldx, (const T *)gamma, mean, rstd, (T *)dx, lddx, part, n, d, r.lanes);
+                }
+                return launched("layer_norm_grad_rows");
+            }));
+        layer_norm_grad_sums<T><<<(unsigned)ceil_div(2 * d, 64), 1024, 0, stream>>>(part, (int)parts, d, (T *)dgamma, (T *)dbeta);
+        return launched("layer_norm_grad_sums");
+    });
+}
+
+size_t chicle_clip_grads_bytes(int32_t count)
+{
+    (void)count;
+    Carver c(nullptr);
+    c.take<double>(CLIP_MOST_PARTS);
+    return c.total();
+}
+
+int chicle_clip_grads(const void *const *in, void *const *out, const int64_t *sizes, const int32_t *types, int32_t count, float max_norm,
+                      float *norm, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (count < 0 || count > 100000 || (count > 0 && (!in || !sizes || !types))) return fail(CHICLE_EINVAL, "no tensors, or too many");
+    if (!placed(norm, 4)) return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    if (out && !(max_norm >= 0.f)) return fail(CHICLE_EINVAL, "max_norm must not be negative");
+    int many[3] = {0, 0, 0};
+    int64_t pieces_all = 0;
+    for (int k = 0; k < count; ++k) {
+        if (!type_ok(types[k]) || sizes[k] < 0) return fail(CHICLE_EINVAL, "tensor %d: unknown type or negative size", k);
+        const int s = size_of(types[k]);
+        if (sizes[k] > 0 && (!placed(in[k], s) || (out && !placed(out[k], s)))) return fail(CHICLE_EINVAL, "tensor %d: a null or misplaced pointer", k);
+        if (sizes[k] > 0) ++many[types[k]];
+        pieces_all += ceil_div(sizes[k], CLIP_PIECE);
+    }
+    if (pieces_all > INT32_MAX / 2) return fail(CHICLE_EINVAL, "too many values");
+    TRY(check_workspace(workspace, workspace_bytes, chicle_clip_grads_bytes(count)));
+    Carver c(workspace);
+    double *part = c.take<double>(CLIP_MOST_PARTS);
+    hipStream_t stream = (hipStream_t)hip_stream;
+    const int64_t launches = ceil_div(many[0], CLIP_TENSORS) + ceil_div(many[1], CLIP_TENSORS) + ceil_div(many[2], CLIP_TENSORS);
+    const int most = launches ? (int)(CLIP_MOST_PARTS / launches) : 0;
+    int parts = 0;
+    for (int scale = 0; scale < (out ? 2 : 1); ++scale) {
+        int first = 0;
+        for (int type = 0; type < 3; ++type)
+            for (int k = 0; k < count;) {
+                ClipTable t;
+                t.tensors = 0;
+                t.first_piece[0] = 0;
+                t.first_part = first;
+                for (; k < count && t.tensors < CLIP_TENSORS; ++k) {
+                    if (types[k] != type || sizes[k] == 0) continue;
+                    t.in[t.tensors] = in[k];
+                    t.out[t.tensors] = out ? out[k] : nullptr;
+                    t.count[t.tensors] = sizes[k];
+                    t.first_piece[t.tensors + 1] = t.first_piece[t.tensors] + (int32_t)ceil_div(sizes[k], CLIP_PIECE);
+                    ++t.tensors;
+                }
+                if (!t.tensors) continue;
+                const int pieces = t.first_piece[t.tensors], grid = pieces < most ? pieces : most;
+                first += grid;
+                TRY(with_type(type, [&](auto e) {
+                    typedef decltype(e) T;
+                    if (scale) clip_scale<T><<<grid, CLIP_THREADS, 0, stream>>>(t, CLIP_PIECE, part, parts, max_norm, norm);
+                    else squares<T><<<grid, CLIP_THREADS, 0, stream>>>(t, CLIP_PIECE, part);
+                    return launched("clip");
+                }));
+            }
+        if (!scale) parts = first;
+    }
+    if (!out || parts == 0) {
+        norm_only<<<1, CLIP_THREADS, 0, stream>>>(part, parts, norm);
+        return launched("norm_only");
+    }
+    return CHICLE_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,339 @@
+// Softmax cross entropy over many classes and its gradients, without keeping the logits.
+//
+//   z_iv = x_i . w_v,  lse_i = log sum_v exp z_iv,  loss_i = lse_i - z_i,label(i)
+//   G_iv = weight_i (exp(z_iv - lse_i) - [v = label(i)]),  dx_i = sum_v G_iv w_v,  dw_v = sum_i G_iv x_i
+//   A row whose label is negative has the loss 0 and G = 0; its x counts nowhere, whatever it holds.
+//
+// The logits exist only as tiles of a product in registers.  `loss_tiles` leaves of a tile, for every row, the largest logit and the
+// sum of exponentials below it, and `loss_rows` joins these.  The gradient forms the logits again, a piece of the classes at a
+// time, and turns them in registers into G, which is stored in 16 bits, once by rows and once by classes, since both products
+// that read it want it along their summed index; rounding G is of the size of the rounding of 16-bit gradients, and 32-bit
+// operands keep G in three planes, which is exact.  Half precision would lose small G: there G comes times the power of two
+// that takes the largest weight to between 2^13 and 2^14, and the products times its inverse.
+//
+// The bound is the matrix cores: 2 n d classes operations for the loss, and three times that again for the gradients, one third of
+// it for the logits that were not kept.  Few rows are bound by reading w.
+#pragma once
+#include "matmul16.hpp"
+
+namespace chicle_train {
+
+// ---- operands laid out for the products -----------------------------------------------------------------------------
+
+__device__ __forceinline__ void split_planes(float x, bf16 *p)
+{
+    const unsigned b = __float_as_uint(x);
+    const float lead = __uint_as_float(b & 0xffff0000u);
+    float rest = x - lead;
+    if ((b & 0x7f800000u) == 0x7f800000u) rest = 0.f;   // infinities and NaN are their leading plane
+    if (x != x) { p[0] = (bf16)x; p[1] = p[2] = (bf16)0.f; return; }
+    const float mid = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+    p[0] = (bf16)lead;
+    p[1] = (bf16)mid;
+    p[2] = (bf16)(rest - mid);
+}
+
+template <typename T> struct Product { typedef T type; static constexpr int PLANES = 1; };
+template <> struct Product<float> { typedef bf16 type; static constexpr int PLANES = 3; };
+
+template <typename T, typename P>
+__device__ __forceinline__ void to_planes(T x, P *p)
+{
+    if constexpr (sizeof(T) == 4) split_planes(x, p);
+    else p[0] = x;
+}
+
+// out[plane][r][c] = in[r][c], zeros in columns [cols, ld): rows of whole slices, sixteen-byte aligned.
+template <typename T>
+__global__ __launch_bounds__(256) void lay_rows(const T *__restrict__ in, int64_t ldi, typename Product<T>::type *__restrict__ out, int64_t ld,
+                                                int64_t plane, int64_t rows, int64_t cols)
+{
+    typedef typename Product<T>::type P;
+    constexpr int N = Product<T>::PLANES;
+    const int64_t per_row = ld / 8;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < rows * per_row; e += (int64_t)gridDim.x * 256) {
+        const int64_t r = e / per_row, c = (e - r * per_row) * 8;
+        P p[N][8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            P q[N];
+            to_planes(c + k < cols ? in[r * ldi + c + k] : (T)0.f, q);
+#pragma unroll
+            for (int i = 0; i < N; ++i) p[i][k] = q[i];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) __builtin_memcpy(out + i * plane + r * ld + c, p[i], 16);
+    }
+}
+
+// out[plane][c][r] = in[r][c] for rows of `in` that count, zeros for the others and in columns [rows, ld).  64 x 64 values to a
+// workgroup; grid: (tiles of c, tiles of r).  labels may be null: every row counts.
+template <typename T>
+__global__ __launch_bounds__(256) void lay_columns(const T *__restrict__ in, int64_t ldi, typename Product<T>::type *__restrict__ out, int64_t ld,
+                                                   int64_t plane, int64_t rows, int64_t cols, const void *labels, int wide, int64_t classes)
+{
+    typedef typename Product<T>::type P;
+    constexpr int N = Product<T>::PLANES;
+    __shared__ T s[64][64 + 4 / sizeof(T) * 1];
+    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
+    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
+        const int64_t r = r0 + e / 64, c = c0 + e % 64;
+        bool has = r < rows && c < cols;
+        if (has && labels) {
+            const int64_t label = index_at(labels, wide, r);
+            has = label >= 0 && label < classes;
+        }
+        s[e / 64][e % 64] = has ? in[r * ldi + c] : (T)0.f;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < 64 * 8; e += 256) {
+        const int64_t c = c0 + e / 8, r = r0 + e % 8 * 8;
+        if (c >= cols || r >= ld) continue;
+        P p[N][8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            P q[N];
+            to_planes(s[e % 8 * 8 + k][e / 8], q);
+#pragma unroll
+            for (int i = 0; i < N; ++i) p[i][k] = q[i];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) __builtin_memcpy(out + i * plane + c * ld + r, p[i], 16);
+    }
+}
+
+// ---- the loss -------------------------------------------------------------------------------------------------------
+
+struct LossRows {
+    const void *labels;
+    int wide, n, classes;
+    const float *lse;            // gradient
+    const float *weight;
+    const float *power;          // half precision: G comes times this; else null
+    float2 *part;                // [row][tile of classes]: largest logit, sum of exponentials below it
+    float *picked;               // [row]: the label's logit
+};
+
+// The row's class, or -1
+__device__ __forceinline__ int label_at(const LossRows &l, int j)
+{
+    const int64_t label = j < l.n ? index_at(l.labels, l.wide, j) : -1;
+    return label >= 0 && label < l.classes ? (int)label : -1;
+}
+
+constexpr float MINUS_INF = -__builtin_inff();
+
+// exp(a - b), 0 where a is minus infinity
+template <bool EXACT> __device__ __forceinline__ float exp_diff(float a, float b)
+{
+    const float x = a - b;
+    return a == MINUS_INF ? 0.f : EXACT ? expf(x) : __expf(x);
+}
+
+// i: classes, j: rows
+template <typename T, typename C, bool EXACT>
+__global__ __launch_bounds__(C::THREADS) void loss_tiles(MmShape s, LossRows l)
+{
+    extern __shared__ __align__(16) char lds[];
+    const MmTile t = mm_tile(s);
+    f32x4 acc[C::MI][C::NJ];
+    mm_multiply<T, C>(s, t, lds, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J;
+    const int i0 = t.i * C::TILE_I + wi * C::MI * 16 + 4 * (lane >> 4), j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
+    __syncthreads();
+    float2 *s_part = (float2 *)lds;                      // [wave_i][row of the tile]
+#pragma unroll
+    for (int nj = 0; nj < C::NJ; ++nj) {
+        const int j = j0 + nj * 16;
+        const int label = label_at(l, j);
+        float m = MINUS_INF;
+#pragma unroll
+        for (int mi = 0; mi < C::MI; ++mi)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = i0 + mi * 16 + r;
+                if (i >= l.classes) acc[mi][nj][r] = MINUS_INF;
+                else if (i == label) l.picked[j] = acc[mi][nj][r];
+                m = fmaxf(m, acc[mi][nj][r]);
+            }
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        float e = 0.f;
+#pragma unroll
+        for (int mi = 0; mi < C::MI; ++mi)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) e += exp_diff<EXACT>(acc[mi][nj][r], m);
+        e += __shfl_xor(e, 16);
+        e += __shfl_xor(e, 32);
+        if (lane < 16) s_part[wi * C::TILE_J + wj * C::NJ * 16 + nj * 16 + lane] = make_float2(m, e);
+    }
+    __syncthreads();
+    for (int q = threadIdx.x; q < C::TILE_J; q += C::THREADS) {
+        const int j = t.j * C::TILE_J + q;
+        if (j >= l.n) continue;
+        float2 x = s_part[q];
+        for (int w = 1; w < C::W_I; ++w) {
+            const float2 y = s_part[w * C::TILE_J + q];
+            const float m = fmaxf(x.x, y.x);
+            x = make_float2(m, x.y * exp_diff<EXACT>(x.x, m) + y.y * exp_diff<EXACT>(y.x, m));
+        }
+        l.part[(int64_t)j * s.tiles_i + t.i] = x;
+    }
+}
+
+// A wavefront to a row.
+__global__ __launch_bounds__(256) void loss_rows(LossRows l, int tiles, float *__restrict__ loss, float *__restrict__ lse_out, int *flags)
+{
+    const int j = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (j >= l.n) return;
+    const float2 *p = l.part + (int64_t)j * tiles;
+    float m = MINUS_INF;
+    for (int i = lane; i < tiles; i += 64) m = fmaxf(m, p[i].x);
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    float e = 0.f;
+    for (int i = lane; i < tiles; i += 64) e += p[i].y * exp_diff<true>(p[i].x, m);
+    e = lanes_sum(e, 64);
+    if (lane) return;
+    const float lse = m + logf(e);
+    const int64_t label = index_at(l.labels, l.wide, j);
+    if (label >= l.classes && flags) atomicOr(flags, FLAG_LABEL_RANGE);
+    lse_out[j] = lse;
+    loss[j] = label >= 0 && label < l.classes ? lse - l.picked[j] : 0.f;
+}
+
+// power[0]: the power of two that takes the largest weight to [2^13, 2^14), power[1] its inverse.  One workgroup.
+__global__ __launch_bounds__(1024) void loss_power(const float *__restrict__ weight, int n, float *power)
+{
+    __shared__ float s[16];
+    float m = 0.f;
+    for (int i = threadIdx.x; i < n; i += 1024) {
+        const float w = fabsf(weight[i]);
+        if (w <= 3.4e38f) m = fmaxf(m, w);               // (no infinities or NaN)
+    }
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
+    int e = 0;
+    frexpf(m, &e);                                       // m in [2^(e-1), 2^e)
+    e = m > 0.f ? max(-100, min(100, 14 - e)) : 0;
+    power[0] = ldexpf(1.f, e);
+    power[1] = ldexpf(1.f, -e);
+}
+
+// ---- the gradients --------------------------------------------------------------------------------------------------
+
+// G of a piece of the classes: s.a is the piece's rows of w, `first` the piece's first class.  g[plane][row][class of the piece], ldg;
+// gt[plane][class of the piece][row], ldt; both are written to their tiles' ends as far as they have room, zeros outside.
+template <typename T, typename C, bool EXACT, int PLANES>
+__global__ __launch_bounds__(C::THREADS) void loss_grad_tiles(MmShape s, LossRows l, int first, int piece, T *__restrict__ g, int64_t ldg, int64_t plane_g,
+                                                              T *__restrict__ gt, int64_t ldt, int64_t plane_t)
+{
+    extern __shared__ __align__(16) char lds[];
+    const MmTile t = mm_tile(s);
+    f32x4 acc[C::MI][C::NJ];
+    mm_multiply<T, C>(s, t, lds, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J;
+    const int i0 = t.i * C::TILE_I + wi * C::MI * 16 + 4 * (lane >> 4), j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
+    const float power = l.power ? l.power[0] : 1.f;
+#pragma unroll
+    for (int nj = 0; nj < C::NJ; ++nj) {
+        const int j = j0 + nj * 16;
+        const int label = label_at(l, j);
+        const float weight = label >= 0 ? l.weight[j] * power : 0.f, lse = label >= 0 ? l.lse[j] : 0.f;
+#pragma unroll
+        for (int mi = 0; mi < C::MI; ++mi) {
+            T v[PLANES][4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = i0 + mi * 16 + r;
+                float p = EXACT ? expf(acc[mi][nj][r] - lse) : __expf(acc[mi][nj][r] - lse);
+                if (first + i == label) p -= 1.f;
+                p = weight != 0.f && i < piece ? p * weight : 0.f;
+                T q[PLANES];
+                if constexpr (PLANES == 3) split_planes(p, q);
+                else q[0] = (T)p;
+#pragma unroll
+                for (int k = 0; k < PLANES; ++k) v[k][r] = q[k];
+            }
+            const int i = i0 + mi * 16;
+#pragma unroll
+            for (int k = 0; k < PLANES; ++k) {
+                if (j < l.n && i < ldg) __builtin_memcpy(g + k * plane_g + (int64_t)j * ldg + i, v[k], 8);
+                if (j < ldt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (i + r < piece) gt[k * plane_t + (int64_t)(i + r) * ldt + j] = v[k][r];
+            }
+        }
+    }
+}
+
+// A product as it is: out[j][i] in 32 bits, split `split` of the sum in its own copy of `out`.
+template <typename T, typename C>
+__global__ __launch_bounds__(C::THREADS) void product_parts(MmShape s, float *__restrict__ out, int64_t ld, int64_t copy)
+{
+    extern __shared__ __align__(16) char lds[];
+    const MmTile t = mm_tile(s);
+    f32x4 acc[C::MI][C::NJ];
+    mm_multiply<T, C>(s, t, lds, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J;
+    const int i0 = t.i * C::TILE_I + wi * C::MI * 16 + 4 * (lane >> 4), j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
+    out += t.split * copy;
+#pragma unroll
+    for (int nj = 0; nj < C::NJ; ++nj)
+#pragma unroll
+        for (int mi = 0; mi < C::MI; ++mi) {
+            const int i = i0 + mi * 16, j = j0 + nj * 16;
+            if (j < s.b.rows && i < s.a.rows) __builtin_memcpy(out + (int64_t)j * ld + i, &acc[mi][nj], 16);
+        }
+}
+
+// ... and as the result itself: out[j][i] = scale * sum, rounded.
+template <typename T, typename C, typename O>
+__global__ __launch_bounds__(C::THREADS) void product_out(MmShape s, O *__restrict__ out, int64_t ld, const float *__restrict__ scale)
+{
+    extern __shared__ __align__(16) char lds[];
+    const MmTile t = mm_tile(s);
+    f32x4 acc[C::MI][C::NJ];
+    mm_multiply<T, C>(s, t, lds, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J;
+    const int i0 = t.i * C::TILE_I + wi * C::MI * 16 + 4 * (lane >> 4), j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
+    const float f = scale ? *scale : 1.f;
+#pragma unroll
+    for (int nj = 0; nj < C::NJ; ++nj)
+#pragma unroll
+        for (int mi = 0; mi < C::MI; ++mi) {
+            const int i = i0 + mi * 16, j = j0 + nj * 16;
+            if (j >= s.b.rows) continue;
+            O v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = (O)(acc[mi][nj][r] * f);
+            O *dst = out + (int64_t)j * ld + i;
+            if (i + 4 <= s.a.rows) __builtin_memcpy(dst, v, sizeof v);
+            else
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (i + r < s.a.rows) dst[r] = v[r];
+        }
+}
+
+// dx = scale * the sum of the copies, in their order.  ld of a copy is a multiple of four.
+template <typename O>
+__global__ __launch_bounds__(256) void sum_parts(const float *__restrict__ part, int64_t ld, int64_t copy, int copies, O *__restrict__ out, int64_t ldo,
+                                                 int64_t rows, int64_t cols, const float *__restrict__ scale)
+{
+    const int64_t per_row = ld / 4;
+    const float f = scale ? *scale : 1.f;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < rows * per_row; e += (int64_t)gridDim.x * 256) {
+        const int64_t r = e / per_row, c = (e - r * per_row) * 4;
+        f32x4 t = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < copies; ++k) t += *(const f32x4 *)(part + k * copy + r * ld + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < cols) out[r * ldo + c + i] = (O)(t[i] * f);
+    }
+}
+
+}  // namespace chicle_train
