@@ -15,6 +15,7 @@ using namespace chicle_train;
 namespace {
 
 constexpr int64_t CLIP_PIECE = 8192;                     // values of a tensor that a workgroup takes at a time
+constexpr int64_t CLIP_FEW_PIECES = 4096;                // up to here the norm costs the scaling workgroups less than a launch
 
 thread_local char last_error[256] = "";
 
@@ -351,9 +352,10 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
 constexpr int64_t EMBED_MOST_D = (1 << 23) - 1;          // blocks of columns are a grid's second dimension
 
 struct EmbedPlan {
-    int64_t pieces, tiles, seen_words;
-    int piece, lanes, bits, passes, digit;
-    unsigned *keys[2], *places[2], *count, *seen;
+    int64_t pieces, tile, ldp, seen_bytes;
+    int tiles, passes, digit;
+    unsigned *keys[2], *places[2], *count;
+    uint8_t *seen;
     float *head, *tail;
     size_t bytes;
 };
@@ -361,20 +363,21 @@ struct EmbedPlan {
 EmbedPlan embed_plan(int64_t n, int64_t d, int64_t n_rows, void *workspace)
 {
     EmbedPlan p = {};
-    p.piece = 32;
-    p.pieces = ceil_div(n, p.piece);
-    p.bits = 1;
-    while (((int64_t)1 << p.bits) <= n_rows) ++p.bits;   // keys are 0 .. n_rows
-    p.passes = n <= SORT_ONE ? 0 : (int)ceil_div(p.bits, SORT_BITS);
-    p.digit = p.passes ? (int)ceil_div(p.bits, p.passes) : 0;
-    p.tiles = ceil_div(n, SORT_TILE);
-    p.seen_words = ceil_div(n_rows, 32);
+    p.pieces = ceil_div(n, EMBED_PIECE);
+    p.ldp = round_up(d, 8);
+    int bits = 1;
+    while (((int64_t)1 << bits) <= n_rows) ++bits;       // keys are 0 .. n_rows
+    p.passes = n <= SORT_ONE ? 0 : (int)ceil_div(bits, SORT_BITS);
+    p.digit = p.passes ? (int)ceil_div(bits, p.passes) : 0;
+    p.tile = round_up(ceil_div(n, SORT_MOST_TILES), SORT_LEAST_TILE);
+    p.tiles = n ? (int)ceil_div(n, p.tile) : 0;
     Carver c(workspace);
     for (int k = 0; k < (p.passes ? 2 : 1); ++k) { p.keys[k] = c.take<unsigned>(n); p.places[k] = c.take<unsigned>(n); }
-    if (p.passes) p.count = c.take<unsigned>(p.tiles << p.digit);
-    p.seen = c.take<unsigned>(p.seen_words);
-    p.head = c.take<float>(p.pieces * d);
-    p.tail = c.take<float>(p.pieces * d);
+    if (p.passes) p.count = c.take<unsigned>((int64_t)p.tiles << p.digit);
+    p.seen_bytes = round_up(n_rows, 16);
+    p.seen = c.take<uint8_t>(p.seen_bytes);
+    p.head = c.take<float>(p.pieces * p.ldp);
+    p.tail = c.take<float>(p.pieces * p.ldp);
     p.bytes = c.total();
     return p;
 }
@@ -476,40 +479,42 @@ int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t l
         });
     TRY(check_workspace(workspace, workspace_bytes, embed_plan(n, d, n_rows, nullptr).bytes));
     const EmbedPlan p = embed_plan(n, d, n_rows, workspace);
-    unsigned *seen = accumulate ? nullptr : p.seen;
+    uint8_t *seen = accumulate ? nullptr : p.seen;
     int last = 0;
     if (!p.passes) {
-        sort_tokens_one<<<1, 1024, 0, stream>>>(ids, wide, (int)n, n_rows, p.keys[0], p.places[0], seen, p.seen_words, flags);
+        sort_tokens_one<<<1, 1024, 0, stream>>>(ids, wide, (int)n, n_rows, p.keys[0], p.places[0], seen, p.seen_bytes, flags);
         TRY(launched("sort_tokens_one"));
     } else
         for (int k = 0; k < p.passes; ++k) {
-            SortPass q = {ids, p.keys[(k + 1) & 1], p.places[(k + 1) & 1], p.keys[k & 1], p.places[k & 1], p.count, seen, n, n_rows, p.seen_words,
-                          wide, k * p.digit, 1 << p.digit, (int)p.tiles, k == 0, k == p.passes - 1, flags};
+            const SortPass q = {ids, p.keys[(k + 1) & 1], p.places[(k + 1) & 1], p.keys[k & 1], p.places[k & 1], p.count, n, n_rows, p.tile,
+                                wide, k * p.digit, p.digit, p.tiles, k == 0, flags, seen, p.seen_bytes};
             sort_count<<<(unsigned)p.tiles, SORT_THREADS, 0, stream>>>(q);
             TRY(launched("sort_count"));
-            sort_offsets<<<1, 1024, 0, stream>>>(p.count, p.tiles << p.digit);
-            TRY(launched("sort_offsets"));
-            sort_scatter<<<(unsigned)p.tiles, SORT_THREADS, 0, stream>>>(q, p.digit);
+            sort_scatter<<<(unsigned)p.tiles, SORT_THREADS, 0, stream>>>(q);
             TRY(launched("sort_scatter"));
             last = k & 1;
         }
     const int vec = 16 / s;
     EmbedGrad g;
-    g.keys = p.keys[last]; g.places = p.places[last]; g.seen = seen;
+    g.keys = p.keys[last]; g.places = p.places[last];
     g.head = p.head; g.tail = p.tail;
-    g.n = n; g.d = d; g.n_rows = n_rows; g.ldo = ldo; g.ldd = ldd;
-    g.piece = p.piece;
+    g.n = n; g.d = d; g.n_rows = n_rows; g.ldo = ldo; g.ldd = ldd; g.ldp = p.ldp;
     g.lanes = pow2_at_least(ceil_div(d, vec), EMBED_THREADS);
-    g.run_blocks = (int)ceil_div(p.pieces, EMBED_THREADS / g.lanes);
+    const int groups = EMBED_THREADS / g.lanes;
+    g.run_blocks = (int)ceil_div(p.pieces, groups);
+    g.zero_rows = (int)(d * s >= ZERO_BYTES ? 1 : ZERO_BYTES / (d * s));
+    g.zero_blocks = accumulate ? 0 : (int)ceil_div(n_rows, g.zero_rows);
+    g.seen = seen;
+    g.accumulate = accumulate;
     g.scale = scale;
-    const int64_t zero_blocks = accumulate ? 0 : p.seen_words < 2048 ? p.seen_words : 2048;
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        embed_grad_runs<T><<<dim3((unsigned)(g.run_blocks + zero_blocks), (unsigned)ceil_div(d, (int64_t)g.lanes * vec)), EMBED_THREADS, 0, stream>>>(
-            g, (const T *)dout, (T *)dtable);
+        const dim3 grid((unsigned)(g.run_blocks + g.zero_blocks), (unsigned)ceil_div(d, (int64_t)g.lanes * vec));
+        embed_grad_runs<T><<<grid, EMBED_THREADS, groups * EMBED_PIECE * sizeof(uint2), stream>>>(g, (const T *)dout, (T *)dtable);
         TRY(launched("embed_grad_runs"));
         if (p.pieces > 1) {
-            embed_grad_join<T><<<dim3((unsigned)(p.pieces - 1), (unsigned)ceil_div(d, 64 * vec)), 64 * JOIN_WAVES, 0, stream>>>(g, (T *)dtable);
+            const dim3 join((unsigned)ceil_div(p.pieces - 1, JOIN_PIECES), (unsigned)ceil_div(d, JOIN_COLUMNS));
+            embed_grad_join<T><<<join, 64 * JOIN_WAVES, 0, stream>>>(g, (T *)dtable);
             TRY(launched("embed_grad_join"));
         }
         return (int)CHICLE_OK;
@@ -578,7 +583,7 @@ int chicle_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t 
                 }
                 return launched("layer_norm_grad_rows");
             }));
-        layer_norm_grad_sums<T><<<(unsigned)ceil_div(2 * d, 64), 1024, 0, stream>>>(part, (int)parts, d, (T *)dgamma, (T *)dbeta);
+        layer_norm_grad_sums<T><<<(unsigned)ceil_div(2 * d, LN_SUM_COLUMNS), 1024, 0, stream>>>(part, (int)parts, d, (T *)dgamma, (T *)dbeta);
         return launched("layer_norm_grad_sums");
     });
 }
@@ -614,6 +619,7 @@ int chicle_clip_grads(const void *const *in, void *const *out, const int64_t *si
     const int64_t launches = ceil_div(many[0], CLIP_TENSORS) + ceil_div(many[1], CLIP_TENSORS) + ceil_div(many[2], CLIP_TENSORS);
     const int most = launches ? (int)(CLIP_MOST_PARTS / launches) : 0;
     int parts = 0;
+    bool apart = false;
     for (int scale = 0; scale < (out ? 2 : 1); ++scale) {
         int first = 0;
         for (int type = 0; type < 3; ++type)
@@ -631,20 +637,23 @@ int chicle_clip_grads(const void *const *in, void *const *out, const int64_t *si
                     ++t.tensors;
                 }
                 if (!t.tensors) continue;
-                const int pieces = t.first_piece[t.tensors], grid = pieces < most ? pieces : most;
+                const int pieces = t.first_piece[t.tensors], grid = scale || pieces < most ? pieces : most;
                 first += grid;
                 TRY(with_type(type, [&](auto e) {
                     typedef decltype(e) T;
-                    if (scale) clip_scale<T><<<grid, CLIP_THREADS, 0, stream>>>(t, CLIP_PIECE, part, parts, max_norm, norm);
+                    if (scale) clip_scale<T><<<grid, CLIP_THREADS, 0, stream>>>(t, CLIP_PIECE, part, apart ? 0 : parts, max_norm, norm);
                     else squares<T><<<grid, CLIP_THREADS, 0, stream>>>(t, CLIP_PIECE, part);
                     return launched("clip");
                 }));
             }
-        if (!scale) parts = first;
-    }
-    if (!out || parts == 0) {
-        norm_only<<<1, CLIP_THREADS, 0, stream>>>(part, parts, norm);
-        return launched("norm_only");
+        if (!scale) {
+            parts = first;
+            apart = !out || parts == 0 || pieces_all > CLIP_FEW_PIECES;
+            if (apart) {
+                norm_only<<<1, CLIP_THREADS, 0, stream>>>(part, parts, norm);
+                TRY(launched("norm_only"));
+            }
+        }
     }
     return CHICLE_OK;
 }

@@ -1,8 +1,8 @@
 // The norm of many tensors together, and the tensors times min(1, max_norm / (norm + 1e-6)).
 //
-// Two launches: every workgroup leaves the sum of squares of its piece, and every workgroup of the second launch adds all of
-// these up by itself, in one order, before it scales its piece.  Sums are held in double: the squares of any finite 32-bit floats
-// add up without overflow.  The bound is the memory: one read and one write, and a second read that comes from the caches as
+// Every workgroup of the first launch leaves the sum of squares of its pieces.  Where there are few pieces, every workgroup of the
+// second launch adds all of these up by itself, in one order, before it scales its piece; where there are many, a launch between
+// the two does it once.  Sums are held in double: the squares of any finite 32-bit floats add up without overflow.  The bound is the memory: one read and one write, and a second read that comes from the caches as
 // far as the tensors fit there.
 #pragma once
 #include "elements.hpp"
@@ -11,7 +11,7 @@ namespace chicle_train {
 
 constexpr int CLIP_TENSORS = 112;            // tensors of one launch: their table is part of the kernel's arguments
 constexpr int CLIP_THREADS = 256;
-constexpr int CLIP_MOST_PARTS = 2048;        // workgroups of all launches of a call
+constexpr int CLIP_MOST_PARTS = 2048;        // workgroups of all launches of a call that add up squares
 
 struct ClipTable {
     const void *in[CLIP_TENSORS];
@@ -39,28 +39,43 @@ __device__ __forceinline__ void clip_pieces(const ClipTable &t, int64_t piece, F
 {
     int k = 0;
     for (int p = blockIdx.x; p < t.first_piece[t.tensors]; p += gridDim.x) {
-        while (p >= t.first_piece[k + 1]) ++k;
+        int hi = t.tensors - 1;                          // the last tensor that begins at this piece or before
+        while (k < hi) {
+            const int mid = (k + hi + 1) / 2;
+            if (t.first_piece[mid] <= p) k = mid;
+            else hi = mid - 1;
+        }
         const int64_t a = (int64_t)(p - t.first_piece[k]) * piece;
         f(k, a, min(t.count[k], a + piece));
     }
 }
 
+// CLIP_AHEAD vectors of a thread are on their way together.
+constexpr int CLIP_AHEAD = 4;
+
 template <typename T>
 __global__ __launch_bounds__(CLIP_THREADS) void squares(ClipTable t, int64_t piece, double *__restrict__ part)
 {
     constexpr int V = Elem<T>::VEC;
-    double sum = 0.0;
+    double sums[CLIP_AHEAD] = {};                        // (sums of their own do not wait for each other)
     clip_pieces(t, piece, [&](int k, int64_t a, int64_t end) {
         const T *p = (const T *)t.in[k];
-        for (int64_t c = a + (int64_t)threadIdx.x * V; c < end; c += CLIP_THREADS * V) {
-            float u[V];
-            load_vec(p, c, end, u);
-            double s = 0.0;
+        for (int64_t c = a + (int64_t)threadIdx.x * V; c < end; c += CLIP_THREADS * V * CLIP_AHEAD) {
+            u32x4 u[CLIP_AHEAD];
 #pragma unroll
-            for (int i = 0; i < V; ++i) s += (double)u[i] * (double)u[i];
-            sum += s;
+            for (int q = 0; q < CLIP_AHEAD; ++q) u[q] = load_raw<T, true>(p, c + q * CLIP_THREADS * V, end);
+#pragma unroll
+            for (int q = 0; q < CLIP_AHEAD; ++q) {
+                float w[V];
+                unpack<T>(u[q], w);
+#pragma unroll
+                for (int i = 0; i < V; ++i) sums[q] += (double)w[i] * (double)w[i];
+            }
         }
     });
+    double sum = 0.0;
+#pragma unroll
+    for (int q = 0; q < CLIP_AHEAD; ++q) sum += sums[q];
     sum = block_sum(sum);
     if (threadIdx.x == 0) part[t.first_part + blockIdx.x] = sum;
 }
@@ -78,25 +93,35 @@ __global__ __launch_bounds__(CLIP_THREADS) void norm_only(const double *__restri
     if (threadIdx.x == 0) *norm_out = norm;
 }
 
+// parts 0: the norm is there already
 template <typename T>
 __global__ __launch_bounds__(CLIP_THREADS) void clip_scale(ClipTable t, int64_t piece, const double *__restrict__ part, int parts,
                                                            float max_norm, float *__restrict__ norm_out)
 {
     constexpr int V = Elem<T>::VEC;
-    const float norm = norm_of_parts(part, parts);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
+    float norm;
+    if (parts) {
+        norm = norm_of_parts(part, parts);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
+    } else norm = *norm_out;
     const float ratio = max_norm / (norm + 1e-6f);
     const float factor = ratio > 1.f ? 1.f : ratio;      // (a norm that is no number makes the factor none)
     clip_pieces(t, piece, [&](int k, int64_t a, int64_t end) {
         const T *p = (const T *)t.in[k];
         T *q = (T *)t.out[k];
         if (factor == 1.f && p == q) return;             // nothing changes
-        for (int64_t c = a + (int64_t)threadIdx.x * V; c < end; c += CLIP_THREADS * V) {
-            float u[V];
-            load_vec(p, c, end, u);
+        for (int64_t c = a + (int64_t)threadIdx.x * V; c < end; c += CLIP_THREADS * V * CLIP_AHEAD) {
+            u32x4 u[CLIP_AHEAD];
 #pragma unroll
-            for (int i = 0; i < V; ++i) u[i] *= factor;
-            store_vec(q, c, end, u);
+            for (int h = 0; h < CLIP_AHEAD; ++h) u[h] = load_raw<T, true>(p, c + h * CLIP_THREADS * V, end);
+#pragma unroll
+            for (int h = 0; h < CLIP_AHEAD; ++h) {
+                float w[V];
+                unpack<T>(u[h], w);
+#pragma unroll
+                for (int i = 0; i < V; ++i) w[i] *= factor;
+                store_vec<T, true>(q, c + h * CLIP_THREADS * V, end, w);
+            }
         }
     });
 }

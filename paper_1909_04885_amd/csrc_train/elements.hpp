@@ -13,36 +13,79 @@ typedef _Float16 f16;
 
 template <typename T> struct Elem { static constexpr int VEC = 16 / (int)sizeof(T); };   // values of one access
 
-// A row may begin at any multiple of its element's size (a slice of a wider buffer): the accesses assume no more.
-template <typename T> struct Vec { T v[Elem<T>::VEC]; };
+// A row may begin at any multiple of its element's size (a slice of a wider buffer): the accesses assume no more.  Sixteen bytes
+// stay what they are until they are used: taking them apart where they are asked for would wait for them there.
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4_at_2 __attribute__((ext_vector_type(4), aligned(2)));
 
 template <typename T>
-__device__ __forceinline__ void load_vec(const T *row, int64_t c, int64_t d, float *out)
+__device__ __forceinline__ void unpack(u32x4 x, float *out)
 {
-    constexpr int V = Elem<T>::VEC;
-    if (c + V <= d) {
-        Vec<T> x;
-        __builtin_memcpy(&x, row + c, 16);
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) out[i] = (float)x.v[i];
+        for (int i = 0; i < 4; ++i) out[i] = __uint_as_float(x[i]);
+    } else if constexpr (__is_same(T, bf16)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { out[2 * i] = __uint_as_float(x[i] << 16); out[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u); }
     } else {
+        T v[8];
+        __builtin_memcpy(v, &x, 16);
 #pragma unroll
-        for (int i = 0; i < V; ++i) out[i] = c + i < d ? (float)row[c + i] : 0.f;
+        for (int i = 0; i < 8; ++i) out[i] = (float)v[i];
     }
 }
 
 template <typename T>
+__device__ __forceinline__ u32x4 pack(const float *in)
+{
+    T v[Elem<T>::VEC];
+#pragma unroll
+    for (int i = 0; i < Elem<T>::VEC; ++i) v[i] = (T)in[i];
+    u32x4 x;
+    __builtin_memcpy(&x, v, 16);
+    return x;
+}
+
+// A vector of a row of d values, zeros past its end.  ONCE: data that is read once, or written and not read soon, is not kept in the
+// caches, which is faster for what does not fit there (reads of 2 GiB: 7.1 instead of 6.4 TB/s).
+template <typename T, bool ONCE = false>
+__device__ __forceinline__ u32x4 load_raw(const T *row, int64_t c, int64_t d)
+{
+    constexpr int V = Elem<T>::VEC;
+    if (__builtin_expect(c + V <= d, 1)) {
+        if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4_at_2 *)(row + c));
+        else return *(const u32x4_at_2 *)(row + c);
+    }
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (c + i < d) x[i] = ((const unsigned *)row)[c + i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (c + i < d) x[i / 2] |= (unsigned)((const uint16_t *)row)[c + i] << (i % 2 * 16);
+    }
+    return x;
+}
+
+template <typename T, bool ONCE = false>
+__device__ __forceinline__ void load_vec(const T *row, int64_t c, int64_t d, float *out)
+{
+    unpack<T>(load_raw<T, ONCE>(row, c, d), out);
+}
+
+template <typename T, bool ONCE = false>
 __device__ __forceinline__ void store_vec(T *row, int64_t c, int64_t d, const float *in)
 {
     constexpr int V = Elem<T>::VEC;
-    if (c + V <= d) {
-        Vec<T> x;
-#pragma unroll
-        for (int i = 0; i < V; ++i) x.v[i] = (T)in[i];
-        __builtin_memcpy(row + c, &x, 16);
+    const u32x4 x = pack<T>(in);
+    if (__builtin_expect(c + V <= d, 1)) {
+        if constexpr (ONCE) __builtin_nontemporal_store((u32x4_at_2)x, (u32x4_at_2 *)(row + c));
+        else *(u32x4_at_2 *)(row + c) = x;
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
+        for (int i = 0; i < V - 1; ++i)
             if (c + i < d) row[c + i] = (T)in[i];
     }
 }

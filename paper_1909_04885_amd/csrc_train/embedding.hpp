@@ -47,29 +47,31 @@ __device__ __forceinline__ unsigned token_key(const void *ids, int wide, int64_t
     return id >= 0 && id < n_rows ? (unsigned)id : (unsigned)n_rows;
 }
 
-// The bit of every row that some token has.  Bits are only ever set, so a stale word costs an atomic and no more.
-__device__ __forceinline__ void mark_row(unsigned *seen, unsigned key, int64_t n_rows)
+// seen[v] = 1 for every row v that some token has: all who mark a row store the same byte.  seen_bytes is a multiple of sixteen.
+__device__ __forceinline__ void clear_seen(uint8_t *seen, int64_t seen_bytes, int64_t thread, int64_t threads)
 {
-    if (seen && (int64_t)key < n_rows) {
-        const unsigned bit = 1u << (key & 31);
-        if (!(__hip_atomic_load(&seen[key >> 5], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & bit)) atomicOr(&seen[key >> 5], bit);
-    }
+    if (seen)
+        for (int64_t i = thread * 16; i < seen_bytes; i += threads * 16) *(u32x4 *)(seen + i) = u32x4{0u, 0u, 0u, 0u};
+}
+__device__ __forceinline__ void mark_seen(uint8_t *seen, unsigned key, int64_t n_rows)
+{
+    if (seen && (int64_t)key < n_rows) seen[key] = 1;
 }
 
 constexpr int SORT_ONE = 4096;               // tokens that one workgroup sorts by itself
 
 // One workgroup: a bitonic network over (key, place) in LDS.
 __global__ __launch_bounds__(1024) void sort_tokens_one(const void *__restrict__ ids, int wide, int n, int64_t n_rows, unsigned *__restrict__ keys_out,
-                                                        unsigned *__restrict__ places_out, unsigned *seen, int64_t seen_words, int *flags)
+                                                        unsigned *__restrict__ places_out, uint8_t *seen, int64_t seen_bytes, int *flags)
 {
     __shared__ unsigned long long s[SORT_ONE];
     int size = 1;
     while (size < n) size <<= 1;
     for (int i = threadIdx.x; i < size; i += 1024)
         s[i] = i < n ? ((unsigned long long)token_key(ids, wide, i, n_rows, flags) << 32) | (unsigned)i : ~0ull;
-    if (seen)
-        for (int64_t i = threadIdx.x; i < seen_words; i += 1024) seen[i] = 0u;
-    __threadfence();
+    clear_seen(seen, seen_bytes, threadIdx.x, 1024);
+    __syncthreads();                                     // (cleared before anything is marked)
+    for (int i = threadIdx.x; i < n; i += 1024) mark_seen(seen, (unsigned)(s[i] >> 32), n_rows);
     __syncthreads();
     for (int k = 2; k <= size; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
@@ -81,26 +83,28 @@ __global__ __launch_bounds__(1024) void sort_tokens_one(const void *__restrict__
             __syncthreads();
         }
     for (int i = threadIdx.x; i < n; i += 1024) {
-        const unsigned key = (unsigned)(s[i] >> 32);
-        keys_out[i] = key;
+        keys_out[i] = (unsigned)(s[i] >> 32);
         places_out[i] = (unsigned)s[i];
-        if (i == 0 || (unsigned)(s[i - 1] >> 32) != key) mark_row(seen, key, n_rows);
     }
 }
 
 // More tokens: passes over digits of the key, the lowest first, each of which keeps the order of equal digits.  A workgroup
-// takes SORT_TILE tokens, wavefront w of it the w-th quarter, 64 tokens at a time in their order.
-constexpr int SORT_TILE = 2048, SORT_WAVES = 4, SORT_THREADS = 64 * SORT_WAVES, SORT_BITS = 10, SORT_BINS = 1 << SORT_BITS;
+// takes a tile of tokens, wavefront w of it the w-th part, 64 tokens at a time in their order.  There are at most
+// SORT_MOST_TILES tiles: every workgroup adds up by itself what the tiles before it hold of each digit, which saves a launch
+// between the counts and the scatter.
+constexpr int SORT_WAVES = 8, SORT_THREADS = 64 * SORT_WAVES, SORT_BITS = 10, SORT_BINS = 1 << SORT_BITS;
+constexpr int SORT_LEAST_TILE = 2048, SORT_MOST_TILES = 128;
 
 struct SortPass {
     const void *ids;             // first pass: the tokens themselves
     const unsigned *keys_in, *places_in;
     unsigned *keys_out, *places_out;
-    unsigned *count;             // [bin][workgroup], then where the bin's tokens of the workgroup go
-    unsigned *seen;              // last pass
-    int64_t n, n_rows, seen_words;
-    int wide, shift, bins, tiles, first, last;
+    unsigned *count;             // [tile][bin]
+    int64_t n, n_rows, tile;     // tokens of a tile: a multiple of SORT_THREADS
+    int wide, shift, bits, tiles, first;
     int *flags;
+    uint8_t *seen;               // null where no rows are filled with zeros
+    int64_t seen_bytes;
 };
 
 __device__ __forceinline__ unsigned sort_key(const SortPass &p, int64_t i, bool flag)
@@ -108,8 +112,7 @@ __device__ __forceinline__ unsigned sort_key(const SortPass &p, int64_t i, bool 
     return p.first ? token_key(p.ids, p.wide, i, p.n_rows, flag ? p.flags : nullptr) : p.keys_in[i];
 }
 
-// Every lane's number of lower lanes with the same digit, and the number of all lanes with it; lanes without a token have the
-// digit `bins` or above and take part in nothing.
+// Every lane's number of lower lanes with the same digit, and the number of all lanes with it; lanes without a token count nowhere.
 __device__ __forceinline__ void match_digit(unsigned digit, bool live, int bits, int &lower, int &all)
 {
     unsigned long long same = __ballot(live);
@@ -125,91 +128,96 @@ __device__ __forceinline__ void match_digit(unsigned digit, bool live, int bits,
 __global__ __launch_bounds__(SORT_THREADS) void sort_count(SortPass p)
 {
     __shared__ unsigned s[SORT_BINS];
-    for (int i = threadIdx.x; i < p.bins; i += SORT_THREADS) s[i] = 0u;
-    if (p.first && p.seen)
-        for (int64_t i = (int64_t)blockIdx.x * SORT_THREADS + threadIdx.x; i < p.seen_words; i += (int64_t)gridDim.x * SORT_THREADS) p.seen[i] = 0u;
+    const int bins = 1 << p.bits;
+    for (int i = threadIdx.x; i < bins; i += SORT_THREADS) s[i] = 0u;
     __syncthreads();
-    const int64_t a = (int64_t)blockIdx.x * SORT_TILE, end = min(p.n, a + SORT_TILE);
-    for (int64_t i = a + threadIdx.x; i < end; i += SORT_THREADS) atomicAdd(&s[(sort_key(p, i, true) >> p.shift) & (p.bins - 1)], 1u);
+    if (p.first) clear_seen(p.seen, p.seen_bytes, (int64_t)blockIdx.x * SORT_THREADS + threadIdx.x, (int64_t)gridDim.x * SORT_THREADS);
+    const int64_t a = (int64_t)blockIdx.x * p.tile, end = min(p.n, a + p.tile);
+    for (int64_t i = a + threadIdx.x; i < end; i += SORT_THREADS) atomicAdd(&s[(sort_key(p, i, true) >> p.shift) & (bins - 1)], 1u);
     __syncthreads();
-    for (int i = threadIdx.x; i < p.bins; i += SORT_THREADS) p.count[(int64_t)i * p.tiles + blockIdx.x] = s[i];
+    for (int i = threadIdx.x; i < bins; i += SORT_THREADS) p.count[(int64_t)blockIdx.x * bins + i] = s[i];
 }
 
-// Exclusive sums over bins * tiles counts, by one workgroup.
-__global__ __launch_bounds__(1024) void sort_offsets(unsigned *count, int64_t total)
+__global__ __launch_bounds__(SORT_THREADS) void sort_scatter(SortPass p)
 {
-    __shared__ unsigned s[16];
-    unsigned carry = 0;
-    for (int64_t base = 0; base < total; base += 4096) {
-        unsigned v[4], sum = 0;
-        const int64_t at = base + (int64_t)threadIdx.x * 4;
-        for (int k = 0; k < 4; ++k) { v[k] = at + k < total ? count[at + k] : 0u; sum += v[k]; }
-        unsigned up = sum;
-        for (int o = 1; o < 64; o <<= 1) {
-            const unsigned t = __shfl_up(up, o);
-            if ((int)(threadIdx.x & 63) >= o) up += t;
-        }
-        __syncthreads();
-        if ((threadIdx.x & 63) == 63) s[threadIdx.x >> 6] = up;
-        __syncthreads();
-        unsigned before = carry + up - sum, all = 0;
-        for (int w = 0; w < 16; ++w) {
-            if (w < (int)(threadIdx.x >> 6)) before += s[w];
-            all += s[w];
-        }
-        carry += all;
-        for (int k = 0; k < 4; ++k)
-            if (at + k < total) { count[at + k] = before; before += v[k]; }
-    }
-}
-
-__global__ __launch_bounds__(SORT_THREADS) void sort_scatter(SortPass p, int bits)
-{
-    __shared__ unsigned s[SORT_WAVES][SORT_BINS];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    __shared__ unsigned s[SORT_WAVES][SORT_BINS];        // a wavefront's tokens of a digit, then where its next one goes
+    __shared__ unsigned totals[SORT_WAVES];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, bins = 1 << p.bits, mask = bins - 1;
     for (int i = threadIdx.x; i < SORT_WAVES * SORT_BINS; i += SORT_THREADS) (&s[0][0])[i] = 0u;
     __syncthreads();
-    constexpr int STEPS = SORT_TILE / SORT_THREADS;
-    const int64_t a = (int64_t)blockIdx.x * SORT_TILE + wave * (SORT_TILE / SORT_WAVES);
-    unsigned key[STEPS], rank[STEPS];
+    const int64_t part = p.tile / SORT_WAVES, a = (int64_t)blockIdx.x * p.tile + wave * part, end = min(p.n, a + part);
+    for (int64_t i = a + lane; i < end; i += 64) atomicAdd(&s[wave][(sort_key(p, i, false) >> p.shift) & mask], 1u);
+    // Two neighbouring bins to a thread: what earlier tiles hold of them, and what all tiles do.
+    constexpr int EACH = SORT_BINS / SORT_THREADS;
+    unsigned before[EACH] = {}, total[EACH] = {}, sum = 0;
+    constexpr int BATCH = 16;                            // tiles whose counts are asked for together
+    if ((int)threadIdx.x * EACH < bins)
+        for (int t = 0; t < p.tiles; t += BATCH) {
+            unsigned c[BATCH][EACH];
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
-        const int64_t i = a + k * 64 + lane;
-        const bool live = i < p.n;
-        key[k] = live ? sort_key(p, i, false) : 0u;
-        const unsigned digit = (key[k] >> p.shift) & (p.bins - 1);
+            for (int q = 0; q < BATCH; ++q)
+#pragma unroll
+                for (int k = 0; k < EACH; ++k) c[q][k] = p.count[min(t + q, p.tiles - 1) * bins + min((int)threadIdx.x * EACH + k, mask)];
+#pragma unroll
+            for (int q = 0; q < BATCH; ++q)
+#pragma unroll
+                for (int k = 0; k < EACH; ++k) {
+                    const unsigned v = t + q < p.tiles && (int)threadIdx.x * EACH + k < bins ? c[q][k] : 0u;
+                    total[k] += v;
+                    if (t + q < (int)blockIdx.x) before[k] += v;
+                }
+        }
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) sum += total[k];
+    unsigned up = sum;
+    for (int o = 1; o < 64; o <<= 1) {
+        const unsigned t = __shfl_up(up, o);
+        if (lane >= o) up += t;
+    }
+    if (lane == 63) totals[wave] = up;
+    __syncthreads();
+    unsigned at = up - sum;
+    for (int w = 0; w < wave; ++w) at += totals[w];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int bin = threadIdx.x * EACH + k;
+        unsigned t = at + before[k];
+        if (bin < bins)
+            for (int w = 0; w < SORT_WAVES; ++w) { const unsigned c = s[w][bin]; s[w][bin] = t; t += c; }
+        at += total[k];
+    }
+    __syncthreads();
+    for (int64_t base = a; base < end; base += 64) {
+        const int64_t i = base + lane;
+        const bool live = i < end;
+        const unsigned key = live ? sort_key(p, i, false) : 0u, digit = (key >> p.shift) & mask;
         int lower, all;
-        match_digit(digit, live, bits, lower, all);
-        const unsigned before = s[wave][digit];
-        rank[k] = before + lower;
+        match_digit(digit, live, p.bits, lower, all);
+        const unsigned next = s[wave][digit];
         __builtin_amdgcn_wave_barrier();
-        if (live && lower == 0) s[wave][digit] = before + all;
+        if (live && lower == 0) s[wave][digit] = next + all;
         __builtin_amdgcn_wave_barrier();
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < p.bins; i += SORT_THREADS) {
-        unsigned t = p.count[(int64_t)i * p.tiles + blockIdx.x];
-        for (int w = 0; w < SORT_WAVES; ++w) { const unsigned c = s[w][i]; s[w][i] = t; t += c; }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
-        const int64_t i = a + k * 64 + lane;
-        if (i >= p.n) continue;
-        const unsigned at = s[wave][(key[k] >> p.shift) & (p.bins - 1)] + rank[k];
-        p.keys_out[at] = key[k];
-        p.places_out[at] = p.first ? (unsigned)i : p.places_in[i];
-        if (p.last) mark_row(p.seen, key[k], p.n_rows);
+        if (live) {
+            p.keys_out[next + lower] = key;
+            p.places_out[next + lower] = p.first ? (unsigned)i : p.places_in[i];
+            if (p.first) mark_seen(p.seen, key, p.n_rows);
+        }
     }
 }
 
 // ---- sums over runs of equal ids ------------------------------------------------------------------------------------
 
+constexpr int EMBED_PIECE = 32;              // tokens of a piece
+constexpr int ZERO_BYTES = 16384;            // of the rows that a workgroup fills with zeros
+
 struct EmbedGrad {
-    const unsigned *keys, *places, *seen;    // sorted; seen is null where the sums are added to what the table's gradient holds
-    float *head, *tail;                      // [piece][d]: what a piece holds of a run that began before it, or that goes on behind it
-    int64_t n, d, n_rows, ldo, ldd;
-    int piece, lanes, run_blocks;            // tokens of a piece, threads of a piece
+    const unsigned *keys, *places;           // sorted
+    float *head, *tail;                      // [piece][ldp]: what a piece holds of a run that began before it, or that goes on behind it
+    int64_t n, d, n_rows, ldo, ldd, ldp;
+    int lanes;                               // threads of a piece
+    int run_blocks, zero_blocks, zero_rows;  // zero_rows: to a workgroup
+    int accumulate;
+    const uint8_t *seen;
     float scale;
 };
 
@@ -220,7 +228,7 @@ __device__ __forceinline__ void give_row(const EmbedGrad &p, T *__restrict__ out
     T *dst = out + row * p.ldo;
 #pragma unroll
     for (int k = 0; k < V; ++k) sum[k] *= p.scale;
-    if (!p.seen) {
+    if (p.accumulate) {
         float old[V];
         load_vec(dst, c, p.d, old);
 #pragma unroll
@@ -229,111 +237,166 @@ __device__ __forceinline__ void give_row(const EmbedGrad &p, T *__restrict__ out
     store_vec(dst, c, p.d, sum);
 }
 
-// Workgroups [0, run_blocks): EMBED_THREADS / lanes pieces each, by blocks of lanes * VEC columns (blockIdx.y).  The rest: rows that no
-// token has, 32 rows (a word of `seen`) at a time.
+// Zeros for the rows that no token has, a few rows to a workgroup: neighbouring workgroups then store side by side, which is faster than
+// long stretches of rows each (524 MB in 75 instead of 144 us).
+template <typename T>
+__device__ __forceinline__ void zero_rows(const EmbedGrad &p, int block, int64_t c, T *__restrict__ out)
+{
+    constexpr int V = Elem<T>::VEC;
+    const int groups = EMBED_THREADS / p.lanes;
+    const float zero[V] = {};
+    const int64_t r0 = (int64_t)block * p.zero_rows, end = min(p.n_rows, r0 + p.zero_rows);
+    if (c >= p.d) return;
+    for (int64_t row = r0 + threadIdx.x / p.lanes; row < end; row += groups)
+        if (!p.seen[row]) store_vec<T, true>(out + row * p.ldo, c, p.d, zero);
+}
+
+// The work of run_blocks workgroups that add up pieces of tokens, EMBED_THREADS / lanes pieces each, and of zero_blocks that store zeros,
+// mixed so that reads and writes go on side by side.  blockIdx.y: blocks of lanes * VEC columns of the pieces.
 template <typename T>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_grad_runs(EmbedGrad p, const T *__restrict__ dout, T *__restrict__ out)
 {
     constexpr int V = Elem<T>::VEC, AHEAD = 8;
-    const int64_t c = ((int64_t)blockIdx.y * p.lanes + threadIdx.x % p.lanes) * V;
-    if ((int)blockIdx.x >= p.run_blocks) {
-        const int groups = EMBED_THREADS / p.lanes, group = threadIdx.x / p.lanes;
-        const int64_t words = (p.n_rows + 31) / 32;
-        if (c >= p.d) return;
-        const float zero[V] = {};
-        for (int64_t w = blockIdx.x - p.run_blocks; w < words; w += gridDim.x - p.run_blocks) {
-            const unsigned seen = p.seen[w];
-            for (int b = group; b < 32; b += groups) {
-                const int64_t row = w * 32 + b;
-                if (row < p.n_rows && !(seen >> b & 1)) store_vec(out + row * p.ldo, c, p.d, zero);
-            }
-        }
+    extern __shared__ uint2 tokens[];                    // (id, place) of the workgroup's pieces
+    const int64_t total = p.run_blocks + p.zero_blocks, b = blockIdx.x;
+    const int zeros_before = (int)(b * p.zero_blocks / total);
+    if ((int)((b + 1) * p.zero_blocks / total) != zeros_before) {
+        zero_rows(p, zeros_before, ((int64_t)blockIdx.y * p.lanes + threadIdx.x % p.lanes) * V, out);
         return;
     }
-    const int64_t piece = (int64_t)blockIdx.x * (EMBED_THREADS / p.lanes) + threadIdx.x / p.lanes;
-    const int64_t a = piece * p.piece, end = min(p.n, a + p.piece);
-    if (a >= p.n || c >= p.d) return;
+    const int groups = EMBED_THREADS / p.lanes, group = threadIdx.x / p.lanes;
+    const int64_t piece0 = (b - zeros_before) * groups, t0 = piece0 * EMBED_PIECE;
+    for (int i = threadIdx.x; i < groups * EMBED_PIECE && t0 + i < p.n; i += EMBED_THREADS) tokens[i] = make_uint2(p.keys[t0 + i], p.places[t0 + i]);
+    __syncthreads();
+    const int64_t piece = piece0 + group, a = piece * EMBED_PIECE;
+    const int many = (int)min((int64_t)EMBED_PIECE, p.n - a);
+    const int64_t c = ((int64_t)blockIdx.y * p.lanes + threadIdx.x % p.lanes) * V;
+    if (many <= 0 || c >= p.d) return;
+    const uint2 *mine = tokens + group * EMBED_PIECE;
     float sum[V] = {};
-    unsigned key = p.keys[a];
+    unsigned key = mine[0].x;
     bool from_before = a > 0 && p.keys[a - 1] == key;
-    for (int64_t t = a; t < end; t += AHEAD) {
-        float u[AHEAD][V];
-        unsigned ks[AHEAD];
+    auto leave = [&](float *part) {
+        float *dst = part + piece * p.ldp + c;           // (rows of parts are padded to whole vectors)
+#pragma unroll
+        for (int k = 0; k < V; k += 4) *(float4 *)(dst + k) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
+    };
+    for (int t = 0; t < many; t += AHEAD) {
+        u32x4 u[AHEAD];
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q)
+            u[q] = load_raw<T, true>(dout + (int64_t)mine[min(t + q, many - 1)].y * p.ldd, c, p.d);
 #pragma unroll
         for (int q = 0; q < AHEAD; ++q) {
-            const int64_t at = min(t + q, end - 1);
-            ks[q] = p.keys[at];
-            load_vec(dout + (int64_t)p.places[at] * p.ldd, c, p.d, u[q]);
-        }
-#pragma unroll
-        for (int q = 0; q < AHEAD; ++q) {
-            if (t + q >= end) break;
-            if (ks[q] != key) {                          // the run before ends inside the piece
-                if (from_before) {
-                    if ((int64_t)key < p.n_rows)
-#pragma unroll
-                        for (int k = 0; k < V; ++k)
-                            if (c + k < p.d) p.head[piece * p.d + c + k] = sum[k];
-                } else if ((int64_t)key < p.n_rows) give_row(p, out, key, c, sum);
-                key = ks[q];
+            if (t + q >= many) break;
+            const unsigned next = mine[t + q].x;
+            if (next != key) {                           // the run before ends inside the piece
+                if ((int64_t)key < p.n_rows) {
+                    if (from_before) leave(p.head);
+                    else give_row(p, out, key, c, sum);
+                }
+                key = next;
                 from_before = false;
 #pragma unroll
                 for (int k = 0; k < V; ++k) sum[k] = 0.f;
             }
+            float w[V];
+            unpack<T>(u[q], w);
 #pragma unroll
-            for (int k = 0; k < V; ++k) sum[k] += u[q][k];
+            for (int k = 0; k < V; ++k) sum[k] += w[k];
         }
     }
     if ((int64_t)key >= p.n_rows) return;
-    const bool goes_on = end < p.n && p.keys[end] == key;
-    if (!from_before && !goes_on) give_row(p, out, key, c, sum);
-    else {
-        float *dst = (from_before ? p.head : p.tail) + piece * p.d;
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (c + k < p.d) dst[c + k] = sum[k];
-    }
+    const bool goes_on = a + many < p.n && p.keys[a + many] == key;
+    if (from_before) leave(p.head);
+    else if (goes_on) leave(p.tail);
+    else give_row(p, out, key, c, sum);
 }
 
 // Runs over several pieces: tail of the piece where the run begins, heads of the pieces up to the one where it ends.  A workgroup
-// looks at one piece and one block of 64 * VEC columns; its wavefronts take every JOIN_WAVES-th of the run's pieces.
-constexpr int JOIN_WAVES = 4;
+// looks at JOIN_PIECES pieces and one block of JOIN_COLUMNS columns.  A wavefront adds up the run that begins in its piece, or, where
+// that is long, all wavefronts take its pieces in turn.
+constexpr int JOIN_WAVES = 16, JOIN_PIECES = JOIN_WAVES, JOIN_LONG = 16, JOIN_COLUMNS = 256;
+
+// The sum of the parts of pieces first, first + step, .. up to last of the run that begins in piece `begin`, four columns to a lane.
+__device__ __forceinline__ float4 sum_of_parts(const EmbedGrad &p, int64_t begin, int64_t first, int64_t last, int step, int64_t c)
+{
+    constexpr int AHEAD = 8;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int64_t q = first; q <= last; q += (int64_t)step * AHEAD) {
+        float4 u[AHEAD];
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h) {
+            const int64_t at = min(q + h * step, last);
+            u[h] = *(const float4 *)((at == begin ? p.tail : p.head) + at * p.ldp + c);
+        }
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h)
+            if (q + h * step <= last) { sum.x += u[h].x; sum.y += u[h].y; sum.z += u[h].z; sum.w += u[h].w; }
+    }
+    return sum;
+}
+
+// The last piece behind `piece` that begins with `key`; the one behind does.  Sorted: those that begin with it come first.
+__device__ __forceinline__ int64_t last_piece(const EmbedGrad &p, int64_t piece, int64_t pieces, unsigned key, int lane)
+{
+    int64_t last = piece + 1;
+    for (int stride = 64 * 64; stride >= 1; stride /= 64)
+        for (;;) {                                       // sixty-four probes, a stride apart
+            const int64_t at = last + (int64_t)(lane + 1) * stride;
+            const unsigned long long same = __ballot(at < pieces && p.keys[min(at, pieces - 1) * EMBED_PIECE] == key);
+            last += (int64_t)__popcll(same) * stride;
+            if (~same) break;
+        }
+    return last;
+}
+
+template <typename T>
+__device__ __forceinline__ void give_columns(const EmbedGrad &p, T *__restrict__ out, int64_t row, int64_t c, float4 sum)
+{
+    T *dst = out + row * p.ldo + c;
+    const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (c + k < p.d) dst[k] = (T)(v[k] * p.scale + (p.accumulate ? (float)dst[k] : 0.f));
+}
 
 template <typename T>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void embed_grad_join(EmbedGrad p, T *__restrict__ out)
 {
-    constexpr int V = Elem<T>::VEC;
-    const int64_t piece = blockIdx.x, end = (piece + 1) * p.piece;
-    if (end >= p.n) return;
-    const unsigned key = p.keys[end - 1];
-    if (p.keys[end] != key || (int64_t)key >= p.n_rows) return;
-    const int64_t a = piece * p.piece;
-    if (a > 0 && p.keys[a - 1] == key && p.keys[a] == key) return;     // the run began before: another piece's work
-    int64_t lo = piece + 1, hi = (p.n - 1) / p.piece;                  // last piece that begins with this id
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) / 2;
-        if (p.keys[mid * p.piece] == key) lo = mid;
-        else hi = mid - 1;
-    }
+    __shared__ float4 s[JOIN_WAVES][64];
+    __shared__ int64_t lasts[JOIN_WAVES];                // last piece of a long run, or 0
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t c = ((int64_t)blockIdx.y * 64 + lane) * V;
-    float sum[V] = {};
-    if (c < p.d)
-        for (int64_t q = piece + wave; q <= lo; q += JOIN_WAVES) {
-            const float *src = (q == piece ? p.tail : p.head) + q * p.d;
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-                if (c + k < p.d) sum[k] += src[c + k];
-        }
-    __shared__ float s[JOIN_WAVES][64][V];
-#pragma unroll
-    for (int k = 0; k < V; ++k) s[wave][lane][k] = sum[k];
+    const int64_t c = (int64_t)blockIdx.y * JOIN_COLUMNS + lane * 4, pieces = (p.n + EMBED_PIECE - 1) / EMBED_PIECE;
+    const int64_t piece = (int64_t)blockIdx.x * JOIN_PIECES + wave, a = piece * EMBED_PIECE, end = a + EMBED_PIECE;
+    int64_t last = 0;
+    unsigned key = 0;
+    if (end < p.n) {
+        key = p.keys[end - 1];
+        const bool began_before = a > 0 && p.keys[a] == key && p.keys[a - 1] == key;
+        if (p.keys[end] == key && (int64_t)key < p.n_rows && !began_before) last = last_piece(p, piece, pieces, key, lane);
+    }
+    const bool is_long = last - piece >= JOIN_LONG;
+    if (lane == 0) lasts[wave] = is_long ? last : 0;
+    if (last > 0 && !is_long && c < p.d) give_columns(p, out, key, c, sum_of_parts(p, piece, piece, last, 1, c));
     __syncthreads();
-    if (wave || c >= p.d) return;
-    for (int w = 1; w < JOIN_WAVES; ++w)
-#pragma unroll
-        for (int k = 0; k < V; ++k) sum[k] += s[w][lane][k];
-    give_row(p, out, key, c, sum);
+    for (int w = 0; w < JOIN_WAVES; ++w) {
+        const int64_t begin = (int64_t)blockIdx.x * JOIN_PIECES + w;
+        last = lasts[w];
+        if (last == 0) continue;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < p.d) sum = sum_of_parts(p, begin, begin + wave, last, JOIN_WAVES, c);
+        s[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && c < p.d) {
+            for (int v = 1; v < JOIN_WAVES; ++v) {
+                const float4 t = s[v][lane];
+                sum.x += t.x; sum.y += t.y; sum.z += t.z; sum.w += t.w;
+            }
+            give_columns(p, out, p.keys[last * EMBED_PIECE], c, sum);
+        }
+        __syncthreads();
+    }
 }
 
 }  // namespace chicle_train

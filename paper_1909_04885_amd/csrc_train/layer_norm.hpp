@@ -50,7 +50,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_rows(const T *__restrict__
     if constexpr (NV > 0) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            load_vec(xr, first + k * step, d, v[k]);
+            load_vec<T, true>(xr, first + k * step, d, v[k]);
 #pragma unroll
             for (int i = 0; i < V; ++i) s.x += v[k][i];
         }
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_rows(const T *__restrict__
         load_vec(beta, c, d, b);
 #pragma unroll
         for (int i = 0; i < V; ++i) u[i] = (u[i] - mean) * rstd * g[i] + b[i];
-        store_vec(yr, c, d, u);
+        store_vec<T, true>(yr, c, d, u);
     };
     if constexpr (NV > 0) {
 #pragma unroll
@@ -117,18 +117,40 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
         for (int64_t c = first; c < d; c += step)
             for (int i = 0; i < V && c + i < d; ++i) mine[c + i] = mine[d + c + i] = 0.f;
     }
+    // The next row is on its way while this one is added up.
+    u32x4 next_x[N], next_dy[N];
+    float next_mean, next_rstd;
+    auto ask = [&](int64_t row) {
+        row = min(row, n - 1);
+        next_mean = mean_in[row];
+        next_rstd = rstd_in[row];
+        if constexpr (NV > 0)
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                next_x[k] = load_raw<T, true>(x + row * ldx, first + k * step, d);
+                next_dy[k] = load_raw<T, true>(dy + row * lddy, first + k * step, d);
+            }
+    };
+    ask((int64_t)blockIdx.x * groups + group);
     for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < n; row0 += (int64_t)gridDim.x * groups) {
         const int64_t row = row0 + group;
         const bool live = row < n;
         const T *xr = x + (live ? row : n - 1) * ldx, *dyr = dy + (live ? row : n - 1) * lddy;
         T *dxr = dx + (live ? row : n - 1) * lddx;
-        const float mean = mean_in[live ? row : n - 1], rstd = rstd_in[live ? row : n - 1];
+        const float mean = next_mean, rstd = next_rstd;
         float h[N][V], g[N][V];                          // xhat and dy
         float2 s = {0.f, 0.f};
+        if constexpr (NV > 0) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) { unpack<T>(next_x[k], h[k]); unpack<T>(next_dy[k], g[k]); }
+        }
+        ask(row + (int64_t)gridDim.x * groups);
         // Past the end of the row dy is zero, so what xhat has there counts nowhere.
         auto take = [&](int64_t c, float *hk, float *gk, const float *gak) {
-            load_vec(xr, c, d, hk);
-            load_vec(dyr, c, d, gk);
+            if constexpr (NV == 0) {
+                load_vec(xr, c, d, hk);
+                load_vec(dyr, c, d, gk);
+            }
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 hk[i] = (hk[i] - mean) * rstd;
@@ -148,7 +170,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
         auto give = [&](int64_t c, const float *hk, float *gk, const float *gak) {
 #pragma unroll
             for (int i = 0; i < V; ++i) gk[i] = rstd * (gk[i] * gak[i] - mg - hk[i] * mh);
-            if (c < d) store_vec(dxr, c, d, gk);
+            if (c < d) store_vec<T, true>(dxr, c, d, gk);
         };
         if constexpr (NV > 0) {
 #pragma unroll
@@ -187,20 +209,29 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
     }
 }
 
-// Sums of the workgroups' parts: 64 columns of [dgamma | dbeta] to a workgroup, sixteen threads to a column.
+// Sums of the workgroups' parts: LN_SUM_COLUMNS columns of [dgamma | dbeta] to a workgroup, 64 threads to a column.
+constexpr int LN_SUM_COLUMNS = 16;
+
 template <typename T>
 __global__ __launch_bounds__(1024) void layer_norm_grad_sums(const float *__restrict__ part, int parts, int64_t d, T *__restrict__ dgamma, T *__restrict__ dbeta)
 {
-    __shared__ float s[16][64];
-    const int col = threadIdx.x & 63, slice = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + col;
+    constexpr int SLICES = 1024 / LN_SUM_COLUMNS;
+    __shared__ float s[SLICES][LN_SUM_COLUMNS + 1];
+    const int col = threadIdx.x % LN_SUM_COLUMNS, slice = threadIdx.x / LN_SUM_COLUMNS;
+    const int64_t c = (int64_t)blockIdx.x * LN_SUM_COLUMNS + col;
     float t = 0.f;
-    if (c < 2 * d)
-        for (int p = slice; p < parts; p += 16) t += part[(int64_t)p * 2 * d + c];
+    if (c < 2 * d) {
+#pragma unroll 8
+        for (int p = slice; p < parts; p += SLICES) t += part[(int64_t)p * 2 * d + c];
+    }
     s[slice][col] = t;
     __syncthreads();
+    for (int half = SLICES / 2; half > 0; half /= 2) {
+        if (slice < half) s[slice][col] += s[slice + half][col];
+        __syncthreads();
+    }
     if (slice || c >= 2 * d) return;
-    for (int i = 1; i < 16; ++i) t += s[i][col];
+    t = s[0][col];
     if (c < d) dgamma[c] = (T)t;
     else dbeta[c - d] = (T)t;
 }

@@ -79,6 +79,8 @@ class TrainOps:
         self._index = self.device.index
         self._types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
         self._wide = {torch.int32: 0, torch.int64: 1}
+        # (the handle of the current stream, without an object around it)
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         self._flags = torch.zeros(1, dtype=torch.int32, device=self.device)
         torch.cuda.synchronize(self.device)          # the word is zero before any stream's work looks at it
 
@@ -87,10 +89,10 @@ class TrainOps:
         """Run a C entry point with the library's GPU current; args end before the stream."""
         t = self._torch.cuda
         if t.current_device() == self._index:
-            rc = fn(*args, t.current_stream(self._index).cuda_stream)
+            rc = fn(*args, self._raw_stream(self._index))
         else:
             with t.device(self._index):
-                rc = fn(*args, t.current_stream(self._index).cuda_stream)
+                rc = fn(*args, self._raw_stream(self._index))
         if rc != OK:
             raise ChicleError(rc, self._L.chicle_train_last_error().decode())
 
@@ -222,26 +224,34 @@ class TrainOps:
         return dx, dgamma, dbeta
 
     # -- clipping
+    def _pointers(self, tensors, name: str):
+        """Addresses, numbers of values and types of contiguous tensors on this GPU."""
+        index, kinds, where, sizes, types = self._index, self._types, [], [], []
+        for g in tensors:
+            kind = kinds.get(g.dtype)
+            if kind is None or not g.is_cuda or g.get_device() != index or not g.is_contiguous():
+                raise ChicleError(EINVAL, "%s must be contiguous float32, bfloat16 or float16 tensors on %s" % (name, self.device))
+            where.append(g.data_ptr())
+            sizes.append(g.numel())
+            types.append(kind)
+        return where, sizes, types
+
     def _clip(self, grads: Sequence, out: Optional[Sequence], max_norm: float):
         k = len(grads)
-        for g in grads:
-            if g.device != self.device or g.dtype not in self._types or not g.is_contiguous():
-                raise ChicleError(EINVAL, "gradients must be contiguous float32, bfloat16 or float16 tensors on %s" % self.device)
-        ins = (ctypes.c_void_p * k)(*[g.data_ptr() for g in grads])
+        where, sizes, types = self._pointers(grads, "gradients")
         outs = None
-        if out is not None:
-            if len(out) != k:
-                raise ChicleError(EINVAL, "one output per gradient")
-            for g, o in zip(grads, out):
-                if o.device != self.device or o.dtype != g.dtype or o.shape != g.shape or not o.is_contiguous():
-                    raise ChicleError(EINVAL, "an output must be contiguous and have its gradient's shape and type")
-            outs = (ctypes.c_void_p * k)(*[o.data_ptr() for o in out])
-        sizes = (ctypes.c_int64 * k)(*[g.numel() for g in grads])
-        types = (ctypes.c_int32 * k)(*[self._types[g.dtype] for g in grads])
+        if out is grads:
+            outs = (ctypes.c_void_p * k)(*where)
+        elif out is not None:
+            to, out_sizes, out_types = self._pointers(out, "outputs")
+            if out_sizes != sizes or out_types != types:
+                raise ChicleError(EINVAL, "an output per gradient, of its type and number of values")
+            outs = (ctypes.c_void_p * k)(*to)
         norm = self._empty((), self._torch.float32)
         nbytes = self._L.chicle_clip_grads_bytes(k)
         ws = self._workspace(nbytes)
-        self._call(self._L.chicle_clip_grads, ins, outs, sizes, types, k, max_norm, norm.data_ptr(), ws.data_ptr(), nbytes)
+        self._call(self._L.chicle_clip_grads, (ctypes.c_void_p * k)(*where), outs, (ctypes.c_int64 * k)(*sizes), (ctypes.c_int32 * k)(*types), k,
+                   max_norm, norm.data_ptr(), ws.data_ptr(), nbytes)
         return norm
 
     def grad_norm(self, grads: Sequence):
