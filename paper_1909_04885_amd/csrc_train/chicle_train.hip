@@ -127,19 +127,23 @@ int with_vectors(int vectors, F f)
 
 // ---- products -------------------------------------------------------------------------------------------------------
 
-typedef MmConfig<256, 256, 2, 4> MmWide;
-typedef MmConfig<128, 128, 2, 2> MmMiddle;
-typedef MmConfig<256, 64, 4, 1> MmThin;
+typedef MmConfig<256, 256, 2, 4, 1> MmWide;
+typedef MmConfig<128, 128, 2, 2, 2> MmMiddle;
+typedef MmConfig<128, 64, 2, 2, 3> MmThin;
 
 enum { WIDE, MIDDLE, THIN };
+constexpr int CUS = 256;                                 // compute units
 
-int mm_tile_i(int c) { return c == MIDDLE ? 128 : 256; }
+int mm_tile_i(int c) { return c == WIDE ? 256 : 128; }
 int mm_tile_j(int c) { return c == WIDE ? 256 : c == MIDDLE ? 128 : 64; }
 
-int mm_choose(int64_t rows_i, int64_t rows_j)
+// Large tiles read the least and run at the matrix cores' rate (1200 against 1000 TFLOP/s of the middle ones), where they fill the chip;
+// `splittable`: the sum is long and may be divided.
+int mm_choose(int64_t rows_i, int64_t rows_j, bool splittable = false)
 {
     if (rows_j <= 64) return THIN;
-    return ceil_div(rows_i, 256) * ceil_div(rows_j, 256) >= 192 ? WIDE : MIDDLE;
+    const int64_t tiles = ceil_div(rows_i, 256) * ceil_div(rows_j, 256);
+    return tiles >= (splittable ? 8 : 192) ? WIDE : MIDDLE;
 }
 
 template <typename F>
@@ -204,12 +208,14 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         if (p.piece > classes) p.piece = classes;
         p.ldg = round_up(p.piece, MM_K);
         p.ldp = round_up(d, 4);
-        p.config_dx = mm_choose(d, n);
-        const int64_t tiles = ceil_div(d, mm_tile_i(p.config_dx)) * ceil_div(n, mm_tile_j(p.config_dx));
         const int64_t slices = p.ldg / MM_K * (p.planes == 3 ? 6 : 1);
-        int64_t splits = tiles >= 256 ? 1 : ceil_div(512, tiles);
+        p.config_dx = mm_choose(d, n, slices >= 512);
+        const int64_t tiles = ceil_div(d, mm_tile_i(p.config_dx)) * ceil_div(n, mm_tile_j(p.config_dx));
+        const int64_t room = CUS * (p.config_dx == WIDE ? 1 : 2);
+        int64_t splits = tiles >= room ? 1 : room / tiles;
         if (splits > slices / 8) splits = slices / 8;
-        p.splits = splits < 1 ? 1 : (int)splits;
+        splits = splits < 1 ? 1 : splits;
+        p.splits = (int)ceil_div(slices, ceil_div(slices, splits));
         p.config_dw = mm_choose(d, p.piece);
         p.xt = c.take<uint16_t>(d * p.ldt * p.planes);
         p.wt = c.take<uint16_t>(d * p.ldg * p.planes);
@@ -263,12 +269,20 @@ MmShape mm_shape(const MmOperand &a, const MmOperand &b, int64_t k, int planes, 
 {
     MmShape s;
     s.a = a; s.b = b;
-    s.k_slices = (int)(k / MM_K);
+    s.k = (int)k;
     s.planes = planes;
     s.tiles_i = (int)ceil_div(a.rows, mm_tile_i(config));
     s.tiles_j = (int)ceil_div(b.rows, mm_tile_j(config));
-    s.splits = splits;
+    const int64_t slices = k / MM_K * (planes == 1 ? 1 : 6);
+    s.per_split = (int)ceil_div(slices, splits);
+    s.splits = (int)ceil_div(slices, s.per_split);       // (none is empty; at most `splits`)
     return s;
+}
+
+template <typename C> unsigned mm_grid(const MmShape &s)
+{
+    const int64_t units = (int64_t)s.tiles_i * s.tiles_j * s.splits;
+    return (unsigned)(units < CUS * C::PER_CU ? units : CUS * C::PER_CU);
 }
 
 // lse and loss of all rows
@@ -284,7 +298,7 @@ int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw
         typedef decltype(c) C;
         auto kernel = loss_tiles<P, C, sizeof(T) == 4>;
         TRY(allow_lds(kernel, C::LDS));
-        kernel<<<(unsigned)(s.tiles_i * s.tiles_j), C::THREADS, C::LDS, stream>>>(s, rows);
+        kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows);
         return launched("loss_tiles");
     }));
     loss_rows<<<(unsigned)ceil_div(p.n, 4), 256, 0, stream>>>(rows, s.tiles_i, loss, lse, flags);
@@ -308,18 +322,19 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
     const float *inverse = scaled ? p.power + 1 : nullptr;
     TRY(loss_lay_columns<T>(x, ldx, p.xt, p.ldt, p.d * p.ldt, p.n, p.d, rows.labels, rows.wide, p.classes, stream));
     const MmOperand xr = {p.x, p.lay_x ? p.ldk : ldx, p.n * p.ldk, (int)p.n}, xc = {p.xt, p.ldt, p.d * p.ldt, (int)p.d};
+    int copies = 0;                                      // of dx, to be added up
     for (int k = 0; k < p.pieces; ++k) {
         const int64_t first = k * p.piece, many = p.classes - first < p.piece ? p.classes - first : p.piece;
         const int64_t ldg = round_up(many, MM_K), plane_g = p.n * ldg, plane_t = many * p.ldt, plane_w = p.d * ldg;
         const MmOperand wr = {(const uint16_t *)p.w + first * (p.lay_w ? p.ldk : ldw), p.lay_w ? p.ldk : ldw, p.classes * p.ldk, (int)many};
         TRY(loss_lay_columns<T>(w + first * ldw, ldw, p.wt, ldg, plane_w, many, p.d, nullptr, 0, 0, stream));
-        const int config_g = mm_choose(many, p.n);
+        const int config_g = PLANES == 3 && p.n > 64 ? MIDDLE : mm_choose(many, p.n);   // (three planes of G: no registers for large tiles)
         TRY(with_config(config_g, [&](auto c) {
-            typedef decltype(c) C;
+            typedef std::conditional_t<PLANES == 3 && std::is_same<decltype(c), MmWide>::value, MmMiddle, decltype(c)> C;
             const MmShape s = mm_shape(wr, xr, p.ldk, p.planes, config_g, 1);
             auto kernel = loss_grad_tiles<P, C, sizeof(T) == 4, PLANES>;
             TRY(allow_lds(kernel, C::LDS));
-            kernel<<<(unsigned)(s.tiles_i * s.tiles_j), C::THREADS, C::LDS, stream>>>(s, rows, (int)first, (int)many, (P *)p.g, ldg, plane_g, (P *)p.gt,
+            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, (int)first, (int)many, (P *)p.g, ldg, plane_g, (P *)p.gt,
                                                                                      p.ldt, plane_t);
             return launched("loss_grad_tiles");
         }));
@@ -329,8 +344,9 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
             const MmShape s = mm_shape(wc, gr, ldg, p.planes, p.config_dx, p.splits);
             auto kernel = product_parts<P, C>;
             TRY(allow_lds(kernel, C::LDS));
-            kernel<<<(unsigned)(s.tiles_i * s.tiles_j * s.splits), C::THREADS, C::LDS, stream>>>(s, p.parts + (int64_t)k * p.splits * p.n * p.ldp, p.ldp,
+            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.parts + (int64_t)copies * p.n * p.ldp, p.ldp,
                                                                                                 p.n * p.ldp);
+            copies += s.splits;
             return launched("product_parts");
         }));
         TRY(with_config(p.config_dw, [&](auto c) {
@@ -338,11 +354,11 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
             const MmShape s = mm_shape(xc, gc, p.ldt, p.planes, p.config_dw, 1);
             auto kernel = product_out<P, C, T>;
             TRY(allow_lds(kernel, C::LDS));
-            kernel<<<(unsigned)(s.tiles_i * s.tiles_j), C::THREADS, C::LDS, stream>>>(s, dw + first * lddw, lddw, inverse);
+            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, dw + first * lddw, lddw, inverse);
             return launched("product_out");
         }));
     }
-    sum_parts<T><<<(unsigned)grid_of(p.n * (p.ldp / 4), 256, 16384), 256, 0, stream>>>(p.parts, p.ldp, p.n * p.ldp, p.splits * p.pieces, dx, lddx, p.n,
+    sum_parts<T><<<(unsigned)grid_of(p.n * (p.ldp / 4), 256, 16384), 256, 0, stream>>>(p.parts, p.ldp, p.n * p.ldp, copies, dx, lddx, p.n,
                                                                                       p.d, inverse);
     return launched("sum_parts");
 }

@@ -50,28 +50,43 @@ __device__ __forceinline__ void clip_pieces(const ClipTable &t, int64_t piece, F
     }
 }
 
-// CLIP_AHEAD vectors of a thread are on their way together.
+// CLIP_AHEAD vectors of a thread are on their way together.  A whole piece, which is nearly every one, is read without looking for the
+// tensor's end.
 constexpr int CLIP_AHEAD = 4;
+
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void clip_ask(const T *p, int64_t c, int64_t end, u32x4 (&u)[CLIP_AHEAD])
+{
+    constexpr int STEP = CLIP_THREADS * Elem<T>::VEC;
+#pragma unroll
+    for (int q = 0; q < CLIP_AHEAD; ++q) {
+        if constexpr (WHOLE) u[q] = __builtin_nontemporal_load((const u32x4_at_2 *)(p + c + q * STEP));
+        else u[q] = load_raw<T, true>(p, c + q * STEP, end);
+    }
+}
 
 template <typename T>
 __global__ __launch_bounds__(CLIP_THREADS) void squares(ClipTable t, int64_t piece, double *__restrict__ part)
 {
-    constexpr int V = Elem<T>::VEC;
+    constexpr int V = Elem<T>::VEC, ALL = CLIP_THREADS * V * CLIP_AHEAD;
     double sums[CLIP_AHEAD] = {};                        // (sums of their own do not wait for each other)
+    auto add = [&](const u32x4 (&u)[CLIP_AHEAD]) {
+#pragma unroll
+        for (int q = 0; q < CLIP_AHEAD; ++q) {
+            float w[V];
+            unpack<T>(u[q], w);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sums[q] += (double)w[i] * (double)w[i];
+        }
+    };
     clip_pieces(t, piece, [&](int k, int64_t a, int64_t end) {
         const T *p = (const T *)t.in[k];
-        for (int64_t c = a + (int64_t)threadIdx.x * V; c < end; c += CLIP_THREADS * V * CLIP_AHEAD) {
-            u32x4 u[CLIP_AHEAD];
-#pragma unroll
-            for (int q = 0; q < CLIP_AHEAD; ++q) u[q] = load_raw<T, true>(p, c + q * CLIP_THREADS * V, end);
-#pragma unroll
-            for (int q = 0; q < CLIP_AHEAD; ++q) {
-                float w[V];
-                unpack<T>(u[q], w);
-#pragma unroll
-                for (int i = 0; i < V; ++i) sums[q] += (double)w[i] * (double)w[i];
-            }
-        }
+        u32x4 u[CLIP_AHEAD];
+        int64_t c = a + (int64_t)threadIdx.x * V;
+        if (end - a == piece)
+            for (; c < end; c += ALL) { clip_ask<T, true>(p, c, end, u); add(u); }
+        else
+            for (; c < end; c += ALL) { clip_ask<T, false>(p, c, end, u); add(u); }
     });
     double sum = 0.0;
 #pragma unroll
@@ -98,7 +113,7 @@ template <typename T>
 __global__ __launch_bounds__(CLIP_THREADS) void clip_scale(ClipTable t, int64_t piece, const double *__restrict__ part, int parts,
                                                            float max_norm, float *__restrict__ norm_out)
 {
-    constexpr int V = Elem<T>::VEC;
+    constexpr int V = Elem<T>::VEC, ALL = CLIP_THREADS * V * CLIP_AHEAD;
     float norm;
     if (parts) {
         norm = norm_of_parts(part, parts);
@@ -110,10 +125,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void clip_scale(ClipTable t, int64_t 
         const T *p = (const T *)t.in[k];
         T *q = (T *)t.out[k];
         if (factor == 1.f && p == q) return;             // nothing changes
-        for (int64_t c = a + (int64_t)threadIdx.x * V; c < end; c += CLIP_THREADS * V * CLIP_AHEAD) {
-            u32x4 u[CLIP_AHEAD];
-#pragma unroll
-            for (int h = 0; h < CLIP_AHEAD; ++h) u[h] = load_raw<T, true>(p, c + h * CLIP_THREADS * V, end);
+        auto scale = [&](int64_t c, const u32x4 (&u)[CLIP_AHEAD]) {
 #pragma unroll
             for (int h = 0; h < CLIP_AHEAD; ++h) {
                 float w[V];
@@ -122,7 +134,13 @@ __global__ __launch_bounds__(CLIP_THREADS) void clip_scale(ClipTable t, int64_t 
                 for (int i = 0; i < V; ++i) w[i] *= factor;
                 store_vec<T, true>(q, c + h * CLIP_THREADS * V, end, w);
             }
-        }
+        };
+        u32x4 u[CLIP_AHEAD];
+        int64_t c = a + (int64_t)threadIdx.x * V;
+        if (end - a == piece)
+            for (; c < end; c += ALL) { clip_ask<T, true>(p, c, end, u); scale(c, u); }
+        else
+            for (; c < end; c += ALL) { clip_ask<T, false>(p, c, end, u); scale(c, u); }
     });
 }
 

@@ -126,59 +126,90 @@ constexpr float MINUS_INF = -__builtin_inff();
 // exp(a - b), 0 where a is minus infinity
 template <bool EXACT> __device__ __forceinline__ float exp_diff(float a, float b)
 {
-    const float x = a - b;
-    return a == MINUS_INF ? 0.f : EXACT ? expf(x) : __expf(x);
+    return a == MINUS_INF ? 0.f : EXACT ? expf(a - b) : __expf(a - b);
+}
+
+// Where a lane's values of a tile lie
+template <typename C> struct TilePlace {
+    int lane, wi, wj, i0, j0;
+    __device__ __forceinline__ explicit TilePlace(const MmTile &t)
+    {
+        lane = threadIdx.x & 63;
+        const int wave = threadIdx.x >> 6;
+        wi = wave / C::W_J;
+        wj = wave % C::W_J;
+        i0 = t.i * C::TILE_I + wi * C::MI * 16 + 4 * (lane >> 4);
+        j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
+    }
+};
+
+constexpr float LOG2E = 1.44269504088896340736f;
+
+// exp(z - m).  EXACT: the library's exponential; else the instruction's, whose error of 2^-22 and |z - m| 2^-24 is far below what
+// 16-bit gradients show.  The difference comes first: of two numbers of the type's lowest value it is zero.
+template <bool EXACT> __device__ __forceinline__ float exp_of(float z, float m)
+{
+    return EXACT ? expf(z - m) : __builtin_amdgcn_exp2f((z - m) * LOG2E);
 }
 
 // i: classes, j: rows
 template <typename T, typename C, bool EXACT>
-__global__ __launch_bounds__(C::THREADS) void loss_tiles(MmShape s, LossRows l)
+__global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_tiles(MmShape s, LossRows l)
 {
-    extern __shared__ __align__(16) char lds[];
-    const MmTile t = mm_tile(s);
-    f32x4 acc[C::MI][C::NJ];
-    mm_multiply<T, C>(s, t, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J;
-    const int i0 = t.i * C::TILE_I + wi * C::MI * 16 + 4 * (lane >> 4), j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
-    __syncthreads();
-    float2 *s_part = (float2 *)lds;                      // [wave_i][row of the tile]
+    mm_tiles<T, C>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ], char *extra) __attribute__((always_inline)) {
+        const TilePlace<C> at(t);
+        float2 *s_part = (float2 *)extra;                // [wave_i][row of the tile]
+        if ((t.i + 1) * C::TILE_I > l.classes) {         // the last tile: what lies past the classes counts nowhere
 #pragma unroll
-    for (int nj = 0; nj < C::NJ; ++nj) {
-        const int j = j0 + nj * 16;
-        const int label = label_at(l, j);
-        float m = MINUS_INF;
+            for (int mi = 0; mi < C::MI; ++mi)
 #pragma unroll
-        for (int mi = 0; mi < C::MI; ++mi)
+                for (int r = 0; r < 4; ++r)
+                    if (at.i0 + mi * 16 + r >= l.classes)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = i0 + mi * 16 + r;
-                if (i >= l.classes) acc[mi][nj][r] = MINUS_INF;
-                else if (i == label) l.picked[j] = acc[mi][nj][r];
-                m = fmaxf(m, acc[mi][nj][r]);
-            }
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32));
-        float e = 0.f;
-#pragma unroll
-        for (int mi = 0; mi < C::MI; ++mi)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) e += exp_diff<EXACT>(acc[mi][nj][r], m);
-        e += __shfl_xor(e, 16);
-        e += __shfl_xor(e, 32);
-        if (lane < 16) s_part[wi * C::TILE_J + wj * C::NJ * 16 + nj * 16 + lane] = make_float2(m, e);
-    }
-    __syncthreads();
-    for (int q = threadIdx.x; q < C::TILE_J; q += C::THREADS) {
-        const int j = t.j * C::TILE_J + q;
-        if (j >= l.n) continue;
-        float2 x = s_part[q];
-        for (int w = 1; w < C::W_I; ++w) {
-            const float2 y = s_part[w * C::TILE_J + q];
-            const float m = fmaxf(x.x, y.x);
-            x = make_float2(m, x.y * exp_diff<EXACT>(x.x, m) + y.y * exp_diff<EXACT>(y.x, m));
+                        for (int nj = 0; nj < C::NJ; ++nj) acc[mi][nj][r] = MINUS_INF;
         }
-        l.part[(int64_t)j * s.tiles_i + t.i] = x;
-    }
+#pragma unroll
+        for (int nj = 0; nj < C::NJ; ++nj) {
+            const int j = at.j0 + nj * 16, rel = label_at(l, j) - at.i0;
+            if (rel >= 0 && rel < C::MI * 16 && (rel & 15) < 4) {          // the label's logit is this lane's
+                float z = 0.f;
+#pragma unroll
+                for (int mi = 0; mi < C::MI; ++mi)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z = rel == mi * 16 + r ? acc[mi][nj][r] : z;
+                l.picked[j] = z;
+            }
+            float m = MINUS_INF;
+#pragma unroll
+            for (int mi = 0; mi < C::MI; ++mi)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) m = fmaxf(m, acc[mi][nj][r]);
+            m = fmaxf(m, __shfl_xor(m, 16));
+            m = fmaxf(m, __shfl_xor(m, 32));
+            const float shift = m == MINUS_INF ? 0.f : m;
+            float e = 0.f;
+#pragma unroll
+            for (int mi = 0; mi < C::MI; ++mi)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) e += exp_of<EXACT>(acc[mi][nj][r], shift);
+            e += __shfl_xor(e, 16);
+            e += __shfl_xor(e, 32);
+            if (at.lane < 16) s_part[at.wi * C::TILE_J + at.wj * C::NJ * 16 + nj * 16 + at.lane] = make_float2(m, e);
+        }
+        __syncthreads();
+        for (int q = threadIdx.x; q < C::TILE_J; q += C::THREADS) {
+            const int j = t.j * C::TILE_J + q;
+            if (j >= l.n) continue;
+            float2 x = s_part[q];
+            for (int w = 1; w < C::W_I; ++w) {
+                const float2 y = s_part[w * C::TILE_J + q];
+                const float m = fmaxf(x.x, y.x);
+                x = make_float2(m, x.y * exp_diff<EXACT>(x.x, m) + y.y * exp_diff<EXACT>(y.x, m));
+            }
+            l.part[(int64_t)j * s.tiles_i + t.i] = x;
+        }
+        // (a tile's slices begin behind another barrier: s_part is read by then)
+    });
 }
 
 // A wavefront to a row.
@@ -227,96 +258,86 @@ __global__ __launch_bounds__(1024) void loss_power(const float *__restrict__ wei
 // G of a piece of the classes: s.a is the piece's rows of w, `first` the piece's first class.  g[plane][row][class of the piece], ldg;
 // gt[plane][class of the piece][row], ldt; both are written to their tiles' ends as far as they have room, zeros outside.
 template <typename T, typename C, bool EXACT, int PLANES>
-__global__ __launch_bounds__(C::THREADS) void loss_grad_tiles(MmShape s, LossRows l, int first, int piece, T *__restrict__ g, int64_t ldg, int64_t plane_g,
-                                                              T *__restrict__ gt, int64_t ldt, int64_t plane_t)
+__global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_grad_tiles(MmShape s, LossRows l, int first, int piece, T *__restrict__ g, int64_t ldg,
+                                                                           int64_t plane_g, T *__restrict__ gt, int64_t ldt, int64_t plane_t)
 {
-    extern __shared__ __align__(16) char lds[];
-    const MmTile t = mm_tile(s);
-    f32x4 acc[C::MI][C::NJ];
-    mm_multiply<T, C>(s, t, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J;
-    const int i0 = t.i * C::TILE_I + wi * C::MI * 16 + 4 * (lane >> 4), j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
     const float power = l.power ? l.power[0] : 1.f;
+    mm_tiles<T, C>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ], char *) __attribute__((always_inline)) {
+        const TilePlace<C> at(t);
 #pragma unroll
-    for (int nj = 0; nj < C::NJ; ++nj) {
-        const int j = j0 + nj * 16;
-        const int label = label_at(l, j);
-        const float weight = label >= 0 ? l.weight[j] * power : 0.f, lse = label >= 0 ? l.lse[j] : 0.f;
+        for (int nj = 0; nj < C::NJ; ++nj) {
+            const int j = at.j0 + nj * 16, label = label_at(l, j);
+            const float weight = label >= 0 ? l.weight[j] * power : 0.f, lse = label >= 0 ? l.lse[j] : 0.f;
+            const int rel = label - first - at.i0;
 #pragma unroll
-        for (int mi = 0; mi < C::MI; ++mi) {
-            T v[PLANES][4];
+            for (int mi = 0; mi < C::MI; ++mi) {
+                T v[PLANES][4];
+                const int i = at.i0 + mi * 16;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = i0 + mi * 16 + r;
-                float p = EXACT ? expf(acc[mi][nj][r] - lse) : __expf(acc[mi][nj][r] - lse);
-                if (first + i == label) p -= 1.f;
-                p = weight != 0.f && i < piece ? p * weight : 0.f;
-                T q[PLANES];
-                if constexpr (PLANES == 3) split_planes(p, q);
-                else q[0] = (T)p;
+                for (int r = 0; r < 4; ++r) {
+                    float p = exp_of<EXACT>(acc[mi][nj][r], lse);
+                    if (rel == mi * 16 + r) p -= 1.f;
+                    p = weight != 0.f && i + r < piece ? p * weight : 0.f;
+                    T q[PLANES];
+                    if constexpr (PLANES == 3) split_planes(p, q);
+                    else q[0] = (T)p;
 #pragma unroll
-                for (int k = 0; k < PLANES; ++k) v[k][r] = q[k];
-            }
-            const int i = i0 + mi * 16;
+                    for (int k = 0; k < PLANES; ++k) v[k][r] = q[k];
+                }
 #pragma unroll
-            for (int k = 0; k < PLANES; ++k) {
-                if (j < l.n && i < ldg) __builtin_memcpy(g + k * plane_g + (int64_t)j * ldg + i, v[k], 8);
-                if (j < ldt)
+                for (int k = 0; k < PLANES; ++k) {
+                    if (j < l.n && i < ldg) __builtin_memcpy(g + k * plane_g + (int64_t)j * ldg + i, v[k], 8);
+                    if (j < ldt)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (i + r < piece) gt[k * plane_t + (int64_t)(i + r) * ldt + j] = v[k][r];
+                        for (int r = 0; r < 4; ++r)
+                            if (i + r < piece) gt[k * plane_t + (int64_t)(i + r) * ldt + j] = v[k][r];
+                }
             }
         }
-    }
+    });
 }
 
 // A product as it is: out[j][i] in 32 bits, split `split` of the sum in its own copy of `out`.
 template <typename T, typename C>
-__global__ __launch_bounds__(C::THREADS) void product_parts(MmShape s, float *__restrict__ out, int64_t ld, int64_t copy)
+__global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_parts(MmShape s, float *__restrict__ out, int64_t ld, int64_t copy)
 {
-    extern __shared__ __align__(16) char lds[];
-    const MmTile t = mm_tile(s);
-    f32x4 acc[C::MI][C::NJ];
-    mm_multiply<T, C>(s, t, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J;
-    const int i0 = t.i * C::TILE_I + wi * C::MI * 16 + 4 * (lane >> 4), j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
-    out += t.split * copy;
+    mm_tiles<T, C>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ], char *) __attribute__((always_inline)) {
+        const TilePlace<C> at(t);
+        float *mine = out + t.split * copy;
 #pragma unroll
-    for (int nj = 0; nj < C::NJ; ++nj)
+        for (int nj = 0; nj < C::NJ; ++nj)
 #pragma unroll
-        for (int mi = 0; mi < C::MI; ++mi) {
-            const int i = i0 + mi * 16, j = j0 + nj * 16;
-            if (j < s.b.rows && i < s.a.rows) __builtin_memcpy(out + (int64_t)j * ld + i, &acc[mi][nj], 16);
-        }
+            for (int mi = 0; mi < C::MI; ++mi) {
+                const int i = at.i0 + mi * 16, j = at.j0 + nj * 16;
+                if (j < s.b.rows && i < s.a.rows) *(f32x4 *)(mine + (int64_t)j * ld + i) = acc[mi][nj];
+            }
+    });
 }
 
 // ... and as the result itself: out[j][i] = scale * sum, rounded.
 template <typename T, typename C, typename O>
-__global__ __launch_bounds__(C::THREADS) void product_out(MmShape s, O *__restrict__ out, int64_t ld, const float *__restrict__ scale)
+__global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_out(MmShape s, O *__restrict__ out, int64_t ld, const float *__restrict__ scale)
 {
-    extern __shared__ __align__(16) char lds[];
-    const MmTile t = mm_tile(s);
-    f32x4 acc[C::MI][C::NJ];
-    mm_multiply<T, C>(s, t, lds, acc);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J;
-    const int i0 = t.i * C::TILE_I + wi * C::MI * 16 + 4 * (lane >> 4), j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
     const float f = scale ? *scale : 1.f;
+    mm_tiles<T, C>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ], char *) __attribute__((always_inline)) {
+        const TilePlace<C> at(t);
 #pragma unroll
-    for (int nj = 0; nj < C::NJ; ++nj)
+        for (int nj = 0; nj < C::NJ; ++nj)
 #pragma unroll
-        for (int mi = 0; mi < C::MI; ++mi) {
-            const int i = i0 + mi * 16, j = j0 + nj * 16;
-            if (j >= s.b.rows) continue;
-            O v[4];
+            for (int mi = 0; mi < C::MI; ++mi) {
+                const int i = at.i0 + mi * 16, j = at.j0 + nj * 16;
+                if (j >= s.b.rows) continue;
+                O v[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = (O)(acc[mi][nj][r] * f);
-            O *dst = out + (int64_t)j * ld + i;
-            if (i + 4 <= s.a.rows) __builtin_memcpy(dst, v, sizeof v);
-            else
+                for (int r = 0; r < 4; ++r) v[r] = (O)(acc[mi][nj][r] * f);
+                O *dst = out + (int64_t)j * ld + i;
+                if (i + 4 <= s.a.rows) __builtin_memcpy(dst, v, sizeof v);
+                else
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (i + r < s.a.rows) dst[r] = v[r];
-        }
+                    for (int r = 0; r < 4; ++r)
+                        if (i + r < s.a.rows) dst[r] = v[r];
+            }
+    });
 }
 
 // dx = scale * the sum of the copies, in their order.  ld of a copy is a multiple of four.
