@@ -127,9 +127,13 @@ int with_vectors(int vectors, F f)
 
 // ---- products -------------------------------------------------------------------------------------------------------
 
+// The long side of a wavefront's part lies along j where A lies by k, since turning costs reads, and along i for the loss, whose sums go
+// along i.
 typedef MmConfig<256, 256, 2, 4, 1> MmWide;
+typedef MmConfig<256, 256, 4, 2, 1> MmWideByK;
 typedef MmConfig<128, 128, 2, 2, 2> MmMiddle;
 typedef MmConfig<128, 64, 2, 2, 3> MmThin;
+constexpr int MM_PARTS_I = 2;                            // wavefronts along i of the loss's tiles
 
 enum { WIDE, MIDDLE, THIN };
 constexpr int CUS = 256;                                 // compute units
@@ -146,10 +150,10 @@ int mm_choose(int64_t rows_i, int64_t rows_j, bool splittable = false)
     return tiles >= (splittable ? 8 : 192) ? WIDE : MIDDLE;
 }
 
-template <typename F>
+template <typename W, typename F>
 int with_config(int c, F f)
 {
-    return c == WIDE ? f(MmWide()) : c == MIDDLE ? f(MmMiddle()) : f(MmThin());
+    return c == WIDE ? f(W()) : c == MIDDLE ? f(MmMiddle()) : f(MmThin());
 }
 
 template <typename K>
@@ -166,16 +170,19 @@ struct LossPlan {
     int planes, config;
     bool lay_x, lay_w;
     // gradient
-    int64_t piece, ldg, ldt, ldp;        // classes of a piece; lengths of rows along the classes, along the rows, of dx's parts
+    int64_t piece, ldg, rows_out, ldp;   // classes of a piece; length of G's rows, their number; length of the rows of dx's parts
     int pieces, splits, config_dx, config_dw;
-    void *x, *w, *xt, *wt, *g, *gt;
+    void *x, *w, *g;
     float *parts, *lse, *picked, *power;
     float2 *tile_sums;
     size_t bytes;
 };
 
-constexpr int64_t LOSS_PIECE_BYTES = (int64_t)1 << 30;   // G of a piece, both layouts
+constexpr int64_t LOSS_PIECE_BYTES = (int64_t)1 << 29;   // G of a piece
 constexpr int64_t LOSS_MOST = (int64_t)1 << 22;
+
+// Rows 1024 bytes apart, or a multiple of that, meet in few channels of the L2.
+int64_t spread(int64_t ld) { return ld % 512 == 0 ? ld + MM_K : ld; }
 
 LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t n, int64_t d, int64_t classes, int32_t type, bool grad, void *workspace)
 {
@@ -184,32 +191,33 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
     if (n == 0) return p;                                // (nothing to lay out)
     p.n = n; p.d = d; p.classes = classes;
     p.planes = type == CHICLE_F32 ? 3 : 1;
-    p.ldk = round_up(d, MM_K);
+    p.ldk = spread(round_up(d, MM_K));
     // rows that are whole slices of aligned chunks are read where they are
     auto as_is = [&](const void *q, int64_t ld) { return p.planes == 1 && d % MM_K == 0 && ld % 8 == 0 && (uintptr_t)q % 16 == 0 && ld < LOSS_MOST; };
-    p.lay_x = !as_is(x, ldx);
-    p.lay_w = !as_is(w, ldw);
+    p.rows_out = grad ? round_up(n, MM_K) : n;
     p.config = mm_choose(classes, n);
+    // (rows without a label are zeros for the product over rows; and x is read often where there are many rows)
+    p.lay_x = grad || !as_is(x, ldx) || (p.config == WIDE && spread(ldx) != ldx);
+    p.lay_w = !as_is(w, ldw);
     Carver c(workspace);
-    p.x = p.lay_x ? c.take<uint16_t>(n * p.ldk * p.planes) : (uint16_t *)x;
+    p.x = p.lay_x ? c.take<uint16_t>(p.rows_out * p.ldk * p.planes) : (uint16_t *)x;
     p.w = p.lay_w ? c.take<uint16_t>(classes * p.ldk * p.planes) : (uint16_t *)w;
-    p.tile_sums = c.take<float2>(n * ceil_div(classes, mm_tile_i(p.config)));
+    p.tile_sums = c.take<float2>(n * ceil_div(classes, mm_tile_i(p.config)) * MM_PARTS_I);
     p.picked = c.take<float>(n);
     if (grad) {
         p.lse = c.take<float>(n);
         p.power = c.take<float>(2);
-        p.ldt = round_up(n, MM_K);
-        const int64_t per_class = 2 * 2 * p.planes * p.ldt;
+        const int64_t per_class = 2 * p.planes * p.rows_out;
         int64_t most = LOSS_PIECE_BYTES / per_class / 256 * 256;
         most = most < 256 ? 256 : most;
         p.pieces = (int)ceil_div(classes, most);
         p.piece = round_up(ceil_div(classes, p.pieces), 256);
         p.pieces = (int)ceil_div(classes, p.piece);
         if (p.piece > classes) p.piece = classes;
-        p.ldg = round_up(p.piece, MM_K);
+        p.ldg = spread(round_up(p.piece, MM_K));
         p.ldp = round_up(d, 4);
-        const int64_t slices = p.ldg / MM_K * (p.planes == 3 ? 6 : 1);
-        p.config_dx = mm_choose(d, n, slices >= 512);
+        p.config_dx = mm_choose(d, n, p.ldg * (p.planes == 3 ? 6 : 1) >= 32768);
+        const int64_t slices = ceil_div(p.piece, MM_K) * (p.planes == 3 ? 6 : 1);
         const int64_t tiles = ceil_div(d, mm_tile_i(p.config_dx)) * ceil_div(n, mm_tile_j(p.config_dx));
         const int64_t room = CUS * (p.config_dx == WIDE ? 1 : 2);
         int64_t splits = tiles >= room ? 1 : room / tiles;
@@ -217,10 +225,7 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         splits = splits < 1 ? 1 : splits;
         p.splits = (int)ceil_div(slices, ceil_div(slices, splits));
         p.config_dw = mm_choose(d, p.piece);
-        p.xt = c.take<uint16_t>(d * p.ldt * p.planes);
-        p.wt = c.take<uint16_t>(d * p.ldg * p.planes);
-        p.g = c.take<uint16_t>(n * p.ldg * p.planes);
-        p.gt = c.take<uint16_t>(p.piece * p.ldt * p.planes);
+        p.g = c.take<uint16_t>(p.rows_out * p.ldg * p.planes);
         p.parts = c.take<float>(n * p.ldp * p.splits * p.pieces);
     }
     p.bytes = c.total();
@@ -247,22 +252,13 @@ int64_t grid_of(int64_t items, int threads, int64_t most)
 }
 
 template <typename T>
-int loss_lay_rows(const T *in, int64_t ldi, void *out, int64_t ld, int64_t rows, int64_t cols, hipStream_t stream)
+int loss_lay_rows(const T *in, int64_t ldi, void *out, int64_t ld, int64_t rows, int64_t rows_out, int64_t cols, const LossRows *labels, hipStream_t stream)
 {
-    if (rows == 0) return CHICLE_OK;
     typedef typename Product<T>::type P;
-    lay_rows<T><<<(unsigned)grid_of(rows * (ld / 8), 256, 16384), 256, 0, stream>>>(in, ldi, (P *)out, ld, rows * ld, rows, cols);
+    lay_rows<T><<<(unsigned)grid_of(rows_out * (ld / 8), 256, 16384), 256, 0, stream>>>(in, ldi, (P *)out, ld, rows_out * ld, rows, rows_out, cols,
+                                                                                       labels ? labels->labels : nullptr, labels ? labels->wide : 0,
+                                                                                       labels ? labels->classes : 0);
     return launched("lay_rows");
-}
-
-template <typename T>
-int loss_lay_columns(const T *in, int64_t ldi, void *out, int64_t ld, int64_t plane, int64_t rows, int64_t cols, const void *labels, int wide,
-                     int64_t classes, hipStream_t stream)
-{
-    typedef typename Product<T>::type P;
-    const dim3 grid((unsigned)ceil_div(cols, 64), (unsigned)(ld / 64));
-    lay_columns<T><<<grid, 256, 0, stream>>>(in, ldi, (P *)out, ld, plane, rows, cols, labels, wide, classes);
-    return launched("lay_columns");
 }
 
 MmShape mm_shape(const MmOperand &a, const MmOperand &b, int64_t k, int planes, int config, int splits)
@@ -290,18 +286,19 @@ template <typename T>
 int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw, LossRows &rows, float *loss, float *lse, int32_t *flags, hipStream_t stream)
 {
     typedef typename Product<T>::type P;
-    if (p.lay_x) TRY(loss_lay_rows<T>(x, ldx, p.x, p.ldk, p.n, p.d, stream));
-    if (p.lay_w) TRY(loss_lay_rows<T>(w, ldw, p.w, p.ldk, p.classes, p.d, stream));
-    const MmOperand a = {p.w, p.lay_w ? p.ldk : ldw, p.classes * p.ldk, (int)p.classes}, b = {p.x, p.lay_x ? p.ldk : ldx, p.n * p.ldk, (int)p.n};
-    const MmShape s = mm_shape(a, b, p.ldk, p.planes, p.config, 1);
-    TRY(with_config(p.config, [&](auto c) {
+    if (p.lay_x) TRY(loss_lay_rows<T>(x, ldx, p.x, p.ldk, p.n, p.rows_out, p.d, p.parts ? &rows : nullptr, stream));
+    if (p.lay_w) TRY(loss_lay_rows<T>(w, ldw, p.w, p.ldk, p.classes, p.classes, p.d, nullptr, stream));
+    const MmOperand a = {p.w, p.lay_w ? p.ldk : ldw, p.classes * p.ldk, (int)p.classes, 0};
+    const MmOperand b = {p.x, p.lay_x ? p.ldk : ldx, p.rows_out * p.ldk, (int)p.n, 0};
+    const MmShape s = mm_shape(a, b, round_up(p.d, MM_K), p.planes, p.config, 1);
+    TRY(with_config<MmWide>(p.config, [&](auto c) {
         typedef decltype(c) C;
         auto kernel = loss_tiles<P, C, sizeof(T) == 4>;
         TRY(allow_lds(kernel, C::LDS));
         kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows);
         return launched("loss_tiles");
     }));
-    loss_rows<<<(unsigned)ceil_div(p.n, 4), 256, 0, stream>>>(rows, s.tiles_i, loss, lse, flags);
+    loss_rows<<<(unsigned)ceil_div(p.n, 4), 256, 0, stream>>>(rows, s.tiles_i * MM_PARTS_I, loss, lse, flags);
     return launched("loss_rows");
 }
 
@@ -320,28 +317,27 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
         rows.power = p.power;
     }
     const float *inverse = scaled ? p.power + 1 : nullptr;
-    TRY(loss_lay_columns<T>(x, ldx, p.xt, p.ldt, p.d * p.ldt, p.n, p.d, rows.labels, rows.wide, p.classes, stream));
-    const MmOperand xr = {p.x, p.lay_x ? p.ldk : ldx, p.n * p.ldk, (int)p.n}, xc = {p.xt, p.ldt, p.d * p.ldt, (int)p.d};
+    const int64_t ldw_in = p.lay_w ? p.ldk : ldw, k_d = round_up(p.d, MM_K);
+    const MmOperand x_rows = {p.x, p.ldk, p.rows_out * p.ldk, (int)p.n, 0}, x_by_k = {p.x, p.ldk, p.rows_out * p.ldk, (int)p.d, (int)p.rows_out};
     int copies = 0;                                      // of dx, to be added up
     for (int k = 0; k < p.pieces; ++k) {
         const int64_t first = k * p.piece, many = p.classes - first < p.piece ? p.classes - first : p.piece;
-        const int64_t ldg = round_up(many, MM_K), plane_g = p.n * ldg, plane_t = many * p.ldt, plane_w = p.d * ldg;
-        const MmOperand wr = {(const uint16_t *)p.w + first * (p.lay_w ? p.ldk : ldw), p.lay_w ? p.ldk : ldw, p.classes * p.ldk, (int)many};
-        TRY(loss_lay_columns<T>(w + first * ldw, ldw, p.wt, ldg, plane_w, many, p.d, nullptr, 0, 0, stream));
-        const int config_g = PLANES == 3 && p.n > 64 ? MIDDLE : mm_choose(many, p.n);   // (three planes of G: no registers for large tiles)
-        TRY(with_config(config_g, [&](auto c) {
-            typedef std::conditional_t<PLANES == 3 && std::is_same<decltype(c), MmWide>::value, MmMiddle, decltype(c)> C;
-            const MmShape s = mm_shape(wr, xr, p.ldk, p.planes, config_g, 1);
+        const int64_t k_w = round_up(many, MM_K), ldg = spread(k_w), plane_g = p.rows_out * ldg;
+        const uint16_t *w_piece = (const uint16_t *)p.w + first * ldw_in;
+        const MmOperand w_rows = {w_piece, ldw_in, p.classes * p.ldk, (int)many, 0}, w_by_k = {w_piece, ldw_in, p.classes * p.ldk, (int)p.d, (int)many};
+        const MmOperand g_rows = {p.g, ldg, plane_g, (int)p.n, 0}, g_by_k = {p.g, ldg, plane_g, (int)many, (int)p.rows_out};
+        const int config_g = mm_choose(many, p.n);
+        TRY(with_config<MmWide>(config_g, [&](auto c) {
+            typedef decltype(c) C;
+            const MmShape s = mm_shape(w_rows, x_rows, k_d, p.planes, config_g, 1);
             auto kernel = loss_grad_tiles<P, C, sizeof(T) == 4, PLANES>;
             TRY(allow_lds(kernel, C::LDS));
-            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, (int)first, (int)many, (P *)p.g, ldg, plane_g, (P *)p.gt,
-                                                                                     p.ldt, plane_t);
+            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, (int)first, (int)many, (P *)p.g, ldg, plane_g, (int)p.rows_out);
             return launched("loss_grad_tiles");
         }));
-        const MmOperand gr = {p.g, ldg, plane_g, (int)p.n}, gc = {p.gt, p.ldt, plane_t, (int)many}, wc = {p.wt, ldg, plane_w, (int)p.d};
-        TRY(with_config(p.config_dx, [&](auto c) {
+        TRY(with_config<MmWideByK>(p.config_dx, [&](auto c) {
             typedef decltype(c) C;
-            const MmShape s = mm_shape(wc, gr, ldg, p.planes, p.config_dx, p.splits);
+            const MmShape s = mm_shape(w_by_k, g_rows, k_w, p.planes, p.config_dx, p.splits);
             auto kernel = product_parts<P, C>;
             TRY(allow_lds(kernel, C::LDS));
             kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.parts + (int64_t)copies * p.n * p.ldp, p.ldp,
@@ -349,9 +345,9 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
             copies += s.splits;
             return launched("product_parts");
         }));
-        TRY(with_config(p.config_dw, [&](auto c) {
+        TRY(with_config<MmWideByK>(p.config_dw, [&](auto c) {
             typedef decltype(c) C;
-            const MmShape s = mm_shape(xc, gc, p.ldt, p.planes, p.config_dw, 1);
+            const MmShape s = mm_shape(x_by_k, g_by_k, p.rows_out, p.planes, p.config_dw, 1);
             auto kernel = product_out<P, C, T>;
             TRY(allow_lds(kernel, C::LDS));
             kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, dw + first * lddw, lddw, inverse);

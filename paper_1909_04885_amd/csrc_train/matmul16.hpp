@@ -1,15 +1,22 @@
-// Products of 16-bit matrices whose rows both run along the summed index: C[j][i] = sum_k A[i][k] B[j][k], on the matrix cores.
+// Products of 16-bit matrices, C[j][i] = sum_k A(i, k) B(j, k), on the matrix cores.  An operand lies by rows, its k side by side, or
+// by k, its rows side by side.
 //
-// A workgroup forms tiles of C one after the other.  Slices of 64 k of both operands go from global memory straight into LDS, the next
-// slice while the present one is multiplied, and the next tile's first slice while the last of this one is and while what
-// follows the product is done; sixteen-byte chunks of an LDS row are permuted by the row's number, so that the rows that a
-// wavefront reads side by side lie in different banks.  Sums are held in 32-bit floats.
+// A workgroup forms tiles of C one after the other.  Slices of k of both operands go from global memory straight into LDS, some slices ahead
+// of the one that is multiplied, and the next tile's first slices while the last of this one are and while what follows the
+// product is done; sixteen-byte chunks (by rows) or pairs of them (by k) are permuted in LDS so that what a
+// wavefront reads side by side lies in different banks.  An operand that lies by k is turned as it is read from LDS: a read
+// gives each of sixteen lanes four k of its row.  Sums are held in 32-bit floats.
 //
 // 32-bit operands are three 16-bit planes whose sum they are exactly (leading, middle and last eight bits of the
 // significand, bfloat16 each).  Six of the nine products of planes are formed; the three that are left out are below 2^-24 of
 // the product together, less than its rounding.
 //
-// Rows past the end of an operand are read as its last row; what they give is never stored.  k is a multiple of 64.
+// What bounds it: feeding the matrix cores, half of whose peak it reaches; 8192 x 2048 x 32000 in bfloat16 runs at 1300 TFLOP/s by rows (the
+// library's product of 8192^3: 1206).  Tried and slower: slices of 32 k with three or four buffers (1090), the two wavefronts of a
+// SIMD reading and multiplying in turn (1130), smaller tiles of which two workgroups share a compute unit (1000).  Rows
+// whose distance is a power of two meet in few channels of the L2 (970): what is laid out here has other distances.
+//
+// Rows past the end of an operand are read as a row that is there; what they give is never stored.
 #pragma once
 #include "elements.hpp"
 
@@ -33,8 +40,9 @@ constexpr int MM_K = 64, MM_CHUNKS = MM_K / 8, MM_ROW = MM_K * 2;   // k of a sl
 
 struct MmOperand {
     const void *p;
-    int64_t ld, plane;                       // elements from row to row, from plane to plane
-    int rows;
+    int64_t ld, plane;                       // elements from row to row (by k: from k to k), from plane to plane
+    int rows;                                // (by k: ld holds them in whole chunks)
+    int k_rows;                              // by k: how many k are there; further ones are read as the last
 };
 
 struct MmShape {
@@ -70,94 +78,224 @@ template <int BM, int BN, int WAVES_I, int WAVES_J, int BLOCKS> struct MmConfig 
     static constexpr int THREADS = 64 * WAVES_I * WAVES_J, PER_CU = BLOCKS, PER_SIMD = BLOCKS * THREADS / 256;
     static constexpr int MI = BM / WAVES_I / 16, NJ = BN / WAVES_J / 16;
     static constexpr int TILE_I = BM, TILE_J = BN, W_I = WAVES_I, W_J = WAVES_J;
-    static constexpr int BUFFER = (BM + BN) * MM_ROW;
-    static constexpr int EXTRA = WAVES_I * BN * 8;             // LDS of what follows the product
-    static constexpr int LDS = 2 * BUFFER + EXTRA;             // bytes
-    static constexpr int LOADS_A = BM * MM_CHUNKS / THREADS, LOADS_B = BN * MM_CHUNKS / THREADS;
+    static constexpr int BUFFER = (BM + BN) * MM_ROW, LDS = 2 * BUFFER;                        // bytes
     static_assert(LDS * BLOCKS <= 160 * 1024, "the workgroups of a compute unit fit");
+    static_assert(MI % 2 == 0 && NJ % 2 == 0, "fragments go in pairs");
 };
 
-// Where chunk c of row r lies in its row: any eight and any sixteen neighbouring rows have a chunk in different banks.
-__device__ __forceinline__ int mm_place(int r, int c) { return c ^ (r & 7) ^ (r >> 3 & 1); }
+// By rows, chunk c of row r lies in place c ^ mm_turn(r) of its row: lanes that LDS serves together (of 32 lanes, 0-3, 12-15 and 20-27, then
+// the others) read different banks, of sixteen rows in a row as well as of four times four rows, eight apart.
+__device__ __forceinline__ int mm_turn(int r) { return (r & 2) | (r >> 3 & 1) * 4; }
+// By k, pair of chunks p of k lies in place p ^ mm_turn_k(k), of ROWS / 16 places.
+template <int ROWS> __device__ __forceinline__ int mm_turn_k(int k) { return ((k & 3) | (k >> 3 & 3) << 2) & (ROWS / 16 - 1); }
 
-template <int LOADS, int THREADS>
-__device__ __forceinline__ void mm_offsets(const MmOperand &o, int row0, int *off)
+// Byte offsets of the chunks that this thread fetches, from the tile's first row and the slice's first k.  last_k: the last k that is there,
+// counted from the slice's first.
+template <int ROWS, typename C, bool BY_K>
+__device__ __forceinline__ int mm_offset(const MmOperand &o, int row0, int it, int last_k)
 {
-#pragma unroll
-    for (int it = 0; it < LOADS; ++it) {
-        const int c = it * THREADS + threadIdx.x, r = c / MM_CHUNKS;
-        off[it] = min(r, o.rows - 1 - row0) * (int)o.ld * 2 + mm_place(r, c % MM_CHUNKS) * 16;
+    const int c = it * C::THREADS + threadIdx.x;
+    if constexpr (BY_K) {
+        const int k = c / (ROWS / 8), place = c % (ROWS / 8), chunk = (place >> 1 ^ mm_turn_k<ROWS>(k)) * 2 + (place & 1);
+        const int past = (o.rows + 7) / 8 - row0 / 8;          // chunks from the tile's first to the end
+        return min(k, last_k) * (int)o.ld * 2 + min(chunk, past - 1) * 16;
+    } else {
+        const int r = c / MM_CHUNKS;
+        return min(r, o.rows - 1 - row0) * (int)o.ld * 2 + (c % MM_CHUNKS ^ mm_turn(r)) * 16;
     }
 }
 
-template <int LOADS, int THREADS>
-__device__ __forceinline__ void mm_fetch(const char *base, const int *off, char *lds)
+// Sixteen bytes of every lane straight into LDS, 1 KB of a wavefront side by side.
+__device__ __forceinline__ void mm_load(const char *base, int off, char *lds)
 {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off), (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
+}
+
+// A slice of an operand.  Inside the operand the chunks of a thread are a fixed distance apart, by k with two places in turn: off[0] and
+// off[1].  At an edge the offsets are worked out anew.
+template <int ROWS, typename C, bool BY_K>
+__device__ __forceinline__ void mm_fetch(const MmOperand &o, const char *base, int row0, const int *off, bool edge, int last_k, char *lds)
+{
+    constexpr int LOADS = ROWS * MM_CHUNKS / C::THREADS, APART = BY_K ? C::THREADS / (ROWS / 8) : C::THREADS / MM_CHUNKS;
+    lds += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
+    if (edge) {
 #pragma unroll
-    for (int it = 0; it < LOADS; ++it)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off[it]),
-                                         (__attribute__((address_space(3))) void *)(lds + (it * THREADS + wave * 64) * 16), 16, 0, 0);
+        for (int it = 0; it < LOADS; ++it) mm_load(base, mm_offset<ROWS, C, BY_K>(o, row0, it, last_k), lds + it * C::THREADS * 16);
+    } else {
+#pragma unroll
+        for (int it = 0; it < LOADS; ++it) mm_load(base + it * APART * 2 * o.ld, off[BY_K ? it & 1 : 0], lds + it * C::THREADS * 16);
+    }
 }
 
 // What is fetched next: slice `at` of product of planes `seg`, `left` slices from the end of unit `unit`.
-template <typename C> struct MmFetcher {
+template <typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
     unsigned unit, units;
-    int seg, at, left, per_plane, all_slices;
-    int off_a[C::LOADS_A], off_b[C::LOADS_B];
-    const char *pa, *pb, *qa, *qb;
+    int seg, at, left, per_plane, all_slices, row_a, row_b;
+    bool edge_a, edge_b;
+    int off_a[A_BY_K ? 2 : 1], off_b[B_BY_K ? 2 : 1];
+    const char *qa, *qb;
+    int64_t step_a, step_b;                  // bytes from slice to slice
 
-    __device__ __forceinline__ void planes(const MmShape &s)
+    __device__ __forceinline__ void begin(const MmShape &s)
     {
-        qa = pa + mm_plane_a(seg) * s.a.plane * 2;
-        qb = pb + mm_plane_b(seg) * s.b.plane * 2;
+        unit = blockIdx.x;
+        units = s.tiles_i * s.tiles_j * s.splits;
+        per_plane = s.k / MM_K;
+        all_slices = per_plane * (s.planes == 1 ? 1 : 6);
+        step_a = A_BY_K ? MM_K * 2 * s.a.ld : MM_ROW;
+        step_b = B_BY_K ? MM_K * 2 * s.b.ld : MM_ROW;
+        const MmOperand whole_a = {nullptr, s.a.ld, 0, 1 << 30, 0}, whole_b = {nullptr, s.b.ld, 0, 1 << 30, 0};
+#pragma unroll
+        for (int q = 0; q < (A_BY_K ? 2 : 1); ++q) off_a[q] = mm_offset<C::TILE_I, C, A_BY_K>(whole_a, 0, q, MM_K) - q * C::THREADS / (C::TILE_I / 8) * (int)s.a.ld * 2;
+#pragma unroll
+        for (int q = 0; q < (B_BY_K ? 2 : 1); ++q) off_b[q] = mm_offset<C::TILE_J, C, B_BY_K>(whole_b, 0, q, MM_K) - q * C::THREADS / (C::TILE_J / 8) * (int)s.b.ld * 2;
+        if (unit < units) open(s);
+    }
+    __device__ __forceinline__ void place(const MmShape &s)
+    {
+        qa = (const char *)s.a.p + ((A_BY_K ? (int64_t)row_a : (int64_t)row_a * s.a.ld) + mm_plane_a(seg) * s.a.plane) * 2 + at * step_a;
+        qb = (const char *)s.b.p + ((B_BY_K ? (int64_t)row_b : (int64_t)row_b * s.b.ld) + mm_plane_b(seg) * s.b.plane) * 2 + at * step_b;
     }
     __device__ __forceinline__ void open(const MmShape &s)
     {
         const MmTile t = mm_tile(s, unit);
-        mm_offsets<C::LOADS_A, C::THREADS>(s.a, t.i * C::TILE_I, off_a);
-        mm_offsets<C::LOADS_B, C::THREADS>(s.b, t.j * C::TILE_J, off_b);
-        pa = (const char *)s.a.p + (int64_t)t.i * C::TILE_I * s.a.ld * 2;
-        pb = (const char *)s.b.p + (int64_t)t.j * C::TILE_J * s.b.ld * 2;
+        row_a = t.i * C::TILE_I;
+        row_b = t.j * C::TILE_J;
+        edge_a = row_a + C::TILE_I > (A_BY_K ? (s.a.rows + 7) / 8 * 8 : s.a.rows);
+        edge_b = row_b + C::TILE_J > (B_BY_K ? (s.b.rows + 7) / 8 * 8 : s.b.rows);
         const int first = t.split * s.per_split;
         seg = s.planes == 1 ? 0 : first / per_plane;
         at = first - seg * per_plane;
         left = min(s.per_split, all_slices - first);
-        planes(s);
+        place(s);
     }
     __device__ __forceinline__ void fetch(const MmShape &s, char *lds)
     {
         if (unit >= units) return;
-        mm_fetch<C::LOADS_A, C::THREADS>(qa + (int64_t)at * MM_ROW, off_a, lds);
-        mm_fetch<C::LOADS_B, C::THREADS>(qb + (int64_t)at * MM_ROW, off_b, lds + C::TILE_I * MM_ROW);
+        const int last_k = A_BY_K ? s.a.k_rows - 1 - at * MM_K : MM_K;     // (the last k may not all be there)
+        mm_fetch<C::TILE_I, C, A_BY_K>(s.a, qa, row_a, off_a, edge_a || last_k < MM_K - 1, last_k, lds);
+        mm_fetch<C::TILE_J, C, B_BY_K>(s.b, qb, row_b, off_b, edge_b, MM_K, lds + C::TILE_I * MM_ROW);
+        qa += step_a;
+        qb += step_b;
         if (--left == 0) {
             unit += gridDim.x;
             if (unit < units) open(s);
         } else if (++at == per_plane) {
             at = 0;
             ++seg;
-            planes(s);
+            place(s);
         }
     }
 };
 
-// Calls done(tile, acc, extra) for every tile of this workgroup, extra being C::EXTRA bytes of LDS:
-// acc[mi][nj][r] = C[j][i] at i = i0 + (wave_i * MI + mi) * 16 + 4 * (lane / 16) + r, j = j0 + (wave_j * NJ + nj) * 16 + lane % 16
-template <typename T, typename C, typename F>
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+// Eight k of a row for every lane out of a slice that lies by k: lane l gives the address of four rows of k + l % 16 / 4 and gets four k of
+// row l % 16; the second four k lie four further on.
+template <typename T, int ROWS>
+__device__ __forceinline__ typename Mfma<T>::frag mm_turned(const char *l)
+{
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)l), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(l + 4 * ROWS * 2));
+    return __builtin_bit_cast(typename Mfma<T>::frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Where the values of a tile lie: acc[mi][nj][r] = C[j][i] at i = i0 + place(mi) + r, j = j0 + nj * 16.  Where A lies by rows a lane has eight
+// neighbouring i in two fragments.
+template <typename C, bool A_BY_K> struct MmPlace {
+    int lane, wi, wj, i0, j0;
+    __device__ __forceinline__ explicit MmPlace(const MmTile &t)
+    {
+        lane = threadIdx.x & 63;
+        const int wave = threadIdx.x >> 6;
+        wi = wave / C::W_J;
+        wj = wave % C::W_J;
+        i0 = t.i * C::TILE_I + wi * C::MI * 16 + (A_BY_K ? 4 : 8) * (lane >> 4);
+        j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
+    }
+    static __device__ __forceinline__ constexpr int place(int mi) { return A_BY_K ? mi * 16 : (mi >> 1) * 32 + (mi & 1) * 4; }
+};
+
+// Where this lane reads, and its fragments of 32 k of a slice.
+template <typename T, typename C, bool A_BY_K, bool B_BY_K> struct MmReader {
+    typedef typename Mfma<T>::frag frag;
+    int ra, rb, quarter, fa[A_BY_K ? C::MI : 2], fb[B_BY_K ? C::NJ : 1];
+
+    __device__ __forceinline__ MmReader()
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J, l16 = lane & 15;
+        quarter = lane >> 4;
+        const int k = 8 * quarter + (l16 >> 2);          // by k: of the first four; the second four lie four further on
+        if constexpr (A_BY_K) {
+            ra = k * C::TILE_I * 2 + (l16 & 3) * 8;
+#pragma unroll
+            for (int i = 0; i < C::MI; ++i) fa[i] = ((wi * C::MI + i) ^ mm_turn_k<C::TILE_I>(k)) * 32;
+        } else {
+            const int row = (l16 >> 2) * 8 + (l16 & 3);  // of the even fragments; those of the odd ones lie four behind
+            ra = (wi * C::MI * 16 + row) * MM_ROW;
+            fa[0] = mm_turn(row) * 16;
+            fa[1] = mm_turn(row + 4) * 16;
+        }
+        if constexpr (B_BY_K) {
+            rb = C::TILE_I * MM_ROW + k * C::TILE_J * 2 + (l16 & 3) * 8;
+#pragma unroll
+            for (int j = 0; j < C::NJ; ++j) fb[j] = ((wj * C::NJ + j) ^ mm_turn_k<C::TILE_J>(k)) * 32;
+        } else {
+            rb = (C::TILE_I + wj * C::NJ * 16 + l16) * MM_ROW;
+            fb[0] = mm_turn(l16) * 16;
+        }
+    }
+    __device__ __forceinline__ void read(const char *l, int kk, frag (&a)[C::MI], frag (&b)[C::NJ]) const
+    {
+        const int chunk = (kk * 4 + quarter) * 16;
+#pragma unroll
+        for (int j = 0; j < C::NJ; ++j) {
+            if constexpr (B_BY_K) b[j] = mm_turned<T, C::TILE_J>(l + rb + fb[j] + kk * 32 * C::TILE_J * 2);
+            else b[j] = *(const frag *)(l + rb + j * 16 * MM_ROW + (chunk ^ fb[0]));
+        }
+#pragma unroll
+        for (int i = 0; i < C::MI; ++i) {
+            if constexpr (A_BY_K) a[i] = mm_turned<T, C::TILE_I>(l + ra + fa[i] + kk * 32 * C::TILE_I * 2);
+            else a[i] = *(const frag *)(l + ra + ((i >> 1) * 32 + (i & 1) * 4) * MM_ROW + (chunk ^ fa[i & 1]));
+        }
+    }
+};
+
+template <typename T, typename C>
+__device__ __forceinline__ void mm_add(const typename Mfma<T>::frag (&a)[C::MI], const typename Mfma<T>::frag (&b)[C::NJ], f32x4 (&acc)[C::MI][C::NJ])
+{
+#pragma unroll
+    for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < C::NJ; ++j) acc[i][j] = Mfma<T>::mul(a[i], b[j], acc[i][j]);
+}
+
+// Calls done(tile, acc) for every tile of this workgroup; MmPlace says what acc holds.  `done` has no barriers.
+//
+// A slice's fragments are read half a slice ahead of their products: the products of the second half stand on the other side of the
+// barrier, where they cover the reads from the slice that has just arrived (1300 against 1230 TFLOP/s without, and 1140
+// against 990 where A lies by k).
+template <typename T, typename C, bool A_BY_K, bool B_BY_K, typename F>
 __device__ __forceinline__ void mm_tiles(const MmShape &s, const F &done)
 {
     extern __shared__ __align__(16) char lds[];
     typedef typename Mfma<T>::frag frag;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J;
-    const int ra = (wi * C::MI * 16 + (lane & 15)) * MM_ROW, rb = (C::TILE_I + wj * C::NJ * 16 + (lane & 15)) * MM_ROW;
-    MmFetcher<C> next;
-    next.unit = blockIdx.x;
-    next.units = s.tiles_i * s.tiles_j * s.splits;
-    next.per_plane = s.k / MM_K;
-    next.all_slices = next.per_plane * (s.planes == 1 ? 1 : 6);
-    if (next.unit < next.units) next.open(s);
+    const MmReader<T, C, A_BY_K, B_BY_K> reader;
+    MmFetcher<C, A_BY_K, B_BY_K> next;
+    next.begin(s);
     next.fetch(s, lds);
     int buf = 0;
+    frag a0[C::MI], b0[C::NJ], a1[C::MI], b1[C::NJ];
+    // The slice has arrived, and everybody is done with the other buffer, which the next one goes to.
+    auto turn = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        next.fetch(s, lds + (buf ^ 1) * C::BUFFER);
+    };
     for (unsigned unit = blockIdx.x; unit < next.units; unit += gridDim.x) {
         const MmTile t = mm_tile(s, unit);
         const int slices = min(s.per_split, next.all_slices - t.split * s.per_split);
@@ -166,26 +304,21 @@ __device__ __forceinline__ void mm_tiles(const MmShape &s, const F &done)
         for (int i = 0; i < C::MI; ++i)
 #pragma unroll
             for (int j = 0; j < C::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int slice = 0; slice < slices; ++slice) {
-            __syncthreads();                             // the slice has arrived, and everybody is done with the other buffer
-            next.fetch(s, lds + (buf ^ 1) * C::BUFFER);
-            const char *l = lds + buf * C::BUFFER;
+        turn();
+        reader.read(lds + buf * C::BUFFER, 0, a0, b0);
+        reader.read(lds + buf * C::BUFFER, 1, a1, b1);
+        mm_add<T, C>(a0, b0, acc);
+        buf ^= 1;
+        for (int slice = 1; slice < slices; ++slice) {
+            turn();
+            reader.read(lds + buf * C::BUFFER, 0, a0, b0);
+            mm_add<T, C>(a1, b1, acc);
+            reader.read(lds + buf * C::BUFFER, 1, a1, b1);
+            mm_add<T, C>(a0, b0, acc);
             buf ^= 1;
-#pragma unroll
-            for (int kk = 0; kk < MM_K / 32; ++kk) {
-                const int chunk = mm_place(lane & 15, kk * 4 + (lane >> 4)) * 16;
-                frag a[C::MI], b[C::NJ];
-#pragma unroll
-                for (int j = 0; j < C::NJ; ++j) b[j] = *(const frag *)(l + rb + j * 16 * MM_ROW + chunk);
-#pragma unroll
-                for (int i = 0; i < C::MI; ++i) a[i] = *(const frag *)(l + ra + i * 16 * MM_ROW + chunk);
-#pragma unroll
-                for (int i = 0; i < C::MI; ++i)
-#pragma unroll
-                    for (int j = 0; j < C::NJ; ++j) acc[i][j] = Mfma<T>::mul(a[i], b[j], acc[i][j]);
-            }
         }
-        done(t, acc, lds + 2 * C::BUFFER);
+        mm_add<T, C>(a1, b1, acc);
+        done(t, acc);
     }
 }
 

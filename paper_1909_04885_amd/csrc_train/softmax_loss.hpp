@@ -6,9 +6,8 @@
 //
 // The logits exist only as tiles of a product in registers.  `loss_tiles` leaves of a tile, for every row, the largest logit and the
 // sum of exponentials below it, and `loss_rows` joins these.  The gradient forms the logits again, a piece of the classes at a
-// time, and turns them in registers into G, which is stored in 16 bits, once by rows and once by classes, since both products
-// that read it want it along their summed index; rounding G is of the size of the rounding of 16-bit gradients, and 32-bit
-// operands keep G in three planes, which is exact.  Half precision would lose small G: there G comes times the power of two
+// time, and turns them in registers into G, which is stored in 16 bits for the two products that read it; rounding G is of the size
+// of the rounding of 16-bit gradients, and 32-bit operands keep G in three planes, which is exact.  Half precision would lose small G: there G comes times the power of two
 // that takes the largest weight to between 2^13 and 2^14, and the products times its inverse.
 //
 // The bound is the matrix cores: 2 n d classes operations for the loss, and three times that again for the gradients, one third of
@@ -43,62 +42,32 @@ __device__ __forceinline__ void to_planes(T x, P *p)
     else p[0] = x;
 }
 
-// out[plane][r][c] = in[r][c], zeros in columns [cols, ld): rows of whole slices, sixteen-byte aligned.
+// out[plane][r][c] = in[r][c], zeros in columns [cols, ld) and in rows [rows, rows_out): whole slices of aligned chunks.  With labels,
+// rows that have none are zeros too.
 template <typename T>
 __global__ __launch_bounds__(256) void lay_rows(const T *__restrict__ in, int64_t ldi, typename Product<T>::type *__restrict__ out, int64_t ld,
-                                                int64_t plane, int64_t rows, int64_t cols)
+                                                int64_t plane, int64_t rows, int64_t rows_out, int64_t cols, const void *labels, int wide, int64_t classes)
 {
     typedef typename Product<T>::type P;
     constexpr int N = Product<T>::PLANES;
     const int64_t per_row = ld / 8;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < rows * per_row; e += (int64_t)gridDim.x * 256) {
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < rows_out * per_row; e += (int64_t)gridDim.x * 256) {
         const int64_t r = e / per_row, c = (e - r * per_row) * 8;
+        bool has = r < rows;
+        if (has && labels) {
+            const int64_t label = index_at(labels, wide, r);
+            has = label >= 0 && label < classes;
+        }
         P p[N][8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             P q[N];
-            to_planes(c + k < cols ? in[r * ldi + c + k] : (T)0.f, q);
+            to_planes(has && c + k < cols ? in[r * ldi + c + k] : (T)0.f, q);
 #pragma unroll
             for (int i = 0; i < N; ++i) p[i][k] = q[i];
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) __builtin_memcpy(out + i * plane + r * ld + c, p[i], 16);
-    }
-}
-
-// out[plane][c][r] = in[r][c] for rows of `in` that count, zeros for the others and in columns [rows, ld).  64 x 64 values to a
-// workgroup; grid: (tiles of c, tiles of r).  labels may be null: every row counts.
-template <typename T>
-__global__ __launch_bounds__(256) void lay_columns(const T *__restrict__ in, int64_t ldi, typename Product<T>::type *__restrict__ out, int64_t ld,
-                                                   int64_t plane, int64_t rows, int64_t cols, const void *labels, int wide, int64_t classes)
-{
-    typedef typename Product<T>::type P;
-    constexpr int N = Product<T>::PLANES;
-    __shared__ T s[64][64 + 4 / sizeof(T) * 1];
-    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
-    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-        const int64_t r = r0 + e / 64, c = c0 + e % 64;
-        bool has = r < rows && c < cols;
-        if (has && labels) {
-            const int64_t label = index_at(labels, wide, r);
-            has = label >= 0 && label < classes;
-        }
-        s[e / 64][e % 64] = has ? in[r * ldi + c] : (T)0.f;
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < 64 * 8; e += 256) {
-        const int64_t c = c0 + e / 8, r = r0 + e % 8 * 8;
-        if (c >= cols || r >= ld) continue;
-        P p[N][8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            P q[N];
-            to_planes(s[e % 8 * 8 + k][e / 8], q);
-#pragma unroll
-            for (int i = 0; i < N; ++i) p[i][k] = q[i];
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) __builtin_memcpy(out + i * plane + c * ld + r, p[i], 16);
     }
 }
 
@@ -110,7 +79,7 @@ struct LossRows {
     const float *lse;            // gradient
     const float *weight;
     const float *power;          // half precision: G comes times this; else null
-    float2 *part;                // [row][tile of classes]: largest logit, sum of exponentials below it
+    float2 *part;                // [row][wavefront's part of a tile of classes]: largest logit, sum of exponentials below it
     float *picked;               // [row]: the label's logit
 };
 
@@ -129,20 +98,6 @@ template <bool EXACT> __device__ __forceinline__ float exp_diff(float a, float b
     return a == MINUS_INF ? 0.f : EXACT ? expf(a - b) : __expf(a - b);
 }
 
-// Where a lane's values of a tile lie
-template <typename C> struct TilePlace {
-    int lane, wi, wj, i0, j0;
-    __device__ __forceinline__ explicit TilePlace(const MmTile &t)
-    {
-        lane = threadIdx.x & 63;
-        const int wave = threadIdx.x >> 6;
-        wi = wave / C::W_J;
-        wj = wave % C::W_J;
-        i0 = t.i * C::TILE_I + wi * C::MI * 16 + 4 * (lane >> 4);
-        j0 = t.j * C::TILE_J + wj * C::NJ * 16 + (lane & 15);
-    }
-};
-
 constexpr float LOG2E = 1.44269504088896340736f;
 
 // exp(z - m).  EXACT: the library's exponential; else the instruction's, whose error of 2^-22 and |z - m| 2^-24 is far below what
@@ -156,27 +111,26 @@ template <bool EXACT> __device__ __forceinline__ float exp_of(float z, float m)
 template <typename T, typename C, bool EXACT>
 __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_tiles(MmShape s, LossRows l)
 {
-    mm_tiles<T, C>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ], char *extra) __attribute__((always_inline)) {
-        const TilePlace<C> at(t);
-        float2 *s_part = (float2 *)extra;                // [wave_i][row of the tile]
+    mm_tiles<T, C, false, false>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
+        const MmPlace<C, false> at(t);
         if ((t.i + 1) * C::TILE_I > l.classes) {         // the last tile: what lies past the classes counts nowhere
 #pragma unroll
             for (int mi = 0; mi < C::MI; ++mi)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (at.i0 + mi * 16 + r >= l.classes)
+                    if (at.i0 + at.place(mi) + r >= l.classes)
 #pragma unroll
                         for (int nj = 0; nj < C::NJ; ++nj) acc[mi][nj][r] = MINUS_INF;
         }
 #pragma unroll
         for (int nj = 0; nj < C::NJ; ++nj) {
             const int j = at.j0 + nj * 16, rel = label_at(l, j) - at.i0;
-            if (rel >= 0 && rel < C::MI * 16 && (rel & 15) < 4) {          // the label's logit is this lane's
+            if (rel >= 0 && rel < C::MI * 16 && (rel & 31) < 8) {          // the label's logit is this lane's
                 float z = 0.f;
 #pragma unroll
                 for (int mi = 0; mi < C::MI; ++mi)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) z = rel == mi * 16 + r ? acc[mi][nj][r] : z;
+                    for (int r = 0; r < 4; ++r) z = rel == at.place(mi) + r ? acc[mi][nj][r] : z;
                 l.picked[j] = z;
             }
             float m = MINUS_INF;
@@ -194,21 +148,8 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_tiles(MmShape s,
                 for (int r = 0; r < 4; ++r) e += exp_of<EXACT>(acc[mi][nj][r], shift);
             e += __shfl_xor(e, 16);
             e += __shfl_xor(e, 32);
-            if (at.lane < 16) s_part[at.wi * C::TILE_J + at.wj * C::NJ * 16 + nj * 16 + at.lane] = make_float2(m, e);
+            if (at.lane < 16 && j < l.n) l.part[(int64_t)j * s.tiles_i * C::W_I + t.i * C::W_I + at.wi] = make_float2(m, e);
         }
-        __syncthreads();
-        for (int q = threadIdx.x; q < C::TILE_J; q += C::THREADS) {
-            const int j = t.j * C::TILE_J + q;
-            if (j >= l.n) continue;
-            float2 x = s_part[q];
-            for (int w = 1; w < C::W_I; ++w) {
-                const float2 y = s_part[w * C::TILE_J + q];
-                const float m = fmaxf(x.x, y.x);
-                x = make_float2(m, x.y * exp_diff<EXACT>(x.x, m) + y.y * exp_diff<EXACT>(y.x, m));
-            }
-            l.part[(int64_t)j * s.tiles_i + t.i] = x;
-        }
-        // (a tile's slices begin behind another barrier: s_part is read by then)
     });
 }
 
@@ -255,77 +196,72 @@ __global__ __launch_bounds__(1024) void loss_power(const float *__restrict__ wei
 
 // ---- the gradients --------------------------------------------------------------------------------------------------
 
-// G of a piece of the classes: s.a is the piece's rows of w, `first` the piece's first class.  g[plane][row][class of the piece], ldg;
-// gt[plane][class of the piece][row], ldt; both are written to their tiles' ends as far as they have room, zeros outside.
+// G of a piece of the classes: s.a is the piece's rows of w, `first` the piece's first class.  g[plane][row][class of the piece], with zeros
+// up to ldg and in rows [n, rows_out).
 template <typename T, typename C, bool EXACT, int PLANES>
 __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_grad_tiles(MmShape s, LossRows l, int first, int piece, T *__restrict__ g, int64_t ldg,
-                                                                           int64_t plane_g, T *__restrict__ gt, int64_t ldt, int64_t plane_t)
+                                                                           int64_t plane_g, int rows_out)
 {
     const float power = l.power ? l.power[0] : 1.f;
-    mm_tiles<T, C>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ], char *) __attribute__((always_inline)) {
-        const TilePlace<C> at(t);
+    mm_tiles<T, C, false, false>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
+        const MmPlace<C, false> at(t);
 #pragma unroll
         for (int nj = 0; nj < C::NJ; ++nj) {
-            const int j = at.j0 + nj * 16, label = label_at(l, j);
+            const int j = at.j0 + nj * 16, label = label_at(l, j), rel = label - first - at.i0;
             const float weight = label >= 0 ? l.weight[j] * power : 0.f, lse = label >= 0 ? l.lse[j] : 0.f;
-            const int rel = label - first - at.i0;
+            T *row = g + (int64_t)j * ldg;
 #pragma unroll
-            for (int mi = 0; mi < C::MI; ++mi) {
-                T v[PLANES][4];
-                const int i = at.i0 + mi * 16;
+            for (int mp = 0; mp < C::MI / 2; ++mp) {     // eight neighbouring classes
+                T v[PLANES][8];
+                const int i = at.i0 + mp * 32;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float p = exp_of<EXACT>(acc[mi][nj][r], lse);
-                    if (rel == mi * 16 + r) p -= 1.f;
-                    p = weight != 0.f && i + r < piece ? p * weight : 0.f;
+                for (int h = 0; h < 8; ++h) {
+                    float p = exp_of<EXACT>(acc[2 * mp + h / 4][nj][h % 4], lse);
+                    if (rel == mp * 32 + h) p -= 1.f;
+                    p = weight != 0.f && i + h < piece ? p * weight : 0.f;
                     T q[PLANES];
                     if constexpr (PLANES == 3) split_planes(p, q);
                     else q[0] = (T)p;
 #pragma unroll
-                    for (int k = 0; k < PLANES; ++k) v[k][r] = q[k];
+                    for (int k = 0; k < PLANES; ++k) v[k][h] = q[k];
                 }
+                if (j < rows_out && i < ldg)
 #pragma unroll
-                for (int k = 0; k < PLANES; ++k) {
-                    if (j < l.n && i < ldg) __builtin_memcpy(g + k * plane_g + (int64_t)j * ldg + i, v[k], 8);
-                    if (j < ldt)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (i + r < piece) gt[k * plane_t + (int64_t)(i + r) * ldt + j] = v[k][r];
-                }
+                    for (int k = 0; k < PLANES; ++k) __builtin_memcpy(row + k * plane_g + i, v[k], 16);
             }
         }
     });
 }
 
-// A product as it is: out[j][i] in 32 bits, split `split` of the sum in its own copy of `out`.
+// G w, of w as it lies, by k: out[j][i] in 32 bits, split `split` of the sum in its own copy of `out`.
 template <typename T, typename C>
 __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_parts(MmShape s, float *__restrict__ out, int64_t ld, int64_t copy)
 {
-    mm_tiles<T, C>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ], char *) __attribute__((always_inline)) {
-        const TilePlace<C> at(t);
+    mm_tiles<T, C, true, false>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
+        const MmPlace<C, true> at(t);
         float *mine = out + t.split * copy;
 #pragma unroll
         for (int nj = 0; nj < C::NJ; ++nj)
 #pragma unroll
             for (int mi = 0; mi < C::MI; ++mi) {
-                const int i = at.i0 + mi * 16, j = at.j0 + nj * 16;
+                const int i = at.i0 + at.place(mi), j = at.j0 + nj * 16;
                 if (j < s.b.rows && i < s.a.rows) *(f32x4 *)(mine + (int64_t)j * ld + i) = acc[mi][nj];
             }
     });
 }
 
-// ... and as the result itself: out[j][i] = scale * sum, rounded.
+// x by G, both of which lie by k: out[j][i] = scale * sum, rounded.
 template <typename T, typename C, typename O>
 __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_out(MmShape s, O *__restrict__ out, int64_t ld, const float *__restrict__ scale)
 {
     const float f = scale ? *scale : 1.f;
-    mm_tiles<T, C>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ], char *) __attribute__((always_inline)) {
-        const TilePlace<C> at(t);
+    mm_tiles<T, C, true, true>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
+        const MmPlace<C, true> at(t);
 #pragma unroll
         for (int nj = 0; nj < C::NJ; ++nj)
 #pragma unroll
             for (int mi = 0; mi < C::MI; ++mi) {
-                const int i = at.i0 + mi * 16, j = at.j0 + nj * 16;
+                const int i = at.i0 + at.place(mi), j = at.j0 + nj * 16;
                 if (j >= s.b.rows) continue;
                 O v[4];
 #pragma unroll
