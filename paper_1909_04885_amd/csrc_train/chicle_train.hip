@@ -168,7 +168,9 @@ int allow_lds(K kernel, int bytes)
 struct LossPlan {
     int64_t n, d, classes, ldk;          // ldk: length of laid-out rows along d
     int planes, config;
-    bool lay_x, lay_w;
+    bool few, few_grad, tiles, lay_x, lay_w;     // few: of the loss, of the gradient; tiles: something goes by products
+    int few_blocks, few_passes, few_threads, few_chunk, few_lds, few_each, few_grad_blocks;
+    float *logits;
     // gradient
     int64_t piece, ldg, rows_out, ldp;   // classes of a piece; length of G's rows, their number; length of the rows of dx's parts
     int pieces, splits, config_dx, config_dw;
@@ -191,21 +193,49 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
     if (n == 0) return p;                                // (nothing to lay out)
     p.n = n; p.d = d; p.classes = classes;
     p.planes = type == CHICLE_F32 ? 3 : 1;
-    p.ldk = spread(round_up(d, MM_K));
     // rows that are whole slices of aligned chunks are read where they are
     auto as_is = [&](const void *q, int64_t ld) { return p.planes == 1 && d % MM_K == 0 && ld % 8 == 0 && (uintptr_t)q % 16 == 0 && ld < LOSS_MOST; };
+    p.lay_w = !as_is(w, ldw);
+    // Few rows read w as it lies; more of them where it would have to be laid out first.
+    p.few = n <= (p.lay_w ? FEW_MOST_ROWS : FEW_ROWS);
+    p.few_grad = n <= FEW_GRAD_ROWS;
+    Carver c(workspace);
+    p.picked = c.take<float>(n);
+    if (p.few) {
+        const int64_t batch = FEW_BATCH / (size_of(type) / 2), all = round_up(d, batch), per_column = n * 2 * p.planes;
+        const bool small = (all + 8) * per_column <= 32 * 1024;            // (several workgroups to a compute unit, else two of eight wavefronts)
+        p.few_threads = small ? 256 : FEW_THREADS;
+        p.few_chunk = (int)all;
+        if ((all + 8) * per_column > 72 * 1024) p.few_chunk = (int)((72 * 1024 / per_column - 8) / batch * batch);
+        const int64_t sums = p.few_threads / 64 * 16 * 4 * (int64_t)sizeof(float2), lds = (p.few_chunk + 8) * per_column;
+        p.few_lds = (int)(lds > sums ? lds : sums);
+        const int64_t blocks = ceil_div(ceil_div(classes, 16), p.few_threads / 64);
+        p.few_blocks = (int)(blocks < 2048 ? blocks : 2048);
+        p.few_passes = (int)ceil_div(blocks, p.few_blocks);
+        p.tile_sums = c.take<float2>(n * p.few_blocks);
+    }
+    if (grad) p.lse = c.take<float>(n);
+    if (grad && p.few_grad) {
+        p.few_each = (int)(round_up(ceil_div(classes, 1024), 8));
+        p.few_grad_blocks = (int)ceil_div(classes, p.few_each);
+        p.ldp = round_up(d, 8);
+        p.logits = c.take<float>(n * round_up(classes, 4));
+        p.parts = c.take<float>(p.few_grad_blocks * n * p.ldp);
+    }
+    p.tiles = grad ? !p.few_grad : !p.few;
+    if (!p.tiles) {
+        p.bytes = c.total();
+        return p;
+    }
+    p.ldk = spread(round_up(d, MM_K));
     p.rows_out = grad ? round_up(n, MM_K) : n;
     p.config = mm_choose(classes, n);
     // (rows without a label are zeros for the product over rows; and x is read often where there are many rows)
     p.lay_x = grad || !as_is(x, ldx) || (p.config == WIDE && spread(ldx) != ldx);
-    p.lay_w = !as_is(w, ldw);
-    Carver c(workspace);
     p.x = p.lay_x ? c.take<uint16_t>(p.rows_out * p.ldk * p.planes) : (uint16_t *)x;
     p.w = p.lay_w ? c.take<uint16_t>(classes * p.ldk * p.planes) : (uint16_t *)w;
-    p.tile_sums = c.take<float2>(n * ceil_div(classes, mm_tile_i(p.config)) * MM_PARTS_I);
-    p.picked = c.take<float>(n);
+    if (!p.few) p.tile_sums = c.take<float2>(n * ceil_div(classes, mm_tile_i(p.config)) * MM_PARTS_I);
     if (grad) {
-        p.lse = c.take<float>(n);
         p.power = c.take<float>(2);
         const int64_t per_class = 2 * p.planes * p.rows_out;
         int64_t most = LOSS_PIECE_BYTES / per_class / 256 * 256;
@@ -261,6 +291,13 @@ int loss_lay_rows(const T *in, int64_t ldi, void *out, int64_t ld, int64_t rows,
     return launched("lay_rows");
 }
 
+template <typename T>
+int run_sum_parts(const float *parts, int64_t ld, int64_t copy, int copies, T *out, int64_t ldo, int64_t rows, int64_t cols, const float *scale, hipStream_t stream)
+{
+    sum_parts<T><<<(unsigned)grid_of(rows * (ld / 4), 256 / SUM_SLICES, 32768), 256, 0, stream>>>(parts, ld, copy, copies, out, ldo, rows, cols, scale);
+    return launched("sum_parts");
+}
+
 MmShape mm_shape(const MmOperand &a, const MmOperand &b, int64_t k, int planes, int config, int splits)
 {
     MmShape s;
@@ -286,8 +323,17 @@ template <typename T>
 int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw, LossRows &rows, float *loss, float *lse, int32_t *flags, hipStream_t stream)
 {
     typedef typename Product<T>::type P;
-    if (p.lay_x) TRY(loss_lay_rows<T>(x, ldx, p.x, p.ldk, p.n, p.rows_out, p.d, p.parts ? &rows : nullptr, stream));
-    if (p.lay_w) TRY(loss_lay_rows<T>(w, ldw, p.w, p.ldk, p.classes, p.classes, p.d, nullptr, stream));
+    if (p.tiles && p.lay_x) TRY(loss_lay_rows<T>(x, ldx, p.x, p.ldk, p.n, p.rows_out, p.d, p.parts ? &rows : nullptr, stream));
+    if (p.tiles && p.lay_w) TRY(loss_lay_rows<T>(w, ldw, p.w, p.ldk, p.classes, p.classes, p.d, nullptr, stream));
+    if (p.few) {
+        auto kernel = p.n <= 16 ? loss_few<T, 1> : p.n <= 32 ? loss_few<T, 2> : loss_few<T, 4>;
+        TRY(allow_lds(kernel, p.few_lds));
+        kernel<<<(unsigned)p.few_blocks, p.few_threads, p.few_lds, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_chunk, p.few_passes, p.logits,
+                                                                             round_up(p.classes, 4));
+        TRY(launched("loss_few"));
+        loss_rows<<<(unsigned)ceil_div(p.n, 4), 256, 0, stream>>>(rows, p.few_blocks, loss, lse, flags);
+        return launched("loss_rows");
+    }
     const MmOperand a = {p.w, p.lay_w ? p.ldk : ldw, p.classes * p.ldk, (int)p.classes, 0};
     const MmOperand b = {p.x, p.lay_x ? p.ldk : ldx, p.rows_out * p.ldk, (int)p.n, 0};
     const MmShape s = mm_shape(a, b, round_up(p.d, MM_K), p.planes, p.config, 1);
@@ -310,6 +356,13 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
     constexpr int PLANES = Product<T>::PLANES;
     TRY(run_loss<T>(p, x, ldx, w, ldw, rows, loss, p.lse, flags, stream));
     rows.lse = p.lse;
+    if (p.few_grad) {
+        const dim3 grid((unsigned)p.few_grad_blocks, (unsigned)ceil_div(p.d, 256 * Elem<T>::VEC));
+        auto kernel = p.n == 1 ? loss_grad_few<T, 1> : p.n == 2 ? loss_grad_few<T, 2> : p.n <= 4 ? loss_grad_few<T, 4> : loss_grad_few<T, 8>;
+        kernel<<<grid, 256, 0, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_each, p.logits, round_up(p.classes, 4), dw, lddw, p.parts, p.ldp);
+        TRY(launched("loss_grad_few"));
+        return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, p.few_grad_blocks, dx, lddx, p.n, p.d, nullptr, stream);
+    }
     const bool scaled = sizeof(T) == 2 && std::is_same<T, f16>::value;
     if (scaled) {
         loss_power<<<1, 1024, 0, stream>>>(rows.weight, (int)p.n, p.power);
@@ -354,9 +407,7 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
             return launched("product_out");
         }));
     }
-    sum_parts<T><<<(unsigned)grid_of(p.n * (p.ldp / 4), 256, 16384), 256, 0, stream>>>(p.parts, p.ldp, p.n * p.ldp, copies, dx, lddx, p.n,
-                                                                                      p.d, inverse);
-    return launched("sum_parts");
+    return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, copies, dx, lddx, p.n, p.d, inverse, stream);
 }
 
 // ---- embedding gradient -----------------------------------------------------------------------------------------------
@@ -435,9 +486,7 @@ int chicle_softmax_loss_grad(const void *x, int64_t ldx, const void *w, int64_t 
     if (n == 0)                                          // no row: the classes' gradient is zero
         return with_type(type, [&](auto t) {
             typedef decltype(t) T;
-            sum_parts<T><<<(unsigned)grid_of(classes * ceil_div(d, 4), 256, 16384), 256, 0, stream>>>(nullptr, round_up(d, 4), 0, 0, (T *)dw, lddw, classes, d,
-                                                                                                     nullptr);
-            return launched("sum_parts");
+            return run_sum_parts<T>(nullptr, round_up(d, 4), 0, 0, (T *)dw, lddw, classes, d, nullptr, stream);
         });
     TRY(check_workspace(workspace, workspace_bytes, loss_plan(x, ldx, w, ldw, n, d, classes, type, true, nullptr).bytes));
     const LossPlan p = loss_plan(x, ldx, w, ldw, n, d, classes, type, true, workspace);
@@ -485,9 +534,7 @@ int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t l
     if (n == 0)
         return with_type(type, [&](auto t) {
             typedef decltype(t) T;
-            sum_parts<T><<<(unsigned)grid_of(n_rows * ceil_div(d, 4), 256, 16384), 256, 0, stream>>>(nullptr, round_up(d, 4), 0, 0, (T *)dtable, ldo, n_rows, d,
-                                                                                                    nullptr);
-            return launched("sum_parts");
+            return run_sum_parts<T>(nullptr, round_up(d, 4), 0, 0, (T *)dtable, ldo, n_rows, d, nullptr, stream);
         });
     TRY(check_workspace(workspace, workspace_bytes, embed_plan(n, d, n_rows, nullptr).bytes));
     const EmbedPlan p = embed_plan(n, d, n_rows, workspace);

@@ -127,10 +127,10 @@ __device__ __forceinline__ void mm_fetch(const MmOperand &o, const char *base, i
     }
 }
 
-// What is fetched next: slice `at` of product of planes `seg`, `left` slices from the end of unit `unit`.
+// What is fetched next: product of planes `seg` of slice `at`, `left` of them from the end of unit `unit`.
 template <typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
     unsigned unit, units;
-    int seg, at, left, per_plane, all_slices, row_a, row_b;
+    int seg, at, left, all_slices, row_a, row_b;
     bool edge_a, edge_b;
     int off_a[A_BY_K ? 2 : 1], off_b[B_BY_K ? 2 : 1];
     const char *qa, *qb;
@@ -140,8 +140,7 @@ template <typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
     {
         unit = blockIdx.x;
         units = s.tiles_i * s.tiles_j * s.splits;
-        per_plane = s.k / MM_K;
-        all_slices = per_plane * (s.planes == 1 ? 1 : 6);
+        all_slices = s.k / MM_K * (s.planes == 1 ? 1 : 6);
         step_a = A_BY_K ? MM_K * 2 * s.a.ld : MM_ROW;
         step_b = B_BY_K ? MM_K * 2 * s.b.ld : MM_ROW;
         const MmOperand whole_a = {nullptr, s.a.ld, 0, 1 << 30, 0}, whole_b = {nullptr, s.b.ld, 0, 1 << 30, 0};
@@ -164,8 +163,8 @@ template <typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
         edge_a = row_a + C::TILE_I > (A_BY_K ? (s.a.rows + 7) / 8 * 8 : s.a.rows);
         edge_b = row_b + C::TILE_J > (B_BY_K ? (s.b.rows + 7) / 8 * 8 : s.b.rows);
         const int first = t.split * s.per_split;
-        seg = s.planes == 1 ? 0 : first / per_plane;
-        at = first - seg * per_plane;
+        at = s.planes == 1 ? first : first / 6;
+        seg = s.planes == 1 ? 0 : first - at * 6;
         left = min(s.per_split, all_slices - first);
         place(s);
     }
@@ -175,14 +174,15 @@ template <typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
         const int last_k = A_BY_K ? s.a.k_rows - 1 - at * MM_K : MM_K;     // (the last k may not all be there)
         mm_fetch<C::TILE_I, C, A_BY_K>(s.a, qa, row_a, off_a, edge_a || last_k < MM_K - 1, last_k, lds);
         mm_fetch<C::TILE_J, C, B_BY_K>(s.b, qb, row_b, off_b, edge_b, MM_K, lds + C::TILE_I * MM_ROW);
-        qa += step_a;
-        qb += step_b;
         if (--left == 0) {
             unit += gridDim.x;
             if (unit < units) open(s);
-        } else if (++at == per_plane) {
-            at = 0;
-            ++seg;
+        } else if (s.planes == 1) {
+            ++at;
+            qa += step_a;
+            qb += step_b;
+        } else {                                         // all products of a slice's planes, then the next slice
+            if (++seg == 6) { seg = 0; ++at; }
             place(s);
         }
     }

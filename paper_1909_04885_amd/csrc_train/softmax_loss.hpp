@@ -276,21 +276,249 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_out(MmShape s
     });
 }
 
-// dx = scale * the sum of the copies, in their order.  ld of a copy is a multiple of four.
+// dx = scale * the sum of the copies, in their order: SUM_SLICES threads to four columns, each of which adds up a run of the copies.
+// ld of a copy is a multiple of four.
+constexpr int SUM_SLICES = 8;
+
 template <typename O>
 __global__ __launch_bounds__(256) void sum_parts(const float *__restrict__ part, int64_t ld, int64_t copy, int copies, O *__restrict__ out, int64_t ldo,
                                                  int64_t rows, int64_t cols, const float *__restrict__ scale)
 {
-    const int64_t per_row = ld / 4;
+    constexpr int EACH = 256 / SUM_SLICES;
+    __shared__ f32x4 s[SUM_SLICES][EACH];
+    const int64_t per_row = ld / 4, all = rows * per_row;
     const float f = scale ? *scale : 1.f;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < rows * per_row; e += (int64_t)gridDim.x * 256) {
-        const int64_t r = e / per_row, c = (e - r * per_row) * 4;
+    const int slice = threadIdx.x / EACH, mine = threadIdx.x % EACH;
+    const int first = (int)((int64_t)copies * slice / SUM_SLICES), end = (int)((int64_t)copies * (slice + 1) / SUM_SLICES);
+    for (int64_t e0 = (int64_t)blockIdx.x * EACH; e0 < all; e0 += (int64_t)gridDim.x * EACH) {
+        const int64_t e = min(e0 + mine, all - 1), r = e / per_row, c = (e - r * per_row) * 4;
+        const float *src = part + r * ld + c;
         f32x4 t = {0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < copies; ++k) t += *(const f32x4 *)(part + k * copy + r * ld + c);
+#pragma unroll 4
+        for (int k = first; k < end; ++k) t += *(const f32x4 *)(src + k * copy);
+        __syncthreads();
+        s[slice][mine] = t;
+        __syncthreads();
+        if (slice || e0 + mine >= all) continue;
+        for (int q = 1; q < SUM_SLICES; ++q) t += s[q][mine];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (c + i < cols) out[r * ldo + c + i] = (O)(t[i] * f);
     }
+}
+
+// ---- few rows -------------------------------------------------------------------------------------------------------
+//
+// Few rows are bound by reading w.  `loss_few` reads it as it lies, whatever its type, distance and alignment: a wavefront takes sixteen
+// classes at a time, its lanes' sixteen bytes being the matrix instruction's operand as they come, and x lies in LDS.  32-bit values are
+// split into their planes on the way.  For the gradient it leaves the logits, which beside w are few bytes, and
+// `loss_grad_few` reads w once more: a thread owns a vector of columns and forms dw's rows and its part of dx in 32 bits.
+
+constexpr int FEW_ROWS = 16, FEW_MOST_ROWS = 64, FEW_GRAD_ROWS = 8, FEW_AHEAD = 8, FEW_BATCH = 32 * FEW_AHEAD, FEW_THREADS = 512;
+
+template <typename T, typename P>
+__device__ __forceinline__ void few_planes(const u32x4 *raw, typename Mfma<P>::frag *f)
+{
+    if constexpr (sizeof(T) == 2) f[0] = __builtin_bit_cast(typename Mfma<P>::frag, raw[0]);
+    else {
+        float v[8];
+        unpack<float>(raw[0], v);
+        unpack<float>(raw[1], v + 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            P q[3];
+            split_planes(v[i], q);
+            f[0][i] = q[0]; f[1][i] = q[1]; f[2][i] = q[2];
+        }
+    }
+}
+
+// Rows 16 nr + l % 16 of x in LDS, `chunk` columns at a time where not all of them fit: x[plane][row][chunk + 8], zeros past d; then (largest,
+// sum) of every wavefront and row.  part[row][workgroup]; logits[row][ldz], may be null.  chunk is a multiple of a batch.
+template <typename T, int NR>
+__global__ __launch_bounds__(FEW_THREADS) void loss_few(const T *__restrict__ x, int64_t ldx, const T *__restrict__ w, int64_t ldw, int64_t d, LossRows l, int chunk,
+                                                 int passes, float *__restrict__ logits, int64_t ldz)
+{
+    typedef typename Product<T>::type P;
+    typedef typename Mfma<P>::frag frag;
+    constexpr int N = Product<T>::PLANES, RAW = sizeof(T) / 2, U = FEW_AHEAD / RAW, BATCH = 32 * U;   // RAW accesses to a fragment, U fragments to a batch
+    constexpr bool EXACT = sizeof(T) == 4;
+    extern __shared__ __align__(16) char lds[];
+    P *xs = (P *)lds;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, l16 = lane & 15, quarter = lane >> 4, ld = chunk + 8;
+    const int k_end = (int)((d + 31) / 32 * 32);
+    int at[NR], label[NR];
+    float m[NR], sum[NR];
+#pragma unroll
+    for (int q = 0; q < NR; ++q) {
+        at[q] = min(16 * q + l16, l.n - 1) * ld + quarter * 8;
+        label[q] = label_at(l, 16 * q + l16);
+        m[q] = MINUS_INF;
+        sum[q] = 0.f;
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        const int64_t v0 = (((int64_t)pass * gridDim.x + blockIdx.x) * waves + wave) * 16;
+        const T *row = w + min(v0 + l16, (int64_t)l.classes - 1) * ldw;
+        f32x4 acc[NR];
+#pragma unroll
+        for (int q = 0; q < NR; ++q) acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto ask = [&](u32x4 (&raw)[U][RAW], int k0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int h = 0; h < RAW; ++h) raw[u][h] = load_raw<T, true>(row, k0 + u * 32 + quarter * 8 + h * 4, d);
+        };
+        auto use = [&](const u32x4 (&raw)[U][RAW], int k0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                frag a[N];
+                few_planes<T, P>(raw[u], a);
+#pragma unroll
+                for (int q = 0; q < NR; ++q) {
+                    frag b[N];
+#pragma unroll
+                    for (int k = 0; k < N; ++k) b[k] = *(const frag *)(xs + k * l.n * ld + at[q] + k0 + u * 32);
+#pragma unroll
+                    for (int z = 0; z < (N == 3 ? 6 : 1); ++z) acc[q] = Mfma<P>::mul(a[N == 3 ? mm_plane_a(z) : 0], b[N == 3 ? mm_plane_b(z) : 0], acc[q]);
+                }
+            }
+        };
+        for (int kc = 0; kc < k_end; kc += chunk) {
+            const int end = min(chunk, k_end - kc);
+            u32x4 raw0[U][RAW], raw1[U][RAW];
+            ask(raw0, kc);                               // (on its way while x goes to LDS)
+            if (pass == 0 || chunk < k_end) {
+                __syncthreads();
+                for (int e = threadIdx.x; e < l.n * (chunk / 8); e += blockDim.x) {
+                    const int r = e / (chunk / 8), c = (e - r * (chunk / 8)) * 8;
+                    u32x4 v[RAW];
+#pragma unroll
+                    for (int h = 0; h < RAW; ++h) v[h] = load_raw<T>(x + r * ldx, kc + c + h * 4, d);
+                    frag f[N];
+                    few_planes<T, P>(v, f);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) *(frag *)(xs + (k * l.n + r) * ld + c) = f[k];
+                }
+                __syncthreads();
+            }
+            for (int k0 = 0; k0 < end; k0 += 2 * BATCH) {
+                if (k0 + BATCH < end) ask(raw1, kc + k0 + BATCH);
+                use(raw0, k0);
+                if (k0 + 2 * BATCH < end) ask(raw0, kc + k0 + 2 * BATCH);
+                if (k0 + BATCH < end) use(raw1, k0 + BATCH);
+            }
+        }
+        // this lane: classes v0 + 4 quarter + r of rows 16 q + l16
+        const int64_t first = v0 + 4 * quarter;
+#pragma unroll
+        for (int q = 0; q < NR; ++q) {
+            const int j = 16 * q + l16;
+            float top = m[q];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (first + r >= l.classes) acc[q][r] = MINUS_INF;
+                else {
+                    if (first + r == label[q]) l.picked[j] = acc[q][r];
+                    if (logits && j < l.n) logits[j * ldz + first + r] = acc[q][r];
+                }
+                top = fmaxf(top, acc[q][r]);
+            }
+            const float shift = top == MINUS_INF ? 0.f : top;
+            sum[q] *= exp_diff<EXACT>(m[q], shift);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[q] += exp_of<EXACT>(acc[q][r], shift);
+            m[q] = top;
+        }
+    }
+    // lanes of one row, then wavefronts
+    __syncthreads();
+    float2 *parts = (float2 *)lds;
+#pragma unroll
+    for (int q = 0; q < NR; ++q) {
+        for (int o = 16; o <= 32; o <<= 1) {
+            const float m2 = __shfl_xor(m[q], o), s2 = __shfl_xor(sum[q], o), top = fmaxf(m[q], m2);
+            sum[q] = sum[q] * exp_diff<EXACT>(m[q], top) + s2 * exp_diff<EXACT>(m2, top);
+            m[q] = top;
+        }
+        if (lane < 16) parts[wave * 16 * NR + 16 * q + lane] = make_float2(m[q], sum[q]);
+    }
+    __syncthreads();
+    const int j = threadIdx.x;
+    if (j >= l.n) return;
+    float2 t = parts[j];
+    for (int v = 1; v < waves; ++v) {
+        const float2 y = parts[v * 16 * NR + j];
+        const float top = fmaxf(t.x, y.x);
+        t = make_float2(top, t.y * exp_diff<EXACT>(t.x, top) + y.y * exp_diff<EXACT>(y.x, top));
+    }
+    l.part[(int64_t)j * gridDim.x + blockIdx.x] = t;
+}
+
+// Workgroup (b, y): classes [b * each, ..), columns from y * 256 * VEC on.  part[b][row][ldp] is its share of dx.
+template <typename T, int ROWS>
+__global__ __launch_bounds__(256) void loss_grad_few(const T *__restrict__ x, int64_t ldx, const T *__restrict__ w, int64_t ldw, int64_t d, LossRows l, int each,
+                                                     const float *__restrict__ logits, int64_t ldz, T *__restrict__ dw, int64_t lddw,
+                                                     float *__restrict__ part, int64_t ldp)
+{
+    constexpr int V = Elem<T>::VEC, CHUNK = 64, AHEAD = 4;
+    __shared__ float g[CHUNK][ROWS];
+    __shared__ int labels[ROWS];
+    const int64_t c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * V;
+    if (threadIdx.x < ROWS) labels[threadIdx.x] = label_at(l, threadIdx.x);
+    __syncthreads();
+    float xv[ROWS][V], sum[ROWS][V] = {};
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) {
+        if (labels[j] >= 0) load_vec(x + j * ldx, c, d, xv[j]);
+        else
+#pragma unroll
+            for (int k = 0; k < V; ++k) xv[j][k] = 0.f;  // (such a row counts nowhere, whatever it holds)
+    }
+    const int64_t v0 = (int64_t)blockIdx.x * each, v1 = min((int64_t)l.classes, v0 + each);
+    for (int64_t v = v0; v < v1; v += CHUNK) {
+        __syncthreads();
+        for (int e = threadIdx.x; e < CHUNK * ROWS; e += 256) {
+            const int j = e / CHUNK, q = e % CHUNK;
+            float p = 0.f;
+            if (labels[j] >= 0 && v + q < v1) {
+                const float weight = l.weight[j];
+                p = expf(logits[j * ldz + v + q] - l.lse[j]) - (v + q == labels[j] ? 1.f : 0.f);
+                p = weight != 0.f ? p * weight : 0.f;
+            }
+            g[q][j] = p;
+        }
+        __syncthreads();
+        const int many = (int)min((int64_t)CHUNK, v1 - v);
+        if (c < d)
+            for (int q0 = 0; q0 < many; q0 += AHEAD) {
+                u32x4 raw[AHEAD];
+#pragma unroll
+                for (int h = 0; h < AHEAD; ++h) raw[h] = load_raw<T, true>(w + (v + min(q0 + h, many - 1)) * ldw, c, d);
+#pragma unroll
+                for (int h = 0; h < AHEAD; ++h) {
+                    if (q0 + h >= many) break;
+                    float wv[V], out[V] = {};
+                    unpack<T>(raw[h], wv);
+#pragma unroll
+                    for (int j = 0; j < ROWS; ++j) {
+                        const float p = g[q0 + h][j];
+#pragma unroll
+                        for (int k = 0; k < V; ++k) {
+                            sum[j][k] += p * wv[k];
+                            out[k] += p * xv[j][k];
+                        }
+                    }
+                    store_vec<T, true>(dw + (v + q0 + h) * lddw, c, d, out);
+                }
+            }
+    }
+    if (c >= d) return;
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j)
+        if (j < l.n)
+#pragma unroll
+            for (int k = 0; k < V; k += 4)
+                *(f32x4 *)(part + ((int64_t)blockIdx.x * l.n + j) * ldp + c + k) = f32x4{sum[j][k], sum[j][k + 1], sum[j][k + 2], sum[j][k + 3]};
 }
 
 }  // namespace chicle_train
