@@ -34,9 +34,9 @@ int launched(const char *what)
     return e == hipSuccess ? CHICLE_OK : fail(CHICLE_EDEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
-#define TRY(expr)                              \
+#define TRY(...)                               \
     do {                                       \
-        const int rc_ = (expr);                \
+        const int rc_ = (__VA_ARGS__);         \
         if (rc_ != CHICLE_OK) return rc_;      \
     } while (0)
 
@@ -141,19 +141,24 @@ constexpr int CUS = 256;                                 // compute units
 int mm_tile_i(int c) { return c == WIDE ? 256 : 128; }
 int mm_tile_j(int c) { return c == WIDE ? 256 : c == MIDDLE ? 128 : 64; }
 
-// Large tiles read the least and run at the matrix cores' rate (1200 against 1000 TFLOP/s of the middle ones), where they fill the chip;
+// 16 bits: large tiles read the least and feed the matrix cores best (1300 against 1000 TFLOP/s of the middle ones), where they fill the chip.
+// 32 bits: the matrix cores are the bound whatever the tile, and what counts is how much of the tiles lies past the last row.
 // `splittable`: the sum is long and may be divided.
-int mm_choose(int64_t rows_i, int64_t rows_j, bool splittable = false)
+int mm_choose(int size, int64_t rows_i, int64_t rows_j, bool splittable = false)
 {
     if (rows_j <= 64) return THIN;
     const int64_t tiles = ceil_div(rows_i, 256) * ceil_div(rows_j, 256);
-    return tiles >= (splittable ? 8 : 192) ? WIDE : MIDDLE;
+    if (size == 2) return tiles >= (splittable ? 8 : 192) ? WIDE : MIDDLE;
+    return ceil_div(rows_j, 128) * 2 == ceil_div(rows_j, 64) ? MIDDLE : THIN;
 }
 
-template <typename W, typename F>
+// f(C()) with the tile; W is the large one of the 16-bit types
+template <typename T, typename W, typename F>
 int with_config(int c, F f)
 {
-    return c == WIDE ? f(W()) : c == MIDDLE ? f(MmMiddle()) : f(MmThin());
+    if constexpr (sizeof(T) == 2)
+        if (c == WIDE) return f(W());
+    return c == MIDDLE ? f(MmMiddle()) : f(MmThin());
 }
 
 template <typename K>
@@ -167,24 +172,25 @@ int allow_lds(K kernel, int bytes)
 
 struct LossPlan {
     int64_t n, d, classes, ldk;          // ldk: length of laid-out rows along d
-    int planes, config;
-    bool few, few_grad, tiles, lay_x, lay_w;     // few: of the loss, of the gradient; tiles: something goes by products
+    int config;
+    bool few, few_grad, tiles, kept, lay_x, lay_w;   // few: of the loss, of the gradient; tiles: something goes by products; kept: the logits
     int few_blocks, few_passes, few_threads, few_chunk, few_lds, few_each, few_grad_blocks;
-    float *logits;
-    // gradient
-    int64_t piece, ldg, rows_out, ldp;   // classes of a piece; length of G's rows, their number; length of the rows of dx's parts
+    // gradient: pieces of the classes, or, with logits kept, of the rows
+    int64_t piece, piece_rows, ldz, ldg, ldp;        // ldz, ldg: length of the rows of the logits and of G; ldp: of the rows of dx's parts
+    int64_t rows_x, rows_g;                          // rows of the laid-out x and of G: whole slices
     int pieces, splits, config_dx, config_dw;
     void *x, *w, *g;
-    float *parts, *lse, *picked, *power;
+    float *logits, *parts, *lse, *picked, *power;
     float2 *tile_sums;
     size_t bytes;
 };
 
-constexpr int64_t LOSS_PIECE_BYTES = (int64_t)1 << 29;   // G of a piece
-constexpr int64_t LOSS_MOST = (int64_t)1 << 22;
+constexpr int64_t LOSS_PIECE_BYTES = (int64_t)1 << 29;   // G of a piece of the classes
+constexpr int64_t LOSS_KEPT_BYTES = (int64_t)1 << 30;    // logits of a piece of the rows
+constexpr int64_t LOSS_MOST = (int64_t)1 << 22, LOSS_MOST_D = (int64_t)1 << 21, LOSS_MOST_CLASSES = (int64_t)1 << 23;
 
-// Rows 1024 bytes apart, or a multiple of that, meet in few channels of the L2.
-int64_t spread(int64_t ld) { return ld % 512 == 0 ? ld + MM_K : ld; }
+// Rows 1024 bytes apart, or a multiple of that, meet in few channels of the L2: half a slice more.
+int64_t spread(int64_t ld, int size) { return ld * size % 1024 == 0 ? ld + MM_ROW / size : ld; }
 
 LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t n, int64_t d, int64_t classes, int32_t type, bool grad, void *workspace)
 {
@@ -192,71 +198,86 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
     p.bytes = ALIGN;
     if (n == 0) return p;                                // (nothing to lay out)
     p.n = n; p.d = d; p.classes = classes;
-    p.planes = type == CHICLE_F32 ? 3 : 1;
+    const int size = size_of(type);
+    const int64_t slice = MM_ROW / size;
     // rows that are whole slices of aligned chunks are read where they are
-    auto as_is = [&](const void *q, int64_t ld) { return p.planes == 1 && d % MM_K == 0 && ld % 8 == 0 && (uintptr_t)q % 16 == 0 && ld < LOSS_MOST; };
-    p.lay_w = !as_is(w, ldw);
-    // Few rows read w as it lies; more of them where it would have to be laid out first.
-    p.few = n <= (p.lay_w ? FEW_MOST_ROWS : FEW_ROWS);
-    p.few_grad = n <= FEW_GRAD_ROWS;
+    auto as_is = [&](const void *q, int64_t ld) { return d % slice == 0 && ld * size % 16 == 0 && (uintptr_t)q % 16 == 0 && ld < LOSS_MOST_D; };
+    // Few rows read w as it lies, up to 64 of them where it would have to be laid out first, or where products cost eight times as much.
+    p.few = n <= (as_is(w, ldw) && size == 2 ? FEW_ROWS / 4 : FEW_ROWS);
+    p.few_grad = grad && n <= FEW_GRAD_ROWS;
+    p.kept = grad && (p.few || size == 4);
+    p.tiles = grad ? !p.few_grad : !p.few;
+    p.lay_w = p.tiles && !as_is(w, ldw);
+    p.piece_rows = n;
     Carver c(workspace);
     p.picked = c.take<float>(n);
+    if (grad) p.lse = c.take<float>(n);
     if (p.few) {
-        const int64_t batch = FEW_BATCH / (size_of(type) / 2), all = round_up(d, batch), per_column = n * 2 * p.planes;
-        const bool small = (all + 8) * per_column <= 32 * 1024;            // (several workgroups to a compute unit, else two of eight wavefronts)
-        p.few_threads = small ? 256 : FEW_THREADS;
+        const int64_t batch = slice / 2 * FEW_AHEAD, all = round_up(d, batch), per_column = n * size, spare = 16 / size;
+        // several workgroups to a compute unit, else two of eight wavefronts
+        p.few_threads = (all + spare) * per_column <= 32 * 1024 ? 256 : FEW_THREADS;
         p.few_chunk = (int)all;
-        if ((all + 8) * per_column > 72 * 1024) p.few_chunk = (int)((72 * 1024 / per_column - 8) / batch * batch);
-        const int64_t sums = p.few_threads / 64 * 16 * 4 * (int64_t)sizeof(float2), lds = (p.few_chunk + 8) * per_column;
+        if ((all + spare) * per_column > 72 * 1024) p.few_chunk = (int)((72 * 1024 / per_column - spare) / batch * batch);
+        const int64_t sums = p.few_threads / 64 * FEW_ROWS * (int64_t)sizeof(float2), lds = (p.few_chunk + spare) * per_column;
         p.few_lds = (int)(lds > sums ? lds : sums);
         const int64_t blocks = ceil_div(ceil_div(classes, 16), p.few_threads / 64);
         p.few_blocks = (int)(blocks < 2048 ? blocks : 2048);
         p.few_passes = (int)ceil_div(blocks, p.few_blocks);
         p.tile_sums = c.take<float2>(n * p.few_blocks);
     }
-    if (grad) p.lse = c.take<float>(n);
-    if (grad && p.few_grad) {
+    p.config = mm_choose(size, classes, n);
+    p.ldz = round_up(classes, 256) + 32;                 // (whole tiles, and not a multiple of 1024 bytes)
+    if (p.kept && !p.few) {                              // as many rows as the logits have room for, at least a tile's
+        const int64_t most = LOSS_KEPT_BYTES / (p.ldz * 4) / 256 * 256;
+        p.pieces = (int)ceil_div(n, most < 256 ? 256 : most);
+        p.piece_rows = round_up(ceil_div(n, p.pieces), 256);
+        p.pieces = (int)ceil_div(n, p.piece_rows);
+        if (p.piece_rows > n) p.piece_rows = n;
+    }
+    if (p.few_grad) {
         p.few_each = (int)(round_up(ceil_div(classes, 1024), 8));
         p.few_grad_blocks = (int)ceil_div(classes, p.few_each);
         p.ldp = round_up(d, 8);
-        p.logits = c.take<float>(n * round_up(classes, 4));
+        p.logits = c.take<float>(n * p.ldz);
         p.parts = c.take<float>(p.few_grad_blocks * n * p.ldp);
     }
-    p.tiles = grad ? !p.few_grad : !p.few;
-    if (!p.tiles) {
-        p.bytes = c.total();
-        return p;
+    if (!p.few) p.tile_sums = c.take<float2>(p.piece_rows * ceil_div(classes, mm_tile_i(p.config)) * MM_PARTS_I);
+    if (p.tiles) {
+        p.ldk = spread(round_up(d, slice), size);
+        p.rows_x = grad ? round_up(n, slice) : n;
+        // (rows without a label are zeros for the product over rows; and x is read often where there are many rows)
+        p.lay_x = grad || !as_is(x, ldx) || (p.config == WIDE && spread(ldx, size) != ldx);
+        p.x = p.lay_x ? c.take<char>(p.rows_x * p.ldk * size) : (char *)x;
+        p.w = p.lay_w ? c.take<char>(classes * p.ldk * size) : (char *)w;
     }
-    p.ldk = spread(round_up(d, MM_K));
-    p.rows_out = grad ? round_up(n, MM_K) : n;
-    p.config = mm_choose(classes, n);
-    // (rows without a label are zeros for the product over rows; and x is read often where there are many rows)
-    p.lay_x = grad || !as_is(x, ldx) || (p.config == WIDE && spread(ldx) != ldx);
-    p.x = p.lay_x ? c.take<uint16_t>(p.rows_out * p.ldk * p.planes) : (uint16_t *)x;
-    p.w = p.lay_w ? c.take<uint16_t>(classes * p.ldk * p.planes) : (uint16_t *)w;
-    if (!p.few) p.tile_sums = c.take<float2>(n * ceil_div(classes, mm_tile_i(p.config)) * MM_PARTS_I);
-    if (grad) {
+    if (grad && p.tiles) {
         p.power = c.take<float>(2);
-        const int64_t per_class = 2 * p.planes * p.rows_out;
-        int64_t most = LOSS_PIECE_BYTES / per_class / 256 * 256;
-        most = most < 256 ? 256 : most;
-        p.pieces = (int)ceil_div(classes, most);
-        p.piece = round_up(ceil_div(classes, p.pieces), 256);
-        p.pieces = (int)ceil_div(classes, p.piece);
-        if (p.piece > classes) p.piece = classes;
-        p.ldg = spread(round_up(p.piece, MM_K));
+        if (p.kept) {
+            p.piece = classes;
+            if (p.few) p.pieces = 1;
+        } else {
+            int64_t most = LOSS_PIECE_BYTES / (size * p.rows_x) / 256 * 256;
+            most = most < 256 ? 256 : most;
+            p.pieces = (int)ceil_div(classes, most);
+            p.piece = round_up(ceil_div(classes, p.pieces), 256);
+            p.pieces = (int)ceil_div(classes, p.piece);
+            if (p.piece > classes) p.piece = classes;
+        }
+        p.rows_g = round_up(p.piece_rows, slice);
+        p.ldg = size == 4 ? p.ldz : spread(round_up(p.piece, slice), size);        // (in 32 bits the logits themselves become G)
         p.ldp = round_up(d, 4);
-        p.config_dx = mm_choose(d, n, p.ldg * (p.planes == 3 ? 6 : 1) >= 32768);
-        const int64_t slices = ceil_div(p.piece, MM_K) * (p.planes == 3 ? 6 : 1);
-        const int64_t tiles = ceil_div(d, mm_tile_i(p.config_dx)) * ceil_div(n, mm_tile_j(p.config_dx));
+        const int64_t slices = ceil_div(p.piece, slice);
+        p.config_dx = mm_choose(size, d, p.piece_rows, slices >= 512);
+        const int64_t tiles = ceil_div(d, mm_tile_i(p.config_dx)) * ceil_div(p.piece_rows, mm_tile_j(p.config_dx));
         const int64_t room = CUS * (p.config_dx == WIDE ? 1 : 2);
         int64_t splits = tiles >= room ? 1 : room / tiles;
         if (splits > slices / 8) splits = slices / 8;
         splits = splits < 1 ? 1 : splits;
         p.splits = (int)ceil_div(slices, ceil_div(slices, splits));
-        p.config_dw = mm_choose(d, p.piece);
-        p.g = c.take<uint16_t>(p.rows_out * p.ldg * p.planes);
-        p.parts = c.take<float>(n * p.ldp * p.splits * p.pieces);
+        p.config_dw = mm_choose(size, d, p.piece);
+        if (p.kept) p.logits = c.take<float>(p.rows_g * p.ldz);
+        p.g = size == 4 ? (void *)p.logits : c.take<char>(p.rows_g * p.ldg * size);
+        p.parts = c.take<float>(p.piece_rows * p.ldp * p.splits * (p.kept ? 1 : p.pieces));
     }
     p.bytes = c.total();
     return p;
@@ -266,7 +287,7 @@ int loss_check(const void *x, int64_t ldx, const void *w, int64_t ldw, const voi
                int32_t type)
 {
     if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
-    if (n < 0 || d < 1 || classes < 1 || n >= LOSS_MOST || d >= LOSS_MOST || classes >= ((int64_t)1 << 30))
+    if (n < 0 || d < 1 || classes < 1 || n >= LOSS_MOST || d >= LOSS_MOST_D || classes >= LOSS_MOST_CLASSES)
         return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, classes %lld", (long long)n, (long long)d, (long long)classes);
     if (ceil_div(classes, 128) * ceil_div(n, 64) > INT32_MAX / 2) return fail(CHICLE_EINVAL, "too many rows times classes");
     if (ldx < d || ldw < d) return fail(CHICLE_EINVAL, "a row distance is shorter than a row");
@@ -284,31 +305,31 @@ int64_t grid_of(int64_t items, int threads, int64_t most)
 template <typename T>
 int loss_lay_rows(const T *in, int64_t ldi, void *out, int64_t ld, int64_t rows, int64_t rows_out, int64_t cols, const LossRows *labels, hipStream_t stream)
 {
-    typedef typename Product<T>::type P;
-    lay_rows<T><<<(unsigned)grid_of(rows_out * (ld / 8), 256, 16384), 256, 0, stream>>>(in, ldi, (P *)out, ld, rows_out * ld, rows, rows_out, cols,
-                                                                                       labels ? labels->labels : nullptr, labels ? labels->wide : 0,
-                                                                                       labels ? labels->classes : 0);
+    lay_rows<T><<<(unsigned)grid_of(rows_out * (ld / MM_CHUNK<T>), 256, 16384), 256, 0, stream>>>(in, ldi, (T *)out, ld, rows, rows_out, cols,
+                                                                                                 labels ? labels->labels : nullptr, labels ? labels->wide : 0,
+                                                                                                 labels ? labels->classes : 0);
     return launched("lay_rows");
 }
 
 template <typename T>
 int run_sum_parts(const float *parts, int64_t ld, int64_t copy, int copies, T *out, int64_t ldo, int64_t rows, int64_t cols, const float *scale, hipStream_t stream)
 {
-    sum_parts<T><<<(unsigned)grid_of(rows * (ld / 4), 256 / SUM_SLICES, 32768), 256, 0, stream>>>(parts, ld, copy, copies, out, ldo, rows, cols, scale);
+    // (several threads to a place where there are many copies to add up: 82 copies of 333 x 252 in 7 instead of 24 us)
+    if (copies >= 16) sum_parts<T, 8><<<(unsigned)grid_of(rows * (ld / 4), 32, 32768), 256, 0, stream>>>(parts, ld, copy, copies, out, ldo, rows, cols, scale);
+    else sum_parts<T, 1><<<(unsigned)grid_of(rows * (ld / 4), 256, 32768), 256, 0, stream>>>(parts, ld, copy, copies, out, ldo, rows, cols, scale);
     return launched("sum_parts");
 }
 
-MmShape mm_shape(const MmOperand &a, const MmOperand &b, int64_t k, int planes, int config, int splits)
+template <typename T>
+MmShape mm_shape(const MmOperand &a, const MmOperand &b, int64_t k, int config, int splits)
 {
     MmShape s;
     s.a = a; s.b = b;
-    s.k = (int)k;
-    s.planes = planes;
+    s.slices = (int)ceil_div(k, MM_K<T>);
     s.tiles_i = (int)ceil_div(a.rows, mm_tile_i(config));
     s.tiles_j = (int)ceil_div(b.rows, mm_tile_j(config));
-    const int64_t slices = k / MM_K * (planes == 1 ? 1 : 6);
-    s.per_split = (int)ceil_div(slices, splits);
-    s.splits = (int)ceil_div(slices, s.per_split);       // (none is empty; at most `splits`)
+    s.per_split = (int)ceil_div(s.slices, splits);
+    s.splits = (int)ceil_div(s.slices, s.per_split);     // (none is empty; at most `splits`)
     return s;
 }
 
@@ -318,96 +339,141 @@ template <typename C> unsigned mm_grid(const MmShape &s)
     return (unsigned)(units < CUS * C::PER_CU ? units : CUS * C::PER_CU);
 }
 
-// lse and loss of all rows
-template <typename T>
-int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw, LossRows &rows, float *loss, float *lse, int32_t *flags, hipStream_t stream)
+// Rows of one call or of a piece of them: `rows` begins with the piece's first row.
+LossRows rows_from(const LossRows &all, int64_t first, int64_t many)
 {
-    typedef typename Product<T>::type P;
-    if (p.tiles && p.lay_x) TRY(loss_lay_rows<T>(x, ldx, p.x, p.ldk, p.n, p.rows_out, p.d, p.parts ? &rows : nullptr, stream));
-    if (p.tiles && p.lay_w) TRY(loss_lay_rows<T>(w, ldw, p.w, p.ldk, p.classes, p.classes, p.d, nullptr, stream));
+    LossRows r = all;
+    r.labels = (const char *)all.labels + first * (all.wide ? 8 : 4);
+    r.n = (int)many;
+    if (all.lse) r.lse = all.lse + first;
+    if (all.weight) r.weight = all.weight + first;
+    r.picked = all.picked + first;
+    return r;
+}
+
+// lse and loss of a piece of the rows, whose laid-out x begins at `first`; logits: null, or where they are kept
+template <typename T>
+int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw, const LossRows &all, int64_t first, int64_t many, float *logits,
+             float *loss, float *lse, int32_t *flags, hipStream_t stream)
+{
+    const LossRows rows = rows_from(all, first, many);
+    int parts;
     if (p.few) {
         auto kernel = p.n <= 16 ? loss_few<T, 1> : p.n <= 32 ? loss_few<T, 2> : loss_few<T, 4>;
         TRY(allow_lds(kernel, p.few_lds));
-        kernel<<<(unsigned)p.few_blocks, p.few_threads, p.few_lds, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_chunk, p.few_passes, p.logits,
-                                                                             round_up(p.classes, 4));
+        kernel<<<(unsigned)p.few_blocks, p.few_threads, p.few_lds, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_chunk, p.few_passes, logits, p.ldz);
         TRY(launched("loss_few"));
-        loss_rows<<<(unsigned)ceil_div(p.n, 4), 256, 0, stream>>>(rows, p.few_blocks, loss, lse, flags);
-        return launched("loss_rows");
+        parts = p.few_blocks;
+    } else {
+        const int64_t ldx_in = p.lay_x ? p.ldk : ldx;
+        const MmOperand a = {p.w, p.lay_w ? p.ldk : ldw, (int)p.classes, 0}, b = {(const T *)p.x + first * ldx_in, ldx_in, (int)many, 0};
+        const MmShape s = mm_shape<T>(a, b, p.d, p.config, 1);
+        TRY(with_config<T, MmWide>(p.config, [&](auto c) {
+            typedef decltype(c) C;
+            auto kernel = loss_tiles<T, C>;
+            TRY(allow_lds(kernel, C::LDS));
+            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, (T *)logits, p.ldz);
+            return launched("loss_tiles");
+        }));
+        parts = s.tiles_i * MM_PARTS_I;
     }
-    const MmOperand a = {p.w, p.lay_w ? p.ldk : ldw, p.classes * p.ldk, (int)p.classes, 0};
-    const MmOperand b = {p.x, p.lay_x ? p.ldk : ldx, p.rows_out * p.ldk, (int)p.n, 0};
-    const MmShape s = mm_shape(a, b, round_up(p.d, MM_K), p.planes, p.config, 1);
-    TRY(with_config<MmWide>(p.config, [&](auto c) {
-        typedef decltype(c) C;
-        auto kernel = loss_tiles<P, C, sizeof(T) == 4>;
-        TRY(allow_lds(kernel, C::LDS));
-        kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows);
-        return launched("loss_tiles");
-    }));
-    loss_rows<<<(unsigned)ceil_div(p.n, 4), 256, 0, stream>>>(rows, s.tiles_i * MM_PARTS_I, loss, lse, flags);
+    loss_rows<<<(unsigned)ceil_div(many, 4), 256, 0, stream>>>(rows, parts, loss + first, lse + first, flags);
     return launched("loss_rows");
+}
+
+// dx and dw of G of rows [row0, row0 + rows) and classes [class0, class0 + classes); `copies` parts of dx are there already
+template <typename T>
+int run_loss_products(const LossPlan &p, int64_t row0, int64_t rows, const T *w, int64_t ldw, int64_t class0, int64_t classes, int64_t ldg, T *dw,
+                      int64_t lddw, const float *inverse, bool add, int &copies, hipStream_t stream)
+{
+    const int64_t rows_g = round_up(rows, MM_K<T>);
+    const MmOperand x_by_k = {(const T *)p.x + row0 * p.ldk, p.ldk, (int)p.d, (int)rows_g}, w_by_k = {w + class0 * ldw, ldw, (int)p.d, (int)classes};
+    const MmOperand g_rows = {p.g, ldg, (int)rows, 0}, g_by_k = {p.g, ldg, (int)classes, (int)rows_g};
+    TRY(with_config<T, MmWideByK>(p.config_dx, [&](auto c) {
+        typedef decltype(c) C;
+        const MmShape s = mm_shape<T>(w_by_k, g_rows, classes, p.config_dx, p.splits);
+        auto kernel = product_parts<T, C>;
+        TRY(allow_lds(kernel, C::LDS));
+        kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.parts + (int64_t)copies * p.piece_rows * p.ldp, p.ldp, p.piece_rows * p.ldp);
+        copies += s.splits;
+        return launched("product_parts");
+    }));
+    return with_config<T, MmWideByK>(p.config_dw, [&](auto c) {
+        typedef decltype(c) C;
+        const MmShape s = mm_shape<T>(x_by_k, g_by_k, rows_g, p.config_dw, 1);
+        auto kernel = product_out<T, C, false>;
+        if constexpr (sizeof(T) == 4)                    // (pieces of the rows)
+            if (add) kernel = product_out<T, C, true>;
+        TRY(allow_lds(kernel, C::LDS));
+        kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, dw + class0 * lddw, lddw, inverse);
+        return launched("product_out");
+    });
+}
+
+template <typename T>
+int run_loss_lay(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw, const LossRows *labels, hipStream_t stream)
+{
+    if (p.tiles && p.lay_x) TRY(loss_lay_rows<T>(x, ldx, p.x, p.ldk, p.n, p.rows_x, p.d, labels, stream));
+    if (p.tiles && p.lay_w) TRY(loss_lay_rows<T>(w, ldw, p.w, p.ldk, p.classes, p.classes, p.d, nullptr, stream));
+    return CHICLE_OK;
 }
 
 template <typename T>
 int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw, LossRows &rows, float *loss, T *dx, int64_t lddx, T *dw,
                   int64_t lddw, int32_t *flags, hipStream_t stream)
 {
-    typedef typename Product<T>::type P;
-    constexpr int PLANES = Product<T>::PLANES;
-    TRY(run_loss<T>(p, x, ldx, w, ldw, rows, loss, p.lse, flags, stream));
     rows.lse = p.lse;
+    TRY(run_loss_lay<T>(p, x, ldx, w, ldw, &rows, stream));
     if (p.few_grad) {
+        TRY(run_loss<T>(p, x, ldx, w, ldw, rows, 0, p.n, p.logits, loss, p.lse, flags, stream));
         const dim3 grid((unsigned)p.few_grad_blocks, (unsigned)ceil_div(p.d, 256 * Elem<T>::VEC));
         auto kernel = p.n == 1 ? loss_grad_few<T, 1> : p.n == 2 ? loss_grad_few<T, 2> : p.n <= 4 ? loss_grad_few<T, 4> : loss_grad_few<T, 8>;
-        kernel<<<grid, 256, 0, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_each, p.logits, round_up(p.classes, 4), dw, lddw, p.parts, p.ldp);
+        kernel<<<grid, 256, 0, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_each, p.logits, p.ldz, dw, lddw, p.parts, p.ldp);
         TRY(launched("loss_grad_few"));
         return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, p.few_grad_blocks, dx, lddx, p.n, p.d, nullptr, stream);
     }
-    const bool scaled = sizeof(T) == 2 && std::is_same<T, f16>::value;
-    if (scaled) {
-        loss_power<<<1, 1024, 0, stream>>>(rows.weight, (int)p.n, p.power);
+    const float *inverse = nullptr;
+    if (sizeof(T) == 2) {
+        loss_power<<<1, 1024, 0, stream>>>(rows.weight, (int)p.n, std::is_same<T, f16>::value ? 16384.f : 1.f, p.power);
         TRY(launched("loss_power"));
         rows.power = p.power;
+        inverse = p.power + 1;
     }
-    const float *inverse = scaled ? p.power + 1 : nullptr;
-    const int64_t ldw_in = p.lay_w ? p.ldk : ldw, k_d = round_up(p.d, MM_K);
-    const MmOperand x_rows = {p.x, p.ldk, p.rows_out * p.ldk, (int)p.n, 0}, x_by_k = {p.x, p.ldk, p.rows_out * p.ldk, (int)p.d, (int)p.rows_out};
-    int copies = 0;                                      // of dx, to be added up
-    for (int k = 0; k < p.pieces; ++k) {
-        const int64_t first = k * p.piece, many = p.classes - first < p.piece ? p.classes - first : p.piece;
-        const int64_t k_w = round_up(many, MM_K), ldg = spread(k_w), plane_g = p.rows_out * ldg;
-        const uint16_t *w_piece = (const uint16_t *)p.w + first * ldw_in;
-        const MmOperand w_rows = {w_piece, ldw_in, p.classes * p.ldk, (int)many, 0}, w_by_k = {w_piece, ldw_in, p.classes * p.ldk, (int)p.d, (int)many};
-        const MmOperand g_rows = {p.g, ldg, plane_g, (int)p.n, 0}, g_by_k = {p.g, ldg, plane_g, (int)many, (int)p.rows_out};
-        const int config_g = mm_choose(many, p.n);
-        TRY(with_config<MmWide>(config_g, [&](auto c) {
-            typedef decltype(c) C;
-            const MmShape s = mm_shape(w_rows, x_rows, k_d, p.planes, config_g, 1);
-            auto kernel = loss_grad_tiles<P, C, sizeof(T) == 4, PLANES>;
-            TRY(allow_lds(kernel, C::LDS));
-            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, (int)first, (int)many, (P *)p.g, ldg, plane_g, (int)p.rows_out);
-            return launched("loss_grad_tiles");
-        }));
-        TRY(with_config<MmWideByK>(p.config_dx, [&](auto c) {
-            typedef decltype(c) C;
-            const MmShape s = mm_shape(w_by_k, g_rows, k_w, p.planes, p.config_dx, p.splits);
-            auto kernel = product_parts<P, C>;
-            TRY(allow_lds(kernel, C::LDS));
-            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.parts + (int64_t)copies * p.n * p.ldp, p.ldp,
-                                                                                                p.n * p.ldp);
-            copies += s.splits;
-            return launched("product_parts");
-        }));
-        TRY(with_config<MmWideByK>(p.config_dw, [&](auto c) {
-            typedef decltype(c) C;
-            const MmShape s = mm_shape(x_by_k, g_by_k, p.rows_out, p.planes, p.config_dw, 1);
-            auto kernel = product_out<P, C, T>;
-            TRY(allow_lds(kernel, C::LDS));
-            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, dw + first * lddw, lddw, inverse);
-            return launched("product_out");
-        }));
+    const T *w_in = (const T *)p.w;
+    const int64_t ldw_in = p.lay_w ? p.ldk : ldw;
+    if (p.kept) {
+        for (int64_t first = 0; first < p.n; first += p.piece_rows) {
+            const int64_t many = p.n - first < p.piece_rows ? p.n - first : p.piece_rows;
+            TRY(run_loss<T>(p, x, ldx, w, ldw, rows, first, many, p.logits, loss, p.lse, flags, stream));
+            const dim3 grid((unsigned)grid_of(p.ldg, 1024, 64), (unsigned)round_up(many, MM_K<T>));
+            loss_grad_kept<T><<<grid, 256, 0, stream>>>(p.logits, p.ldz, rows_from(rows, first, many), (T *)p.g, p.ldg);
+            TRY(launched("loss_grad_kept"));
+            int copies = 0;
+            TRY(run_loss_products<T>(p, first, many, w_in, ldw_in, 0, p.classes, p.ldg, dw, lddw, inverse, first > 0, copies, stream));
+            TRY(run_sum_parts<T>(p.parts, p.ldp, p.piece_rows * p.ldp, copies, dx + first * lddx, lddx, many, p.d, inverse, stream));
+        }
+        return CHICLE_OK;
     }
-    return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, copies, dx, lddx, p.n, p.d, inverse, stream);
+    if constexpr (sizeof(T) == 2) {
+        TRY(run_loss<T>(p, x, ldx, w, ldw, rows, 0, p.n, nullptr, loss, p.lse, flags, stream));
+        int copies = 0;                                  // of dx, to be added up
+        for (int64_t first = 0; first < p.classes; first += p.piece) {
+            const int64_t many = p.classes - first < p.piece ? p.classes - first : p.piece, ldg = spread(round_up(many, MM_K<T>), 2);
+            const MmOperand w_rows = {w_in + first * ldw_in, ldw_in, (int)many, 0}, x_rows = {p.x, p.ldk, (int)p.n, 0};
+            const int config = mm_choose(2, many, p.n);
+            TRY(with_config<T, MmWide>(config, [&](auto c) {
+                typedef decltype(c) C;
+                const MmShape s = mm_shape<T>(w_rows, x_rows, p.d, config, 1);
+                auto kernel = loss_grad_tiles<T, C>;
+                TRY(allow_lds(kernel, C::LDS));
+                kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, (int)first, (int)many, (T *)p.g, ldg, (int)p.rows_g);
+                return launched("loss_grad_tiles");
+            }));
+            TRY(run_loss_products<T>(p, 0, p.n, w_in, ldw_in, first, many, ldg, dw, lddw, inverse, false, copies, stream));
+        }
+        return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, copies, dx, lddx, p.n, p.d, inverse, stream);
+    }
+    return CHICLE_OK;
 }
 
 // ---- embedding gradient -----------------------------------------------------------------------------------------------
@@ -454,7 +520,7 @@ const char *chicle_train_last_error(void) { return last_error; }
 size_t chicle_softmax_loss_bytes(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t n, int64_t d, int64_t classes, int32_t type,
                                  int32_t with_grad)
 {
-    if (!type_ok(type) || n < 0 || d < 1 || classes < 1 || n >= LOSS_MOST || d >= LOSS_MOST || classes >= ((int64_t)1 << 30)) return 0;
+    if (!type_ok(type) || n < 0 || d < 1 || classes < 1 || n >= LOSS_MOST || d >= LOSS_MOST_D || classes >= LOSS_MOST_CLASSES) return 0;
     return loss_plan(x, ldx, w, ldw, n, d, classes, type, with_grad != 0, nullptr).bytes;
 }
 
@@ -470,7 +536,8 @@ int chicle_softmax_loss(const void *x, int64_t ldx, const void *w, int64_t ldw, 
     LossRows rows = {labels, wide, (int)n, (int)classes, nullptr, nullptr, nullptr, p.tile_sums, p.picked};
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        return run_loss<T>(p, (const T *)x, ldx, (const T *)w, ldw, rows, loss, lse, flags, (hipStream_t)hip_stream);
+        TRY(run_loss_lay<T>(p, (const T *)x, ldx, (const T *)w, ldw, nullptr, (hipStream_t)hip_stream));
+        return run_loss<T>(p, (const T *)x, ldx, (const T *)w, ldw, rows, 0, n, nullptr, loss, lse, flags, (hipStream_t)hip_stream);
     });
 }
 

@@ -1,20 +1,17 @@
-// Products of 16-bit matrices, C[j][i] = sum_k A(i, k) B(j, k), on the matrix cores.  An operand lies by rows, its k side by side, or
-// by k, its rows side by side.
+// Products of matrices, C[j][i] = sum_k A(i, k) B(j, k), on the matrix cores, in 16 bits or in 32.  An operand lies by rows, its k side by
+// side, or by k, its rows side by side.
 //
-// A workgroup forms tiles of C one after the other.  Slices of k of both operands go from global memory straight into LDS, some slices ahead
-// of the one that is multiplied, and the next tile's first slices while the last of this one are and while what follows the
-// product is done; sixteen-byte chunks (by rows) or pairs of them (by k) are permuted in LDS so that what a
-// wavefront reads side by side lies in different banks.  An operand that lies by k is turned as it is read from LDS: a read
-// gives each of sixteen lanes four k of its row.  Sums are held in 32-bit floats.
+// A workgroup forms tiles of C one after the other.  Slices of 128 bytes of k of both operands go from global memory straight into LDS, a
+// slice ahead of the one that is multiplied, and the next tile's first slice while the last of this one is and while what follows the
+// product is done; sixteen-byte chunks are permuted in LDS so that what a wavefront reads side by side lies in different banks.
+// An operand that lies by k is turned as it is read from LDS: in 16 bits a read gives each of sixteen lanes four k of its row,
+// in 32 bits a read takes one k.  Sums are held in 32-bit floats.
 //
-// 32-bit operands are three 16-bit planes whose sum they are exactly (leading, middle and last eight bits of the
-// significand, bfloat16 each).  Six of the nine products of planes are formed; the three that are left out are below 2^-24 of
-// the product together, less than its rounding.
-//
-// What bounds it: feeding the matrix cores, half of whose peak it reaches; 8192 x 2048 x 32000 in bfloat16 runs at 1300 TFLOP/s by rows (the
-// library's product of 8192^3: 1206).  Tried and slower: slices of 32 k with three or four buffers (1090), the two wavefronts of a
-// SIMD reading and multiplying in turn (1130), smaller tiles of which two workgroups share a compute unit (1000).  Rows
-// whose distance is a power of two meet in few channels of the L2 (970): what is laid out here has other distances.
+// What bounds it, in 16 bits: feeding the matrix cores, half of whose peak it reaches; 8192 x 2048 x 32000 in bfloat16 runs at 1300 TFLOP/s by
+// rows (the library's product of 8192^3: 1206).  Tried and slower: slices of 32 k with three or four buffers (1090), the two
+// wavefronts of a SIMD reading and multiplying in turn (1130), smaller tiles of which two workgroups share a compute unit
+// (1000).  Rows whose distance is a power of two meet in few channels of the L2 (970): what is laid out here has other
+// distances.  In 32 bits: the matrix cores' rate, an eighth of that (157 TFLOP/s).
 //
 // Rows past the end of an operand are read as a row that is there; what they give is never stored.
 #pragma once
@@ -26,35 +23,41 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 
+// The product of a lane's sixteen bytes of A and of B, k by k: 32 k of a wavefront in 16 bits, 16 in 32 bits.  Which k a lane holds does not
+// matter, as long as it holds the same of both.
 template <typename T> struct Mfma;
 template <> struct Mfma<bf16> {
     typedef bf16x8 frag;
-    static __device__ __forceinline__ f32x4 mul(frag a, frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static constexpr int STEPS = 1;
+    static __device__ __forceinline__ f32x4 step(frag a, frag b, int, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mfma<f16> {
     typedef f16x8 frag;
-    static __device__ __forceinline__ f32x4 mul(frag a, frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static constexpr int STEPS = 1;
+    static __device__ __forceinline__ f32x4 step(frag a, frag b, int, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mfma<float> {
+    typedef f32x4 frag;
+    static constexpr int STEPS = 4;
+    static __device__ __forceinline__ f32x4 step(frag a, frag b, int e, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0); }
 };
 
-constexpr int MM_K = 64, MM_CHUNKS = MM_K / 8, MM_ROW = MM_K * 2;   // k of a slice, sixteen-byte chunks and bytes of its row
+constexpr int MM_ROW = 128, MM_CHUNKS = MM_ROW / 16;           // bytes of a slice's row, chunks of it
+template <typename T> constexpr int MM_K = MM_ROW / (int)sizeof(T);    // k of a slice
+template <typename T> constexpr int MM_CHUNK = 16 / (int)sizeof(T);    // values of a chunk
 
 struct MmOperand {
     const void *p;
-    int64_t ld, plane;                       // elements from row to row (by k: from k to k), from plane to plane
+    int64_t ld;                              // elements from row to row (by k: from k to k); 64 rows lie within 2 GB
     int rows;                                // (by k: ld holds them in whole chunks)
     int k_rows;                              // by k: how many k are there; further ones are read as the last
 };
 
 struct MmShape {
     MmOperand a, b;
-    int k;                                   // of one plane, whole slices
-    int planes;                              // 1 or 3
+    int slices;                              // of the whole sum
     int tiles_i, tiles_j, splits, per_split; // per_split: slices of a split of the sum
 };
-
-// Planes of the products that are formed, four bits each.
-__device__ __forceinline__ int mm_plane_a(int s) { return (0x201100 >> (4 * s)) & 3; }
-__device__ __forceinline__ int mm_plane_b(int s) { return (0x021010 >> (4 * s)) & 3; }
 
 struct MmTile { int i, j, split; };
 
@@ -86,51 +89,55 @@ template <int BM, int BN, int WAVES_I, int WAVES_J, int BLOCKS> struct MmConfig 
 // By rows, chunk c of row r lies in place c ^ mm_turn(r) of its row: lanes that LDS serves together (of 32 lanes, 0-3, 12-15 and 20-27, then
 // the others) read different banks, of sixteen rows in a row as well as of four times four rows, eight apart.
 __device__ __forceinline__ int mm_turn(int r) { return (r & 2) | (r >> 3 & 1) * 4; }
-// By k, pair of chunks p of k lies in place p ^ mm_turn_k(k), of ROWS / 16 places.
-template <int ROWS> __device__ __forceinline__ int mm_turn_k(int k) { return ((k & 3) | (k >> 3 & 3) << 2) & (ROWS / 16 - 1); }
+// By k, chunk c of k lies in place c ^ mm_turn_k(k), of ROWS / MM_CHUNK places.
+template <typename T, int ROWS> __device__ __forceinline__ int mm_turn_k(int k)
+{
+    return (sizeof(T) == 2 ? ((k & 3) | (k >> 3 & 3) << 2) << 1 : (k >> 2 & 3) << 2) & (ROWS / MM_CHUNK<T> - 1);
+}
 
-// Byte offsets of the chunks that this thread fetches, from the tile's first row and the slice's first k.  last_k: the last k that is there,
-// counted from the slice's first.
-template <int ROWS, typename C, bool BY_K>
-__device__ __forceinline__ int mm_offset(const MmOperand &o, int row0, int it, int last_k)
+// Byte offset of the chunk that this thread fetches the it-th, from the tile's first row and the slice's first k.  last_k: the last k that is
+// there, counted from the slice's first.
+template <typename T, int ROWS, typename C, bool BY_K>
+__device__ __forceinline__ int64_t mm_offset(const MmOperand &o, int row0, int it, int last_k)
 {
     const int c = it * C::THREADS + threadIdx.x;
     if constexpr (BY_K) {
-        const int k = c / (ROWS / 8), place = c % (ROWS / 8), chunk = (place >> 1 ^ mm_turn_k<ROWS>(k)) * 2 + (place & 1);
-        const int past = (o.rows + 7) / 8 - row0 / 8;          // chunks from the tile's first to the end
-        return min(k, last_k) * (int)o.ld * 2 + min(chunk, past - 1) * 16;
+        constexpr int PLACES = ROWS / MM_CHUNK<T>;
+        const int k = c / PLACES, chunk = c % PLACES ^ mm_turn_k<T, ROWS>(k);
+        const int past = (o.rows + MM_CHUNK<T> - 1) / MM_CHUNK<T> - row0 / MM_CHUNK<T>;        // chunks from the tile's first to the end
+        return min(k, last_k) * o.ld * (int)sizeof(T) + min(chunk, past - 1) * 16;
     } else {
         const int r = c / MM_CHUNKS;
-        return min(r, o.rows - 1 - row0) * (int)o.ld * 2 + (c % MM_CHUNKS ^ mm_turn(r)) * 16;
+        return min(r, o.rows - 1 - row0) * o.ld * (int)sizeof(T) + (c % MM_CHUNKS ^ mm_turn(r)) * 16;
     }
 }
 
 // Sixteen bytes of every lane straight into LDS, 1 KB of a wavefront side by side.
-__device__ __forceinline__ void mm_load(const char *base, int off, char *lds)
+template <typename O> __device__ __forceinline__ void mm_load(const char *base, O off, char *lds)
 {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off), (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
 }
 
 // A slice of an operand.  Inside the operand the chunks of a thread are a fixed distance apart, by k with two places in turn: off[0] and
 // off[1].  At an edge the offsets are worked out anew.
-template <int ROWS, typename C, bool BY_K>
+template <typename T, int ROWS, typename C, bool BY_K>
 __device__ __forceinline__ void mm_fetch(const MmOperand &o, const char *base, int row0, const int *off, bool edge, int last_k, char *lds)
 {
-    constexpr int LOADS = ROWS * MM_CHUNKS / C::THREADS, APART = BY_K ? C::THREADS / (ROWS / 8) : C::THREADS / MM_CHUNKS;
+    constexpr int LOADS = ROWS * MM_CHUNKS / C::THREADS, APART = BY_K ? C::THREADS / (ROWS / MM_CHUNK<T>) : C::THREADS / MM_CHUNKS;
     lds += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
     if (edge) {
 #pragma unroll
-        for (int it = 0; it < LOADS; ++it) mm_load(base, mm_offset<ROWS, C, BY_K>(o, row0, it, last_k), lds + it * C::THREADS * 16);
+        for (int it = 0; it < LOADS; ++it) mm_load(base, mm_offset<T, ROWS, C, BY_K>(o, row0, it, last_k), lds + it * C::THREADS * 16);
     } else {
 #pragma unroll
-        for (int it = 0; it < LOADS; ++it) mm_load(base + it * APART * 2 * o.ld, off[BY_K ? it & 1 : 0], lds + it * C::THREADS * 16);
+        for (int it = 0; it < LOADS; ++it) mm_load(base + it * APART * (int)sizeof(T) * o.ld, off[BY_K ? it & 1 : 0], lds + it * C::THREADS * 16);
     }
 }
 
-// What is fetched next: product of planes `seg` of slice `at`, `left` of them from the end of unit `unit`.
-template <typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
+// What is fetched next: slice `at`, `left` slices from the end of unit `unit`.
+template <typename T, typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
     unsigned unit, units;
-    int seg, at, left, all_slices, row_a, row_b;
+    int at, left, row_a, row_b;
     bool edge_a, edge_b;
     int off_a[A_BY_K ? 2 : 1], off_b[B_BY_K ? 2 : 1];
     const char *qa, *qb;
@@ -140,65 +147,66 @@ template <typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
     {
         unit = blockIdx.x;
         units = s.tiles_i * s.tiles_j * s.splits;
-        all_slices = s.k / MM_K * (s.planes == 1 ? 1 : 6);
-        step_a = A_BY_K ? MM_K * 2 * s.a.ld : MM_ROW;
-        step_b = B_BY_K ? MM_K * 2 * s.b.ld : MM_ROW;
-        const MmOperand whole_a = {nullptr, s.a.ld, 0, 1 << 30, 0}, whole_b = {nullptr, s.b.ld, 0, 1 << 30, 0};
+        step_a = A_BY_K ? MM_ROW * s.a.ld : MM_ROW;
+        step_b = B_BY_K ? MM_ROW * s.b.ld : MM_ROW;
+        const MmOperand whole_a = {nullptr, s.a.ld, 1 << 30, 0}, whole_b = {nullptr, s.b.ld, 1 << 30, 0};
 #pragma unroll
-        for (int q = 0; q < (A_BY_K ? 2 : 1); ++q) off_a[q] = mm_offset<C::TILE_I, C, A_BY_K>(whole_a, 0, q, MM_K) - q * C::THREADS / (C::TILE_I / 8) * (int)s.a.ld * 2;
+        for (int q = 0; q < (A_BY_K ? 2 : 1); ++q)
+            off_a[q] = (int)(mm_offset<T, C::TILE_I, C, A_BY_K>(whole_a, 0, q, MM_K<T>) - q * (C::THREADS / (C::TILE_I / MM_CHUNK<T>)) * s.a.ld * (int)sizeof(T));
 #pragma unroll
-        for (int q = 0; q < (B_BY_K ? 2 : 1); ++q) off_b[q] = mm_offset<C::TILE_J, C, B_BY_K>(whole_b, 0, q, MM_K) - q * C::THREADS / (C::TILE_J / 8) * (int)s.b.ld * 2;
+        for (int q = 0; q < (B_BY_K ? 2 : 1); ++q)
+            off_b[q] = (int)(mm_offset<T, C::TILE_J, C, B_BY_K>(whole_b, 0, q, MM_K<T>) - q * (C::THREADS / (C::TILE_J / MM_CHUNK<T>)) * s.b.ld * (int)sizeof(T));
         if (unit < units) open(s);
     }
-    __device__ __forceinline__ void place(const MmShape &s)
+    static __device__ __forceinline__ int whole_rows(const MmOperand &o, bool by_k)
     {
-        qa = (const char *)s.a.p + ((A_BY_K ? (int64_t)row_a : (int64_t)row_a * s.a.ld) + mm_plane_a(seg) * s.a.plane) * 2 + at * step_a;
-        qb = (const char *)s.b.p + ((B_BY_K ? (int64_t)row_b : (int64_t)row_b * s.b.ld) + mm_plane_b(seg) * s.b.plane) * 2 + at * step_b;
+        return by_k ? (o.rows + MM_CHUNK<T> - 1) / MM_CHUNK<T> * MM_CHUNK<T> : o.rows;
     }
     __device__ __forceinline__ void open(const MmShape &s)
     {
         const MmTile t = mm_tile(s, unit);
         row_a = t.i * C::TILE_I;
         row_b = t.j * C::TILE_J;
-        edge_a = row_a + C::TILE_I > (A_BY_K ? (s.a.rows + 7) / 8 * 8 : s.a.rows);
-        edge_b = row_b + C::TILE_J > (B_BY_K ? (s.b.rows + 7) / 8 * 8 : s.b.rows);
-        const int first = t.split * s.per_split;
-        at = s.planes == 1 ? first : first / 6;
-        seg = s.planes == 1 ? 0 : first - at * 6;
-        left = min(s.per_split, all_slices - first);
-        place(s);
+        edge_a = row_a + C::TILE_I > whole_rows(s.a, A_BY_K);
+        edge_b = row_b + C::TILE_J > whole_rows(s.b, B_BY_K);
+        at = t.split * s.per_split;
+        left = min(s.per_split, s.slices - at);
+        qa = (const char *)s.a.p + (A_BY_K ? (int64_t)row_a : (int64_t)row_a * s.a.ld) * (int)sizeof(T) + at * step_a;
+        qb = (const char *)s.b.p + (B_BY_K ? (int64_t)row_b : (int64_t)row_b * s.b.ld) * (int)sizeof(T) + at * step_b;
     }
     __device__ __forceinline__ void fetch(const MmShape &s, char *lds)
     {
         if (unit >= units) return;
-        const int last_k = A_BY_K ? s.a.k_rows - 1 - at * MM_K : MM_K;     // (the last k may not all be there)
-        mm_fetch<C::TILE_I, C, A_BY_K>(s.a, qa, row_a, off_a, edge_a || last_k < MM_K - 1, last_k, lds);
-        mm_fetch<C::TILE_J, C, B_BY_K>(s.b, qb, row_b, off_b, edge_b, MM_K, lds + C::TILE_I * MM_ROW);
+        const int last_k = A_BY_K ? s.a.k_rows - 1 - at * MM_K<T> : MM_K<T>;   // (the last k may not all be there)
+        mm_fetch<T, C::TILE_I, C, A_BY_K>(s.a, qa, row_a, off_a, edge_a || last_k < MM_K<T> - 1, last_k, lds);
+        mm_fetch<T, C::TILE_J, C, B_BY_K>(s.b, qb, row_b, off_b, edge_b, MM_K<T>, lds + C::TILE_I * MM_ROW);
+        ++at;
+        qa += step_a;
+        qb += step_b;
         if (--left == 0) {
             unit += gridDim.x;
             if (unit < units) open(s);
-        } else if (s.planes == 1) {
-            ++at;
-            qa += step_a;
-            qb += step_b;
-        } else {                                         // all products of a slice's planes, then the next slice
-            if (++seg == 6) { seg = 0; ++at; }
-            place(s);
         }
     }
 };
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-// Eight k of a row for every lane out of a slice that lies by k: lane l gives the address of four rows of k + l % 16 / 4 and gets four k of
-// row l % 16; the second four k lie four further on.
+// A lane's sixteen bytes of row l % 16 out of a slice that lies by k.  16 bits: lane l gives the address of four rows of k + l % 16 / 4 and
+// gets four k of its own; the second four k lie four further on.  32 bits: one k after the other.
 template <typename T, int ROWS>
 __device__ __forceinline__ typename Mfma<T>::frag mm_turned(const char *l)
 {
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)l), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(l + 4 * ROWS * 2));
-    return __builtin_bit_cast(typename Mfma<T>::frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    if constexpr (sizeof(T) == 4) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = *(const float *)(l + e * ROWS * 4);
+        return v;
+    } else {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)l), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(l + 4 * ROWS * 2));
+        return __builtin_bit_cast(typename Mfma<T>::frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
 }
 
 // Where the values of a tile lie: acc[mi][nj][r] = C[j][i] at i = i0 + place(mi) + r, j = j0 + nj * 16.  Where A lies by rows a lane has eight
@@ -217,20 +225,24 @@ template <typename C, bool A_BY_K> struct MmPlace {
     static __device__ __forceinline__ constexpr int place(int mi) { return A_BY_K ? mi * 16 : (mi >> 1) * 32 + (mi & 1) * 4; }
 };
 
-// Where this lane reads, and its fragments of 32 k of a slice.
+// Where this lane reads, and its fragments of half a slice.
 template <typename T, typename C, bool A_BY_K, bool B_BY_K> struct MmReader {
     typedef typename Mfma<T>::frag frag;
     int ra, rb, quarter, fa[A_BY_K ? C::MI : 2], fb[B_BY_K ? C::NJ : 1];
 
+    // by k: the lane's first k, its place in a row of k, and the bytes of a fragment's sixteen rows, which lie in whole chunks
+    static __device__ __forceinline__ int k_of(int lane) { return sizeof(T) == 2 ? 8 * (lane >> 4) + ((lane & 15) >> 2) : 4 * (lane >> 4); }
+    static __device__ __forceinline__ int in_row(int lane) { return sizeof(T) == 2 ? (lane & 3) * 8 : (lane & 15) * 4; }
+    static constexpr int FRAG = 16 * (int)sizeof(T);
+
     __device__ __forceinline__ MmReader()
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J, l16 = lane & 15;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / C::W_J, wj = wave % C::W_J, l16 = lane & 15, k = k_of(lane);
         quarter = lane >> 4;
-        const int k = 8 * quarter + (l16 >> 2);          // by k: of the first four; the second four lie four further on
         if constexpr (A_BY_K) {
-            ra = k * C::TILE_I * 2 + (l16 & 3) * 8;
+            ra = k * C::TILE_I * (int)sizeof(T) + in_row(lane);
 #pragma unroll
-            for (int i = 0; i < C::MI; ++i) fa[i] = ((wi * C::MI + i) ^ mm_turn_k<C::TILE_I>(k)) * 32;
+            for (int i = 0; i < C::MI; ++i) fa[i] = (wi * C::MI + i) * FRAG ^ mm_turn_k<T, C::TILE_I>(k) * 16;
         } else {
             const int row = (l16 >> 2) * 8 + (l16 & 3);  // of the even fragments; those of the odd ones lie four behind
             ra = (wi * C::MI * 16 + row) * MM_ROW;
@@ -238,25 +250,26 @@ template <typename T, typename C, bool A_BY_K, bool B_BY_K> struct MmReader {
             fa[1] = mm_turn(row + 4) * 16;
         }
         if constexpr (B_BY_K) {
-            rb = C::TILE_I * MM_ROW + k * C::TILE_J * 2 + (l16 & 3) * 8;
+            rb = C::TILE_I * MM_ROW + k * C::TILE_J * (int)sizeof(T) + in_row(lane);
 #pragma unroll
-            for (int j = 0; j < C::NJ; ++j) fb[j] = ((wj * C::NJ + j) ^ mm_turn_k<C::TILE_J>(k)) * 32;
+            for (int j = 0; j < C::NJ; ++j) fb[j] = (wj * C::NJ + j) * FRAG ^ mm_turn_k<T, C::TILE_J>(k) * 16;
         } else {
             rb = (C::TILE_I + wj * C::NJ * 16 + l16) * MM_ROW;
             fb[0] = mm_turn(l16) * 16;
         }
     }
-    __device__ __forceinline__ void read(const char *l, int kk, frag (&a)[C::MI], frag (&b)[C::NJ]) const
+    __device__ __forceinline__ void read(const char *l, int half, frag (&a)[C::MI], frag (&b)[C::NJ]) const
     {
-        const int chunk = (kk * 4 + quarter) * 16;
+        constexpr int K = MM_K<T> / 2;
+        const int chunk = (half * 4 + quarter) * 16;
 #pragma unroll
         for (int j = 0; j < C::NJ; ++j) {
-            if constexpr (B_BY_K) b[j] = mm_turned<T, C::TILE_J>(l + rb + fb[j] + kk * 32 * C::TILE_J * 2);
+            if constexpr (B_BY_K) b[j] = mm_turned<T, C::TILE_J>(l + rb + fb[j] + half * K * C::TILE_J * (int)sizeof(T));
             else b[j] = *(const frag *)(l + rb + j * 16 * MM_ROW + (chunk ^ fb[0]));
         }
 #pragma unroll
         for (int i = 0; i < C::MI; ++i) {
-            if constexpr (A_BY_K) a[i] = mm_turned<T, C::TILE_I>(l + ra + fa[i] + kk * 32 * C::TILE_I * 2);
+            if constexpr (A_BY_K) a[i] = mm_turned<T, C::TILE_I>(l + ra + fa[i] + half * K * C::TILE_I * (int)sizeof(T));
             else a[i] = *(const frag *)(l + ra + ((i >> 1) * 32 + (i & 1) * 4) * MM_ROW + (chunk ^ fa[i & 1]));
         }
     }
@@ -266,9 +279,11 @@ template <typename T, typename C>
 __device__ __forceinline__ void mm_add(const typename Mfma<T>::frag (&a)[C::MI], const typename Mfma<T>::frag (&b)[C::NJ], f32x4 (&acc)[C::MI][C::NJ])
 {
 #pragma unroll
-    for (int i = 0; i < C::MI; ++i)
+    for (int e = 0; e < Mfma<T>::STEPS; ++e)             // (a product never waits for the one before)
 #pragma unroll
-        for (int j = 0; j < C::NJ; ++j) acc[i][j] = Mfma<T>::mul(a[i], b[j], acc[i][j]);
+        for (int i = 0; i < C::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < C::NJ; ++j) acc[i][j] = Mfma<T>::step(a[i], b[j], e, acc[i][j]);
 }
 
 // Calls done(tile, acc) for every tile of this workgroup; MmPlace says what acc holds.  `done` has no barriers.
@@ -282,7 +297,7 @@ __device__ __forceinline__ void mm_tiles(const MmShape &s, const F &done)
     extern __shared__ __align__(16) char lds[];
     typedef typename Mfma<T>::frag frag;
     const MmReader<T, C, A_BY_K, B_BY_K> reader;
-    MmFetcher<C, A_BY_K, B_BY_K> next;
+    MmFetcher<T, C, A_BY_K, B_BY_K> next;
     next.begin(s);
     next.fetch(s, lds);
     int buf = 0;
@@ -298,7 +313,7 @@ __device__ __forceinline__ void mm_tiles(const MmShape &s, const F &done)
     };
     for (unsigned unit = blockIdx.x; unit < next.units; unit += gridDim.x) {
         const MmTile t = mm_tile(s, unit);
-        const int slices = min(s.per_split, next.all_slices - t.split * s.per_split);
+        const int slices = min(s.per_split, s.slices - t.split * s.per_split);
         f32x4 acc[C::MI][C::NJ];
 #pragma unroll
         for (int i = 0; i < C::MI; ++i)

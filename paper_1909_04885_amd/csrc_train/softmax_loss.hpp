@@ -4,70 +4,39 @@
 //   G_iv = weight_i (exp(z_iv - lse_i) - [v = label(i)]),  dx_i = sum_v G_iv w_v,  dw_v = sum_i G_iv x_i
 //   A row whose label is negative has the loss 0 and G = 0; its x counts nowhere, whatever it holds.
 //
-// The logits exist only as tiles of a product in registers.  `loss_tiles` leaves of a tile, for every row, the largest logit and the
-// sum of exponentials below it, and `loss_rows` joins these.  The gradient forms the logits again, a piece of the classes at a
-// time, and turns them in registers into G, which is stored in 16 bits for the two products that read it; rounding G is of the size
-// of the rounding of 16-bit gradients, and 32-bit operands keep G in three planes, which is exact.  Half precision would lose small G: there G comes times the power of two
-// that takes the largest weight to between 2^13 and 2^14, and the products times its inverse.
+// The loss: logits exist only as tiles of a product in registers.  `loss_tiles` leaves of a wavefront's part of a tile, for every row, the
+// largest logit and the sum of exponentials below it, and `loss_rows` joins these.
 //
-// The bound is the matrix cores: 2 n d classes operations for the loss, and three times that again for the gradients, one third of
-// it for the logits that were not kept.  Few rows are bound by reading w.
+// The gradient in 16 bits forms the logits again, a piece of the classes at a time, and turns them in registers into G, which is stored in
+// 16 bits for the two products that read it; rounding G is of the size of the rounding of the gradients themselves, and of no
+// direction: G comes divided by the largest weight, and the products times it, so that a weight that all rows share, which would be
+// rounded to the same side everywhere, is not rounded at all.  Half precision would lose small G: there it comes 2^14 times as large.  In 32 bits a product costs eight times as much, and the logits of a piece of the rows are
+// kept until they are G; so are those of few rows, which are few bytes beside w.
+//
+// The bound is the matrix cores: 2 n d classes operations for the loss, and twice that again for the gradients (three times in 16 bits).
+// Few rows are bound by reading w.
 #pragma once
-#include "matmul16.hpp"
+#include "matmul.hpp"
 
 namespace chicle_train {
 
 // ---- operands laid out for the products -----------------------------------------------------------------------------
 
-__device__ __forceinline__ void split_planes(float x, bf16 *p)
-{
-    const unsigned b = __float_as_uint(x);
-    const float lead = __uint_as_float(b & 0xffff0000u);
-    float rest = x - lead;
-    if ((b & 0x7f800000u) == 0x7f800000u) rest = 0.f;   // infinities and NaN are their leading plane
-    if (x != x) { p[0] = (bf16)x; p[1] = p[2] = (bf16)0.f; return; }
-    const float mid = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
-    p[0] = (bf16)lead;
-    p[1] = (bf16)mid;
-    p[2] = (bf16)(rest - mid);
-}
-
-template <typename T> struct Product { typedef T type; static constexpr int PLANES = 1; };
-template <> struct Product<float> { typedef bf16 type; static constexpr int PLANES = 3; };
-
-template <typename T, typename P>
-__device__ __forceinline__ void to_planes(T x, P *p)
-{
-    if constexpr (sizeof(T) == 4) split_planes(x, p);
-    else p[0] = x;
-}
-
-// out[plane][r][c] = in[r][c], zeros in columns [cols, ld) and in rows [rows, rows_out): whole slices of aligned chunks.  With labels,
-// rows that have none are zeros too.
+// out[r][c] = in[r][c], zeros in columns [cols, ld) and in rows [rows, rows_out): whole slices of aligned chunks.  With labels, rows that
+// have none are zeros too.
 template <typename T>
-__global__ __launch_bounds__(256) void lay_rows(const T *__restrict__ in, int64_t ldi, typename Product<T>::type *__restrict__ out, int64_t ld,
-                                                int64_t plane, int64_t rows, int64_t rows_out, int64_t cols, const void *labels, int wide, int64_t classes)
+__global__ __launch_bounds__(256) void lay_rows(const T *__restrict__ in, int64_t ldi, T *__restrict__ out, int64_t ld, int64_t rows, int64_t rows_out,
+                                                int64_t cols, const void *labels, int wide, int64_t classes)
 {
-    typedef typename Product<T>::type P;
-    constexpr int N = Product<T>::PLANES;
-    const int64_t per_row = ld / 8;
+    const int64_t per_row = ld / MM_CHUNK<T>;
     for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < rows_out * per_row; e += (int64_t)gridDim.x * 256) {
-        const int64_t r = e / per_row, c = (e - r * per_row) * 8;
+        const int64_t r = e / per_row, c = (e - r * per_row) * MM_CHUNK<T>;
         bool has = r < rows;
         if (has && labels) {
             const int64_t label = index_at(labels, wide, r);
             has = label >= 0 && label < classes;
         }
-        P p[N][8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            P q[N];
-            to_planes(has && c + k < cols ? in[r * ldi + c + k] : (T)0.f, q);
-#pragma unroll
-            for (int i = 0; i < N; ++i) p[i][k] = q[i];
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) __builtin_memcpy(out + i * plane + r * ld + c, p[i], 16);
+        *(u32x4 *)(out + r * ld + c) = has ? load_raw(in + r * ldi, c, cols) : u32x4{0u, 0u, 0u, 0u};
     }
 }
 
@@ -78,7 +47,7 @@ struct LossRows {
     int wide, n, classes;
     const float *lse;            // gradient
     const float *weight;
-    const float *power;          // half precision: G comes times this; else null
+    const float *power;          // 16 bits: G comes times this; else null
     float2 *part;                // [row][wavefront's part of a tile of classes]: largest logit, sum of exponentials below it
     float *picked;               // [row]: the label's logit
 };
@@ -107,10 +76,11 @@ template <bool EXACT> __device__ __forceinline__ float exp_of(float z, float m)
     return EXACT ? expf(z - m) : __builtin_amdgcn_exp2f((z - m) * LOG2E);
 }
 
-// i: classes, j: rows
-template <typename T, typename C, bool EXACT>
-__global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_tiles(MmShape s, LossRows l)
+// i: classes, j: rows.  logits (32 bits): null, or [row][ldz], where they are kept.
+template <typename T, typename C>
+__global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_tiles(MmShape s, LossRows l, T *__restrict__ logits, int64_t ldz)
 {
+    constexpr bool EXACT = sizeof(T) == 4;
     mm_tiles<T, C, false, false>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
         const MmPlace<C, false> at(t);
         if ((t.i + 1) * C::TILE_I > l.classes) {         // the last tile: what lies past the classes counts nowhere
@@ -133,6 +103,10 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_tiles(MmShape s,
                     for (int r = 0; r < 4; ++r) z = rel == at.place(mi) + r ? acc[mi][nj][r] : z;
                 l.picked[j] = z;
             }
+            if constexpr (EXACT)
+                if (logits && j < l.n)                   // (rows of logits are whole tiles long)
+#pragma unroll
+                    for (int mi = 0; mi < C::MI; ++mi) *(f32x4 *)(logits + (int64_t)j * ldz + at.i0 + at.place(mi)) = acc[mi][nj];
             float m = MINUS_INF;
 #pragma unroll
             for (int mi = 0; mi < C::MI; ++mi)
@@ -173,8 +147,8 @@ __global__ __launch_bounds__(256) void loss_rows(LossRows l, int tiles, float *_
     loss[j] = label >= 0 && label < l.classes ? lse - l.picked[j] : 0.f;
 }
 
-// power[0]: the power of two that takes the largest weight to [2^13, 2^14), power[1] its inverse.  One workgroup.
-__global__ __launch_bounds__(1024) void loss_power(const float *__restrict__ weight, int n, float *power)
+// power[0]: what takes the largest weight to `top`, power[1] its inverse.  One workgroup.
+__global__ __launch_bounds__(1024) void loss_power(const float *__restrict__ weight, int n, float top, float *power)
 {
     __shared__ float s[16];
     float m = 0.f;
@@ -187,20 +161,18 @@ __global__ __launch_bounds__(1024) void loss_power(const float *__restrict__ wei
     __syncthreads();
     if (threadIdx.x) return;
     for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
-    int e = 0;
-    frexpf(m, &e);                                       // m in [2^(e-1), 2^e)
-    e = m > 0.f ? max(-100, min(100, 14 - e)) : 0;
-    power[0] = ldexpf(1.f, e);
-    power[1] = ldexpf(1.f, -e);
+    const bool plain = m < 1e-30f || m > 1e30f;          // (no weight, or one whose inverse is out of range)
+    power[0] = plain ? 1.f : top / m;
+    power[1] = plain ? 1.f : m / top;
 }
 
 // ---- the gradients --------------------------------------------------------------------------------------------------
 
-// G of a piece of the classes: s.a is the piece's rows of w, `first` the piece's first class.  g[plane][row][class of the piece], with zeros
-// up to ldg and in rows [n, rows_out).
-template <typename T, typename C, bool EXACT, int PLANES>
+// G of a piece of the classes, 16 bits: s.a is the piece's rows of w, `first` the piece's first class.  g[row][class of the piece], with
+// zeros up to ldg and in rows [n, rows_out).
+template <typename T, typename C>
 __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_grad_tiles(MmShape s, LossRows l, int first, int piece, T *__restrict__ g, int64_t ldg,
-                                                                           int64_t plane_g, int rows_out)
+                                                                           int rows_out)
 {
     const float power = l.power ? l.power[0] : 1.f;
     mm_tiles<T, C, false, false>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
@@ -212,25 +184,42 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_grad_tiles(MmSha
             T *row = g + (int64_t)j * ldg;
 #pragma unroll
             for (int mp = 0; mp < C::MI / 2; ++mp) {     // eight neighbouring classes
-                T v[PLANES][8];
+                T v[8];
                 const int i = at.i0 + mp * 32;
 #pragma unroll
                 for (int h = 0; h < 8; ++h) {
-                    float p = exp_of<EXACT>(acc[2 * mp + h / 4][nj][h % 4], lse);
+                    float p = exp_of<false>(acc[2 * mp + h / 4][nj][h % 4], lse);
                     if (rel == mp * 32 + h) p -= 1.f;
-                    p = weight != 0.f && i + h < piece ? p * weight : 0.f;
-                    T q[PLANES];
-                    if constexpr (PLANES == 3) split_planes(p, q);
-                    else q[0] = (T)p;
-#pragma unroll
-                    for (int k = 0; k < PLANES; ++k) v[k][h] = q[k];
+                    v[h] = (T)(weight != 0.f && i + h < piece ? p * weight : 0.f);
                 }
-                if (j < rows_out && i < ldg)
-#pragma unroll
-                    for (int k = 0; k < PLANES; ++k) __builtin_memcpy(row + k * plane_g + i, v[k], 16);
+                if (j < rows_out && i < ldg) __builtin_memcpy(row + i, v, 16);
             }
         }
     });
+}
+
+// G of logits that were kept: g[row][class] of all classes, zeros up to ldg and in rows [n, rows_out).  g may be the logits themselves.
+// Grid: (columns, rows).
+template <typename T>
+__global__ __launch_bounds__(256) void loss_grad_kept(const float *logits, int64_t ldz, LossRows l, T *g, int64_t ldg)
+{
+    const int j = blockIdx.y, label = label_at(l, j);
+    const float power = l.power ? l.power[0] : 1.f;
+    const float weight = label >= 0 ? l.weight[j] * power : 0.f, lse = label >= 0 ? l.lse[j] : 0.f;
+    for (int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; c < ldg; c += (int64_t)gridDim.x * 1024) {
+        T v[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            float p = 0.f;
+            if (weight != 0.f && c + h < l.classes) {
+                p = expf(logits[j * ldz + c + h] - lse);
+                if (c + h == label) p -= 1.f;
+                p *= weight;
+            }
+            v[h] = (T)p;
+        }
+        __builtin_memcpy(g + j * ldg + c, v, sizeof v);
+    }
 }
 
 // G w, of w as it lies, by k: out[j][i] in 32 bits, split `split` of the sum in its own copy of `out`.
@@ -250,9 +239,9 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_parts(MmShape
     });
 }
 
-// x by G, both of which lie by k: out[j][i] = scale * sum, rounded.
-template <typename T, typename C, typename O>
-__global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_out(MmShape s, O *__restrict__ out, int64_t ld, const float *__restrict__ scale)
+// x by G, both of which lie by k: out[j][i] = scale * sum, rounded; or added to what out holds.
+template <typename T, typename C, bool ADD>
+__global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_out(MmShape s, T *__restrict__ out, int64_t ld, const float *__restrict__ scale)
 {
     const float f = scale ? *scale : 1.f;
     mm_tiles<T, C, true, true>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
@@ -263,10 +252,14 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_out(MmShape s
             for (int mi = 0; mi < C::MI; ++mi) {
                 const int i = at.i0 + at.place(mi), j = at.j0 + nj * 16;
                 if (j >= s.b.rows) continue;
-                O v[4];
+                T *dst = out + (int64_t)j * ld + i;
+                if constexpr (ADD)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = (O)(acc[mi][nj][r] * f);
-                O *dst = out + (int64_t)j * ld + i;
+                    for (int r = 0; r < 4; ++r)
+                        if (i + r < s.a.rows) acc[mi][nj][r] += (float)dst[r];
+                T v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = (T)(acc[mi][nj][r] * f);
                 if (i + 4 <= s.a.rows) __builtin_memcpy(dst, v, sizeof v);
                 else
 #pragma unroll
@@ -276,82 +269,70 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_out(MmShape s
     });
 }
 
-// dx = scale * the sum of the copies, in their order: SUM_SLICES threads to four columns, each of which adds up a run of the copies.
-// ld of a copy is a multiple of four.
-constexpr int SUM_SLICES = 8;
-
-template <typename O>
+// dx = scale * the sum of the copies, in their order: SLICES threads to four columns, each of which adds up a run of the copies.  ld of a copy
+// is a multiple of four.
+template <typename O, int SLICES>
 __global__ __launch_bounds__(256) void sum_parts(const float *__restrict__ part, int64_t ld, int64_t copy, int copies, O *__restrict__ out, int64_t ldo,
                                                  int64_t rows, int64_t cols, const float *__restrict__ scale)
 {
-    constexpr int EACH = 256 / SUM_SLICES;
-    __shared__ f32x4 s[SUM_SLICES][EACH];
+    constexpr int EACH = 256 / SLICES;
+    __shared__ f32x4 s[SLICES][EACH];
     const int64_t per_row = ld / 4, all = rows * per_row;
     const float f = scale ? *scale : 1.f;
     const int slice = threadIdx.x / EACH, mine = threadIdx.x % EACH;
-    const int first = (int)((int64_t)copies * slice / SUM_SLICES), end = (int)((int64_t)copies * (slice + 1) / SUM_SLICES);
+    const int first = (int)((int64_t)copies * slice / SLICES), end = (int)((int64_t)copies * (slice + 1) / SLICES);
     for (int64_t e0 = (int64_t)blockIdx.x * EACH; e0 < all; e0 += (int64_t)gridDim.x * EACH) {
         const int64_t e = min(e0 + mine, all - 1), r = e / per_row, c = (e - r * per_row) * 4;
         const float *src = part + r * ld + c;
         f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int k = first; k < end; ++k) t += *(const f32x4 *)(src + k * copy);
-        __syncthreads();
-        s[slice][mine] = t;
-        __syncthreads();
+        if constexpr (SLICES > 1) {
+            __syncthreads();
+            s[slice][mine] = t;
+            __syncthreads();
+            for (int q = 1; q < SLICES; ++q) t += slice == 0 ? s[q][mine] : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
         if (slice || e0 + mine >= all) continue;
-        for (int q = 1; q < SUM_SLICES; ++q) t += s[q][mine];
+        O v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < cols) out[r * ldo + c + i] = (O)(t[i] * f);
+        for (int i = 0; i < 4; ++i) v[i] = (O)(t[i] * f);
+        O *dst = out + r * ldo + c;
+        if (c + 4 <= cols) __builtin_memcpy(dst, v, sizeof v);
+        else
+            for (int i = 0; i < 3; ++i)
+                if (c + i < cols) dst[i] = v[i];
     }
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------
 //
-// Few rows are bound by reading w.  `loss_few` reads it as it lies, whatever its type, distance and alignment: a wavefront takes sixteen
-// classes at a time, its lanes' sixteen bytes being the matrix instruction's operand as they come, and x lies in LDS.  32-bit values are
-// split into their planes on the way.  For the gradient it leaves the logits, which beside w are few bytes, and
-// `loss_grad_few` reads w once more: a thread owns a vector of columns and forms dw's rows and its part of dx in 32 bits.
+// Few rows are bound by reading w.  `loss_few` reads it as it lies, whatever its distance and alignment: a wavefront takes sixteen classes at a
+// time, its lanes' sixteen bytes being the matrix instruction's operand as they come, and x lies in LDS.  For the gradient it leaves
+// the logits.  `loss_grad_few`, for the fewest rows, reads w once more: a thread owns a vector of columns and forms dw's rows and its
+// part of dx in 32 bits.
 
-constexpr int FEW_ROWS = 16, FEW_MOST_ROWS = 64, FEW_GRAD_ROWS = 8, FEW_AHEAD = 8, FEW_BATCH = 32 * FEW_AHEAD, FEW_THREADS = 512;
+constexpr int FEW_ROWS = 64, FEW_GRAD_ROWS = 8, FEW_AHEAD = 8, FEW_THREADS = 512;
+template <typename T> constexpr int FEW_BATCH = MM_K<T> / 2 * FEW_AHEAD;   // k of a batch of accesses
 
-template <typename T, typename P>
-__device__ __forceinline__ void few_planes(const u32x4 *raw, typename Mfma<P>::frag *f)
-{
-    if constexpr (sizeof(T) == 2) f[0] = __builtin_bit_cast(typename Mfma<P>::frag, raw[0]);
-    else {
-        float v[8];
-        unpack<float>(raw[0], v);
-        unpack<float>(raw[1], v + 4);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            P q[3];
-            split_planes(v[i], q);
-            f[0][i] = q[0]; f[1][i] = q[1]; f[2][i] = q[2];
-        }
-    }
-}
-
-// Rows 16 nr + l % 16 of x in LDS, `chunk` columns at a time where not all of them fit: x[plane][row][chunk + 8], zeros past d; then (largest,
+// Rows 16 q + l % 16 of x in LDS, `chunk` columns at a time where not all of them fit: x[row][chunk + one chunk], zeros past d; then (largest,
 // sum) of every wavefront and row.  part[row][workgroup]; logits[row][ldz], may be null.  chunk is a multiple of a batch.
 template <typename T, int NR>
-__global__ __launch_bounds__(FEW_THREADS) void loss_few(const T *__restrict__ x, int64_t ldx, const T *__restrict__ w, int64_t ldw, int64_t d, LossRows l, int chunk,
-                                                 int passes, float *__restrict__ logits, int64_t ldz)
+__global__ __launch_bounds__(FEW_THREADS) void loss_few(const T *__restrict__ x, int64_t ldx, const T *__restrict__ w, int64_t ldw, int64_t d, LossRows l,
+                                                        int chunk, int passes, float *__restrict__ logits, int64_t ldz)
 {
-    typedef typename Product<T>::type P;
-    typedef typename Mfma<P>::frag frag;
-    constexpr int N = Product<T>::PLANES, RAW = sizeof(T) / 2, U = FEW_AHEAD / RAW, BATCH = 32 * U;   // RAW accesses to a fragment, U fragments to a batch
+    typedef typename Mfma<T>::frag frag;
+    constexpr int U = FEW_AHEAD, K = MM_K<T> / 2, V = MM_CHUNK<T>;         // K of an access
     constexpr bool EXACT = sizeof(T) == 4;
     extern __shared__ __align__(16) char lds[];
-    P *xs = (P *)lds;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, l16 = lane & 15, quarter = lane >> 4, ld = chunk + 8;
-    const int k_end = (int)((d + 31) / 32 * 32);
+    T *xs = (T *)lds;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, l16 = lane & 15, quarter = lane >> 4, ld = chunk + V;
+    const int k_end = (int)((d + K - 1) / K * K);
     int at[NR], label[NR];
     float m[NR], sum[NR];
 #pragma unroll
     for (int q = 0; q < NR; ++q) {
-        at[q] = min(16 * q + l16, l.n - 1) * ld + quarter * 8;
+        at[q] = min(16 * q + l16, l.n - 1) * ld + quarter * V;
         label[q] = label_at(l, 16 * q + l16);
         m[q] = MINUS_INF;
         sum[q] = 0.f;
@@ -362,45 +343,33 @@ __global__ __launch_bounds__(FEW_THREADS) void loss_few(const T *__restrict__ x,
         f32x4 acc[NR];
 #pragma unroll
         for (int q = 0; q < NR; ++q) acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
-        auto ask = [&](u32x4 (&raw)[U][RAW], int k0) __attribute__((always_inline)) {
+        auto ask = [&](u32x4 (&raw)[U], int k0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = load_raw<T, true>(row, k0 + u * K + quarter * V, d);
+        };
+        auto use = [&](const u32x4 (&raw)[U], int k0) __attribute__((always_inline)) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int h = 0; h < RAW; ++h) raw[u][h] = load_raw<T, true>(row, k0 + u * 32 + quarter * 8 + h * 4, d);
-        };
-        auto use = [&](const u32x4 (&raw)[U][RAW], int k0) __attribute__((always_inline)) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                frag a[N];
-                few_planes<T, P>(raw[u], a);
-#pragma unroll
                 for (int q = 0; q < NR; ++q) {
-                    frag b[N];
+                    const frag b = *(const frag *)(xs + at[q] + k0 + u * K);
 #pragma unroll
-                    for (int k = 0; k < N; ++k) b[k] = *(const frag *)(xs + k * l.n * ld + at[q] + k0 + u * 32);
-#pragma unroll
-                    for (int z = 0; z < (N == 3 ? 6 : 1); ++z) acc[q] = Mfma<P>::mul(a[N == 3 ? mm_plane_a(z) : 0], b[N == 3 ? mm_plane_b(z) : 0], acc[q]);
+                    for (int e = 0; e < Mfma<T>::STEPS; ++e) acc[q] = Mfma<T>::step(__builtin_bit_cast(frag, raw[u]), b, e, acc[q]);
                 }
-            }
         };
         for (int kc = 0; kc < k_end; kc += chunk) {
             const int end = min(chunk, k_end - kc);
-            u32x4 raw0[U][RAW], raw1[U][RAW];
+            u32x4 raw0[U], raw1[U];
             ask(raw0, kc);                               // (on its way while x goes to LDS)
             if (pass == 0 || chunk < k_end) {
                 __syncthreads();
-                for (int e = threadIdx.x; e < l.n * (chunk / 8); e += blockDim.x) {
-                    const int r = e / (chunk / 8), c = (e - r * (chunk / 8)) * 8;
-                    u32x4 v[RAW];
-#pragma unroll
-                    for (int h = 0; h < RAW; ++h) v[h] = load_raw<T>(x + r * ldx, kc + c + h * 4, d);
-                    frag f[N];
-                    few_planes<T, P>(v, f);
-#pragma unroll
-                    for (int k = 0; k < N; ++k) *(frag *)(xs + (k * l.n + r) * ld + c) = f[k];
+                for (int e = threadIdx.x; e < l.n * (chunk / V); e += blockDim.x) {
+                    const int r = e / (chunk / V), c = (e - r * (chunk / V)) * V;
+                    *(u32x4 *)(xs + r * ld + c) = load_raw<T>(x + r * ldx, kc + c, d);
                 }
                 __syncthreads();
             }
+            constexpr int BATCH = FEW_BATCH<T>;
             for (int k0 = 0; k0 < end; k0 += 2 * BATCH) {
                 if (k0 + BATCH < end) ask(raw1, kc + k0 + BATCH);
                 use(raw0, k0);

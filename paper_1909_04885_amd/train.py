@@ -63,7 +63,7 @@ def load_train_library():
 
 
 class TrainOps:
-    """The operators on one GPU.  Holds the library, the device and one flag word; safe to use on several streams."""
+    """The operators on one GPU.  Holds the library, the device and one flag word; may be used on several streams."""
 
     def __init__(self, device: str = "cuda:0"):
         import torch
@@ -81,8 +81,7 @@ class TrainOps:
         self._wide = {torch.int32: 0, torch.int64: 1}
         # (the handle of the current stream, without an object around it)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
-        self._flags = torch.zeros(1, dtype=torch.int32, device=self.device)
-        torch.cuda.synchronize(self.device)          # the word is zero before any stream's work looks at it
+        self._flag_word = None
 
     # -- helpers
     def _call(self, fn, *args):
@@ -101,6 +100,13 @@ class TrainOps:
 
     def _workspace(self, nbytes: int):
         return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
+
+    def _flags(self):
+        """The address of the word in which kernels note a label or token out of range; made when it is first needed."""
+        if self._flag_word is None:
+            self._flag_word = self._torch.zeros(1, dtype=self._torch.int32, device=self.device)
+            self._torch.cuda.synchronize(self.device)   # it is zero before any stream's work looks at it
+        return self._flag_word.data_ptr()
 
     def _matrix(self, a, name: str, type_of=None, cols: Optional[int] = None):
         """A 2-D tensor of a supported type on this GPU, rows of unit stride that do not overlap: (type, row distance)."""
@@ -140,7 +146,7 @@ class TrainOps:
         nbytes = self._L.chicle_softmax_loss_bytes(xp, ldx, wp, ldw, n, d, c, t, 0)
         ws = self._workspace(nbytes)
         self._call(self._L.chicle_softmax_loss, xp, ldx, wp, ldw, lp, wide, n, d, c, t, loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes,
-                   self._flags.data_ptr())
+                   self._flags())
         return loss, lse
 
     def softmax_loss_grad(self, x, w, labels, row_weight):
@@ -156,7 +162,7 @@ class TrainOps:
         nbytes = self._L.chicle_softmax_loss_bytes(xp, ldx, wp, ldw, n, d, c, t, 1)
         ws = self._workspace(nbytes)
         self._call(self._L.chicle_softmax_loss_grad, xp, ldx, wp, ldw, lp, wide, rp, n, d, c, t, loss.data_ptr(), dx.data_ptr(), d, dw.data_ptr(), d,
-                   ws.data_ptr(), nbytes, self._flags.data_ptr())
+                   ws.data_ptr(), nbytes, self._flags())
         return loss, dx, dw
 
     # -- table lookup
@@ -168,7 +174,7 @@ class TrainOps:
         ip, wide = self._indices(flat, "ids")
         n = flat.shape[0]
         out = self._empty((*ids.shape, d), table.dtype)
-        self._call(self._L.chicle_embed, table.data_ptr(), ld, rows, ip, wide, n, d, t, scale, out.data_ptr(), d, self._flags.data_ptr())
+        self._call(self._L.chicle_embed, table.data_ptr(), ld, rows, ip, wide, n, d, t, scale, out.data_ptr(), d, self._flags())
         return out
 
     def embed_grad(self, ids, dout, n_rows: int, scale: float = 1.0, into=None):
@@ -193,7 +199,7 @@ class TrainOps:
         nbytes = self._L.chicle_embed_grad_bytes(n, d, n_rows)
         ws = self._workspace(nbytes)
         self._call(self._L.chicle_embed_grad, ip, wide, dout.data_ptr(), ldd, n, d, n_rows, t, scale, int(into is not None), out.data_ptr(), ldo,
-                   ws.data_ptr(), nbytes, self._flags.data_ptr())
+                   ws.data_ptr(), nbytes, self._flags())
         return out
 
     # -- layer norm
@@ -264,7 +270,8 @@ class TrainOps:
 
     def sync(self):
         """Wait for the current stream; raise if a label or token since the last sync was past the end."""
-        bits = int(self._flags.item())
+        self._flags()
+        bits = int(self._flag_word.item())
         if bits:
-            self._flags.zero_()
+            self._flag_word.zero_()
             raise ChicleError(EDEVICE, "%s out of range" % " and ".join(s for b, s in ((1, "a label"), (2, "a token")) if bits & b))
