@@ -88,27 +88,28 @@ int pow2_at_least(int64_t x, int most)
 
 struct RowShape { int lanes, vectors, threads; };        // vectors 0: the row is not held
 
-// Threads of a row and vectors of each: up to `most_values` values to a thread.
-RowShape row_shape(int64_t d, int vec, int most_values)
+// Threads of a row and vectors of each: up to `first_values` values to a thread, then up to LN_MOST_THREADS threads, then up to `most_values`.
+RowShape row_shape(int64_t d, int vec, int first_values, int most_values)
 {
     const int64_t v = ceil_div(d, vec);
     const int most = most_values / vec;
     RowShape s;
     s.vectors = 1;
     s.lanes = pow2_at_least(v, 256);
-    while ((int64_t)s.lanes * s.vectors < v && s.vectors < most) s.vectors *= 2;
+    while ((int64_t)s.lanes * s.vectors < v && s.vectors < first_values / vec) s.vectors *= 2;
     while ((int64_t)s.lanes * s.vectors < v && s.lanes < LN_MOST_THREADS) s.lanes *= 2;
+    while ((int64_t)s.lanes * s.vectors < v && s.vectors < most) s.vectors *= 2;
     if ((int64_t)s.lanes * s.vectors < v) s.vectors = 0;
     s.threads = s.lanes > 256 ? s.lanes : 256;
     return s;
 }
 
-constexpr int LN_FORWARD_VALUES = 32, LN_GRAD_VALUES = 8;
+constexpr int LN_FORWARD_VALUES = 32, LN_GRAD_VALUES = 16;
 constexpr int LN_GRAD_GRID = 1024;
 
 int64_t layer_norm_parts(int64_t n, int64_t d, int32_t type)
 {
-    const RowShape s = row_shape(d, 16 / size_of(type), LN_GRAD_VALUES);
+    const RowShape s = row_shape(d, 16 / size_of(type), LN_GRAD_VALUES / 2, LN_GRAD_VALUES);
     const int64_t g = ceil_div(n, s.threads / s.lanes);
     return g < LN_GRAD_GRID ? g : LN_GRAD_GRID;
 }
@@ -174,13 +175,14 @@ struct LossPlan {
     int64_t n, d, classes, ldk;          // ldk: length of laid-out rows along d
     int config;
     bool few, few_grad, tiles, kept, lay_x, lay_w;   // few: of the loss, of the gradient; tiles: something goes by products; kept: the logits
+    int loss_splits;                     // of the loss's sums, more than 1 where tiles are few
     int few_blocks, few_passes, few_threads, few_chunk, few_lds, few_each, few_grad_blocks;
     // gradient: pieces of the classes, or, with logits kept, of the rows
     int64_t piece, piece_rows, ldz, ldg, ldp;        // ldz, ldg: length of the rows of the logits and of G; ldp: of the rows of dx's parts
     int64_t rows_x, rows_g;                          // rows of the laid-out x and of G: whole slices
     int pieces, splits, config_dx, config_dw;
     void *x, *w, *g;
-    float *logits, *parts, *lse, *picked, *power;
+    float *logits, *parts, *rest_parts, *lse, *picked, *power;
     float2 *tile_sums;
     size_t bytes;
 };
@@ -192,6 +194,15 @@ constexpr int64_t LOSS_MOST = (int64_t)1 << 22, LOSS_MOST_D = (int64_t)1 << 21, 
 // Rows 1024 bytes apart, or a multiple of that, meet in few channels of the L2: half a slice more.
 int64_t spread(int64_t ld, int size) { return ld * size % 1024 == 0 ? ld + MM_ROW / size : ld; }
 
+// Classes at the end of a piece whose tiles of dw are split: those past the last whole round of tiles, where they are less than half a round.
+int64_t dw_rest(int config, int64_t d, int64_t classes, int64_t slices)
+{
+    const int64_t across = ceil_div(d, 256), tiles = across * ceil_div(classes, 256), over = tiles % CUS;
+    if (config != WIDE || tiles < CUS || over == 0 || over * 2 > CUS || slices < 16) return 0;
+    const int64_t rest = classes - tiles / CUS * CUS / across * 256;
+    return across * ceil_div(rest, 256) * 2 > CUS ? 0 : rest;
+}
+
 LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t n, int64_t d, int64_t classes, int32_t type, bool grad, void *workspace)
 {
     LossPlan p = {};
@@ -202,10 +213,20 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
     const int64_t slice = MM_ROW / size;
     // rows that are whole slices of aligned chunks are read where they are
     auto as_is = [&](const void *q, int64_t ld) { return d % slice == 0 && ld * size % 16 == 0 && (uintptr_t)q % 16 == 0 && ld < LOSS_MOST_D; };
-    // Few rows read w as it lies, up to 64 of them where it would have to be laid out first, or where products cost eight times as much.
-    p.few = n <= (as_is(w, ldw) && size == 2 ? FEW_ROWS / 4 : FEW_ROWS);
+    // Few rows read w as it lies, more of them where it would have to be laid out first or where products cost eight times as much.
+    p.few = n <= (size == 4 ? FEW_ROWS : as_is(w, ldw) ? 16 : 64);
     p.few_grad = grad && n <= FEW_GRAD_ROWS;
-    p.kept = grad && (p.few || size == 4);
+    p.config = mm_choose(size, classes, n);
+    p.loss_splits = 1;
+    if (!p.few) {
+        // tiles that leave half of the chip idle (in 32 bits: some of it), and sums long enough to be divided
+        const int64_t tiles = ceil_div(classes, mm_tile_i(p.config)) * ceil_div(n, mm_tile_j(p.config)), slices = ceil_div(d, slice), room = 2 * CUS;
+        if (tiles * (size == 4 ? 1 : 2) <= CUS && slices >= 16) {
+            const int64_t most = room / tiles < slices / 4 ? room / tiles : slices / 4;
+            p.loss_splits = (int)ceil_div(slices, ceil_div(slices, most));
+        }
+    }
+    p.kept = grad && (p.few || size == 4 || p.loss_splits > 1);
     p.tiles = grad ? !p.few_grad : !p.few;
     p.lay_w = p.tiles && !as_is(w, ldw);
     p.piece_rows = n;
@@ -225,9 +246,8 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         p.few_passes = (int)ceil_div(blocks, p.few_blocks);
         p.tile_sums = c.take<float2>(n * p.few_blocks);
     }
-    p.config = mm_choose(size, classes, n);
     p.ldz = round_up(classes, 256) + 32;                 // (whole tiles, and not a multiple of 1024 bytes)
-    if (p.kept && !p.few) {                              // as many rows as the logits have room for, at least a tile's
+    if (p.kept && !p.few && p.loss_splits == 1) {        // as many rows as the logits have room for, at least a tile's
         const int64_t most = LOSS_KEPT_BYTES / (p.ldz * 4) / 256 * 256;
         p.pieces = (int)ceil_div(n, most < 256 ? 256 : most);
         p.piece_rows = round_up(ceil_div(n, p.pieces), 256);
@@ -241,7 +261,8 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         p.logits = c.take<float>(n * p.ldz);
         p.parts = c.take<float>(p.few_grad_blocks * n * p.ldp);
     }
-    if (!p.few) p.tile_sums = c.take<float2>(p.piece_rows * ceil_div(classes, mm_tile_i(p.config)) * MM_PARTS_I);
+    if (p.loss_splits > 1 && !grad) p.logits = c.take<float>(n * p.ldz * p.loss_splits);
+    if (!p.few && p.loss_splits == 1) p.tile_sums = c.take<float2>(p.piece_rows * ceil_div(classes, mm_tile_i(p.config)) * MM_PARTS_I);
     if (p.tiles) {
         p.ldk = spread(round_up(d, slice), size);
         p.rows_x = grad ? round_up(n, slice) : n;
@@ -254,7 +275,7 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         p.power = c.take<float>(2);
         if (p.kept) {
             p.piece = classes;
-            if (p.few) p.pieces = 1;
+            if (p.few || p.loss_splits > 1) p.pieces = 1;
         } else {
             int64_t most = LOSS_PIECE_BYTES / (size * p.rows_x) / 256 * 256;
             most = most < 256 ? 256 : most;
@@ -275,9 +296,10 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         splits = splits < 1 ? 1 : splits;
         p.splits = (int)ceil_div(slices, ceil_div(slices, splits));
         p.config_dw = mm_choose(size, d, p.piece);
-        if (p.kept) p.logits = c.take<float>(p.rows_g * p.ldz);
+        if (p.kept) p.logits = c.take<float>(p.rows_g * p.ldz * p.loss_splits);
         p.g = size == 4 ? (void *)p.logits : c.take<char>(p.rows_g * p.ldg * size);
         p.parts = c.take<float>(p.piece_rows * p.ldp * p.splits * (p.kept ? 1 : p.pieces));
+        if (p.config_dw == WIDE) p.rest_parts = c.take<float>((int64_t)CUS * 256 * 256);     // (splits of the last tiles of dw, a round of them)
     }
     p.bytes = c.total();
     return p;
@@ -360,6 +382,8 @@ int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw
     int parts;
     if (p.few) {
         auto kernel = p.n <= 16 ? loss_few<T, 1> : p.n <= 32 ? loss_few<T, 2> : loss_few<T, 4>;
+        if constexpr (sizeof(T) == 4)
+            if (p.n > 64) kernel = loss_few<T, 6>;
         TRY(allow_lds(kernel, p.few_lds));
         kernel<<<(unsigned)p.few_blocks, p.few_threads, p.few_lds, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_chunk, p.few_passes, logits, p.ldz);
         TRY(launched("loss_few"));
@@ -367,7 +391,19 @@ int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw
     } else {
         const int64_t ldx_in = p.lay_x ? p.ldk : ldx;
         const MmOperand a = {p.w, p.lay_w ? p.ldk : ldw, (int)p.classes, 0}, b = {(const T *)p.x + first * ldx_in, ldx_in, (int)many, 0};
-        const MmShape s = mm_shape<T>(a, b, p.d, p.config, 1);
+        const MmShape s = mm_shape<T>(a, b, p.d, p.config, p.loss_splits);
+        if (p.loss_splits > 1) {
+            const int64_t copy = (p.rows_g ? p.rows_g : p.n) * p.ldz;
+            TRY(with_config<T, MmMiddle>(p.config, [&](auto c) {
+                typedef decltype(c) C;
+                auto kernel = product_parts<T, C, false, false>;
+                TRY(allow_lds(kernel, C::LDS));
+                kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.logits, p.ldz, copy);
+                return launched("product_parts");
+            }));
+            loss_join<<<(unsigned)many, 256, 0, stream>>>(rows, p.logits, p.ldz, copy, s.splits, loss + first, lse + first, flags);
+            return launched("loss_join");
+        }
         TRY(with_config<T, MmWide>(p.config, [&](auto c) {
             typedef decltype(c) C;
             auto kernel = loss_tiles<T, C>;
@@ -388,26 +424,40 @@ int run_loss_products(const LossPlan &p, int64_t row0, int64_t rows, const T *w,
 {
     const int64_t rows_g = round_up(rows, MM_K<T>);
     const MmOperand x_by_k = {(const T *)p.x + row0 * p.ldk, p.ldk, (int)p.d, (int)rows_g}, w_by_k = {w + class0 * ldw, ldw, (int)p.d, (int)classes};
-    const MmOperand g_rows = {p.g, ldg, (int)rows, 0}, g_by_k = {p.g, ldg, (int)classes, (int)rows_g};
+    const MmOperand g_rows = {p.g, ldg, (int)rows, 0};
     TRY(with_config<T, MmWideByK>(p.config_dx, [&](auto c) {
         typedef decltype(c) C;
         const MmShape s = mm_shape<T>(w_by_k, g_rows, classes, p.config_dx, p.splits);
-        auto kernel = product_parts<T, C>;
+        auto kernel = product_parts<T, C, true, false>;
         TRY(allow_lds(kernel, C::LDS));
         kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.parts + (int64_t)copies * p.piece_rows * p.ldp, p.ldp, p.piece_rows * p.ldp);
         copies += s.splits;
         return launched("product_parts");
     }));
-    return with_config<T, MmWideByK>(p.config_dw, [&](auto c) {
+    // dw: the last classes' tiles, where a few of them would keep the chip for another round, go by splits of the sum
+    const int64_t rest = dw_rest(p.config_dw, p.d, classes, rows_g / MM_K<T>), most = classes - rest;
+    const MmOperand g_most = {p.g, ldg, (int)most, (int)rows_g}, g_rest = {(const T *)p.g + most, ldg, (int)rest, (int)rows_g};
+    TRY(with_config<T, MmWideByK>(p.config_dw, [&](auto c) {
         typedef decltype(c) C;
-        const MmShape s = mm_shape<T>(x_by_k, g_by_k, rows_g, p.config_dw, 1);
+        const MmShape s = mm_shape<T>(x_by_k, g_most, rows_g, p.config_dw, 1);
         auto kernel = product_out<T, C, false>;
         if constexpr (sizeof(T) == 4)                    // (pieces of the rows)
             if (add) kernel = product_out<T, C, true>;
         TRY(allow_lds(kernel, C::LDS));
         kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, dw + class0 * lddw, lddw, inverse);
         return launched("product_out");
-    });
+    }));
+    if (rest == 0) return CHICLE_OK;
+    if constexpr (sizeof(T) == 2) {
+        typedef MmWideByK C;
+        const MmShape s = mm_shape<T>(x_by_k, g_rest, rows_g, WIDE, (int)(CUS / (ceil_div(p.d, 256) * ceil_div(rest, 256))));
+        auto kernel = product_parts<T, C, true, true>;
+        TRY(allow_lds(kernel, C::LDS));
+        kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.rest_parts, p.ldp, rest * p.ldp);
+        TRY(launched("product_parts"));
+        return run_sum_parts<T>(p.rest_parts, p.ldp, rest * p.ldp, s.splits, dw + (class0 + most) * lddw, lddw, rest, p.d, inverse, stream);
+    }
+    return CHICLE_OK;
 }
 
 template <typename T>
@@ -483,6 +533,7 @@ constexpr int64_t EMBED_MOST_D = (1 << 23) - 1;          // blocks of columns ar
 struct EmbedPlan {
     int64_t pieces, tile, ldp, seen_bytes;
     int tiles, passes, digit;
+    bool one;                            // one workgroup sorts
     unsigned *keys[2], *places[2], *count;
     uint8_t *seen;
     float *head, *tail;
@@ -496,13 +547,14 @@ EmbedPlan embed_plan(int64_t n, int64_t d, int64_t n_rows, void *workspace)
     p.ldp = round_up(d, 8);
     int bits = 1;
     while (((int64_t)1 << bits) <= n_rows) ++bits;       // keys are 0 .. n_rows
-    p.passes = n <= SORT_ONE ? 0 : (int)ceil_div(bits, SORT_BITS);
-    p.digit = p.passes ? (int)ceil_div(bits, p.passes) : 0;
+    p.passes = (int)ceil_div(bits, SORT_BITS);
+    p.digit = (int)ceil_div(bits, p.passes);
+    p.one = n <= SORT_ONE;
     p.tile = round_up(ceil_div(n, SORT_MOST_TILES), SORT_LEAST_TILE);
     p.tiles = n ? (int)ceil_div(n, p.tile) : 0;
     Carver c(workspace);
-    for (int k = 0; k < (p.passes ? 2 : 1); ++k) { p.keys[k] = c.take<unsigned>(n); p.places[k] = c.take<unsigned>(n); }
-    if (p.passes) p.count = c.take<unsigned>((int64_t)p.tiles << p.digit);
+    for (int k = 0; k < (p.one ? 1 : 2); ++k) { p.keys[k] = c.take<unsigned>(n); p.places[k] = c.take<unsigned>(n); }
+    if (!p.one) p.count = c.take<unsigned>((int64_t)p.tiles << p.digit);
     p.seen_bytes = round_up(n_rows, 16);
     p.seen = c.take<uint8_t>(p.seen_bytes);
     p.head = c.take<float>(p.pieces * p.ldp);
@@ -607,8 +659,9 @@ int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t l
     const EmbedPlan p = embed_plan(n, d, n_rows, workspace);
     uint8_t *seen = accumulate ? nullptr : p.seen;
     int last = 0;
-    if (!p.passes) {
-        sort_tokens_one<<<1, 1024, 0, stream>>>(ids, wide, (int)n, n_rows, p.keys[0], p.places[0], seen, p.seen_bytes, flags);
+    if (p.one) {
+        auto kernel = n <= SORT_ONE_THREADS ? sort_tokens_one<1> : sort_tokens_one<4>;
+        kernel<<<1, SORT_ONE_THREADS, 0, stream>>>(ids, wide, (int)n, n_rows, p.passes, p.digit, p.keys[0], p.places[0], seen, p.seen_bytes, flags);
         TRY(launched("sort_tokens_one"));
     } else
         for (int k = 0; k < p.passes; ++k) {
@@ -657,7 +710,7 @@ int chicle_layer_norm(const void *x, int64_t ldx, const void *gamma, const void 
     const int s = size_of(type);
     if (!placed(x, s) || !placed(y, s) || !placed(gamma, s) || !placed(beta, s) || !placed(mean, 4) || !placed(rstd, 4))
         return fail(CHICLE_EINVAL, "a null or misplaced pointer");
-    const RowShape r = row_shape(d, 16 / s, LN_FORWARD_VALUES);
+    const RowShape r = row_shape(d, 16 / s, LN_FORWARD_VALUES / 2, LN_FORWARD_VALUES);
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
         return with_vectors(r.vectors, [&](auto v) {
@@ -695,7 +748,7 @@ int chicle_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t 
     TRY(check_workspace(workspace, workspace_bytes, chicle_layer_norm_grad_bytes(n, d, type)));
     Carver c(workspace);
     float *part = c.take<float>(parts * 2 * d);
-    const RowShape r = row_shape(d, 16 / s, LN_GRAD_VALUES);
+    const RowShape r = row_shape(d, 16 / s, LN_GRAD_VALUES / 2, LN_GRAD_VALUES);
     hipStream_t stream = (hipStream_t)hip_stream;
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;

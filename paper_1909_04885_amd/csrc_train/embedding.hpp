@@ -58,41 +58,98 @@ __device__ __forceinline__ void mark_seen(uint8_t *seen, unsigned key, int64_t n
     if (seen && (int64_t)key < n_rows) seen[key] = 1;
 }
 
-constexpr int SORT_ONE = 4096;               // tokens that one workgroup sorts by itself
+constexpr int SORT_BITS = 10, SORT_BINS = 1 << SORT_BITS;      // of a digit
 
-// One workgroup: a bitonic network over (key, place) in LDS.
-__global__ __launch_bounds__(1024) void sort_tokens_one(const void *__restrict__ ids, int wide, int n, int64_t n_rows, unsigned *__restrict__ keys_out,
-                                                        unsigned *__restrict__ places_out, uint8_t *seen, int64_t seen_bytes, int *flags)
+// Every lane's number of lower lanes with the same digit, and the number of all lanes with it; lanes without a token count nowhere.
+__device__ __forceinline__ void match_digit(unsigned digit, bool live, int bits, int &lower, int &all)
 {
-    __shared__ unsigned long long s[SORT_ONE];
-    int size = 1;
-    while (size < n) size <<= 1;
-    for (int i = threadIdx.x; i < size; i += 1024)
-        s[i] = i < n ? ((unsigned long long)token_key(ids, wide, i, n_rows, flags) << 32) | (unsigned)i : ~0ull;
-    clear_seen(seen, seen_bytes, threadIdx.x, 1024);
-    __syncthreads();                                     // (cleared before anything is marked)
-    for (int i = threadIdx.x; i < n; i += 1024) mark_seen(seen, (unsigned)(s[i] >> 32), n_rows);
-    __syncthreads();
-    for (int k = 2; k <= size; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int i = threadIdx.x; i < size / 2; i += 1024) {
-                const int a = 2 * i - (i & (j - 1)), b = a + j;
-                const unsigned long long x = s[a], y = s[b];
-                if ((x > y) == ((a & k) == 0)) { s[a] = y; s[b] = x; }
-            }
-            __syncthreads();
-        }
-    for (int i = threadIdx.x; i < n; i += 1024) {
-        keys_out[i] = (unsigned)(s[i] >> 32);
-        places_out[i] = (unsigned)s[i];
+    unsigned long long same = __ballot(live);
+    for (int b = 0; b < bits; ++b) {
+        const unsigned long long ones = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? ones : ~ones;
     }
+    const int lane = threadIdx.x & 63;
+    lower = __popcll(same & ((1ull << lane) - 1));
+    all = __popcll(same);
+}
+
+// As many tokens as one workgroup sorts by itself, in one launch: passes over digits of the key, the lowest first, each of which keeps the order
+// of equal digits.  A wavefront holds STEPS times 64 tokens in their order; where its tokens of a digit go follows from what the
+// wavefronts hold of every digit.
+constexpr int SORT_ONE_THREADS = 1024, SORT_ONE_WAVES = SORT_ONE_THREADS / 64, SORT_ONE = 4 * SORT_ONE_THREADS;
+
+template <int STEPS>
+__global__ __launch_bounds__(SORT_ONE_THREADS) void sort_tokens_one(const void *__restrict__ ids, int wide, int n, int64_t n_rows, int passes, int bits,
+                                                                    unsigned *__restrict__ keys_out, unsigned *__restrict__ places_out, uint8_t *seen,
+                                                                    int64_t seen_bytes, int *flags)
+{
+    constexpr int ALL = STEPS * SORT_ONE_THREADS;
+    __shared__ unsigned keys[ALL];
+    __shared__ uint16_t places[ALL];
+    __shared__ uint16_t count[SORT_ONE_WAVES][SORT_BINS];
+    __shared__ unsigned totals[SORT_ONE_WAVES];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = wave * 64 * STEPS + lane, bin = threadIdx.x, mask = (1 << bits) - 1;
+    unsigned key[STEPS];
+    int place[STEPS], rank[STEPS];
+    clear_seen(seen, seen_bytes, threadIdx.x, SORT_ONE_THREADS);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        place[s] = first + s * 64;
+        key[s] = place[s] < n ? token_key(ids, wide, place[s], n_rows, flags) : 0u;
+    }
+    __syncthreads();                                     // (cleared before anything is marked)
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+        if (place[s] < n) mark_seen(seen, key[s], n_rows);
+    for (int pass = 0; pass < passes; ++pass) {
+        for (int i = threadIdx.x; i < SORT_ONE_WAVES * SORT_BINS / 2; i += SORT_ONE_THREADS) ((unsigned *)&count[0][0])[i] = 0u;
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const int digit = key[s] >> (pass * bits) & mask;
+            int lower, all;
+            match_digit(digit, first + s * 64 < n, bits, lower, all);
+            rank[s] = count[wave][digit] + lower;
+            __builtin_amdgcn_wave_barrier();
+            if (first + s * 64 < n && lower == 0) count[wave][digit] = (uint16_t)(rank[s] + all);
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+        unsigned sum = 0;
+        for (int w = 0; w < SORT_ONE_WAVES; ++w) sum += count[w][bin];
+        unsigned up = sum;
+        for (int o = 1; o < 64; o <<= 1) {
+            const unsigned t = __shfl_up(up, o);
+            if (lane >= o) up += t;
+        }
+        if (lane == 63) totals[wave] = up;
+        __syncthreads();
+        unsigned at = up - sum;
+        for (int w = 0; w < wave; ++w) at += totals[w];
+        for (int w = 0; w < SORT_ONE_WAVES; ++w) { const unsigned c = count[w][bin]; count[w][bin] = (uint16_t)at; at += c; }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            if (first + s * 64 < n) {
+                const int to = count[wave][key[s] >> (pass * bits) & mask] + rank[s];
+                keys[to] = key[s];
+                places[to] = (uint16_t)place[s];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            if (first + s * 64 < n) { key[s] = keys[first + s * 64]; place[s] = places[first + s * 64]; }
+    }
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+        if (first + s * 64 < n) { keys_out[first + s * 64] = key[s]; places_out[first + s * 64] = place[s]; }
 }
 
 // More tokens: passes over digits of the key, the lowest first, each of which keeps the order of equal digits.  A workgroup
 // takes a tile of tokens, wavefront w of it the w-th part, 64 tokens at a time in their order.  There are at most
 // SORT_MOST_TILES tiles: every workgroup adds up by itself what the tiles before it hold of each digit, which saves a launch
 // between the counts and the scatter.
-constexpr int SORT_WAVES = 8, SORT_THREADS = 64 * SORT_WAVES, SORT_BITS = 10, SORT_BINS = 1 << SORT_BITS;
+constexpr int SORT_WAVES = 8, SORT_THREADS = 64 * SORT_WAVES;
 constexpr int SORT_LEAST_TILE = 2048, SORT_MOST_TILES = 128;
 
 struct SortPass {
@@ -110,19 +167,6 @@ struct SortPass {
 __device__ __forceinline__ unsigned sort_key(const SortPass &p, int64_t i, bool flag)
 {
     return p.first ? token_key(p.ids, p.wide, i, p.n_rows, flag ? p.flags : nullptr) : p.keys_in[i];
-}
-
-// Every lane's number of lower lanes with the same digit, and the number of all lanes with it; lanes without a token count nowhere.
-__device__ __forceinline__ void match_digit(unsigned digit, bool live, int bits, int &lower, int &all)
-{
-    unsigned long long same = __ballot(live);
-    for (int b = 0; b < bits; ++b) {
-        const unsigned long long ones = __ballot((digit >> b) & 1);
-        same &= (digit >> b) & 1 ? ones : ~ones;
-    }
-    const int lane = threadIdx.x & 63;
-    lower = __popcll(same & ((1ull << lane) - 1));
-    all = __popcll(same);
 }
 
 __global__ __launch_bounds__(SORT_THREADS) void sort_count(SortPass p)

@@ -109,22 +109,25 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
     const int lane = threadIdx.x % lanes, group = threadIdx.x / lanes, groups = blockDim.x / lanes;
     const int64_t first = (int64_t)lane * V, step = (int64_t)lanes * V;
     float *mine = part + (int64_t)blockIdx.x * 2 * d;
-    float sg[N][V] = {}, sb[N][V] = {}, ga[N][V];
+    constexpr bool HELD = NV == 1 || (NV > 1 && THREADS <= 256);           // gamma in registers, where there are enough
+    float sg[N][V] = {}, sb[N][V] = {}, ga[HELD ? N : 1][V];
     if constexpr (NV > 0) {
+        if constexpr (HELD)
 #pragma unroll
-        for (int k = 0; k < NV; ++k) load_vec(gamma, first + k * step, d, ga[k]);
+            for (int k = 0; k < NV; ++k) load_vec(gamma, first + k * step, d, ga[k]);
     } else {
         for (int64_t c = first; c < d; c += step)
             for (int i = 0; i < V && c + i < d; ++i) mine[c + i] = mine[d + c + i] = 0.f;
     }
-    // The next row is on its way while this one is added up.
-    u32x4 next_x[N], next_dy[N];
+    // The next row is on its way while this one is added up, where there are registers for it.
+    constexpr bool AHEAD = HELD;
+    u32x4 next_x[AHEAD ? N : 1], next_dy[AHEAD ? N : 1];
     float next_mean, next_rstd;
     auto ask = [&](int64_t row) {
         row = min(row, n - 1);
         next_mean = mean_in[row];
         next_rstd = rstd_in[row];
-        if constexpr (NV > 0)
+        if constexpr (AHEAD)
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 next_x[k] = load_raw<T, true>(x + row * ldx, first + k * step, d);
@@ -140,14 +143,14 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
         const float mean = next_mean, rstd = next_rstd;
         float h[N][V], g[N][V];                          // xhat and dy
         float2 s = {0.f, 0.f};
-        if constexpr (NV > 0) {
+        if constexpr (AHEAD) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) { unpack<T>(next_x[k], h[k]); unpack<T>(next_dy[k], g[k]); }
         }
         ask(row + (int64_t)gridDim.x * groups);
         // Past the end of the row dy is zero, so what xhat has there counts nowhere.
         auto take = [&](int64_t c, float *hk, float *gk, const float *gak) {
-            if constexpr (NV == 0) {
+            if constexpr (!AHEAD) {
                 load_vec(xr, c, d, hk);
                 load_vec(dyr, c, d, gk);
             }
@@ -160,7 +163,10 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
         };
         if constexpr (NV > 0) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) take(first + k * step, h[k], g[k], ga[k]);
+            for (int k = 0; k < NV; ++k) {
+                if constexpr (!HELD) load_vec(gamma, first + k * step, d, ga[0]);
+                take(first + k * step, h[k], g[k], ga[HELD ? k : 0]);
+            }
         } else {
             for (int64_t c = first; c < d; c += step) { load_vec(gamma, c, d, ga[0]); take(c, h[0], g[0], ga[0]); }
         }
@@ -177,7 +183,8 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
             for (int k = 0; k < NV; ++k) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) { sg[k][i] += g[k][i] * h[k][i]; sb[k][i] += g[k][i]; }
-                give(first + k * step, h[k], g[k], ga[k]);
+                if constexpr (!HELD) load_vec(gamma, first + k * step, d, ga[0]);
+                give(first + k * step, h[k], g[k], ga[HELD ? k : 0]);
             }
         } else {
             for (int64_t c = first; c < d; c += step) {
@@ -189,7 +196,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
         }
     }
     if constexpr (NV > 0) {
-        // the groups of a workgroup one after the other
+        // the groups of a workgroup by halves
         for (int k = 0; k < NV; ++k)
             for (int which = 0; which < 2; ++which) {
                 float *u = which ? sb[k] : sg[k];
@@ -197,13 +204,17 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
 #pragma unroll
                 for (int i = 0; i < V; ++i) group_sums[threadIdx.x * V + i] = u[i];
                 __syncthreads();
+                for (int half = groups / 2; half > 0; half /= 2) {
+                    if (group < half)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) group_sums[threadIdx.x * V + i] += group_sums[(threadIdx.x + half * lanes) * V + i];
+                    __syncthreads();
+                }
                 if (group == 0)
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        float t = 0.f;
-                        for (int q = 0; q < groups; ++q) t += group_sums[(q * lanes + lane) * V + i];
                         const int64_t c = first + k * step + i;
-                        if (c < d) mine[which * d + c] = t;
+                        if (c < d) mine[which * d + c] = group_sums[threadIdx.x * V + i];
                     }
             }
     }

@@ -147,6 +147,40 @@ __global__ __launch_bounds__(256) void loss_rows(LossRows l, int tiles, float *_
     loss[j] = label >= 0 && label < l.classes ? lse - l.picked[j] : 0.f;
 }
 
+// The same of logits that come in several parts, where there are few tiles and each is a long sum: a workgroup to a row.  The first part is
+// left as their sum.
+__global__ __launch_bounds__(256) void loss_join(LossRows l, float *parts, int64_t ldz, int64_t copy, int copies, float *__restrict__ loss,
+                                                 float *__restrict__ lse_out, int *flags)
+{
+    __shared__ float s[8], picked;
+    const int j = blockIdx.x, label = label_at(l, j), wave = threadIdx.x >> 6;
+    float *z = parts + j * ldz;
+    float m = MINUS_INF;
+    for (int c = threadIdx.x; c < l.classes; c += 256) {
+        float t = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < copies; ++k) t += z[k * copy + c];
+        z[c] = t;
+        if (c == label) picked = t;
+        m = fmaxf(m, t);
+    }
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if ((threadIdx.x & 63) == 0) s[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    const float shift = m == MINUS_INF ? 0.f : m;
+    float e = 0.f;
+    for (int c = threadIdx.x; c < l.classes; c += 256) e += exp_of<true>(z[c], shift);
+    e = lanes_sum(e, 64);
+    if ((threadIdx.x & 63) == 0) s[4 + wave] = e;
+    __syncthreads();
+    if (threadIdx.x) return;
+    const float lse = m + logf((s[4] + s[5]) + (s[6] + s[7]));
+    if (index_at(l.labels, l.wide, j) >= l.classes && flags) atomicOr(flags, FLAG_LABEL_RANGE);
+    lse_out[j] = lse;
+    loss[j] = label >= 0 ? lse - picked : 0.f;
+}
+
 // power[0]: what takes the largest weight to `top`, power[1] its inverse.  One workgroup.
 __global__ __launch_bounds__(1024) void loss_power(const float *__restrict__ weight, int n, float top, float *power)
 {
@@ -222,12 +256,12 @@ __global__ __launch_bounds__(256) void loss_grad_kept(const float *logits, int64
     }
 }
 
-// G w, of w as it lies, by k: out[j][i] in 32 bits, split `split` of the sum in its own copy of `out`.
-template <typename T, typename C>
+// A product as it is: out[j][i] in 32 bits, split `split` of the sum in its own copy of `out`.
+template <typename T, typename C, bool A_BY_K, bool B_BY_K>
 __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_parts(MmShape s, float *__restrict__ out, int64_t ld, int64_t copy)
 {
-    mm_tiles<T, C, true, false>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
-        const MmPlace<C, true> at(t);
+    mm_tiles<T, C, A_BY_K, B_BY_K>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
+        const MmPlace<C, A_BY_K> at(t);
         float *mine = out + t.split * copy;
 #pragma unroll
         for (int nj = 0; nj < C::NJ; ++nj)
@@ -312,7 +346,7 @@ __global__ __launch_bounds__(256) void sum_parts(const float *__restrict__ part,
 // the logits.  `loss_grad_few`, for the fewest rows, reads w once more: a thread owns a vector of columns and forms dw's rows and its
 // part of dx in 32 bits.
 
-constexpr int FEW_ROWS = 64, FEW_GRAD_ROWS = 8, FEW_AHEAD = 8, FEW_THREADS = 512;
+constexpr int FEW_ROWS = 96, FEW_GRAD_ROWS = 8, FEW_AHEAD = 8, FEW_THREADS = 512;
 template <typename T> constexpr int FEW_BATCH = MM_K<T> / 2 * FEW_AHEAD;   // k of a batch of accesses
 
 // Rows 16 q + l % 16 of x in LDS, `chunk` columns at a time where not all of them fit: x[row][chunk + one chunk], zeros past d; then (largest,
@@ -349,13 +383,15 @@ __global__ __launch_bounds__(FEW_THREADS) void loss_few(const T *__restrict__ x,
         };
         auto use = [&](const u32x4 (&raw)[U], int k0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u) {
+                frag b[NR];
 #pragma unroll
-                for (int q = 0; q < NR; ++q) {
-                    const frag b = *(const frag *)(xs + at[q] + k0 + u * K);
+                for (int q = 0; q < NR; ++q) b[q] = *(const frag *)(xs + at[q] + k0 + u * K);
 #pragma unroll
-                    for (int e = 0; e < Mfma<T>::STEPS; ++e) acc[q] = Mfma<T>::step(__builtin_bit_cast(frag, raw[u]), b, e, acc[q]);
-                }
+                for (int e = 0; e < Mfma<T>::STEPS; ++e)
+#pragma unroll
+                    for (int q = 0; q < NR; ++q) acc[q] = Mfma<T>::step(__builtin_bit_cast(frag, raw[u]), b[q], e, acc[q]);
+            }
         };
         for (int kc = 0; kc < k_end; kc += chunk) {
             const int end = min(chunk, k_end - kc);

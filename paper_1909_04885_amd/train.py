@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from typing import Optional, Sequence
 
 from .binding import EDEVICE, EINVAL, OK, ChicleError
@@ -60,6 +61,11 @@ def load_train_library():
         fn.argtypes = args
     _lib = L
     return L
+
+
+def _at(a: array) -> int:
+    """The address of a host array, which stays where it is while it is not changed."""
+    return a.buffer_info()[0] if len(a) else 0
 
 
 class TrainOps:
@@ -231,33 +237,26 @@ class TrainOps:
 
     # -- clipping
     def _pointers(self, tensors, name: str):
-        """Addresses, numbers of values and types of contiguous tensors on this GPU."""
-        index, kinds, where, sizes, types = self._index, self._types, [], [], []
-        for g in tensors:
-            kind = kinds.get(g.dtype)
-            if kind is None or not g.is_cuda or g.get_device() != index or not g.is_contiguous():
-                raise ChicleError(EINVAL, "%s must be contiguous float32, bfloat16 or float16 tensors on %s" % (name, self.device))
-            where.append(g.data_ptr())
-            sizes.append(g.numel())
-            types.append(kind)
-        return where, sizes, types
+        """Addresses, numbers of values and types of contiguous tensors on this GPU (a list at a time: there are many)."""
+        k = len(tensors)
+        kinds = [self._types.get(g.dtype) for g in tensors]
+        if None in kinds or [g.get_device() for g in tensors] != [self._index] * k or False in [g.is_contiguous() for g in tensors]:
+            raise ChicleError(EINVAL, "%s must be contiguous float32, bfloat16 or float16 tensors on %s" % (name, self.device))
+        return array("Q", [g.data_ptr() for g in tensors]), array("q", [g.numel() for g in tensors]), array("i", kinds)
 
     def _clip(self, grads: Sequence, out: Optional[Sequence], max_norm: float):
         k = len(grads)
         where, sizes, types = self._pointers(grads, "gradients")
-        outs = None
-        if out is grads:
-            outs = (ctypes.c_void_p * k)(*where)
-        elif out is not None:
+        to = where if out is grads else None
+        if out is not None and to is None:
             to, out_sizes, out_types = self._pointers(out, "outputs")
             if out_sizes != sizes or out_types != types:
                 raise ChicleError(EINVAL, "an output per gradient, of its type and number of values")
-            outs = (ctypes.c_void_p * k)(*to)
         norm = self._empty((), self._torch.float32)
         nbytes = self._L.chicle_clip_grads_bytes(k)
         ws = self._workspace(nbytes)
-        self._call(self._L.chicle_clip_grads, (ctypes.c_void_p * k)(*where), outs, (ctypes.c_int64 * k)(*sizes), (ctypes.c_int32 * k)(*types), k,
-                   max_norm, norm.data_ptr(), ws.data_ptr(), nbytes)
+        self._call(self._L.chicle_clip_grads, _at(where), None if to is None else _at(to), _at(sizes), _at(types), k, max_norm,
+                   norm.data_ptr(), ws.data_ptr(), nbytes)
         return norm
 
     def grad_norm(self, grads: Sequence):

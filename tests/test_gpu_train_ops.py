@@ -52,7 +52,8 @@ def check_loss(ops, x, w, labels, weight):
 @pytest.mark.parametrize("n, d, classes, extra, shift", [
     (1, 64, 1, 0, 0), (1, 1, 2, 0, 0), (1, 200, 1000, 0, 0), (2, 64, 255, 0, 0), (3, 65, 257, 1, 0), (7, 63, 300, 0, 1), (16, 128, 513, 0, 0),
     (17, 100, 700, 3, 5), (64, 64, 640, 0, 0), (65, 192, 1000, 8, 0), (100, 250, 2000, 6, 0), (128, 512, 1024, 0, 0), (129, 320, 777, 0, 3), (257, 96, 4111, 0, 0),
-    (600, 130, 3001, 0, 0), (2500, 64, 500, 0, 0)])
+    (600, 130, 3001, 0, 0), (2500, 64, 500, 0, 0),
+    (24, 1030, 900, 2, 0), (70, 1100, 300, 0, 0), (96, 600, 500, 0, 0), (97, 700, 515, 0, 1), (130, 1024, 900, 0, 0), (300, 2050, 700, 0, 0), (64, 2048, 40, 0, 0)])
 @pytest.mark.parametrize("dtype", TYPES, ids=NAME.get)
 def test_softmax_loss(ops, dtype, n, d, classes, extra, shift):
     print("\ncase softmax_loss", NAME[dtype], n, d, classes, extra, shift, flush=True)
@@ -74,6 +75,27 @@ def test_softmax_loss_over_several_pieces_of_the_classes(ops, dtype):
     x, w = rows(g, n, d, dtype), rows(g, classes, d, dtype, 0, 0, 0.5)
     labels = torch.randint(-1, classes, (n,), generator=g, device="cuda", dtype=torch.int32)
     check_loss(ops, x, w, labels, torch.full((n,), 1.0 / n, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=NAME.get)
+def test_softmax_loss_whose_last_classes_are_less_than_a_round_of_tiles(ops, dtype):
+    n, d, classes = 1100, 70, 70001
+    print("\ncase softmax_loss last tiles", NAME[dtype], n, d, classes, flush=True)
+    g = gen(7)
+    x, w = rows(g, n, d, dtype), rows(g, classes, d, dtype, 0, 0, 0.3)
+    labels = torch.randint(-1, classes, (n,), generator=g, device="cuda")
+    labels[:50] = torch.arange(classes - 50, classes, device="cuda")
+    check_loss(ops, x, w, labels, torch.rand(n, generator=g, device="cuda"))
+
+
+def test_softmax_loss_over_several_pieces_of_the_rows(ops):
+    """In 32 bits: more classes than the kept logits have room for beside all rows."""
+    n, d, classes = 700, 16, 500001
+    print("\ncase softmax_loss row pieces", n, d, classes, flush=True)
+    g = gen(6)
+    x, w = rows(g, n, d, F32), rows(g, classes, d, F32, 0, 0, 0.5)
+    labels = torch.randint(-1, classes, (n,), generator=g, device="cuda")
+    check_loss(ops, x, w, labels, torch.rand(n, generator=g, device="cuda"))
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=NAME.get)
@@ -125,6 +147,23 @@ def test_classes_masked_by_the_lowest_value(ops, dtype):
     ref.within(dx, r["dx"], r["off_dx"])
     ref.within(dw[keep], r["dw"], r["off_dw"])
     assert not dw[masked].any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=NAME.get)
+@pytest.mark.parametrize("n", [30, 500])
+def test_a_weight_that_all_rows_share_is_not_rounded(ops, dtype, n):
+    """One weight that is no power of two: what is left is the rounding of the gradients, and that of probabilities, to no side.  A weight
+    rounded with its row's gradient would take all of dw off by the same part, up to the type's unit round-off."""
+    g = gen(n)
+    x, w = rows(g, n, 64, dtype), rows(g, 4000, 64, dtype, 0, 0, 0.2)
+    labels = torch.randint(0, 4000, (n,), generator=g, device="cuda", dtype=torch.int32)
+    u = ref.U[dtype]
+    weight = torch.full((n,), (1 + 0.45 * u) * 2.0 ** -4, device="cuda")   # (rounds down to 2^-4)
+    r = ref.softmax_loss(x, w, labels, weight)
+    _, dx, dw = ops.softmax_loss_grad(x, w, labels, weight)
+    for got, want in ((dx, r["dx"]), (dw, r["dw"])):
+        along = float((got.double() * want).sum() / (want * want).sum())   # thousands of roundings to either side, each below u / 2
+        assert abs(along - 1) < 0.15 * u, along
 
 
 def test_large_logits_neither_overflow_nor_vanish(ops):
