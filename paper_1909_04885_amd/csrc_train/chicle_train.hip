@@ -3,6 +3,7 @@
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
+#include <algorithm>
 #include "../../include/chicle_train.h"
 #include "clip.hpp"
 #include "elements.hpp"
@@ -104,12 +105,16 @@ RowShape row_shape(int64_t d, int vec, int first_values, int most_values)
     return s;
 }
 
+constexpr int CUS = 256;                                 // compute units
 constexpr int LN_FORWARD_VALUES = 32, LN_GRAD_VALUES = 16;
+// Workgroups of the gradient: whole rounds of what the compute units hold at once, up to this many.  At 65,536 x 4096 in 16 bits,
+// where 768 are held, 768 take 306 us and 1024 (a round and a third) 390 us; at 30,000 x 4096 in 32 bits, where 512 are, 768 take
+// 300 us and 1024 267 us.
 constexpr int LN_GRAD_GRID = 1024;
 
 int64_t layer_norm_parts(int64_t n, int64_t d, int32_t type)
 {
-    const RowShape s = row_shape(d, 16 / size_of(type), LN_GRAD_VALUES / 2, LN_GRAD_VALUES);
+    const RowShape s = row_shape(d, 16 / size_of(type), LN_GRAD_VALUES, LN_GRAD_VALUES);
     const int64_t g = ceil_div(n, s.threads / s.lanes);
     return g < LN_GRAD_GRID ? g : LN_GRAD_GRID;
 }
@@ -137,7 +142,6 @@ typedef MmConfig<128, 64, 2, 2, 3> MmThin;
 constexpr int MM_PARTS_I = 2;                            // wavefronts along i of the loss's tiles
 
 enum { WIDE, MIDDLE, THIN };
-constexpr int CUS = 256;                                 // compute units
 
 int mm_tile_i(int c) { return c == WIDE ? 256 : 128; }
 int mm_tile_j(int c) { return c == WIDE ? 256 : c == MIDDLE ? 128 : 64; }
@@ -744,11 +748,11 @@ int chicle_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t 
     if (!placed(gamma, s) || !placed(dgamma, s) || !placed(dbeta, s) ||
         (n > 0 && (!placed(dy, s) || !placed(x, s) || !placed(dx, s) || !placed(mean, 4) || !placed(rstd, 4))))
         return fail(CHICLE_EINVAL, "a null or misplaced pointer");
-    const int64_t parts = layer_norm_parts(n, d, type);
+    int64_t parts = layer_norm_parts(n, d, type);
     TRY(check_workspace(workspace, workspace_bytes, chicle_layer_norm_grad_bytes(n, d, type)));
     Carver c(workspace);
     float *part = c.take<float>(parts * 2 * d);
-    const RowShape r = row_shape(d, 16 / s, LN_GRAD_VALUES / 2, LN_GRAD_VALUES);
+    const RowShape r = row_shape(d, 16 / s, LN_GRAD_VALUES, LN_GRAD_VALUES);
     hipStream_t stream = (hipStream_t)hip_stream;
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
@@ -757,7 +761,12 @@ int chicle_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t 
                 constexpr int NV = decltype(v)::value;
                 if constexpr (NV * Elem<T>::VEC <= LN_GRAD_VALUES) {
                     auto kernel = r.threads > 256 ? layer_norm_grad_rows<T, NV, LN_MOST_THREADS> : layer_norm_grad_rows<T, NV, 256>;
-                    kernel<<<(unsigned)parts, r.threads, (size_t)r.threads * Elem<T>::VEC * sizeof(float), stream>>>(
+                    const size_t lds = (size_t)r.threads * Elem<T>::VEC * sizeof(float);
+                    int resident = 0;
+                    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, r.threads, lds) != hipSuccess || resident < 1) resident = 1;
+                    const int64_t round = std::min<int64_t>((int64_t)resident * CUS, LN_GRAD_GRID);
+                    parts = std::min(parts, LN_GRAD_GRID / round * round);
+                    kernel<<<(unsigned)parts, r.threads, lds, stream>>>(
                         (const T *)dy, lddy, (const T *)x, ldx, (const T *)gamma, mean, rstd, (T *)dx, lddx, part, n, d, r.lanes);
                 }
                 return launched("layer_norm_grad_rows");

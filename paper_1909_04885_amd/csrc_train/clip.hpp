@@ -50,19 +50,15 @@ __device__ __forceinline__ void clip_pieces(const ClipTable &t, int64_t piece, F
     }
 }
 
-// CLIP_AHEAD vectors of a thread are on their way together.  A whole piece, which is nearly every one, is read without looking for the
-// tensor's end.
+// CLIP_AHEAD vectors of a thread are on their way together.
 constexpr int CLIP_AHEAD = 4;
 
-template <typename T, bool WHOLE>
+template <typename T>
 __device__ __forceinline__ void clip_ask(const T *p, int64_t c, int64_t end, u32x4 (&u)[CLIP_AHEAD])
 {
     constexpr int STEP = CLIP_THREADS * Elem<T>::VEC;
 #pragma unroll
-    for (int q = 0; q < CLIP_AHEAD; ++q) {
-        if constexpr (WHOLE) u[q] = __builtin_nontemporal_load((const u32x4_at_2 *)(p + c + q * STEP));
-        else u[q] = load_raw<T, true>(p, c + q * STEP, end);
-    }
+    for (int q = 0; q < CLIP_AHEAD; ++q) u[q] = ask_raw<T, true>(p, c + q * STEP, end);
 }
 
 template <typename T>
@@ -70,11 +66,11 @@ __global__ __launch_bounds__(CLIP_THREADS) void squares(ClipTable t, int64_t pie
 {
     constexpr int V = Elem<T>::VEC, ALL = CLIP_THREADS * V * CLIP_AHEAD;
     double sums[CLIP_AHEAD] = {};                        // (sums of their own do not wait for each other)
-    auto add = [&](const u32x4 (&u)[CLIP_AHEAD]) {
+    auto add = [&](int64_t c, int64_t end, const u32x4 (&u)[CLIP_AHEAD]) {
 #pragma unroll
         for (int q = 0; q < CLIP_AHEAD; ++q) {
             float w[V];
-            unpack<T>(u[q], w);
+            unpack<T>(settle<T>(u[q], c + q * CLIP_THREADS * V, end), w);
 #pragma unroll
             for (int i = 0; i < V; ++i) sums[q] += (double)w[i] * (double)w[i];
         }
@@ -82,11 +78,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void squares(ClipTable t, int64_t pie
     clip_pieces(t, piece, [&](int k, int64_t a, int64_t end) {
         const T *p = (const T *)t.in[k];
         u32x4 u[CLIP_AHEAD];
-        int64_t c = a + (int64_t)threadIdx.x * V;
-        if (end - a == piece)
-            for (; c < end; c += ALL) { clip_ask<T, true>(p, c, end, u); add(u); }
-        else
-            for (; c < end; c += ALL) { clip_ask<T, false>(p, c, end, u); add(u); }
+        for (int64_t c = a + (int64_t)threadIdx.x * V; c < end; c += ALL) { clip_ask(p, c, end, u); add(c, end, u); }
     });
     double sum = 0.0;
 #pragma unroll
@@ -129,18 +121,14 @@ __global__ __launch_bounds__(CLIP_THREADS) void clip_scale(ClipTable t, int64_t 
 #pragma unroll
             for (int h = 0; h < CLIP_AHEAD; ++h) {
                 float w[V];
-                unpack<T>(u[h], w);
+                unpack<T>(settle<T>(u[h], c + h * CLIP_THREADS * V, end), w);
 #pragma unroll
                 for (int i = 0; i < V; ++i) w[i] *= factor;
                 store_vec<T, true>(q, c + h * CLIP_THREADS * V, end, w);
             }
         };
         u32x4 u[CLIP_AHEAD];
-        int64_t c = a + (int64_t)threadIdx.x * V;
-        if (end - a == piece)
-            for (; c < end; c += ALL) { clip_ask<T, true>(p, c, end, u); scale(c, u); }
-        else
-            for (; c < end; c += ALL) { clip_ask<T, false>(p, c, end, u); scale(c, u); }
+        for (int64_t c = a + (int64_t)threadIdx.x * V; c < end; c += ALL) { clip_ask(p, c, end, u); scale(c, u); }
     });
 }
 

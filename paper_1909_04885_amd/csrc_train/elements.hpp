@@ -46,15 +46,18 @@ __device__ __forceinline__ u32x4 pack(const float *in)
     return x;
 }
 
-// A vector of a row of d values, zeros past its end.  ONCE: data that is read once, or written and not read soon, is not kept in the
-// caches, which is faster for what does not fit there (reads of 2 GiB: 7.1 instead of 6.4 TB/s).
+// A vector of a row of d values, zeros past its end, in two steps.  `ask_raw` asks for sixteen bytes that lie in the row, the last of the row
+// where the vector ends behind it; `settle` moves those to their place, when they are used.  So a load never waits for
+// itself, whatever d is.  (Rows shorter than a vector are put together value by value.)  ONCE: data that is read once, or written and not
+// read soon, is not kept in the caches, which is faster for what does not fit there (reads of 2 GiB: 7.1 instead of 6.4 TB/s).
 template <typename T, bool ONCE = false>
-__device__ __forceinline__ u32x4 load_raw(const T *row, int64_t c, int64_t d)
+__device__ __forceinline__ u32x4 ask_raw(const T *row, int64_t c, int64_t d)
 {
     constexpr int V = Elem<T>::VEC;
-    if (__builtin_expect(c + V <= d, 1)) {
-        if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4_at_2 *)(row + c));
-        else return *(const u32x4_at_2 *)(row + c);
+    if (d >= V) {
+        const T *p = row + (c < d - V ? c : d - V);
+        if constexpr (ONCE) return __builtin_nontemporal_load((const u32x4_at_2 *)p);
+        else return *(const u32x4_at_2 *)p;
     }
     u32x4 x = {0u, 0u, 0u, 0u};
     if constexpr (sizeof(T) == 4) {
@@ -67,6 +70,26 @@ __device__ __forceinline__ u32x4 load_raw(const T *row, int64_t c, int64_t d)
             if (c + i < d) x[i / 2] |= (unsigned)((const uint16_t *)row)[c + i] << (i % 2 * 16);
     }
     return x;
+}
+
+template <typename T>
+__device__ __forceinline__ u32x4 settle(u32x4 x, int64_t c, int64_t d)
+{
+    constexpr int V = Elem<T>::VEC;
+    if (__builtin_expect(c + V > d && d >= V, 0)) {
+        const int64_t past = c + V - d;                  // values that are not the vector's, at the front
+        const int bits = past < V ? (int)past * 8 * (int)sizeof(T) : 128;
+        const unsigned long long lo = (unsigned long long)x[1] << 32 | x[0], hi = (unsigned long long)x[3] << 32 | x[2];
+        const unsigned long long a = bits >= 128 ? 0ull : bits >= 64 ? hi >> (bits - 64) : lo >> bits | hi << (64 - bits), b = bits >= 64 ? 0ull : hi >> bits;
+        x = u32x4{(unsigned)a, (unsigned)(a >> 32), (unsigned)b, (unsigned)(b >> 32)};
+    }
+    return x;
+}
+
+template <typename T, bool ONCE = false>
+__device__ __forceinline__ u32x4 load_raw(const T *row, int64_t c, int64_t d)
+{
+    return settle<T>(ask_raw<T, ONCE>(row, c, d), c, d);
 }
 
 template <typename T, bool ONCE = false>

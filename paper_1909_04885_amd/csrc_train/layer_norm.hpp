@@ -48,9 +48,14 @@ __global__ __launch_bounds__(THREADS) void layer_norm_rows(const T *__restrict__
     float v[NV ? NV : 1][V];
     float2 s = {0.f, 0.f};
     if constexpr (NV > 0) {
+        constexpr int RAW = NV * V <= 16 || THREADS <= 256 ? NV : 1;       // vectors that are asked for together, as registers allow
+        u32x4 raw[RAW];
+#pragma unroll
+        for (int k = 0; k < RAW; ++k) raw[k] = ask_raw<T, true>(xr, first + k * step, d);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            load_vec<T, true>(xr, first + k * step, d, v[k]);
+            if (RAW == 1 && k > 0) raw[0] = ask_raw<T, true>(xr, first + k * step, d);
+            unpack<T>(settle<T>(raw[RAW == 1 ? 0 : k], first + k * step, d), v[k]);
 #pragma unroll
             for (int i = 0; i < V; ++i) s.x += v[k][i];
         }
@@ -96,6 +101,14 @@ __global__ __launch_bounds__(THREADS) void layer_norm_rows(const T *__restrict__
     }
 }
 
+// The same pointer, of which the compiler does not know that it is: what is loaded from it is not kept from an earlier load.
+template <typename T>
+__device__ __forceinline__ const T *fresh(const T *p)
+{
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
 // Gradients.  Workgroup b takes rows b * groups + group, then gridDim.x * groups further on, and leaves its sums of dy xhat and
 // of dy by column in part[b][0 .. d) and part[b][d .. 2 d): the sums over rows have one order whatever the timing.
 template <typename T, int NV, int THREADS>
@@ -107,7 +120,8 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
     constexpr int V = Elem<T>::VEC, N = NV ? NV : 1;
     extern __shared__ __align__(16) float group_sums[];
     const int lane = threadIdx.x % lanes, group = threadIdx.x / lanes, groups = blockDim.x / lanes;
-    const int64_t first = (int64_t)lane * V, step = (int64_t)lanes * V;
+    int64_t first = (int64_t)lane * V;
+    const int64_t step = (int64_t)lanes * V;
     float *mine = part + (int64_t)blockIdx.x * 2 * d;
     constexpr bool HELD = NV == 1 || (NV > 1 && THREADS <= 256);           // gamma in registers, where there are enough
     float sg[N][V] = {}, sb[N][V] = {}, ga[HELD ? N : 1][V];
@@ -130,8 +144,8 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
         if constexpr (AHEAD)
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                next_x[k] = load_raw<T, true>(x + row * ldx, first + k * step, d);
-                next_dy[k] = load_raw<T, true>(dy + row * lddy, first + k * step, d);
+                next_x[k] = ask_raw<T, true>(x + row * ldx, first + k * step, d);
+                next_dy[k] = ask_raw<T, true>(dy + row * lddy, first + k * step, d);
             }
     };
     ask((int64_t)blockIdx.x * groups + group);
@@ -145,9 +159,13 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
         float2 s = {0.f, 0.f};
         if constexpr (AHEAD) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) { unpack<T>(next_x[k], h[k]); unpack<T>(next_dy[k], g[k]); }
+            for (int k = 0; k < NV; ++k) {
+                unpack<T>(settle<T>(next_x[k], first + k * step, d), h[k]);
+                unpack<T>(settle<T>(next_dy[k], first + k * step, d), g[k]);
+            }
         }
         ask(row + (int64_t)gridDim.x * groups);
+        if constexpr (NV > 1 && !HELD) asm volatile("" : "+v"(first));     // (nor addresses from the row before: the registers are full)
         // Past the end of the row dy is zero, so what xhat has there counts nowhere.
         auto take = [&](int64_t c, float *hk, float *gk, const float *gak) {
             if constexpr (!AHEAD) {
@@ -164,7 +182,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
         if constexpr (NV > 0) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                if constexpr (!HELD) load_vec(gamma, first + k * step, d, ga[0]);
+                if constexpr (!HELD) load_vec(fresh(gamma), first + k * step, d, ga[0]);
                 take(first + k * step, h[k], g[k], ga[HELD ? k : 0]);
             }
         } else {
@@ -183,7 +201,7 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
             for (int k = 0; k < NV; ++k) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) { sg[k][i] += g[k][i] * h[k][i]; sb[k][i] += g[k][i]; }
-                if constexpr (!HELD) load_vec(gamma, first + k * step, d, ga[0]);
+                if constexpr (!HELD) load_vec(fresh(gamma), first + k * step, d, ga[0]);
                 give(first + k * step, h[k], g[k], ga[HELD ? k : 0]);
             }
         } else {
