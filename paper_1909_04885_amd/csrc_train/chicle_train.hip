@@ -119,6 +119,18 @@ int64_t layer_norm_parts(int64_t n, int64_t d, int32_t type)
     return g < LN_GRAD_GRID ? g : LN_GRAD_GRID;
 }
 
+// f(first row, rows, workgroups) for all n rows, `per` to a workgroup: a launch has fewer than 2^32 threads, of which a workgroup here has up to 2^10.
+template <typename F>
+int with_rows(int64_t n, int per, F f)
+{
+    const int64_t most = ((int64_t)1 << 21) * per;
+    for (int64_t first = 0; first < n; first += most) {
+        const int64_t many = n - first < most ? n - first : most;
+        TRY(f(first, many, (unsigned)ceil_div(many, per)));
+    }
+    return CHICLE_OK;
+}
+
 template <typename F>
 int with_vectors(int vectors, F f)
 {
@@ -180,7 +192,7 @@ struct LossPlan {
     int config;
     bool few, few_grad, tiles, kept, lay_x, lay_w;   // few: of the loss, of the gradient; tiles: something goes by products; kept: the logits
     int loss_splits;                     // of the loss's sums, more than 1 where tiles are few
-    int few_blocks, few_passes, few_threads, few_chunk, few_lds, few_each, few_grad_blocks;
+    int few_blocks, few_passes, few_chunk, few_lds, few_each, few_grad_blocks;
     // gradient: pieces of the classes, or, with logits kept, of the rows
     int64_t piece, piece_rows, ldz, ldg, ldp;        // ldz, ldg: length of the rows of the logits and of G; ldp: of the rows of dx's parts
     int64_t rows_x, rows_g;                          // rows of the laid-out x and of G: whole slices
@@ -207,6 +219,17 @@ int64_t dw_rest(int config, int64_t d, int64_t classes, int64_t slices)
     return across * ceil_div(rest, 256) * 2 > CUS ? 0 : rest;
 }
 
+// Up to how many rows the loss reads w as it lies instead of by products; with the gradient too, so that both give the same loss.
+// In us, 50,000 classes, as it lies / by products.  16 bits, w aligned: 4 rows of 1024 33 / 25, 64 rows 48 / 26; w not aligned, so that products need
+// it laid out first: 1 row of 1001 46 / 60, 33 rows 55 / 62, but with the gradient, which needs that anyway, 16 rows 157 / 151, 48 rows 175 / 156.
+// 32 bits, aligned: 16 rows of 1024 60 / 86, 24 rows 86 / 84; not aligned: 32 rows of 1001 94 / 149, with the gradient 323 / 303, 48 rows
+// 134 / 150 and 392 / 329.
+int64_t few_rows(int size, bool aligned)
+{
+    if (size == 4) return aligned ? FEW_ROWS / 2 : FEW_ROWS;
+    return aligned ? 0 : FEW_ROWS / 2;
+}
+
 LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t n, int64_t d, int64_t classes, int32_t type, bool grad, void *workspace)
 {
     LossPlan p = {};
@@ -217,21 +240,22 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
     const int64_t slice = MM_ROW / size;
     // rows that are whole slices of aligned chunks are read where they are
     auto as_is = [&](const void *q, int64_t ld) { return d % slice == 0 && ld * size % 16 == 0 && (uintptr_t)q % 16 == 0 && ld < LOSS_MOST_D; };
-    // Few rows read w as it lies, more of them where it would have to be laid out first or where products cost eight times as much.
-    p.few = n <= (size == 4 ? FEW_ROWS : as_is(w, ldw) ? 16 : 64);
-    p.few_grad = grad && n <= FEW_GRAD_ROWS;
+    p.few = n <= few_rows(size, as_is(w, ldw));
+    p.few_grad = grad && n <= (size == 4 ? FEW_GRAD_ROWS : FEW_GRAD_ROWS / 2);
     p.config = mm_choose(size, classes, n);
     p.loss_splits = 1;
     if (!p.few) {
-        // tiles that leave half of the chip idle (in 32 bits: some of it), and sums long enough to be divided
+        // Tiles that leave much of the chip idle, and sums long enough to be divided.  In us, divided / not, 16 bits: 128 rows of 4096 and
+        // 1000 classes (8 tiles) 19 / 45, 256 and 3000 (48) 37 / 47, 8000 classes of 128 rows (63) 49 / 46, of 256 rows of 2048 (126) 39 / 28.
+        // 32 bits: 512 rows of 2048 and 4000 classes (128) 91 / 144.
         const int64_t tiles = ceil_div(classes, mm_tile_i(p.config)) * ceil_div(n, mm_tile_j(p.config)), slices = ceil_div(d, slice), room = 2 * CUS;
-        if (tiles * (size == 4 ? 1 : 2) <= CUS && slices >= 16) {
+        if (tiles * (size == 4 ? 1 : 4) <= CUS && slices >= 16) {
             const int64_t most = room / tiles < slices / 4 ? room / tiles : slices / 4;
             p.loss_splits = (int)ceil_div(slices, ceil_div(slices, most));
         }
     }
-    p.kept = grad && (p.few || size == 4 || p.loss_splits > 1);
-    p.tiles = grad ? !p.few_grad : !p.few;
+    p.kept = grad && (p.few || size == 4 || p.config != WIDE);
+    p.tiles = !p.few || (grad && !p.few_grad);
     p.lay_w = p.tiles && !as_is(w, ldw);
     p.piece_rows = n;
     Carver c(workspace);
@@ -239,13 +263,11 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
     if (grad) p.lse = c.take<float>(n);
     if (p.few) {
         const int64_t batch = slice / 2 * FEW_AHEAD, all = round_up(d, batch), per_column = n * size, spare = 16 / size;
-        // several workgroups to a compute unit, else two of eight wavefronts
-        p.few_threads = (all + spare) * per_column <= 32 * 1024 ? 256 : FEW_THREADS;
         p.few_chunk = (int)all;
         if ((all + spare) * per_column > 72 * 1024) p.few_chunk = (int)((72 * 1024 / per_column - spare) / batch * batch);
-        const int64_t sums = p.few_threads / 64 * FEW_ROWS * (int64_t)sizeof(float2), lds = (p.few_chunk + spare) * per_column;
+        const int64_t sums = FEW_THREADS / 64 * FEW_ROWS * (int64_t)sizeof(float2), lds = (p.few_chunk + spare) * per_column;
         p.few_lds = (int)(lds > sums ? lds : sums);
-        const int64_t blocks = ceil_div(ceil_div(classes, 16), p.few_threads / 64);
+        const int64_t blocks = ceil_div(ceil_div(classes, 16), FEW_THREADS / 64);
         p.few_blocks = (int)(blocks < 2048 ? blocks : 2048);
         p.few_passes = (int)ceil_div(blocks, p.few_blocks);
         p.tile_sums = c.take<float2>(n * p.few_blocks);
@@ -262,7 +284,7 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         p.few_each = (int)(round_up(ceil_div(classes, 1024), 8));
         p.few_grad_blocks = (int)ceil_div(classes, p.few_each);
         p.ldp = round_up(d, 8);
-        p.logits = c.take<float>(n * p.ldz);
+        p.logits = c.take<float>(n * p.ldz * p.loss_splits);
         p.parts = c.take<float>(p.few_grad_blocks * n * p.ldp);
     }
     if (p.loss_splits > 1 && !grad) p.logits = c.take<float>(n * p.ldz * p.loss_splits);
@@ -275,7 +297,7 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         p.x = p.lay_x ? c.take<char>(p.rows_x * p.ldk * size) : (char *)x;
         p.w = p.lay_w ? c.take<char>(classes * p.ldk * size) : (char *)w;
     }
-    if (grad && p.tiles) {
+    if (grad && !p.few_grad) {
         p.power = c.take<float>(2);
         if (p.kept) {
             p.piece = classes;
@@ -385,11 +407,11 @@ int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw
     const LossRows rows = rows_from(all, first, many);
     int parts;
     if (p.few) {
-        auto kernel = p.n <= 16 ? loss_few<T, 1> : p.n <= 32 ? loss_few<T, 2> : loss_few<T, 4>;
+        auto kernel = loss_few<T, 1>;
         if constexpr (sizeof(T) == 4)
-            if (p.n > 64) kernel = loss_few<T, 6>;
+            if (p.n > 16) kernel = loss_few<T, 2>;
         TRY(allow_lds(kernel, p.few_lds));
-        kernel<<<(unsigned)p.few_blocks, p.few_threads, p.few_lds, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_chunk, p.few_passes, logits, p.ldz);
+        kernel<<<(unsigned)p.few_blocks, FEW_THREADS, p.few_lds, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_chunk, p.few_passes, logits, p.ldz);
         TRY(launched("loss_few"));
         parts = p.few_blocks;
     } else {
@@ -410,9 +432,9 @@ int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw
         }
         TRY(with_config<T, MmWide>(p.config, [&](auto c) {
             typedef decltype(c) C;
-            auto kernel = loss_tiles<T, C>;
+            auto kernel = loss_tiles<T, C, sizeof(T) == 4 || !std::is_same<C, MmWide>::value>;
             TRY(allow_lds(kernel, C::LDS));
-            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, (T *)logits, p.ldz);
+            kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, logits, p.ldz);
             return launched("loss_tiles");
         }));
         parts = s.tiles_i * MM_PARTS_I;
@@ -481,7 +503,9 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
     if (p.few_grad) {
         TRY(run_loss<T>(p, x, ldx, w, ldw, rows, 0, p.n, p.logits, loss, p.lse, flags, stream));
         const dim3 grid((unsigned)p.few_grad_blocks, (unsigned)ceil_div(p.d, 256 * Elem<T>::VEC));
-        auto kernel = p.n == 1 ? loss_grad_few<T, 1> : p.n == 2 ? loss_grad_few<T, 2> : p.n <= 4 ? loss_grad_few<T, 4> : loss_grad_few<T, 8>;
+        auto kernel = p.n == 1 ? loss_grad_few<T, 1> : p.n == 2 ? loss_grad_few<T, 2> : loss_grad_few<T, 4>;
+        if constexpr (sizeof(T) == 4)
+            if (p.n > 4) kernel = loss_grad_few<T, 8>;
         kernel<<<grid, 256, 0, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_each, p.logits, p.ldz, dw, lddw, p.parts, p.ldp);
         TRY(launched("loss_grad_few"));
         return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, p.few_grad_blocks, dx, lddx, p.n, p.d, nullptr, stream);
@@ -499,7 +523,7 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
         for (int64_t first = 0; first < p.n; first += p.piece_rows) {
             const int64_t many = p.n - first < p.piece_rows ? p.n - first : p.piece_rows;
             TRY(run_loss<T>(p, x, ldx, w, ldw, rows, first, many, p.logits, loss, p.lse, flags, stream));
-            const dim3 grid((unsigned)grid_of(p.ldg, 1024, 64), (unsigned)round_up(many, MM_K<T>));
+            const dim3 grid((unsigned)round_up(many, MM_K<T>), (unsigned)grid_of(p.ldg, 1024, 64));
             loss_grad_kept<T><<<grid, 256, 0, stream>>>(p.logits, p.ldz, rows_from(rows, first, many), (T *)p.g, p.ldg);
             TRY(launched("loss_grad_kept"));
             int copies = 0;
@@ -632,9 +656,11 @@ int chicle_embed(const void *table, int64_t ld, int64_t n_rows, const void *ids,
     const int lanes = pow2_at_least(ceil_div(d, 16 / s), EMBED_THREADS);
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        embed_rows<T><<<(unsigned)ceil_div(n, EMBED_THREADS / lanes), EMBED_THREADS, 0, (hipStream_t)hip_stream>>>(
-            (const T *)table, ld, n_rows, ids, wide, (T *)out, ldo, n, d, lanes, scale, flags);
-        return launched("embed_rows");
+        return with_rows(n, EMBED_THREADS / lanes, [&](int64_t first, int64_t many, unsigned grid) {
+            embed_rows<T><<<grid, EMBED_THREADS, 0, (hipStream_t)hip_stream>>>(
+                (const T *)table, ld, n_rows, (const char *)ids + first * (wide ? 8 : 4), wide, (T *)out + first * ldo, ldo, many, d, lanes, scale, flags);
+            return launched("embed_rows");
+        });
     });
 }
 
@@ -684,7 +710,11 @@ int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t l
     g.n = n; g.d = d; g.n_rows = n_rows; g.ldo = ldo; g.ldd = ldd; g.ldp = p.ldp;
     g.lanes = pow2_at_least(ceil_div(d, vec), EMBED_THREADS);
     const int groups = EMBED_THREADS / g.lanes;
-    g.run_blocks = (int)ceil_div(p.pieces, groups);
+    // Longer pieces leave fewer parts to be joined, where there are workgroups enough: 131,072 tokens of 2048 in 16 bits 228 instead of 251 us,
+    // 16,000 tokens 71 instead of 64, 131,072 tokens of 512 (four pieces to a workgroup) 81 and 80.
+    g.piece = groups == 1 && n >= 2 * EMBED_PIECE * 2048 ? 2 * EMBED_PIECE : EMBED_PIECE;
+    const int64_t pieces = ceil_div(n, g.piece);
+    g.run_blocks = (int)ceil_div(pieces, groups);
     g.zero_rows = (int)(d * s >= ZERO_BYTES ? 1 : ZERO_BYTES / (d * s));
     g.zero_blocks = accumulate ? 0 : (int)ceil_div(n_rows, g.zero_rows);
     g.seen = seen;
@@ -693,10 +723,10 @@ int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t l
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
         const dim3 grid((unsigned)(g.run_blocks + g.zero_blocks), (unsigned)ceil_div(d, (int64_t)g.lanes * vec));
-        embed_grad_runs<T><<<grid, EMBED_THREADS, groups * EMBED_PIECE * sizeof(uint2), stream>>>(g, (const T *)dout, (T *)dtable);
+        embed_grad_runs<T><<<grid, EMBED_THREADS, (size_t)groups * g.piece * sizeof(uint2), stream>>>(g, (const T *)dout, (T *)dtable);
         TRY(launched("embed_grad_runs"));
-        if (p.pieces > 1) {
-            const dim3 join((unsigned)ceil_div(p.pieces - 1, JOIN_PIECES), (unsigned)ceil_div(d, JOIN_COLUMNS));
+        if (pieces > 1) {
+            const dim3 join((unsigned)ceil_div(pieces - 1, JOIN_PIECES), (unsigned)ceil_div(d, JOIN_COLUMNS));
             embed_grad_join<T><<<join, 64 * JOIN_WAVES, 0, stream>>>(g, (T *)dtable);
             TRY(launched("embed_grad_join"));
         }
@@ -721,10 +751,13 @@ int chicle_layer_norm(const void *x, int64_t ldx, const void *gamma, const void 
             constexpr int NV = decltype(v)::value;
             if constexpr (NV * Elem<T>::VEC <= LN_FORWARD_VALUES) {
                 auto kernel = r.threads > 256 ? layer_norm_rows<T, NV, LN_MOST_THREADS> : layer_norm_rows<T, NV, 256>;
-                kernel<<<(unsigned)ceil_div(n, r.threads / r.lanes), r.threads, 0, (hipStream_t)hip_stream>>>(
-                    (const T *)x, ldx, (const T *)gamma, (const T *)beta, (T *)y, ldy, mean, rstd, n, d, r.lanes, eps);
+                return with_rows(n, r.threads / r.lanes, [&](int64_t first, int64_t many, unsigned grid) {
+                    kernel<<<grid, r.threads, 0, (hipStream_t)hip_stream>>>((const T *)x + first * ldx, ldx, (const T *)gamma, (const T *)beta,
+                                                                            (T *)y + first * ldy, ldy, mean + first, rstd + first, many, d, r.lanes, eps);
+                    return launched("layer_norm_rows");
+                });
             }
-            return launched("layer_norm_rows");
+            return (int)CHICLE_OK;
         });
     });
 }

@@ -251,14 +251,14 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_scatter(SortPass p)
 
 // ---- sums over runs of equal ids ------------------------------------------------------------------------------------
 
-constexpr int EMBED_PIECE = 32;              // tokens of a piece
+constexpr int EMBED_PIECE = 32;              // tokens of the shortest pieces
 constexpr int ZERO_BYTES = 16384;            // of the rows that a workgroup fills with zeros
 
 struct EmbedGrad {
     const unsigned *keys, *places;           // sorted
     float *head, *tail;                      // [piece][ldp]: what a piece holds of a run that began before it, or that goes on behind it
     int64_t n, d, n_rows, ldo, ldd, ldp;
-    int lanes;                               // threads of a piece
+    int piece, lanes;                        // tokens and threads of a piece
     int run_blocks, zero_blocks, zero_rows;  // zero_rows: to a workgroup
     int accumulate;
     const uint8_t *seen;
@@ -309,14 +309,14 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_grad_runs(EmbedGrad p, co
         return;
     }
     const int groups = EMBED_THREADS / p.lanes, group = threadIdx.x / p.lanes;
-    const int64_t piece0 = b * groups, t0 = piece0 * EMBED_PIECE;
-    for (int i = threadIdx.x; i < groups * EMBED_PIECE && t0 + i < p.n; i += EMBED_THREADS) tokens[i] = make_uint2(p.keys[t0 + i], p.places[t0 + i]);
+    const int64_t piece0 = b * groups, t0 = piece0 * p.piece;
+    for (int i = threadIdx.x; i < groups * p.piece && t0 + i < p.n; i += EMBED_THREADS) tokens[i] = make_uint2(p.keys[t0 + i], p.places[t0 + i]);
     __syncthreads();
-    const int64_t piece = piece0 + group, a = piece * EMBED_PIECE;
-    const int many = (int)min((int64_t)EMBED_PIECE, p.n - a);
+    const int64_t piece = piece0 + group, a = piece * p.piece;
+    const int many = (int)min((int64_t)p.piece, p.n - a);
     const int64_t c = ((int64_t)blockIdx.y * p.lanes + threadIdx.x % p.lanes) * V;
     if (many <= 0 || c >= p.d) return;
-    const uint2 *mine = tokens + group * EMBED_PIECE;
+    const uint2 *mine = tokens + group * p.piece;
     float sum[V] = {};
     unsigned key = mine[0].x;
     bool from_before = a > 0 && p.keys[a - 1] == key;
@@ -388,7 +388,7 @@ __device__ __forceinline__ int64_t last_piece(const EmbedGrad &p, int64_t piece,
     for (int stride = 64 * 64; stride >= 1; stride /= 64)
         for (;;) {                                       // sixty-four probes, a stride apart
             const int64_t at = last + (int64_t)(lane + 1) * stride;
-            const unsigned long long same = __ballot(at < pieces && p.keys[min(at, pieces - 1) * EMBED_PIECE] == key);
+            const unsigned long long same = __ballot(at < pieces && p.keys[min(at, pieces - 1) * p.piece] == key);
             last += (int64_t)__popcll(same) * stride;
             if (~same) break;
         }
@@ -411,8 +411,8 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void embed_grad_join(EmbedGrad p, 
     __shared__ float4 s[JOIN_WAVES][64];
     __shared__ int64_t lasts[JOIN_WAVES];                // last piece of a long run, or 0
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t c = (int64_t)blockIdx.y * JOIN_COLUMNS + lane * 4, pieces = (p.n + EMBED_PIECE - 1) / EMBED_PIECE;
-    const int64_t piece = (int64_t)blockIdx.x * JOIN_PIECES + wave, a = piece * EMBED_PIECE, end = a + EMBED_PIECE;
+    const int64_t c = (int64_t)blockIdx.y * JOIN_COLUMNS + lane * 4, pieces = (p.n + p.piece - 1) / p.piece;
+    const int64_t piece = (int64_t)blockIdx.x * JOIN_PIECES + wave, a = piece * p.piece, end = a + p.piece;
     int64_t last = 0;
     unsigned key = 0;
     if (end < p.n) {
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void embed_grad_join(EmbedGrad p, 
                 const float4 t = s[v][lane];
                 sum.x += t.x; sum.y += t.y; sum.z += t.z; sum.w += t.w;
             }
-            give_columns(p, out, p.keys[last * EMBED_PIECE], c, sum);
+            give_columns(p, out, p.keys[last * p.piece], c, sum);
         }
         __syncthreads();
     }

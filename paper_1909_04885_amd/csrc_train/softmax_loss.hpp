@@ -10,8 +10,9 @@
 // The gradient in 16 bits forms the logits again, a piece of the classes at a time, and turns them in registers into G, which is stored in
 // 16 bits for the two products that read it; rounding G is of the size of the rounding of the gradients themselves, and of no
 // direction: G comes divided by the largest weight, and the products times it, so that a weight that all rows share, which would be
-// rounded to the same side everywhere, is not rounded at all.  Half precision would lose small G: there it comes 2^14 times as large.  In 32 bits a product costs eight times as much, and the logits of a piece of the rows are
-// kept until they are G; so are those of few rows, which are few bytes beside w.
+// rounded to the same side everywhere, is not rounded at all.  Half precision would lose small G: there it comes 2^14 times as large.  In 32 bits a
+// product costs eight times as much, and the logits of a piece of the rows are kept until they are G; so are those of few rows and of
+// few classes, which are few bytes.
 //
 // The bound is the matrix cores: 2 n d classes operations for the loss, and twice that again for the gradients (three times in 16 bits).
 // Few rows are bound by reading w.
@@ -76,9 +77,9 @@ template <bool EXACT> __device__ __forceinline__ float exp_of(float z, float m)
     return EXACT ? expf(z - m) : __builtin_amdgcn_exp2f((z - m) * LOG2E);
 }
 
-// i: classes, j: rows.  logits (32 bits): null, or [row][ldz], where they are kept.
-template <typename T, typename C>
-__global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_tiles(MmShape s, LossRows l, T *__restrict__ logits, int64_t ldz)
+// i: classes, j: rows.  logits: null, or [row][ldz], where they are kept (KEEP: they may be).
+template <typename T, typename C, bool KEEP>
+__global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_tiles(MmShape s, LossRows l, float *__restrict__ logits, int64_t ldz)
 {
     constexpr bool EXACT = sizeof(T) == 4;
     mm_tiles<T, C, false, false>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_tiles(MmShape s,
                     for (int r = 0; r < 4; ++r) z = rel == at.place(mi) + r ? acc[mi][nj][r] : z;
                 l.picked[j] = z;
             }
-            if constexpr (EXACT)
+            if constexpr (KEEP)
                 if (logits && j < l.n)                   // (rows of logits are whole tiles long)
 #pragma unroll
                     for (int mi = 0; mi < C::MI; ++mi) *(f32x4 *)(logits + (int64_t)j * ldz + at.i0 + at.place(mi)) = acc[mi][nj];
@@ -233,14 +234,14 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_grad_tiles(MmSha
 }
 
 // G of logits that were kept: g[row][class] of all classes, zeros up to ldg and in rows [n, rows_out).  g may be the logits themselves.
-// Grid: (columns, rows).
+// Grid: (rows, columns).
 template <typename T>
 __global__ __launch_bounds__(256) void loss_grad_kept(const float *logits, int64_t ldz, LossRows l, T *g, int64_t ldg)
 {
-    const int j = blockIdx.y, label = label_at(l, j);
+    const int j = blockIdx.x, label = label_at(l, j);
     const float power = l.power ? l.power[0] : 1.f;
     const float weight = label >= 0 ? l.weight[j] * power : 0.f, lse = label >= 0 ? l.lse[j] : 0.f;
-    for (int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; c < ldg; c += (int64_t)gridDim.x * 1024) {
+    for (int64_t c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4; c < ldg; c += (int64_t)gridDim.y * 1024) {
         T v[4];
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
@@ -346,7 +347,7 @@ __global__ __launch_bounds__(256) void sum_parts(const float *__restrict__ part,
 // the logits.  `loss_grad_few`, for the fewest rows, reads w once more: a thread owns a vector of columns and forms dw's rows and its
 // part of dx in 32 bits.
 
-constexpr int FEW_ROWS = 96, FEW_GRAD_ROWS = 8, FEW_AHEAD = 8, FEW_THREADS = 512;
+constexpr int FEW_ROWS = 32, FEW_GRAD_ROWS = 8, FEW_AHEAD = 8, FEW_THREADS = 512;
 template <typename T> constexpr int FEW_BATCH = MM_K<T> / 2 * FEW_AHEAD;   // k of a batch of accesses
 
 // Rows 16 q + l % 16 of x in LDS, `chunk` columns at a time where not all of them fit: x[row][chunk + one chunk], zeros past d; then (largest,

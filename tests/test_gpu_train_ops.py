@@ -98,6 +98,12 @@ def test_softmax_loss_over_several_pieces_of_the_rows(ops):
     check_loss(ops, x, w, labels, torch.rand(n, generator=g, device="cuda"))
 
 
+def test_softmax_loss_of_more_rows_than_a_second_grid_dimension_holds(ops):
+    g = gen(31)
+    x, w = rows(g, 70001, 5, F32), rows(g, 3, 5, F32)
+    check_loss(ops, x, w, torch.randint(0, 3, (70001,), generator=g, device="cuda", dtype=torch.int32), torch.rand(70001, generator=g, device="cuda") / 70001)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=NAME.get)
 def test_softmax_loss_no_row_has_a_label(ops, dtype):
     g = gen(3)
@@ -388,6 +394,15 @@ def test_embed_grad(ops, dtype, kind, n, d, n_rows):
     untouched[ids[ids >= 0].long()] = False
     assert torch.equal(into[untouched], before[untouched])
     ops.sync()
+
+
+def test_embed_grad_of_many_wide_rows(ops):
+    g = gen(32)
+    n, d, n_rows = 2 ** 17 + 45, 1034, 3001
+    ids = token_ids(g, n, n_rows, "zipf", False)
+    dout = rows(g, n, d, BF16)
+    want, off = ref.embed_grad(ids, dout, n_rows, 0.6)
+    ref.within(ops.embed_grad(ids, dout, n_rows, 0.6), want, off)
 
 
 def test_embed_without_tokens(ops):
