@@ -15,7 +15,10 @@
 // few classes, which are few bytes.
 //
 // The bound is the matrix cores: 2 n d classes operations for the loss, and twice that again for the gradients (three times in 16 bits).
-// Few rows are bound by reading w.
+// With gradients, 8192 rows of 2048 and 128,000 classes in bfloat16: 14.9 ms, 1150 TFLOP/s of the four products; 4096 rows of 1024 and
+// 50,021 classes: 1.65 ms, 1020; 333 rows of 250 and 20,000 classes in 32 bits: 168 us, 60 TFLOP/s of 154, three products of 8 to 11
+// slices each, most of whose time is their beginning and end.  Few rows are bound by reading w: one row against 32,000 classes of
+// 1024 in bfloat16 18.5 us, 14 of them the product at 4.7 TB/s.
 #pragma once
 #include "matmul.hpp"
 
@@ -342,7 +345,7 @@ __global__ __launch_bounds__(256) void sum_parts(const float *__restrict__ part,
 
 // ---- few rows -------------------------------------------------------------------------------------------------------
 //
-// Few rows are bound by reading w.  `loss_few` reads it as it lies, whatever its distance and alignment: a wavefront takes sixteen classes at a
+// Few rows are bound by reading w, and laying it out would read and write it once more.  `loss_few` reads it as it lies, whatever its distance and alignment: a wavefront takes sixteen classes at a
 // time, its lanes' sixteen bytes being the matrix instruction's operand as they come, and x lies in LDS.  For the gradient it leaves
 // the logits.  `loss_grad_few`, for the fewest rows, reads w once more: a thread owns a vector of columns and forms dw's rows and its
 // part of dx in 32 bits.
