@@ -161,7 +161,9 @@ int mm_tile_j(int c) { return c == WIDE ? 256 : c == MIDDLE ? 128 : 64; }
 
 // 16 bits: large tiles read the least and feed the matrix cores best (1300 against 1000 TFLOP/s of the middle ones), where they fill the chip:
 // losses of 512 rows of 1024 and 16,000 classes (126 large tiles) 25 us in middle and 69 in large ones, 700 rows and 20,000 (237) 44 and 41.
-// 32 bits: the matrix cores are the bound whatever the tile, and what counts is how much of the tiles lies past the last row.
+// 32 bits: the matrix cores are the bound whatever the tile, and what counts is how much of the tiles lies past the last row, and that they share
+// out well: gradients of 333 rows of 250 and 20,000 classes 168 us in middle and 160 in thin tiles, 1000 rows of 1024 and 10,000 597 and
+// 578, 4096 rows of 512 and 30,000 3323 and 3481 (tiles of 64 x 64: 163, 616, 3670).
 // `splittable`: the sum is long and may be divided; the gradients of 512 rows of 1024 and 50,000 classes (8 large tiles) take 287 us with middle
 // tiles and 294 with large ones, of 4096 rows (64) 1699 and 1637; of 1024 rows of 2048 and 12,000 classes, whose sum is short, 238 and 243.
 int mm_choose(int size, int64_t rows_i, int64_t rows_j, bool splittable = false)
@@ -169,7 +171,8 @@ int mm_choose(int size, int64_t rows_i, int64_t rows_j, bool splittable = false)
     if (rows_j <= 64) return THIN;
     const int64_t tiles = ceil_div(rows_i, 256) * ceil_div(rows_j, 256);
     if (size == 2) return tiles >= (splittable ? 64 : 192) ? WIDE : MIDDLE;
-    return ceil_div(rows_j, 128) * 2 == ceil_div(rows_j, 64) ? MIDDLE : THIN;
+    const int64_t middle = ceil_div(rows_j, 128);
+    return middle * 2 == ceil_div(rows_j, 64) && middle * ceil_div(rows_i, 128) >= 4 * CUS ? MIDDLE : THIN;
 }
 
 // f(C()) with the tile; W is the large one of the 16-bit types

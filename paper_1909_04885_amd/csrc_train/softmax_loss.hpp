@@ -16,7 +16,7 @@
 //
 // The bound is the matrix cores: 2 n d classes operations for the loss, and twice that again for the gradients (three times in 16 bits).
 // With gradients, 8192 rows of 2048 and 128,000 classes in bfloat16: 14.9 ms, 1150 TFLOP/s of the four products; 4096 rows of 1024 and
-// 50,021 classes: 1.65 ms, 1020; 333 rows of 250 and 20,000 classes in 32 bits: 168 us, 60 TFLOP/s of 154, three products of 8 to 11
+// 50,021 classes: 1.65 ms, 1020; 333 rows of 250 and 20,000 classes in 32 bits: 160 us, 62 TFLOP/s of 154, three products of 8 to 11
 // slices each, most of whose time is their beginning and end.  Few rows are bound by reading w: one row against 32,000 classes of
 // 1024 in bfloat16 18.5 us, 14 of them the product at 4.7 TB/s.
 #pragma once
