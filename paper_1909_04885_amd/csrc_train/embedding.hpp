@@ -11,8 +11,8 @@
 //
 // The bound is the memory: dout is read once, the table's gradient written once.  Lookup of 16,001 x 2048 in half precision: 17 us
 // (4.9 TB/s).  Gradient of 131,072 tokens into 128,000 x 2048 in bfloat16: 229 us (4.6 TB/s; sorting 36, sums and zeros 173, joining 20);
-// of 30,011 into 200,000 x 256 in 32 bits: 76 us (3.1 TB/s; sorting 29).  Below some thousand tokens four launches and the passes of
-// the sort are what it takes: 64 tokens of 256 into 32,000 rows 24 us.
+// of 30,011 into 200,000 x 256 in 32 bits: 72 us (3.3 TB/s; sorting 29).  Below some thousand tokens four launches and the passes of
+// the sort are what it takes: 64 tokens of 256 into 32,000 rows 23 us.
 #pragma once
 #include "elements.hpp"
 
@@ -258,6 +258,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_scatter(SortPass p)
 
 constexpr int EMBED_PIECE = 32;              // tokens of the shortest pieces
 constexpr int ZERO_BYTES = 16384;            // of the rows that a workgroup fills with zeros
+constexpr int ZERO_AHEAD = 4;
 
 struct EmbedGrad {
     const unsigned *keys, *places;           // sorted
@@ -296,8 +297,14 @@ __device__ __forceinline__ void zero_rows(const EmbedGrad &p, int block, int64_t
     const float zero[V] = {};
     const int64_t r0 = (int64_t)block * p.zero_rows, end = min(p.n_rows, r0 + p.zero_rows);
     if (c >= p.d) return;
-    for (int64_t row = r0 + threadIdx.x / p.lanes; row < end; row += groups)
-        if (!p.seen[row]) store_vec<T, true>(out + row * p.ldo, c, p.d, zero);
+    for (int64_t row = r0 + threadIdx.x / p.lanes; row < end; row += ZERO_AHEAD * groups) {
+        bool seen[ZERO_AHEAD];                           // (asked for together)
+#pragma unroll
+        for (int q = 0; q < ZERO_AHEAD; ++q) seen[q] = row + q * groups >= end || p.seen[row + q * groups];
+#pragma unroll
+        for (int q = 0; q < ZERO_AHEAD; ++q)
+            if (!seen[q]) store_vec<T, true>(out + (row + q * groups) * p.ldo, c, p.d, zero);
+    }
 }
 
 // The work of run_blocks workgroups that add up pieces of tokens, EMBED_THREADS / lanes pieces each, and then of zero_blocks that store
@@ -306,7 +313,7 @@ __device__ __forceinline__ void zero_rows(const EmbedGrad &p, int block, int64_t
 template <typename T>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_grad_runs(EmbedGrad p, const T *__restrict__ dout, T *__restrict__ out)
 {
-    constexpr int V = Elem<T>::VEC, AHEAD = 8;
+    constexpr int V = Elem<T>::VEC, AHEAD = 16;
     extern __shared__ uint2 tokens[];                    // (id, place) of the workgroup's pieces
     const int64_t b = blockIdx.x;
     if (b >= p.run_blocks) {
@@ -316,15 +323,16 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_grad_runs(EmbedGrad p, co
     const int groups = EMBED_THREADS / p.lanes, group = threadIdx.x / p.lanes;
     const int64_t piece0 = b * groups, t0 = piece0 * p.piece;
     for (int i = threadIdx.x; i < groups * p.piece && t0 + i < p.n; i += EMBED_THREADS) tokens[i] = make_uint2(p.keys[t0 + i], p.places[t0 + i]);
-    __syncthreads();
     const int64_t piece = piece0 + group, a = piece * p.piece;
     const int many = (int)min((int64_t)p.piece, p.n - a);
+    const unsigned before = many > 0 && a > 0 ? p.keys[a - 1] : 0u, after = many > 0 && a + many < p.n ? p.keys[a + many] : 0u;
+    __syncthreads();
     const int64_t c = ((int64_t)blockIdx.y * p.lanes + threadIdx.x % p.lanes) * V;
     if (many <= 0 || c >= p.d) return;
     const uint2 *mine = tokens + group * p.piece;
     float sum[V] = {};
     unsigned key = mine[0].x;
-    bool from_before = a > 0 && p.keys[a - 1] == key;
+    bool from_before = a > 0 && before == key;
     auto leave = [&](float *part) {
         float *dst = part + piece * p.ldp + c;           // (rows of parts are padded to whole vectors)
 #pragma unroll
@@ -356,7 +364,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_grad_runs(EmbedGrad p, co
         }
     }
     if ((int64_t)key >= p.n_rows) return;
-    const bool goes_on = a + many < p.n && p.keys[a + many] == key;
+    const bool goes_on = a + many < p.n && after == key;
     if (from_before) leave(p.head);
     else if (goes_on) leave(p.tail);
     else give_row(p, out, key, c, sum);
