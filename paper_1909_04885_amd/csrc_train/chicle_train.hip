@@ -570,7 +570,7 @@ constexpr int64_t EMBED_MOST_D = (1 << 23) - 1;          // blocks of columns ar
 
 struct EmbedPlan {
     int64_t pieces, tile, ldp, seen_bytes;
-    int tiles, passes, digit;
+    int piece, tiles, passes, digit;
     bool one;                            // one workgroup sorts
     unsigned *keys[2], *places[2], *count;
     uint8_t *seen;
@@ -581,7 +581,10 @@ struct EmbedPlan {
 EmbedPlan embed_plan(int64_t n, int64_t d, int64_t n_rows, void *workspace)
 {
     EmbedPlan p = {};
-    p.pieces = ceil_div(n, EMBED_PIECE);
+    // A piece is a chain of its tokens, 0.3 us each, and what it leaves is to be joined.  In us, into 32,000 rows, pieces of 8 / 16 / 32: 500 tokens
+    // of 64 18.5 / 19.7 / 23.1, 8000 of 256 39 / 41 / 45, 4000 of 1024 45 / 44 / 45, 16,000 of 1024 54 / 48 / 52; 131,072 of 2048 16 / 32: 288 / 252.
+    p.piece = n * d <= (int64_t)1 << 21 ? 8 : n * d <= (int64_t)1 << 24 ? 16 : 32;
+    p.pieces = ceil_div(n, p.piece);
     p.ldp = round_up(d, 8);
     int bits = 1;
     while (((int64_t)1 << bits) <= n_rows) ++bits;       // keys are 0 .. n_rows
@@ -720,9 +723,9 @@ int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t l
     g.n = n; g.d = d; g.n_rows = n_rows; g.ldo = ldo; g.ldd = ldd; g.ldp = p.ldp;
     g.lanes = pow2_at_least(ceil_div(d, vec), EMBED_THREADS);
     const int groups = EMBED_THREADS / g.lanes;
-    // Longer pieces leave fewer parts to be joined, where there are workgroups enough: 131,072 tokens of 2048 in 16 bits 228 instead of 251 us,
+    // Where there are workgroups enough, still longer ones: 131,072 tokens of 2048 in 16 bits 228 instead of 251 us,
     // 16,000 tokens 71 instead of 64, 131,072 tokens of 512 (four pieces to a workgroup) 81 and 80.
-    g.piece = groups == 1 && n >= 2 * EMBED_PIECE * 2048 ? 2 * EMBED_PIECE : EMBED_PIECE;
+    g.piece = groups == 1 && p.pieces >= 2 * 2048 && p.piece == 32 ? 64 : p.piece;
     const int64_t pieces = ceil_div(n, g.piece);
     g.run_blocks = (int)ceil_div(pieces, groups);
     g.zero_rows = (int)(d * s >= ZERO_BYTES ? 1 : ZERO_BYTES / (d * s));

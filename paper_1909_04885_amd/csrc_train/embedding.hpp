@@ -12,7 +12,7 @@
 // The bound is the memory: dout is read once, the table's gradient written once.  Lookup of 16,001 x 2048 in half precision: 17 us
 // (4.9 TB/s).  Gradient of 131,072 tokens into 128,000 x 2048 in bfloat16: 229 us (4.6 TB/s; sorting 36, sums and zeros 173, joining 20);
 // of 30,011 into 200,000 x 256 in 32 bits: 72 us (3.3 TB/s; sorting 29).  Below some thousand tokens four launches and the passes of
-// the sort are what it takes: 64 tokens of 256 into 32,000 rows 23 us.
+// the sort are what it takes: 64 tokens of 256 into 32,000 rows 19 us.
 #pragma once
 #include "elements.hpp"
 
@@ -256,7 +256,6 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_scatter(SortPass p)
 
 // ---- sums over runs of equal ids ------------------------------------------------------------------------------------
 
-constexpr int EMBED_PIECE = 32;              // tokens of the shortest pieces
 constexpr int ZERO_BYTES = 16384;            // of the rows that a workgroup fills with zeros
 constexpr int ZERO_AHEAD = 4;
 
