@@ -17,7 +17,8 @@
  *   - matrices are row-major with unit column stride; ld is the distance of rows in elements (at least the row's length); data
  *     begins at any multiple of its element's size; outputs overlap no inputs unless said otherwise;
  *   - type (chicle_type) is that of all matrices and parameter vectors of a call.  Sums, statistics and losses are held in
- *     32 bits or more, and results of a 16-bit type are rounded once, where they are stored;
+ *     32 bits or more (the loss's derivatives by the logits, in 16-bit types, to twice the type's bits), and results of a 16-bit
+ *     type are rounded once, where they are stored;
  *   - label and token arrays hold 32-bit integers, or 64-bit ones where `wide` is not 0.  A negative one means "none": no loss, a row
  *     of zeros, no gradient.  One past the end is treated like that too, and sets a bit of *flags (1: label, 2: token), an
  *     int32 of the caller's, or NULL;

@@ -210,7 +210,7 @@ struct LossPlan {
 };
 
 // 8192 rows of 2048 and 128,000 classes in 16 bits with a quarter of it: 15.2 ms, this 15.4, four times as much 15.6; but every piece has its parts of dx.
-constexpr int64_t LOSS_PIECE_BYTES = (int64_t)1 << 29;   // G of a piece of the classes
+constexpr int64_t LOSS_PIECE_BYTES = (int64_t)1 << 30;   // both planes of G of a piece of the classes
 // 16,384 rows of 512 and 50,000 classes in 32 bits with a quarter of it: 24.1 ms, this 22.4, four times as much 22.3.
 constexpr int64_t LOSS_KEPT_BYTES = (int64_t)1 << 30;    // logits of a piece of the rows
 constexpr int64_t LOSS_MOST = (int64_t)1 << 22, LOSS_MOST_D = (int64_t)1 << 21, LOSS_MOST_CLASSES = (int64_t)1 << 23;
@@ -239,13 +239,15 @@ int64_t few_rows(int size, bool aligned)
     return aligned ? 0 : FEW_ROWS / 2;
 }
 
+constexpr int planes_of_g(int size) { return size == 2 ? 2 : 1; }
+
 LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t n, int64_t d, int64_t classes, int32_t type, bool grad, void *workspace)
 {
     LossPlan p = {};
     p.bytes = ALIGN;
     if (n == 0) return p;                                // (nothing to lay out)
     p.n = n; p.d = d; p.classes = classes;
-    const int size = size_of(type);
+    const int size = size_of(type), planes = planes_of_g(size);
     const int64_t slice = MM_ROW / size;
     // rows that are whole slices of aligned chunks are read where they are
     auto as_is = [&](const void *q, int64_t ld) { return d % slice == 0 && ld * size % 16 == 0 && (uintptr_t)q % 16 == 0 && ld < LOSS_MOST_D; };
@@ -313,7 +315,7 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
             p.piece = classes;
             if (p.few || p.loss_splits > 1) p.pieces = 1;
         } else {
-            int64_t most = LOSS_PIECE_BYTES / (size * p.rows_x) / 256 * 256;
+            int64_t most = LOSS_PIECE_BYTES / (planes * size * p.rows_x) / 256 * 256;
             most = most < 256 ? 256 : most;
             p.pieces = (int)ceil_div(classes, most);
             p.piece = round_up(ceil_div(classes, p.pieces), 256);
@@ -323,7 +325,7 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         p.rows_g = round_up(p.piece_rows, slice);
         p.ldg = size == 4 ? p.ldz : spread(round_up(p.piece, slice), size);        // (in 32 bits the logits themselves become G)
         p.ldp = round_up(d, 4);
-        const int64_t slices = ceil_div(p.piece, slice);
+        const int64_t slices = ceil_div(p.piece, slice) * planes;
         p.config_dx = mm_choose(size, d, p.piece_rows, slices >= 512);
         const int64_t tiles = ceil_div(d, mm_tile_i(p.config_dx)) * ceil_div(p.piece_rows, mm_tile_j(p.config_dx));
         const int64_t room = CUS * (p.config_dx == WIDE ? 1 : 2);
@@ -333,7 +335,7 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         p.splits = (int)ceil_div(slices, ceil_div(slices, splits));
         p.config_dw = mm_choose(size, d, p.piece);
         if (p.kept) p.logits = c.take<float>(p.rows_g * p.ldz * p.loss_splits);
-        p.g = size == 4 ? (void *)p.logits : c.take<char>(p.rows_g * p.ldg * size);
+        p.g = size == 4 ? (void *)p.logits : c.take<char>(planes * p.rows_g * p.ldg * size);
         p.parts = c.take<float>(p.piece_rows * p.ldp * p.splits * (p.kept ? 1 : p.pieces));
         if (p.config_dw == WIDE) p.rest_parts = c.take<float>((int64_t)CUS * 256 * 256);     // (splits of the last tiles of dw, a round of them)
     }
@@ -379,11 +381,13 @@ int run_sum_parts(const float *parts, int64_t ld, int64_t copy, int copies, T *o
 }
 
 template <typename T>
-MmShape mm_shape(const MmOperand &a, const MmOperand &b, int64_t k, int config, int splits)
+MmShape mm_shape(const MmOperand &a, const MmOperand &b, int64_t k, int config, int splits, int planes = 1, int64_t plane = 0)
 {
     MmShape s;
     s.a = a; s.b = b;
-    s.slices = (int)ceil_div(k, MM_K<T>);
+    s.planes = planes;
+    s.plane = plane;
+    s.slices = (int)ceil_div(k, MM_K<T>) * planes;
     s.tiles_i = (int)ceil_div(a.rows, mm_tile_i(config));
     s.tiles_j = (int)ceil_div(b.rows, mm_tile_j(config));
     s.per_split = (int)ceil_div(s.slices, splits);
@@ -458,12 +462,13 @@ template <typename T>
 int run_loss_products(const LossPlan &p, int64_t row0, int64_t rows, const T *w, int64_t ldw, int64_t class0, int64_t classes, int64_t ldg, T *dw,
                       int64_t lddw, const float *inverse, bool add, int &copies, hipStream_t stream)
 {
-    const int64_t rows_g = round_up(rows, MM_K<T>);
+    constexpr int planes = planes_of_g(sizeof(T));
+    const int64_t rows_g = round_up(rows, MM_K<T>), plane = p.rows_g * ldg;
     const MmOperand x_by_k = {(const T *)p.x + row0 * p.ldk, p.ldk, (int)p.d, (int)rows_g}, w_by_k = {w + class0 * ldw, ldw, (int)p.d, (int)classes};
     const MmOperand g_rows = {p.g, ldg, (int)rows, 0};
     TRY(with_config<T, MmWideByK>(p.config_dx, [&](auto c) {
         typedef decltype(c) C;
-        const MmShape s = mm_shape<T>(w_by_k, g_rows, classes, p.config_dx, p.splits);
+        const MmShape s = mm_shape<T>(w_by_k, g_rows, classes, p.config_dx, p.splits, planes, plane);
         auto kernel = product_parts<T, C, true, false>;
         TRY(allow_lds(kernel, C::LDS));
         kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.parts + (int64_t)copies * p.piece_rows * p.ldp, p.ldp, p.piece_rows * p.ldp);
@@ -471,11 +476,11 @@ int run_loss_products(const LossPlan &p, int64_t row0, int64_t rows, const T *w,
         return launched("product_parts");
     }));
     // dw: the last classes' tiles, where a few of them would keep the chip for another round, go by splits of the sum
-    const int64_t rest = dw_rest(p.config_dw, p.d, classes, rows_g / MM_K<T>), most = classes - rest;
+    const int64_t rest = dw_rest(p.config_dw, p.d, classes, rows_g / MM_K<T> * planes), most = classes - rest;
     const MmOperand g_most = {p.g, ldg, (int)most, (int)rows_g}, g_rest = {(const T *)p.g + most, ldg, (int)rest, (int)rows_g};
     TRY(with_config<T, MmWideByK>(p.config_dw, [&](auto c) {
         typedef decltype(c) C;
-        const MmShape s = mm_shape<T>(x_by_k, g_most, rows_g, p.config_dw, 1);
+        const MmShape s = mm_shape<T>(x_by_k, g_most, rows_g, p.config_dw, 1, planes, plane);
         auto kernel = product_out<T, C, false>;
         if constexpr (sizeof(T) == 4)                    // (pieces of the rows)
             if (add) kernel = product_out<T, C, true>;
@@ -486,7 +491,7 @@ int run_loss_products(const LossPlan &p, int64_t row0, int64_t rows, const T *w,
     if (rest == 0) return CHICLE_OK;
     if constexpr (sizeof(T) == 2) {
         typedef MmWideByK C;
-        const MmShape s = mm_shape<T>(x_by_k, g_rest, rows_g, WIDE, (int)(CUS / (ceil_div(p.d, 256) * ceil_div(rest, 256))));
+        const MmShape s = mm_shape<T>(x_by_k, g_rest, rows_g, WIDE, (int)(CUS / (ceil_div(p.d, 256) * ceil_div(rest, 256))), planes, plane);
         auto kernel = product_parts<T, C, true, true>;
         TRY(allow_lds(kernel, C::LDS));
         kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.rest_parts, p.ldp, rest * p.ldp);
@@ -521,8 +526,8 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
         return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, p.few_grad_blocks, dx, lddx, p.n, p.d, nullptr, stream);
     }
     const float *inverse = nullptr;
-    if (sizeof(T) == 2) {
-        loss_power<<<1, 1024, 0, stream>>>(rows.weight, (int)p.n, std::is_same<T, f16>::value ? 16384.f : 1.f, p.power);
+    if (std::is_same<T, f16>::value) {
+        loss_power<<<1, 1024, 0, stream>>>(rows.weight, (int)p.n, 16384.f, p.power);
         TRY(launched("loss_power"));
         rows.power = p.power;
         inverse = p.power + 1;
@@ -534,7 +539,7 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
             const int64_t many = p.n - first < p.piece_rows ? p.n - first : p.piece_rows;
             TRY(run_loss<T>(p, x, ldx, w, ldw, rows, first, many, p.logits, loss, p.lse, flags, stream));
             const dim3 grid((unsigned)round_up(many, MM_K<T>), (unsigned)grid_of(p.ldg, 1024, 64));
-            loss_grad_kept<T><<<grid, 256, 0, stream>>>(p.logits, p.ldz, rows_from(rows, first, many), (T *)p.g, p.ldg);
+            loss_grad_kept<T><<<grid, 256, 0, stream>>>(p.logits, p.ldz, rows_from(rows, first, many), (T *)p.g, p.ldg, p.rows_g * p.ldg);
             TRY(launched("loss_grad_kept"));
             int copies = 0;
             TRY(run_loss_products<T>(p, first, many, w_in, ldw_in, 0, p.classes, p.ldg, dw, lddw, inverse, first > 0, copies, stream));
@@ -554,7 +559,7 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
                 const MmShape s = mm_shape<T>(w_rows, x_rows, p.d, config, 1);
                 auto kernel = loss_grad_tiles<T, C>;
                 TRY(allow_lds(kernel, C::LDS));
-                kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, (int)first, (int)many, (T *)p.g, ldg, (int)p.rows_g);
+                kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, (int)first, (int)many, (T *)p.g, ldg, p.rows_g * ldg, (int)p.rows_g);
                 return launched("loss_grad_tiles");
             }));
             TRY(run_loss_products<T>(p, 0, p.n, w_in, ldw_in, first, many, ldg, dw, lddw, inverse, false, copies, stream));

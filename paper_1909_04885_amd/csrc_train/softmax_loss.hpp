@@ -7,16 +7,18 @@
 // The loss: logits exist only as tiles of a product in registers.  `loss_tiles` leaves of a wavefront's part of a tile, for every row, the
 // largest logit and the sum of exponentials below it, and `loss_rows` joins these.
 //
-// The gradient in 16 bits forms the logits again, a piece of the classes at a time, and turns them in registers into G, which is stored in
-// 16 bits for the two products that read it; rounding G is of the size of the rounding of the gradients themselves, and of no
-// direction: G comes divided by the largest weight, and the products times it, so that a weight that all rows share, which would be
-// rounded to the same side everywhere, is not rounded at all.  Half precision would lose small G: there it comes 2^14 times as large.  In 32 bits a
+// The gradient in 16 bits forms the logits again, a piece of the classes at a time, and turns them in registers into G, which is stored for
+// the two products that read it.  Rows of G add up to zero, so what all classes (or those that a row's softmax lies on) have in
+// common drops out of dx; 8 or 11 bits of G do not add up to zero, and leave that common part times their errors: with classes around a common mean
+// the relative error of dx was 0.033 in bfloat16, where the rounding of dx itself is 0.0017.  G is held in two planes that add up to it,
+// the second what the first's rounding leaves, 16 bits or 22 together, and each goes through the products.  Half precision would
+// lose small G: there it comes 2^14 times as large, divided by the largest weight, and the products times it.  In 32 bits a
 // product costs eight times as much, and the logits of a piece of the rows are kept until they are G; so are those of few rows and of
 // few classes, which are few bytes.
 //
-// The bound is the matrix cores: 2 n d classes operations for the loss, and twice that again for the gradients (three times in 16 bits).
-// With gradients, 8192 rows of 2048 and 128,000 classes in bfloat16: 14.9 ms, 1150 TFLOP/s of the four products; 4096 rows of 1024 and
-// 50,021 classes: 1.65 ms, 1020; 333 rows of 250 and 20,000 classes in 32 bits: 160 us, 62 TFLOP/s of 154, three products of 8 to 11
+// The bound is the matrix cores: 2 n d classes operations for the loss, and twice that again for the gradients (five times in 16 bits).
+// With gradients, 8192 rows of 2048 and 128,000 classes in bfloat16: 22.7 ms, 1135 TFLOP/s of the six products; 4096 rows of 1024 and
+// 50,021 classes: 2.46 ms, 1020; 333 rows of 250 and 20,000 classes in 32 bits: 160 us, 62 TFLOP/s of 154, three products of 8 to 11
 // slices each, most of whose time is their beginning and end.  Few rows are bound by reading w: one row against 32,000 classes of
 // 1024 in bfloat16 16 us, 13.5 of them the product at 4.8 TB/s.
 #pragma once
@@ -51,7 +53,7 @@ struct LossRows {
     int wide, n, classes;
     const float *lse;            // gradient
     const float *weight;
-    const float *power;          // 16 bits: G comes times this; else null
+    const float *power;          // half precision: G comes times this; else null
     float2 *part;                // [row][wavefront's part of a tile of classes]: largest logit, sum of exponentials below it
     float *picked;               // [row]: the label's logit
 };
@@ -218,11 +220,19 @@ __global__ __launch_bounds__(1024) void loss_power(const float *__restrict__ wei
 
 // ---- the gradients --------------------------------------------------------------------------------------------------
 
+// The two planes of x: what is rounded, and what that leaves (nothing of an infinity).
+template <typename T> __device__ __forceinline__ void two_planes(float x, T &high, T &low)
+{
+    high = (T)x;
+    const float rest = x - (float)high;
+    low = (T)(__builtin_isinf(x) || __builtin_isinf((float)high) ? 0.f : rest);
+}
+
 // G of a piece of the classes, 16 bits: s.a is the piece's rows of w, `first` the piece's first class.  g[row][class of the piece], with
-// zeros up to ldg and in rows [n, rows_out).
+// zeros up to ldg and in rows [n, rows_out), the second plane `plane` values further on.
 template <typename T, typename C>
 __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_grad_tiles(MmShape s, LossRows l, int first, int piece, T *__restrict__ g, int64_t ldg,
-                                                                           int rows_out)
+                                                                           int64_t plane, int rows_out)
 {
     const float power = l.power ? l.power[0] : 1.f;
     mm_tiles<T, C, false, false>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
@@ -234,30 +244,33 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void loss_grad_tiles(MmSha
             T *row = g + (int64_t)j * ldg;
 #pragma unroll
             for (int mp = 0; mp < C::MI / 2; ++mp) {     // eight neighbouring classes
-                T v[8];
+                T v[8], low[8];
                 const int i = at.i0 + mp * 32;
 #pragma unroll
                 for (int h = 0; h < 8; ++h) {
                     float p = exp_of<false>(acc[2 * mp + h / 4][nj][h % 4], lse);
                     if (rel == mp * 32 + h) p -= 1.f;
-                    v[h] = (T)(weight != 0.f && i + h < piece ? p * weight : 0.f);
+                    two_planes(weight != 0.f && i + h < piece ? p * weight : 0.f, v[h], low[h]);
                 }
-                if (j < rows_out && i < ldg) __builtin_memcpy(row + i, v, 16);
+                if (j < rows_out && i < ldg) {
+                    __builtin_memcpy(row + i, v, 16);
+                    __builtin_memcpy(row + plane + i, low, 16);
+                }
             }
         }
     });
 }
 
-// G of logits that were kept: g[row][class] of all classes, zeros up to ldg and in rows [n, rows_out).  g may be the logits themselves.
-// Grid: (rows, columns).
+// G of logits that were kept: g[row][class] of all classes, zeros up to ldg and in rows [n, rows_out).  In 32 bits g may be the logits
+// themselves; in 16 the second plane lies `plane` values further on.  Grid: (rows, columns).
 template <typename T>
-__global__ __launch_bounds__(256) void loss_grad_kept(const float *logits, int64_t ldz, LossRows l, T *g, int64_t ldg)
+__global__ __launch_bounds__(256) void loss_grad_kept(const float *logits, int64_t ldz, LossRows l, T *g, int64_t ldg, int64_t plane)
 {
     const int j = blockIdx.x, label = label_at(l, j);
     const float power = l.power ? l.power[0] : 1.f;
     const float weight = label >= 0 ? l.weight[j] * power : 0.f, lse = label >= 0 ? l.lse[j] : 0.f;
     for (int64_t c = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4; c < ldg; c += (int64_t)gridDim.y * 1024) {
-        T v[4];
+        T v[4], low[4];
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
             float p = 0.f;
@@ -266,9 +279,11 @@ __global__ __launch_bounds__(256) void loss_grad_kept(const float *logits, int64
                 if (c + h == label) p -= 1.f;
                 p *= weight;
             }
-            v[h] = (T)p;
+            if constexpr (sizeof(T) == 4) v[h] = p;
+            else two_planes(p, v[h], low[h]);
         }
         __builtin_memcpy(g + j * ldg + c, v, sizeof v);
+        if constexpr (sizeof(T) == 2) __builtin_memcpy(g + plane + j * ldg + c, low, sizeof low);
     }
 }
 
