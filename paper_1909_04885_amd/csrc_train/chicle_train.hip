@@ -527,7 +527,7 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
     }
     const float *inverse = nullptr;
     if (std::is_same<T, f16>::value) {
-        loss_power<<<1, 1024, 0, stream>>>(rows.weight, (int)p.n, 16384.f, p.power);
+        loss_power<<<1, 1024, 0, stream>>>(rows, 16384.f, p.power);
         TRY(launched("loss_power"));
         rows.power = p.power;
         inverse = p.power + 1;

@@ -199,21 +199,21 @@ __global__ __launch_bounds__(256) void loss_join(LossRows l, float *parts, int64
     loss[j] = label >= 0 ? lse - picked : 0.f;
 }
 
-// power[0]: what takes the largest weight to `top`, power[1] its inverse.  One workgroup.
-__global__ __launch_bounds__(1024) void loss_power(const float *__restrict__ weight, int n, float top, float *power)
+// power[0]: what takes the largest weight of a row with a label to `top`, power[1] its inverse.  One workgroup.
+__global__ __launch_bounds__(1024) void loss_power(LossRows l, float top, float *power)
 {
     __shared__ float s[16];
     float m = 0.f;
-    for (int i = threadIdx.x; i < n; i += 1024) {
-        const float w = fabsf(weight[i]);
-        if (w <= 3.4e38f) m = fmaxf(m, w);               // (no infinities or NaN)
+    for (int i = threadIdx.x; i < l.n; i += 1024) {
+        const float w = label_at(l, i) >= 0 ? fabsf(l.weight[i]) : 0.f;
+        if (!__builtin_isinf(w)) m = fmaxf(m, w);        // (NaN neither)
     }
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = m;
     __syncthreads();
     if (threadIdx.x) return;
     for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
-    const bool plain = m < 1e-30f || m > 1e30f;          // (no weight, or one whose inverse is out of range)
+    const bool plain = m < 1e-30f;                       // (no weight, or one whose inverse is out of range)
     power[0] = plain ? 1.f : top / m;
     power[1] = plain ? 1.f : m / top;
 }
