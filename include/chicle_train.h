@@ -40,7 +40,9 @@ enum chicle_type { CHICLE_F32 = 0, CHICLE_BF16 = 1, CHICLE_F16 = 2 };
 /* Softmax cross entropy of rows x (n x d) against classes w (classes x d):
  *   lse_i = log sum_v exp(x_i . w_v),  loss_i = lse_i - x_i . w_label(i),  0 for a row without a label.
  * The logits are not kept (softmax_loss_grad keeps those of a piece of the rows in 32 bits, at most 1 GB or 256 rows of them, and in 16
- * bits those of up to 64 rows or of less than 192 tiles of 256 x 256).  n may be 0.  Limits: n, d and classes below 2^22, 2^21 and 2^23, and n * classes below 2^42.
+ * bits those of up to 64 rows or of less than 192 tiles of 256 x 256; else in 16 bits its workspace is x laid out, dx in 32 bits and their
+ * derivatives for a piece of the classes, 1 GB or 4 bytes for every row and min(8 d, 2^24 / d) classes, and w, if its rows are no whole
+ * slices of 128 bytes).  n may be 0.  Limits: n, d and classes below 2^22, 2^21 and 2^23, and n * classes below 2^42.
  * Errors: EINVAL (arguments), ENOMEM (workspace), EDEVICE. */
 size_t chicle_softmax_loss_bytes(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t n, int64_t d, int64_t classes, int32_t type,
                                  int32_t with_grad);

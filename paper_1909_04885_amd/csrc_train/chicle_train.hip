@@ -209,8 +209,8 @@ struct LossPlan {
     size_t bytes;
 };
 
-// 8192 rows of 2048 and 128,000 classes in 16 bits with a quarter of it: 15.2 ms, this 15.4, four times as much 15.6; but every piece has its parts of dx.
-constexpr int64_t LOSS_PIECE_BYTES = (int64_t)1 << 30;   // both planes of G of a piece of the classes
+// 8192 rows of 2048 and 128,000 classes in 16 bits with a quarter of it: 15.2 ms, this 15.4, four times as much 15.6.
+constexpr int64_t LOSS_PIECE_BYTES = (int64_t)1 << 30;   // both planes of G of a piece of the classes, or more of long batches
 // 16,384 rows of 512 and 50,000 classes in 32 bits with a quarter of it: 24.1 ms, this 22.4, four times as much 22.3.
 constexpr int64_t LOSS_KEPT_BYTES = (int64_t)1 << 30;    // logits of a piece of the rows
 constexpr int64_t LOSS_MOST = (int64_t)1 << 22, LOSS_MOST_D = (int64_t)1 << 21, LOSS_MOST_CLASSES = (int64_t)1 << 23;
@@ -315,7 +315,11 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
             p.piece = classes;
             if (p.few || p.loss_splits > 1) p.pieces = 1;
         } else {
-            int64_t most = LOSS_PIECE_BYTES / (planes * size * p.rows_x) / 256 * 256;
+            // At least a round of dw's large tiles to a piece, or eight classes to a column, so that long batches do not come in small pieces: 65,536
+            // rows of 1024 and 128,000 classes 143 ms without (4096 classes to a piece), 105 with (8192), 131,072 rows of 1024 438 and 210, of 512
+            // (64,000 classes) 191 and 116, 65,536 rows of 2048 99 and 92.
+            const int64_t least = std::min<int64_t>(8 * d, CUS * 256 * 256 / d);
+            int64_t most = std::max(LOSS_PIECE_BYTES / (planes * size * p.rows_x), least) / 256 * 256;
             most = most < 256 ? 256 : most;
             p.pieces = (int)ceil_div(classes, most);
             p.piece = round_up(ceil_div(classes, p.pieces), 256);
@@ -336,7 +340,7 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         p.config_dw = mm_choose(size, d, p.piece);
         if (p.kept) p.logits = c.take<float>(p.rows_g * p.ldz * p.loss_splits);
         p.g = size == 4 ? (void *)p.logits : c.take<char>(planes * p.rows_g * p.ldg * size);
-        p.parts = c.take<float>(p.piece_rows * p.ldp * p.splits * (p.kept ? 1 : p.pieces));
+        p.parts = c.take<float>(p.piece_rows * p.ldp * p.splits);
         if (p.config_dw == WIDE) p.rest_parts = c.take<float>((int64_t)CUS * 256 * 256);     // (splits of the last tiles of dw, a round of them)
     }
     p.bytes = c.total();
@@ -457,7 +461,8 @@ int run_loss(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_t ldw
     return launched("loss_rows");
 }
 
-// dx and dw of G of rows [row0, row0 + rows) and classes [class0, class0 + classes); `copies` parts of dx are there already
+// dx and dw of G of rows [row0, row0 + rows) and classes [class0, class0 + classes), dx in `copies` parts.  A piece that is not the first adds
+// what all pieces share: in 32 bits, pieces of the rows, dw, in 16 bits, pieces of the classes, the parts of dx.
 template <typename T>
 int run_loss_products(const LossPlan &p, int64_t row0, int64_t rows, const T *w, int64_t ldw, int64_t class0, int64_t classes, int64_t ldg, T *dw,
                       int64_t lddw, const float *inverse, bool add, int &copies, hipStream_t stream)
@@ -470,9 +475,11 @@ int run_loss_products(const LossPlan &p, int64_t row0, int64_t rows, const T *w,
         typedef decltype(c) C;
         const MmShape s = mm_shape<T>(w_by_k, g_rows, classes, p.config_dx, p.splits, planes, plane);
         auto kernel = product_parts<T, C, true, false>;
+        if constexpr (sizeof(T) == 2)
+            if (add) kernel = product_parts<T, C, true, false, true>;
         TRY(allow_lds(kernel, C::LDS));
-        kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.parts + (int64_t)copies * p.piece_rows * p.ldp, p.ldp, p.piece_rows * p.ldp);
-        copies += s.splits;
+        kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, p.parts, p.ldp, p.piece_rows * p.ldp);
+        if (copies < s.splits) copies = s.splits;        // (the first piece's: no later one has more classes)
         return launched("product_parts");
     }));
     // dw: the last classes' tiles, where a few of them would keep the chip for another round, go by splits of the sum
@@ -482,7 +489,7 @@ int run_loss_products(const LossPlan &p, int64_t row0, int64_t rows, const T *w,
         typedef decltype(c) C;
         const MmShape s = mm_shape<T>(x_by_k, g_most, rows_g, p.config_dw, 1, planes, plane);
         auto kernel = product_out<T, C, false>;
-        if constexpr (sizeof(T) == 4)                    // (pieces of the rows)
+        if constexpr (sizeof(T) == 4)
             if (add) kernel = product_out<T, C, true>;
         TRY(allow_lds(kernel, C::LDS));
         kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, dw + class0 * lddw, lddw, inverse);
@@ -549,7 +556,7 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
     }
     if constexpr (sizeof(T) == 2) {
         TRY(run_loss<T>(p, x, ldx, w, ldw, rows, 0, p.n, nullptr, loss, p.lse, flags, stream));
-        int copies = 0;                                  // of dx, to be added up
+        int copies = 0;
         for (int64_t first = 0; first < p.classes; first += p.piece) {
             const int64_t many = p.classes - first < p.piece ? p.classes - first : p.piece, ldg = spread(round_up(many, MM_K<T>), 2);
             const MmOperand w_rows = {w_in + first * ldw_in, ldw_in, (int)many, 0}, x_rows = {p.x, p.ldk, (int)p.n, 0};
@@ -562,7 +569,7 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
                 kernel<<<mm_grid<C>(s), C::THREADS, C::LDS, stream>>>(s, rows, (int)first, (int)many, (T *)p.g, ldg, p.rows_g * ldg, (int)p.rows_g);
                 return launched("loss_grad_tiles");
             }));
-            TRY(run_loss_products<T>(p, 0, p.n, w_in, ldw_in, first, many, ldg, dw, lddw, inverse, false, copies, stream));
+            TRY(run_loss_products<T>(p, 0, p.n, w_in, ldw_in, first, many, ldg, dw, lddw, inverse, first > 0, copies, stream));
         }
         return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, copies, dx, lddx, p.n, p.d, inverse, stream);
     }

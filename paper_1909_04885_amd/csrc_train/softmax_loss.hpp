@@ -287,8 +287,8 @@ __global__ __launch_bounds__(256) void loss_grad_kept(const float *logits, int64
     }
 }
 
-// A product as it is: out[j][i] in 32 bits, split `split` of the sum in its own copy of `out`.
-template <typename T, typename C, bool A_BY_K, bool B_BY_K>
+// A product as it is: out[j][i] in 32 bits, split `split` of the sum in its own copy of `out`; or added to what is there.
+template <typename T, typename C, bool A_BY_K, bool B_BY_K, bool ADD = false>
 __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_parts(MmShape s, float *__restrict__ out, int64_t ld, int64_t copy)
 {
     mm_tiles<T, C, A_BY_K, B_BY_K>(s, [&](const MmTile &t, f32x4 (&acc)[C::MI][C::NJ]) __attribute__((always_inline)) {
@@ -299,7 +299,10 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_parts(MmShape
 #pragma unroll
             for (int mi = 0; mi < C::MI; ++mi) {
                 const int i = at.i0 + at.place(mi), j = at.j0 + nj * 16;
-                if (j < s.b.rows && i < s.a.rows) *(f32x4 *)(mine + (int64_t)j * ld + i) = acc[mi][nj];
+                if (j >= s.b.rows || i >= s.a.rows) continue;
+                f32x4 *dst = (f32x4 *)(mine + (int64_t)j * ld + i);
+                if constexpr (ADD) *dst += acc[mi][nj];
+                else *dst = acc[mi][nj];
             }
     });
 }

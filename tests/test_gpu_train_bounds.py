@@ -102,3 +102,14 @@ def test_the_weight_of_a_row_without_a_label_counts_nowhere(ops, dtype, n, value
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     with pytest.raises(chicle.ChicleError, match="label"):
         ops.sync()
+
+
+@pytest.mark.parametrize("n, d, classes", [(50000, 72, 12000), (20000, 16, 30000), (16384, 200, 32700)])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=NAME.get)
+def test_pieces_of_the_classes_share_the_rows_gradient(ops, dtype, n, d, classes):
+    """Several pieces, each added to what the ones before left: in large tiles, in middle tiles whose sums are divided, in large ones that are."""
+    print("\ncase pieces", NAME[dtype], n, d, classes, flush=True)
+    g = gen(n)
+    x, w = normal(g, n, d, dtype), normal(g, classes, d, dtype, 1.0 / math.sqrt(d))
+    labels = torch.randint(-1, classes, (n,), generator=g, device="cuda", dtype=torch.int32)
+    check_gradients(ops, x, w, labels, torch.rand(n, generator=g, device="cuda"))

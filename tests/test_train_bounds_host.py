@@ -1,0 +1,20 @@
+"""CPU-side checks of what the training operators ask for: memory in proportion to the data."""
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_1909_04885_amd as m
+    return m.load_train_library()
+
+
+@pytest.mark.parametrize("kind", [1, 2])
+@pytest.mark.parametrize("d", [250, 1024, 4096])
+def test_workspace_of_the_losss_gradient_grows_with_the_rows_and_not_faster(lib, kind, d):
+    classes, rows = 128000, [32768, 65536, 131072, 262144, 1 << 20]
+    size = [lib.chicle_softmax_loss_bytes(4096, d, 4096, d, n, d, classes, kind, 1) for n in rows]
+    for n, s in zip(rows, size):
+        # x and w laid out, dx in 32 bits, two planes of a gigabyte or of min(8 d, 2^24 / d) classes, a maximum and a sum of every row and half a tile of 256 classes
+        wide = (d + 127) // 64 * 64
+        assert s <= 2 * (n + classes) * wide + 4 * n * wide + max(4 * n * min(8 * d, (1 << 24) // d), 1 << 30) + n * (classes // 256) * 2 * 8 + (1 << 28), n
+        assert s < 2 * n * classes                       # less than the logits would take
