@@ -113,3 +113,20 @@ def test_pieces_of_the_classes_share_the_rows_gradient(ops, dtype, n, d, classes
     x, w = normal(g, n, d, dtype), normal(g, classes, d, dtype, 1.0 / math.sqrt(d))
     labels = torch.randint(-1, classes, (n,), generator=g, device="cuda", dtype=torch.int32)
     check_gradients(ops, x, w, labels, torch.rand(n, generator=g, device="cuda"))
+
+
+@pytest.mark.parametrize("n, d, classes, extra", [(4100, 1030, 33001, 3), (4096, 1024, 33000, 0)])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=NAME.get)
+def test_large_tiles_of_long_sums(ops, dtype, n, d, classes, extra):
+    """Tiles of 256 x 256 in every product, sixteen slices of k and more, dx's sum divided; once with remainders on all sides, once with w read as
+    it lies."""
+    print("\ncase large tiles", NAME[dtype], n, d, classes, flush=True)
+    g = gen(classes)
+    x, w = normal(g, n, d, dtype, 1.0, extra), normal(g, classes, d, dtype, 1.0 / math.sqrt(d), extra)
+    labels = torch.randint(-1, classes, (n,), generator=g, device="cuda")
+    labels[-40:] = torch.arange(classes - 40, classes, device="cuda")
+    first = check_gradients(ops, x, w, labels, torch.rand(n, generator=g, device="cuda"))
+    del first
+    weight = torch.full((n,), 1.0, device="cuda")
+    a, b = ops.softmax_loss_grad(x, w, labels, weight), ops.softmax_loss_grad(x, w, labels, weight)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))   # whatever the timing
