@@ -51,7 +51,8 @@ int chicle_softmax_loss(const void *x, int64_t ldx, const void *w, int64_t ldw, 
                         void *hip_stream);
 
 /* The same with the gradients of sum_i row_weight_i loss_i: dx (n x d) and dw (classes x d).  A row without a label counts nowhere,
- * whatever x and row_weight hold there, and its dx is 0.  row_weight: n floats. */
+ * whatever x and row_weight hold there, and its dx is 0.  row_weight: n floats.  In half precision the derivatives by the logits have one scale
+ * for all rows: each is off by up to 2^-39 of the largest weight of a row with a label, which a row shows whose weight is less than some 2^-20 of it. */
 int chicle_softmax_loss_grad(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *labels, int32_t wide, const float *row_weight,
                              int64_t n, int64_t d, int64_t classes, int32_t type, float *loss, void *dx, int64_t lddx, void *dw, int64_t lddw,
                              void *workspace, size_t workspace_bytes, int32_t *flags, void *hip_stream);

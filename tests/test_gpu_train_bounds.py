@@ -130,3 +130,27 @@ def test_large_tiles_of_long_sums(ops, dtype, n, d, classes, extra):
     weight = torch.full((n,), 1.0, device="cuda")
     a, b = ops.softmax_loss_grad(x, w, labels, weight), ops.softmax_loss_grad(x, w, labels, weight)
     assert all(torch.equal(s, t) for s, t in zip(a, b))   # whatever the timing
+
+
+@pytest.mark.parametrize("n", [3, 200, 5000])
+@pytest.mark.parametrize("scale", [2.0 ** -6, 1.0, 4096.0])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=NAME.get)
+def test_weights_of_many_powers_of_two_in_one_call(ops, dtype, scale, n):
+    """Every row of dx against its own weight, down to 2^-18 of the largest."""
+    g = gen(n + 1)
+    x, w = normal(g, n, 64, dtype), normal(g, 3100, 64, dtype, 0.2)
+    labels = torch.randint(0, 3100, (n,), generator=g, device="cuda", dtype=torch.int32)
+    weight = scale * (1 + torch.rand(n, generator=g, device="cuda")) * 2.0 ** -torch.randint(0, 18, (n,), generator=g, device="cuda").float()
+    check_gradients(ops, x, w, labels, weight)
+
+
+@pytest.mark.parametrize("n, d, classes, extra, shift", [
+    (1, 64, 1, 0, 0), (1, 200, 1000, 0, 0), (3, 65, 257, 1, 0), (17, 100, 700, 3, 5), (24, 1030, 900, 2, 0), (65, 192, 1000, 8, 0), (100, 250, 2000, 6, 0),
+    (128, 512, 1024, 0, 0), (129, 320, 777, 0, 3), (300, 2050, 700, 0, 0), (600, 130, 3001, 0, 0), (2500, 64, 500, 0, 0)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=NAME.get)
+def test_gradients_of_all_sizes(ops, dtype, n, d, classes, extra, shift):
+    print("\ncase all sizes", NAME[dtype], n, d, classes, extra, shift, flush=True)
+    g = gen(n * d + classes)
+    x, w = normal(g, n, d, dtype, 1.0, extra, shift), normal(g, classes, d, dtype, 2.0 / math.sqrt(d), extra, shift)
+    labels = torch.randint(-1 if n > 1 else 0, classes, (n,), generator=g, device="cuda")
+    check_gradients(ops, x, w, labels, torch.rand(n, generator=g, device="cuda"))
