@@ -376,11 +376,12 @@ int loss_lay_rows(const T *in, int64_t ldi, void *out, int64_t ld, int64_t rows,
 }
 
 template <typename T>
-int run_sum_parts(const float *parts, int64_t ld, int64_t copy, int copies, T *out, int64_t ldo, int64_t rows, int64_t cols, const float *scale, hipStream_t stream)
+int run_sum_parts(const float *parts, int64_t ld, int64_t copy, int copies, T *out, int64_t ldo, int64_t rows, int64_t cols, const float *scale, hipStream_t stream,
+                  const LossRows &labels = LossRows())
 {
     // (several threads to a place where there are many copies to add up: 82 copies of 333 x 252 in 7 instead of 24 us)
-    if (copies >= 16) sum_parts<T, 8><<<(unsigned)grid_of(rows * (ld / 4), 32, 32768), 256, 0, stream>>>(parts, ld, copy, copies, out, ldo, rows, cols, scale);
-    else sum_parts<T, 1><<<(unsigned)grid_of(rows * (ld / 4), 256, 32768), 256, 0, stream>>>(parts, ld, copy, copies, out, ldo, rows, cols, scale);
+    if (copies >= 16) sum_parts<T, 8><<<(unsigned)grid_of(rows * (ld / 4), 32, 32768), 256, 0, stream>>>(parts, ld, copy, copies, out, ldo, rows, cols, scale, labels);
+    else sum_parts<T, 1><<<(unsigned)grid_of(rows * (ld / 4), 256, 32768), 256, 0, stream>>>(parts, ld, copy, copies, out, ldo, rows, cols, scale, labels);
     return launched("sum_parts");
 }
 
@@ -530,7 +531,7 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
             if (p.n > 4) kernel = loss_grad_few<T, 8>;
         kernel<<<grid, 256, 0, stream>>>(x, ldx, w, ldw, p.d, rows, p.few_each, p.logits, p.ldz, dw, lddw, p.parts, p.ldp);
         TRY(launched("loss_grad_few"));
-        return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, p.few_grad_blocks, dx, lddx, p.n, p.d, nullptr, stream);
+        return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, p.few_grad_blocks, dx, lddx, p.n, p.d, nullptr, stream, rows);
     }
     const float *inverse = nullptr;
     if (std::is_same<T, f16>::value) {
@@ -550,7 +551,8 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
             TRY(launched("loss_grad_kept"));
             int copies = 0;
             TRY(run_loss_products<T>(p, first, many, w_in, ldw_in, 0, p.classes, p.ldg, dw, lddw, inverse, first > 0, copies, stream));
-            TRY(run_sum_parts<T>(p.parts, p.ldp, p.piece_rows * p.ldp, copies, dx + first * lddx, lddx, many, p.d, inverse, stream));
+            TRY(run_sum_parts<T>(p.parts, p.ldp, p.piece_rows * p.ldp, copies, dx + first * lddx, lddx, many, p.d, inverse, stream,
+                                   rows_from(rows, first, many)));
         }
         return CHICLE_OK;
     }
@@ -571,7 +573,7 @@ int run_loss_grad(const LossPlan &p, const T *x, int64_t ldx, const T *w, int64_
             }));
             TRY(run_loss_products<T>(p, 0, p.n, w_in, ldw_in, first, many, ldg, dw, lddw, inverse, first > 0, copies, stream));
         }
-        return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, copies, dx, lddx, p.n, p.d, inverse, stream);
+        return run_sum_parts<T>(p.parts, p.ldp, p.n * p.ldp, copies, dx, lddx, p.n, p.d, inverse, stream, rows);
     }
     return CHICLE_OK;
 }

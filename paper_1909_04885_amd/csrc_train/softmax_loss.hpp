@@ -337,11 +337,11 @@ __global__ __launch_bounds__(C::THREADS, C::PER_SIMD) void product_out(MmShape s
     });
 }
 
-// dx = scale * the sum of the copies, in their order: SLICES threads to four columns, each of which adds up a run of the copies.  ld of a copy
-// is a multiple of four.
+// out = scale * the sum of the copies, in their order: SLICES threads to four columns, each of which adds up a run of the copies.  ld of a copy
+// is a multiple of four.  l.labels: null, or the rows are those of x, and one without a label is zero, whatever w holds.
 template <typename O, int SLICES>
 __global__ __launch_bounds__(256) void sum_parts(const float *__restrict__ part, int64_t ld, int64_t copy, int copies, O *__restrict__ out, int64_t ldo,
-                                                 int64_t rows, int64_t cols, const float *__restrict__ scale)
+                                                 int64_t rows, int64_t cols, const float *__restrict__ scale, LossRows l)
 {
     constexpr int EACH = 256 / SLICES;
     __shared__ f32x4 s[SLICES][EACH];
@@ -362,6 +362,7 @@ __global__ __launch_bounds__(256) void sum_parts(const float *__restrict__ part,
             for (int q = 1; q < SLICES; ++q) t += slice == 0 ? s[q][mine] : f32x4{0.f, 0.f, 0.f, 0.f};
         }
         if (slice || e0 + mine >= all) continue;
+        if (l.labels && label_at(l, (int)r) < 0) t = f32x4{0.f, 0.f, 0.f, 0.f};
         O v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = (O)(t[i] * f);

@@ -154,3 +154,17 @@ def test_gradients_of_all_sizes(ops, dtype, n, d, classes, extra, shift):
     x, w = normal(g, n, d, dtype, 1.0, extra, shift), normal(g, classes, d, dtype, 2.0 / math.sqrt(d), extra, shift)
     labels = torch.randint(-1 if n > 1 else 0, classes, (n,), generator=g, device="cuda")
     check_gradients(ops, x, w, labels, torch.rand(n, generator=g, device="cuda"))
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("n", [3, 40, 300, 4100])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=NAME.get)
+def test_the_gradient_of_a_row_without_a_label_is_zero_whatever_the_classes_hold(ops, dtype, n, value):
+    g = gen(n)
+    x, w = normal(g, n, 64, dtype), normal(g, 3100, 64, dtype)
+    w[7, 3] = value
+    labels = torch.randint(0, 3100, (n,), generator=g, device="cuda", dtype=torch.int32)
+    labels[n // 2] = -5
+    loss, dx, _ = ops.softmax_loss_grad(x, w, labels, torch.ones(n, device="cuda"))
+    assert not dx[n // 2].any() and float(loss[n // 2]) == 0.0
+    assert torch.isnan(dx[0]).any()                      # (that of the others is hidden nowhere)
