@@ -85,6 +85,9 @@ size_t chicle_clip_grads_bytes(int32_t count);
 int chicle_clip_grads(const void *const *in, void *const *out, const int64_t *sizes, const int32_t *types, int32_t count, float max_norm,
                       float *norm, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* *out = *flags, and *flags = 0, in one step beside what other streams' work reports: no report is lost, none is taken twice. */
+int chicle_train_take_flags(int32_t *flags, int32_t *out, void *hip_stream);
+
 /* Message for the last failure on the calling thread (host). */
 const char *chicle_train_last_error(void);
 

@@ -906,4 +906,11 @@ int chicle_clip_grads(const void *const *in, void *const *out, const int64_t *si
     return CHICLE_OK;
 }
 
+int chicle_train_take_flags(int32_t *flags, int32_t *out, void *hip_stream)
+{
+    if (!placed(flags, 4) || !placed(out, 4)) return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    take_flags<<<1, 1, 0, (hipStream_t)hip_stream>>>(flags, out);
+    return launched("take_flags");
+}
+
 }  // extern "C"

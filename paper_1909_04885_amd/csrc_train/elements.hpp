@@ -128,4 +128,6 @@ __device__ __forceinline__ int64_t index_at(const void *p, int wide, int64_t i)
 
 constexpr int FLAG_LABEL_RANGE = 1, FLAG_ID_RANGE = 2;
 
+__global__ void take_flags(int *flags, int *out) { *out = atomicExch(flags, 0); }
+
 }  // namespace chicle_train

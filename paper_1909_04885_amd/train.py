@@ -22,7 +22,8 @@ _lib = None
 TRAIN_EXPORTS = [
     "chicle_softmax_loss_bytes", "chicle_softmax_loss", "chicle_softmax_loss_grad", "chicle_embed",
     "chicle_embed_grad_bytes", "chicle_embed_grad", "chicle_layer_norm", "chicle_layer_norm_grad_bytes",
-    "chicle_layer_norm_grad", "chicle_clip_grads_bytes", "chicle_clip_grads", "chicle_train_last_error",
+    "chicle_layer_norm_grad", "chicle_clip_grads_bytes", "chicle_clip_grads", "chicle_train_take_flags",
+    "chicle_train_last_error",
 ]
 
 
@@ -53,6 +54,7 @@ def load_train_library():
         "chicle_layer_norm_grad": (i32, [vp, i64, vp, i64, vp, vp, vp, i64, i64, i32, vp, i64, vp, vp, vp, sz, vp]),
         "chicle_clip_grads_bytes": (sz, [i32]),
         "chicle_clip_grads": (i32, [vp, vp, vp, vp, i32, f32, vp, vp, sz, vp]),
+        "chicle_train_take_flags": (i32, [vp, vp, vp]),
         "chicle_train_last_error": (ctypes.c_char_p, []),
     }
     for name, (res, args) in sig.items():
@@ -69,7 +71,7 @@ def _at(a: array) -> int:
 
 
 class TrainOps:
-    """The operators on one GPU.  Holds the library, the device and one flag word; may be used on several streams."""
+    """The operators on one GPU.  Holds the library, the device and one flag word; may be used by several threads and on several streams."""
 
     def __init__(self, device: str = "cuda:0"):
         import torch
@@ -87,7 +89,9 @@ class TrainOps:
         self._wide = {torch.int32: 0, torch.int64: 1}
         # (the handle of the current stream, without an object around it)
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
-        self._flag_word = None
+        # in this word kernels note a label or token out of range; made here, so that any thread's first call, and a captured one, finds it
+        self._flag_word = torch.zeros(1, dtype=torch.int32, device=self.device)
+        torch.cuda.synchronize(self.device)             # it is zero before any stream's work looks at it
 
     # -- helpers
     def _call(self, fn, *args):
@@ -108,10 +112,6 @@ class TrainOps:
         return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
 
     def _flags(self):
-        """The address of the word in which kernels note a label or token out of range; made when it is first needed."""
-        if self._flag_word is None:
-            self._flag_word = self._torch.zeros(1, dtype=self._torch.int32, device=self.device)
-            self._torch.cuda.synchronize(self.device)   # it is zero before any stream's work looks at it
         return self._flag_word.data_ptr()
 
     def _matrix(self, a, name: str, type_of=None, cols: Optional[int] = None):
@@ -268,9 +268,10 @@ class TrainOps:
         return self._clip(grads, grads if out is None else out, max_norm)
 
     def sync(self):
-        """Wait for the current stream; raise if a label or token since the last sync was past the end."""
-        self._flags()
-        bits = int(self._flag_word.item())
+        """Wait for the current stream; raise if a label or token was past the end that no sync has raised yet.  What another stream
+        reports meanwhile is raised by this sync or by a later one."""
+        taken = self._empty(1, self._torch.int32)
+        self._call(self._L.chicle_train_take_flags, self._flags(), taken.data_ptr())
+        bits = int(taken.item())
         if bits:
-            self._flag_word.zero_()
             raise ChicleError(EDEVICE, "%s out of range" % " and ".join(s for b, s in ((1, "a label"), (2, "a token")) if bits & b))

@@ -1,0 +1,86 @@
+"""How the training operators are called: from several threads, on several streams, into graphs, beside automatic differentiation."""
+import threading
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture()
+def ops():
+    import paper_1909_04885_amd as chicle
+    return chicle.TrainOps("cuda:0")
+
+
+def test_the_first_calls_come_from_several_threads(ops):
+    """All of them report to one word, which lives as long as the kernels that look at it."""
+    import paper_1909_04885_amd as chicle
+    word = ops._flags()
+    table, ids = torch.randn(10, 24, device="cuda"), torch.arange(8, device="cuda", dtype=torch.int32)
+    past = torch.full((3,), 10, device="cuda", dtype=torch.int32)
+    seen, begin = [], threading.Barrier(8)
+
+    def work(k):
+        begin.wait()
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                ops.embed(table, ids)
+            if k == 5:
+                ops.embed(table, past)
+            seen.append(ops._flags())
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(8)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert set(seen) == {word} and len(seen) == 8
+    with pytest.raises(chicle.ChicleError, match="token"):
+        ops.sync()
+    ops.sync()
+
+
+def test_a_report_is_taken_by_one_sync_and_none_is_lost(ops):
+    """Syncs of several threads, each behind its own report: every report is raised once at least, and none is left."""
+    import paper_1909_04885_amd as chicle
+    table, past = torch.randn(10, 24, device="cuda"), torch.full((3,), 10, device="cuda", dtype=torch.int32)
+    x, w, label = torch.randn(3, 24, device="cuda"), torch.randn(5, 24, device="cuda"), torch.full((3,), 5, device="cuda", dtype=torch.int32)
+    raised = []
+
+    def work(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(50):
+                ops.embed(table, past) if k % 2 else ops.softmax_loss(x, w, label)
+                try:
+                    ops.sync()
+                except chicle.ChicleError as e:
+                    raised.append(str(e))
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    ops.sync()
+    assert any("token" in s for s in raised) and any("label" in s for s in raised)
+
+
+def test_the_first_call_may_be_captured(ops):
+    table, ids = torch.randn(50, 24, device="cuda"), torch.arange(20, device="cuda", dtype=torch.int32)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ops.embed(table, ids, 2.0)
+    for k in range(3):
+        ids.copy_(torch.randint(0, 50, (20,), device="cuda", dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, table[ids.long()] * 2.0), k
+    ids[4] = 50
+    graph.replay()
+    import paper_1909_04885_amd as chicle
+    with pytest.raises(chicle.ChicleError, match="token"):
+        ops.sync()

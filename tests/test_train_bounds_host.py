@@ -18,3 +18,10 @@ def test_workspace_of_the_losss_gradient_grows_with_the_rows_and_not_faster(lib,
         wide = (d + 127) // 64 * 64
         assert s <= 2 * (n + classes) * wide + 4 * n * wide + max(4 * n * min(8 * d, (1 << 24) // d), 1 << 30) + n * (classes // 256) * 2 * 8 + (1 << 28), n
         assert s < 2 * n * classes                       # less than the logits would take
+
+
+def test_refusals_of_taking_flags(lib):
+    import ctypes
+    p, odd = ctypes.c_void_p(4096), ctypes.c_void_p(4098)
+    for flags, out in ((None, p), (p, None), (odd, p), (p, odd)):
+        assert lib.chicle_train_take_flags(flags, out, None) == -1
