@@ -4,7 +4,8 @@ The method names are the C entry points without the `chicle_` prefix.  Everythin
 (PyTorch-ROCm supplies device memory and the stream); results are new tensors unless an output is given.
 Work is enqueued on the current stream of the device and nothing waits for it; results and workspace come from
 torch's allocator on that stream, so a tensor that was made on another stream has to be ready there, as for any
-torch operation.  If the shared library is missing or a call fails this raises; there is no fallback path.
+torch operation.  Nothing is recorded for automatic differentiation: while that is on, tensors that require a gradient are
+refused (but for gradients that are clipped, as by torch's own clipping), and what is written in place gets a new version.  If the shared library is missing or a call fails this raises; there is no fallback path.
 """
 from __future__ import annotations
 
@@ -85,6 +86,7 @@ class TrainOps:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
+        self._new_version = torch.autograd.graph.increment_version
         self._types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
         self._wide = {torch.int32: 0, torch.int64: 1}
         # (the handle of the current stream, without an object around it)
@@ -105,6 +107,9 @@ class TrainOps:
         if rc != OK:
             raise ChicleError(rc, self._L.chicle_train_last_error().decode())
 
+    def _no_graph(self, name: str):
+        raise ChicleError(EINVAL, "%s requires a gradient, and nothing is recorded here: detach it, or call under torch.no_grad()" % name)
+
     def _empty(self, shape, dtype):
         return self._torch.empty(shape, dtype=dtype, device=self.device)
 
@@ -120,6 +125,8 @@ class TrainOps:
             raise ChicleError(EINVAL, "%s must be a 2-D float32, bfloat16 or float16 tensor on %s" % (name, self.device))
         if type_of is not None and a.dtype != type_of.dtype:
             raise ChicleError(EINVAL, "%s must have the type %s" % (name, type_of.dtype))
+        if a.requires_grad and self._torch.is_grad_enabled():
+            self._no_graph(name)
         n, d = a.shape
         if d < 1 or (cols is not None and d != cols):
             raise ChicleError(EINVAL, "%s has %d columns" % (name, d))
@@ -131,6 +138,8 @@ class TrainOps:
     def _vector(self, a, name: str, size: int, dtype):
         if a.device != self.device or a.dim() != 1 or a.shape[0] != size or a.dtype != dtype or not a.is_contiguous():
             raise ChicleError(EINVAL, "%s must be a contiguous %s tensor of %d values on %s" % (name, dtype, size, self.device))
+        if a.requires_grad and self._torch.is_grad_enabled():
+            self._no_graph(name)
         return a.data_ptr()
 
     def _indices(self, a, name: str, size: Optional[int] = None):
@@ -206,6 +215,8 @@ class TrainOps:
         ws = self._workspace(nbytes)
         self._call(self._L.chicle_embed_grad, ip, wide, dout.data_ptr(), ldd, n, d, n_rows, t, scale, int(into is not None), out.data_ptr(), ldo,
                    ws.data_ptr(), nbytes, self._flags())
+        if into is not None:
+            self._new_version(into)
         return out
 
     # -- layer norm
@@ -257,6 +268,8 @@ class TrainOps:
         ws = self._workspace(nbytes)
         self._call(self._L.chicle_clip_grads, _at(where), None if to is None else _at(to), _at(sizes), _at(types), k, max_norm,
                    norm.data_ptr(), ws.data_ptr(), nbytes)
+        if out is not None:
+            self._new_version(out)
         return norm
 
     def grad_norm(self, grads: Sequence):

@@ -84,3 +84,47 @@ def test_the_first_call_may_be_captured(ops):
     import paper_1909_04885_amd as chicle
     with pytest.raises(chicle.ChicleError, match="token"):
         ops.sync()
+
+
+def test_what_requires_a_gradient_is_refused_while_gradients_are_recorded(ops):
+    import paper_1909_04885_amd as chicle
+    x, w, v, ids = torch.randn(4, 8, device="cuda"), torch.randn(10, 8, device="cuda"), torch.ones(8, device="cuda"), torch.arange(4, device="cuda")
+    ones = torch.ones(4, device="cuda")
+
+    def calls(x, w, v, ones):
+        yield lambda: ops.softmax_loss(x, w, ids)
+        yield lambda: ops.softmax_loss_grad(x, w, ids, ones)
+        yield lambda: ops.embed(w, ids)
+        yield lambda: ops.embed_grad(ids, x, 10)
+        yield lambda: ops.embed_grad(ids, x.detach(), 10, into=w)
+        yield lambda: ops.layer_norm(x, v, v.detach())
+        yield lambda: ops.layer_norm_grad(x, x.detach(), v.detach(), ones.detach(), ones.detach())
+
+    asked = [t.clone().requires_grad_() for t in (x, w, v, ones)]
+    for k, call in enumerate(calls(*asked)):
+        with pytest.raises(chicle.ChicleError, match="requires a gradient"):
+            call()
+            pytest.fail("call %d was not refused" % k)
+    with torch.no_grad():
+        for call in calls(*asked):
+            call()
+    for call in calls(x, w, v, ones):
+        call()
+    with torch.inference_mode():
+        ops.clip_grads([torch.ones(5, device="cuda")], 1.0)
+
+
+def test_what_is_written_in_place_has_a_new_version(ops):
+    a = torch.randn(6, 8, device="cuda", requires_grad=True)
+    for write in (lambda t: ops.clip_grads([t], 1.0), lambda t: ops.clip_grads([torch.ones_like(t)], 1.0, [t]),
+                  lambda t: ops.embed_grad(torch.arange(6, device="cuda"), torch.ones_like(t), 6, into=t)):
+        saved = torch.randn(6, 8, device="cuda")
+        product = (a * saved).sum()
+        write(saved)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            product.backward()
+    saved = torch.randn(6, 8, device="cuda")
+    product = (a * saved).sum()
+    ops.grad_norm([saved])
+    ops.clip_grads([saved], 1.0, [torch.empty_like(saved)])
+    product.backward()
