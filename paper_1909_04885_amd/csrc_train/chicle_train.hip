@@ -239,15 +239,13 @@ int64_t few_rows(int size, bool aligned)
     return aligned ? 0 : FEW_ROWS / 2;
 }
 
-constexpr int planes_of_g(int size) { return size == 2 ? 2 : 1; }
-
 LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64_t n, int64_t d, int64_t classes, int32_t type, bool grad, void *workspace)
 {
     LossPlan p = {};
     p.bytes = ALIGN;
     if (n == 0) return p;                                // (nothing to lay out)
     p.n = n; p.d = d; p.classes = classes;
-    const int size = size_of(type), planes = planes_of_g(size);
+    const int size = size_of(type), planes = size == 2 ? MM_PLANES<bf16, true> : MM_PLANES<float, true>;
     const int64_t slice = MM_ROW / size;
     // rows that are whole slices of aligned chunks are read where they are
     auto as_is = [&](const void *q, int64_t ld) { return d % slice == 0 && ld * size % 16 == 0 && (uintptr_t)q % 16 == 0 && ld < LOSS_MOST_D; };
@@ -390,7 +388,6 @@ MmShape mm_shape(const MmOperand &a, const MmOperand &b, int64_t k, int config, 
 {
     MmShape s;
     s.a = a; s.b = b;
-    s.planes = planes;
     s.plane = plane;
     s.slices = (int)ceil_div(k, MM_K<T>) * planes;
     s.tiles_i = (int)ceil_div(a.rows, mm_tile_i(config));
@@ -468,7 +465,7 @@ template <typename T>
 int run_loss_products(const LossPlan &p, int64_t row0, int64_t rows, const T *w, int64_t ldw, int64_t class0, int64_t classes, int64_t ldg, T *dw,
                       int64_t lddw, const float *inverse, bool add, int &copies, hipStream_t stream)
 {
-    constexpr int planes = planes_of_g(sizeof(T));
+    constexpr int planes = MM_PLANES<T, true>;
     const int64_t rows_g = round_up(rows, MM_K<T>), plane = p.rows_g * ldg;
     const MmOperand x_by_k = {(const T *)p.x + row0 * p.ldk, p.ldk, (int)p.d, (int)rows_g}, w_by_k = {w + class0 * ldw, ldw, (int)p.d, (int)classes};
     const MmOperand g_rows = {p.g, ldg, (int)rows, 0};

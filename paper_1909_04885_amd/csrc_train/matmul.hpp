@@ -53,12 +53,13 @@ struct MmOperand {
     int k_rows;                              // by k: how many k are there; further ones are read as the last
 };
 
-// B may come as two planes that add up to it, whose slices are multiplied in turn, each with the same slice of A.
+// Where A lies by k, in 16 bits, B is two planes that add up to it, whose slices are multiplied in turn, each with the same slice of A.
+template <typename T, bool A_BY_K> constexpr int MM_PLANES = A_BY_K && sizeof(T) == 2 ? 2 : 1;
+
 struct MmShape {
     MmOperand a, b;
-    int planes;                              // 1 or 2
     int64_t plane;                           // elements from B's first plane to its second
-    int slices;                              // of the whole sum, of both planes
+    int slices;                              // of the whole sum, of all planes
     int tiles_i, tiles_j, splits, per_split; // per_split: slices of a split of the sum
 };
 
@@ -139,6 +140,7 @@ __device__ __forceinline__ void mm_fetch(const MmOperand &o, const char *base, i
 
 // What is fetched next: slice `at`, `left` slices from the end of unit `unit`.
 template <typename T, typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
+    static constexpr int ODD = MM_PLANES<T, A_BY_K> - 1;       // a slice's bits that say its plane, and their number
     unsigned unit, units;
     int at, left, row_a, row_b;
     bool edge_a, edge_b;
@@ -152,7 +154,7 @@ template <typename T, typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
         units = s.tiles_i * s.tiles_j * s.splits;
         step_a = A_BY_K ? MM_ROW * s.a.ld : MM_ROW;
         step_b = B_BY_K ? MM_ROW * s.b.ld : MM_ROW;
-        plane = s.planes > 1 ? s.plane * (int)sizeof(T) : 0;
+        plane = ODD ? s.plane * (int)sizeof(T) : 0;
         const MmOperand whole_a = {nullptr, s.a.ld, 1 << 30, 0}, whole_b = {nullptr, s.b.ld, 1 << 30, 0};
 #pragma unroll
         for (int q = 0; q < (A_BY_K ? 2 : 1); ++q)
@@ -175,16 +177,16 @@ template <typename T, typename C, bool A_BY_K, bool B_BY_K> struct MmFetcher {
         edge_b = row_b + C::TILE_J > whole_rows(s.b, B_BY_K);
         at = t.split * s.per_split;
         left = min(s.per_split, s.slices - at);
-        qa = (const char *)s.a.p + (A_BY_K ? (int64_t)row_a : (int64_t)row_a * s.a.ld) * (int)sizeof(T) + (at >> (s.planes - 1)) * step_a;
-        qb = (const char *)s.b.p + (B_BY_K ? (int64_t)row_b : (int64_t)row_b * s.b.ld) * (int)sizeof(T) + (at >> (s.planes - 1)) * step_b + (at & (s.planes - 1)) * plane;
+        qa = (const char *)s.a.p + (A_BY_K ? (int64_t)row_a : (int64_t)row_a * s.a.ld) * (int)sizeof(T) + (at >> ODD) * step_a;
+        qb = (const char *)s.b.p + (B_BY_K ? (int64_t)row_b : (int64_t)row_b * s.b.ld) * (int)sizeof(T) + (at >> ODD) * step_b + (at & ODD) * plane;
     }
     __device__ __forceinline__ void fetch(const MmShape &s, char *lds)
     {
         if (unit >= units) return;
-        const int last_k = A_BY_K ? s.a.k_rows - 1 - (at >> (s.planes - 1)) * MM_K<T> : MM_K<T>;   // (the last k may not all be there)
+        const int last_k = A_BY_K ? s.a.k_rows - 1 - (at >> ODD) * MM_K<T> : MM_K<T>;   // (the last k may not all be there)
         mm_fetch<T, C::TILE_I, C, A_BY_K>(s.a, qa, row_a, off_a, edge_a || last_k < MM_K<T> - 1, last_k, lds);
         mm_fetch<T, C::TILE_J, C, B_BY_K>(s.b, qb, row_b, off_b, edge_b, MM_K<T>, lds + C::TILE_I * MM_ROW);
-        const bool further = (++at & (s.planes - 1)) == 0;                 // (all planes of this k are done)
+        const bool further = (++at & ODD) == 0;          // (all planes of this k are done)
         qa += further ? step_a : 0;
         qb += further ? step_b - plane : plane;
         if (--left == 0) {
