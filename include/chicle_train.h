@@ -80,7 +80,8 @@ int chicle_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t 
 
 /* The 2-norm of `count` tensors together (norm: one float), and, where out is not NULL, out_k = in_k * min(1, max_norm / (norm + 1e-6)).
  * in, out, sizes and types are host arrays of count entries: device pointers of contiguous tensors, numbers of values and
- * chicle_types.  out_k may be in_k.  A norm that is infinite or no number scales as the formula says.  Limit: 100000 tensors. */
+ * chicle_types.  out_k may be in_k, and overlaps no other tensor of the call (outputs that overlap one another are refused).  A norm that is infinite
+ * or no number scales as the formula says.  Limit: 100000 tensors. */
 size_t chicle_clip_grads_bytes(int32_t count);
 int chicle_clip_grads(const void *const *in, void *const *out, const int64_t *sizes, const int32_t *types, int32_t count, float max_norm,
                       float *norm, void *workspace, size_t workspace_bytes, void *hip_stream);

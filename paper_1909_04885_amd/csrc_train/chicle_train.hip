@@ -4,6 +4,8 @@
 #include <stdio.h>
 #include <string.h>
 #include <algorithm>
+#include <memory>
+#include <new>
 #include "../../include/chicle_train.h"
 #include "clip.hpp"
 #include "elements.hpp"
@@ -63,6 +65,21 @@ int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 int size_of(int32_t type) { return type == CHICLE_F32 ? 4 : 2; }
 bool type_ok(int32_t type) { return type == CHICLE_F32 || type == CHICLE_BF16 || type == CHICLE_F16; }
 bool placed(const void *p, int size) { return p && (uintptr_t)p % (uintptr_t)size == 0; }
+
+// Whether two of the tensors that are written overlap: workgroups would scale there beside each other, each what another may have scaled.
+int check_apart(void *const *out, const int64_t *sizes, const int32_t *types, int count)
+{
+    struct Range { uintptr_t begin, end; };
+    std::unique_ptr<Range[]> r(new (std::nothrow) Range[count]);
+    if (!r) return fail(CHICLE_ENOMEM, "no host memory for %d tensors", count);
+    int many = 0;
+    for (int k = 0; k < count; ++k)
+        if (sizes[k] > 0) r[many++] = {(uintptr_t)out[k], (uintptr_t)out[k] + (uintptr_t)sizes[k] * size_of(types[k])};
+    std::sort(r.get(), r.get() + many, [](const Range &a, const Range &b) { return a.begin < b.begin; });
+    for (int k = 1; k < many; ++k)
+        if (r[k].begin < r[k - 1].end) return fail(CHICLE_EINVAL, "memory that is written twice, by tensors that overlap");
+    return CHICLE_OK;
+}
 
 int check_workspace(const void *workspace, size_t have, size_t need)
 {
@@ -857,6 +874,7 @@ int chicle_clip_grads(const void *const *in, void *const *out, const int64_t *si
         pieces_all += ceil_div(sizes[k], CLIP_PIECE);
     }
     if (pieces_all > INT32_MAX / 2) return fail(CHICLE_EINVAL, "too many values");
+    if (out) TRY(check_apart(out, sizes, types, count));
     TRY(check_workspace(workspace, workspace_bytes, chicle_clip_grads_bytes(count)));
     Carver c(workspace);
     double *part = c.take<double>(CLIP_MOST_PARTS);

@@ -277,7 +277,8 @@ class TrainOps:
         return self._clip(grads, None, 0.0)
 
     def clip_grads(self, grads: Sequence, max_norm: float, out: Optional[Sequence] = None):
-        """grads times min(1, max_norm / (norm + 1e-6)), in place or into `out`; returns the norm before it."""
+        """grads times min(1, max_norm / (norm + 1e-6)), in place or into `out`; returns the norm before it.  What is written overlaps
+        nothing but, where it is the same tensor, its own gradient."""
         return self._clip(grads, grads if out is None else out, max_norm)
 
     def sync(self):

@@ -128,3 +128,18 @@ def test_what_is_written_in_place_has_a_new_version(ops):
     ops.grad_norm([saved])
     ops.clip_grads([saved], 1.0, [torch.empty_like(saved)])
     product.backward()
+
+
+def test_memory_that_would_be_written_twice_is_refused(ops):
+    """Two workgroups would scale it beside each other, each what the other may have scaled."""
+    import paper_1909_04885_amd as chicle
+    a, b, empty = torch.ones(50000, device="cuda"), torch.ones(7, device="cuda"), torch.empty(0, device="cuda")
+    for call in (lambda: ops.clip_grads([a, b, a], 1.0), lambda: ops.clip_grads([a, a], 1.0, [b.new_empty(50000)] * 2),
+                 lambda: ops.clip_grads([b, a[100:], a[:101]], 1.0)):
+        with pytest.raises(chicle.ChicleError, match="twice"):
+            call()
+    assert a.eq(1).all()
+    assert abs(float(ops.grad_norm([a, a])) - 100000 ** 0.5) < 1e-3      # (read twice it may be)
+    ops.clip_grads([a, a], 1.0, [torch.empty_like(a), torch.empty_like(a)])
+    ops.clip_grads([a[100:], a[:100]], 1e9)
+    ops.clip_grads([empty, b, empty, empty[:0]], 1.0)

@@ -25,3 +25,15 @@ def test_refusals_of_taking_flags(lib):
     p, odd = ctypes.c_void_p(4096), ctypes.c_void_p(4098)
     for flags, out in ((None, p), (p, None), (odd, p), (p, odd)):
         assert lib.chicle_train_take_flags(flags, out, None) == -1
+
+
+def test_outputs_of_clipping_that_overlap_are_refused(lib):
+    import ctypes
+    ins, sizes, types = (ctypes.c_void_p * 3)(4096, 8192, 16384), (ctypes.c_int64 * 3)(10, 100, 10), (ctypes.c_int32 * 3)(0, 1, 0)
+    norm, ws = ctypes.c_void_p(4096), ctypes.c_void_p(4096)
+    for out in ((4096, 8192, 4096), (16384, 4096, 4292), (8188, 8192, 4096), (4096, 4132, 9000)):
+        assert lib.chicle_clip_grads(ins, (ctypes.c_void_p * 3)(*out), sizes, types, 3, 1.0, norm, ws, 1 << 40, None) == -1, out
+        assert b"twice" in lib.chicle_train_last_error()
+    # side by side, and one of no values beside another: these get as far as the workspace
+    for out, many in (((4096, 8192, 4136), (10, 100, 10)), ((8192, 8192, 4096), (10, 0, 10))):
+        assert lib.chicle_clip_grads(ins, (ctypes.c_void_p * 3)(*out), (ctypes.c_int64 * 3)(*many), types, 3, 1.0, norm, ws, 0, None) == -2
