@@ -137,7 +137,8 @@ int64_t layer_norm_parts(int64_t n, int64_t d, int32_t type)
     return g < LN_GRAD_GRID ? g : LN_GRAD_GRID;
 }
 
-// f(first row, rows, workgroups) for all n rows, `per` to a workgroup: a launch has fewer than 2^32 threads, of which a workgroup here has up to 2^10.
+// f(first row, rows, workgroups) for all n rows (or columns), `per` to a workgroup: a launch has fewer than 2^32 threads, of which a workgroup here has
+// up to 2^10.
 template <typename F>
 int with_rows(int64_t n, int per, F f)
 {
@@ -845,8 +846,10 @@ int chicle_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t 
                 }
                 return launched("layer_norm_grad_rows");
             }));
-        layer_norm_grad_sums<T><<<(unsigned)ceil_div(2 * d, LN_SUM_COLUMNS), 1024, 0, stream>>>(part, (int)parts, d, (T *)dgamma, (T *)dbeta);
-        return launched("layer_norm_grad_sums");
+        return with_rows(2 * d, LN_SUM_COLUMNS, [&](int64_t first, int64_t, unsigned grid) {
+            layer_norm_grad_sums<T><<<grid, 1024, 0, stream>>>(part, (int)parts, d, first, (T *)dgamma, (T *)dbeta);
+            return launched("layer_norm_grad_sums");
+        });
     });
 }
 

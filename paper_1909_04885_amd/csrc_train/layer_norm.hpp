@@ -240,16 +240,17 @@ __global__ __launch_bounds__(THREADS) void layer_norm_grad_rows(const T *__restr
     }
 }
 
-// Sums of the workgroups' parts: LN_SUM_COLUMNS columns of [dgamma | dbeta] to a workgroup, 64 threads to a column.
+// Sums of the workgroups' parts: LN_SUM_COLUMNS columns of [dgamma | dbeta] to a workgroup, from `first` on, 64 threads to a column.
 constexpr int LN_SUM_COLUMNS = 16;
 
 template <typename T>
-__global__ __launch_bounds__(1024) void layer_norm_grad_sums(const float *__restrict__ part, int parts, int64_t d, T *__restrict__ dgamma, T *__restrict__ dbeta)
+__global__ __launch_bounds__(1024) void layer_norm_grad_sums(const float *__restrict__ part, int parts, int64_t d, int64_t first, T *__restrict__ dgamma,
+                                                             T *__restrict__ dbeta)
 {
     constexpr int SLICES = 1024 / LN_SUM_COLUMNS;
     __shared__ float s[SLICES][LN_SUM_COLUMNS + 1];
     const int col = threadIdx.x % LN_SUM_COLUMNS, slice = threadIdx.x / LN_SUM_COLUMNS;
-    const int64_t c = (int64_t)blockIdx.x * LN_SUM_COLUMNS + col;
+    const int64_t c = first + (int64_t)blockIdx.x * LN_SUM_COLUMNS + col;
     float t = 0.f;
     if (c < 2 * d) {
 #pragma unroll 8

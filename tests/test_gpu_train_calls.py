@@ -143,3 +143,20 @@ def test_memory_that_would_be_written_twice_is_refused(ops):
     ops.clip_grads([a, a], 1.0, [torch.empty_like(a), torch.empty_like(a)])
     ops.clip_grads([a[100:], a[:100]], 1e9)
     ops.clip_grads([empty, b, empty, empty[:0]], 1.0)
+
+
+def test_layer_norm_of_rows_whose_columns_fill_more_than_a_launch(ops):
+    """2^25 columns and more: the sums over rows of the gradients by weight and bias have 2 d columns, 16 to a workgroup of 1024 threads."""
+    n, d = 2, (1 << 25) + 21
+    print("\ncase layer_norm_grad", n, d, flush=True)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x, dy = (torch.randn(n, d, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    gamma = (torch.rand(d, generator=g, device="cuda") + 0.5).to(torch.bfloat16)
+    _, mean, rstd = ops.layer_norm(x, gamma, gamma)
+    dx, dgamma, dbeta = ops.layer_norm_grad(dy, x, gamma, mean, rstd)
+    h = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    # two terms of each sum, and the rounding of the result
+    for got, terms in ((dgamma, dy.double() * h), (dbeta, dy.double())):
+        want = terms.sum(0)
+        assert bool(((got.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -20 * terms.abs().sum(0)).all())
