@@ -758,6 +758,7 @@ int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t l
     const int64_t pieces = ceil_div(n, g.piece);
     g.run_blocks = (int)ceil_div(pieces, groups);
     g.zero_rows = (int)(d * s >= ZERO_BYTES ? 1 : ZERO_BYTES / (d * s));
+    while (g.run_blocks + ceil_div(n_rows, g.zero_rows) >= (int64_t)1 << 24) g.zero_rows *= 2;     // (a launch has fewer than 2^32 threads)
     g.zero_blocks = accumulate ? 0 : (int)ceil_div(n_rows, g.zero_rows);
     g.seen = seen;
     g.accumulate = accumulate;

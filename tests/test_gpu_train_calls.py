@@ -160,3 +160,27 @@ def test_layer_norm_of_rows_whose_columns_fill_more_than_a_launch(ops):
     for got, terms in ((dgamma, dy.double() * h), (dbeta, dy.double())):
         want = terms.sum(0)
         assert bool(((got.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -20 * terms.abs().sum(0)).all())
+
+
+def test_gradient_of_a_table_whose_rows_fill_more_than_a_launch(ops):
+    """2^24 rows of 8200 bytes: zeros for a row or two to a workgroup."""
+    n_rows, d = (1 << 24) + 3, 4100
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("138 GB are not free")
+    print("\ncase embed_grad", n_rows, d, flush=True)
+    before = torch.ones(n_rows, d, dtype=torch.bfloat16, device="cuda")
+    at = before.data_ptr()
+    del before                                           # (the result's memory, which holds ones)
+    ids = torch.tensor([n_rows - 1, 5, -1, 5, 1 << 23], device="cuda")
+    dout = torch.randn(5, d, device="cuda").to(torch.bfloat16)
+    got = ops.embed_grad(ids, dout, n_rows)
+    assert got.data_ptr() == at
+    assert torch.equal(got[n_rows - 1], dout[0]) and torch.equal(got[1 << 23], dout[4])
+    assert torch.equal(got[5], (dout[1].float() + dout[3].float()).to(torch.bfloat16))
+    got[ids[[0, 1, 4]]] = 0
+    step = 1 << 20
+    for a in range(0, n_rows, step):
+        assert not got[a:a + step].any(), a
+    del got
+    torch.cuda.empty_cache()
