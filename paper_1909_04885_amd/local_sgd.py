@@ -57,15 +57,22 @@ def evaluate(ops: TrainOps, model: TokenModel, tokens, labels, batch: int = 8192
     return total / max(1, int((labels >= 0).sum()))
 
 
+def step_rows(step: int, batch: int, n: int, device=None):
+    """The rows of a solver's step, counted over all rounds: `batch` of its n rows after those of the step before, and from the first again."""
+    import torch
+    return torch.arange(step * batch, (step + 1) * batch, device=device) % n
+
+
 def local_steps(ops: TrainOps, model: TokenModel, tokens, labels, steps: int, batch: int, rate: float, momentum: float, max_norm: float,
-                loss_scale: float) -> List:
-    """H = `steps` steps of SGD with momentum on one solver's rows, from the shared model; returns the solver's model."""
+                loss_scale: float, first: int = 0) -> List:
+    """H = `steps` steps of SGD with momentum on one solver's rows, from the shared model; returns the solver's model.  `first`: the steps that it has
+    made in the rounds before."""
     import torch
     own = [p.clone() for p in model.master]
     velocity = [torch.zeros_like(p) for p in own]
     n = tokens.shape[0]
     for h in range(steps):
-        at = torch.arange(h * batch, (h + 1) * batch, device=tokens.device) % n
+        at = step_rows(first + h, batch, n, tokens.device)
         some, target = tokens[at], labels[at]
         count = (target >= 0).sum().clamp(min=1).float()
         row_weight = (loss_scale / count).expand(at.numel()).contiguous()
@@ -88,14 +95,15 @@ def run_rounds(ops: TrainOps, model: TokenModel, tokens, labels, solvers: int, r
                       [torch.empty(0, dtype=torch.long, device=tokens.device)]) for s in range(solvers)]
     loss_scale = 1024.0 if model.dtype == torch.float16 else 1.0
     losses, seconds = [evaluate(ops, model, tokens, labels)], 0.0
-    for _ in range(rounds):
+    for r in range(rounds):
         torch.cuda.synchronize()
         began = time.perf_counter()
         merged = [torch.zeros_like(p) for p in model.master]
         for own_rows in rows:
             if own_rows.numel() == 0:
                 continue
-            own = local_steps(ops, model, tokens[own_rows], labels[own_rows], steps, batch, rate, momentum, max_norm, loss_scale)
+            own = local_steps(ops, model, tokens[own_rows], labels[own_rows], steps, batch, rate, momentum, max_norm, loss_scale,
+                              r * steps)
             for m, p in zip(merged, own):
                 m.add_(p, alpha=own_rows.numel() / n)
         model.master = merged
