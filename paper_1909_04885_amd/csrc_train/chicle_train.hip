@@ -752,9 +752,11 @@ int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t l
     g.n = n; g.d = d; g.n_rows = n_rows; g.ldo = ldo; g.ldd = ldd; g.ldp = p.ldp;
     g.lanes = pow2_at_least(ceil_div(d, vec), EMBED_THREADS);
     const int groups = EMBED_THREADS / g.lanes;
-    // Where there are workgroups enough, still longer ones: 131,072 tokens of 2048 in 16 bits 228 instead of 251 us,
-    // 16,000 tokens 71 instead of 64, 131,072 tokens of 512 (four pieces to a workgroup) 81 and 80.
-    g.piece = groups == 1 && p.pieces >= 2 * 2048 && p.piece == 32 ? 64 : p.piece;
+    // Where a workgroup has one piece and two to a compute unit are left, still longer ones.  In us, pieces of 32 / 64: 2048 columns of 16 bits into
+    // 2000 rows, 16,000 tokens 48 / 55, 24,000 57 / 58, 32,768 65 / 62, 48,000 81 / 77; into 128,000 rows 16,000 130 / 130, 32,768 146 / 141, 65,536
+    // 178 / 170, 131,072 247 / 226; 4096 columns 16,000 100 / 108, 65,536 205 / 188; 600 columns of 32 bits 28,000 57 / 62, 48,000 69 / 69, 1024
+    // columns 65,536 104 / 99.  131,072 tokens of 512 in 16 bits (four pieces to a workgroup): 80 / 81.
+    g.piece = groups == 1 && p.pieces >= 4 * CUS && p.piece == 32 ? 64 : p.piece;
     const int64_t pieces = ceil_div(n, g.piece);
     g.run_blocks = (int)ceil_div(pieces, groups);
     g.zero_rows = (int)(d * s >= ZERO_BYTES ? 1 : ZERO_BYTES / (d * s));

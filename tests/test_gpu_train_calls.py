@@ -184,3 +184,19 @@ def test_gradient_of_a_table_whose_rows_fill_more_than_a_launch(ops):
         assert not got[a:a + step].any(), a
     del got
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n", [32736, 32737, 40001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_gradient_of_a_table_about_where_pieces_get_longer(ops, dtype, n):
+    import train_reference as ref
+    d, n_rows = 1100, 700
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    ids = torch.randint(-1, n_rows, (n,), generator=g, device="cuda", dtype=torch.int32)
+    ids[5000:9000] = 7                                   # a run over many pieces
+    dout = torch.randn(n, d, generator=g, device="cuda").to(dtype)
+    want, off = ref.embed_grad(ids, dout, n_rows, 0.7)
+    got = ops.embed_grad(ids, dout, n_rows, 0.7)
+    ref.within(got, want, off)
+    assert torch.equal(got, ops.embed_grad(ids, dout, n_rows, 0.7))
