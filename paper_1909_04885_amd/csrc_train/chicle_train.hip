@@ -126,8 +126,9 @@ RowShape row_shape(int64_t d, int vec, int first_values, int most_values)
 constexpr int CUS = 256;                                 // compute units
 constexpr int LN_FORWARD_VALUES = 32, LN_GRAD_VALUES = 16;
 // Workgroups of the gradient: whole rounds of what the compute units hold at once, up to this many.  At 65,536 x 4096 in 16 bits,
-// where 768 are held, 768 take 306 us and 1024 (a round and a third) 390 us; at 30,000 x 4096 in 32 bits, where 512 are, 768 take
-// 300 us and 1024 267 us.
+// where 768 are held, 768 take 306 us and 1024 (a round and a third) 390 us.  In us, up to 256 / 512 / 768 / this many: 65,536 x 4096 in 16 bits
+// 599 / 345 / 298 / 298, 30,000 x 4096 in 32 bits 330 / 255 / 253 / 263, 9001 x 1537 88 / 55 / 50 / 48, 4096 x 1024 32 / 23 / 23 / 23.  What it costs is the
+// parts' bytes in short batches of wide rows: 4096 x 4096 in 16 bits 52 / 44 / 47 / 47, in 32 58 / 52 / 52 / 64, 1024 x 16,384 in 16 bits 59 / 88 / 117 / 150.
 constexpr int LN_GRAD_GRID = 1024;
 
 int64_t layer_norm_parts(int64_t n, int64_t d, int32_t type)
@@ -182,13 +183,14 @@ int mm_tile_j(int c) { return c == WIDE ? 256 : c == MIDDLE ? 128 : 64; }
 // 32 bits: the matrix cores are the bound whatever the tile, and what counts is how much of the tiles lies past the last row, and that they share
 // out well: gradients of 333 rows of 250 and 20,000 classes 168 us in middle and 160 in thin tiles, 1000 rows of 1024 and 10,000 597 and
 // 578, 4096 rows of 512 and 30,000 3323 and 3481 (tiles of 64 x 64: 163, 616, 3670).
-// `splittable`: the sum is long and may be divided; the gradients of 512 rows of 1024 and 50,000 classes (8 large tiles) take 287 us with middle
-// tiles and 294 with large ones, of 4096 rows (64) 1699 and 1637; of 1024 rows of 2048 and 12,000 classes, whose sum is short, 238 and 243.
+// `splittable`: the sum is long and may be divided, from 256 slices on.  Gradients in us, middle / large tiles, 1024 columns: 512 rows (8 large tiles) and
+// 50,000 classes 405 / 401, 2048 rows (32) 1386 / 1314, 4096 rows (64) 2656 / 2500, with 16,000 classes (500 slices) 848 / 803, with 12,000
+// (375) 661 / 661, with 6000 (188) 365 / 361.
 int mm_choose(int size, int64_t rows_i, int64_t rows_j, bool splittable = false)
 {
     if (rows_j <= 64) return THIN;
     const int64_t tiles = ceil_div(rows_i, 256) * ceil_div(rows_j, 256);
-    if (size == 2) return tiles >= (splittable ? 64 : 192) ? WIDE : MIDDLE;
+    if (size == 2) return tiles >= (splittable ? 32 : 192) ? WIDE : MIDDLE;
     const int64_t middle = ceil_div(rows_j, 128);
     return middle * 2 == ceil_div(rows_j, 64) && middle * ceil_div(rows_i, 128) >= 4 * CUS ? MIDDLE : THIN;
 }
@@ -227,7 +229,7 @@ struct LossPlan {
     size_t bytes;
 };
 
-// 8192 rows of 2048 and 128,000 classes in 16 bits with a quarter of it: 15.2 ms, this 15.4, four times as much 15.6.
+// 8192 rows of 2048 and 128,000 classes in 16 bits with a quarter of it: 23.0 ms, this 23.0, four times as much 23.3.
 constexpr int64_t LOSS_PIECE_BYTES = (int64_t)1 << 30;   // both planes of G of a piece of the classes, or more of long batches
 // 16,384 rows of 512 and 50,000 classes in 32 bits with a quarter of it: 24.1 ms, this 22.4, four times as much 22.3.
 constexpr int64_t LOSS_KEPT_BYTES = (int64_t)1 << 30;    // logits of a piece of the rows
@@ -237,7 +239,7 @@ constexpr int64_t LOSS_MOST = (int64_t)1 << 22, LOSS_MOST_D = (int64_t)1 << 21, 
 int64_t spread(int64_t ld, int size) { return ld * size % 1024 == 0 ? ld + MM_ROW / size : ld; }
 
 // Classes at the end of a piece whose tiles of dw are split: those past the last whole round of tiles, where they are less than half a round
-// (the gradients of 4096 rows of 1024 and 50,021 classes 1771 instead of 1855 us).
+// (the gradients of 4096 rows of 1024 and 50,021 classes 2503 instead of 2676 us).
 int64_t dw_rest(int config, int64_t d, int64_t classes, int64_t slices)
 {
     const int64_t across = ceil_div(d, 256), tiles = across * ceil_div(classes, 256), over = tiles % CUS;
@@ -248,7 +250,7 @@ int64_t dw_rest(int config, int64_t d, int64_t classes, int64_t slices)
 
 // Up to how many rows the loss reads w as it lies instead of by products; with the gradient too, so that both give the same loss.
 // In us, 50,000 classes, as it lies / by products.  16 bits, w aligned: 4 rows of 1024 33 / 25, 64 rows 48 / 26; w not aligned, so that products need
-// it laid out first: 1 row of 1001 46 / 60, 33 rows 55 / 62, but with the gradient, which needs that anyway, 16 rows 157 / 151, 48 rows 175 / 156.
+// it laid out first: 1 row of 1001 46 / 60, 33 rows 55 / 62, but with the gradient, which needs that anyway, 16 rows 168 / 144.
 // 32 bits, aligned: 16 rows of 1024 60 / 86, 24 rows 86 / 84; not aligned: 32 rows of 1001 94 / 149, with the gradient 323 / 303, 48 rows
 // 134 / 150 and 392 / 329.
 int64_t few_rows(int size, bool aligned)
@@ -268,7 +270,8 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
     // rows that are whole slices of aligned chunks are read where they are
     auto as_is = [&](const void *q, int64_t ld) { return d % slice == 0 && ld * size % 16 == 0 && (uintptr_t)q % 16 == 0 && ld < LOSS_MOST_D; };
     p.few = n <= few_rows(size, as_is(w, ldw));
-    // (16 bits: 4 rows of 1024 and 50,000 classes 96 us this way, 107 by products, 8 rows 124 and 109; 32 bits: 8 rows 167 and 208)
+    // (16 bits: 4 rows of 1024 and 50,000 classes 78 us this way, 116 by products, 8 rows 109 and 117, of 4096 and 8000 classes 118 and 92, of 1001 and
+    // 50,000 188 and 166; 32 bits: 8 rows 167 and 208)
     p.few_grad = grad && n <= (size == 4 ? FEW_GRAD_ROWS : FEW_GRAD_ROWS / 2);
     p.config = mm_choose(size, classes, n);
     p.loss_splits = 1;
@@ -346,7 +349,7 @@ LossPlan loss_plan(const void *x, int64_t ldx, const void *w, int64_t ldw, int64
         p.ldg = size == 4 ? p.ldz : spread(round_up(p.piece, slice), size);        // (in 32 bits the logits themselves become G)
         p.ldp = round_up(d, 4);
         const int64_t slices = ceil_div(p.piece, slice) * planes;
-        p.config_dx = mm_choose(size, d, p.piece_rows, slices >= 512);
+        p.config_dx = mm_choose(size, d, p.piece_rows, slices >= 256);
         const int64_t tiles = ceil_div(d, mm_tile_i(p.config_dx)) * ceil_div(p.piece_rows, mm_tile_j(p.config_dx));
         const int64_t room = CUS * (p.config_dx == WIDE ? 1 : 2);
         int64_t splits = tiles >= room ? 1 : room / tiles;
