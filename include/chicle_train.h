@@ -57,7 +57,7 @@ int chicle_softmax_loss_grad(const void *x, int64_t ldx, const void *w, int64_t 
                              int64_t n, int64_t d, int64_t classes, int32_t type, float *loss, void *dx, int64_t lddx, void *dw, int64_t lddw,
                              void *workspace, size_t workspace_bytes, int32_t *flags, void *hip_stream);
 
-/* out_i = scale * table[id_i]; table has n_rows rows of d values. */
+/* out_i = scale * table[id_i]; table has n_rows rows of d values.  Limits: n and n_rows below 2^31, d below 2^23. */
 int chicle_embed(const void *table, int64_t ld, int64_t n_rows, const void *ids, int32_t wide, int64_t n, int64_t d, int32_t type, float scale,
                  void *out, int64_t ldo, int32_t *flags, void *hip_stream);
 
@@ -69,7 +69,7 @@ int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t l
                       int32_t accumulate, void *dtable, int64_t ldo, void *workspace, size_t workspace_bytes, int32_t *flags, void *hip_stream);
 
 /* Layer norm over rows of d values: y = (x - mean) rstd gamma + beta, rstd = 1 / sqrt(var + eps); mean and rstd (n floats each) are
- * what the gradient takes. */
+ * what the gradient takes.  Limits: n and d below 2^31. */
 int chicle_layer_norm(const void *x, int64_t ldx, const void *gamma, const void *beta, int64_t n, int64_t d, int32_t type, float eps,
                       void *y, int64_t ldy, float *mean, float *rstd, void *hip_stream);
 
