@@ -4,7 +4,9 @@
  * Beside CoCoA the uni-tasks of the paper run local SGD (Section 2.2, Section 5.1): every solver makes some steps on the
  * samples of its chunks and the trainer merges the models.  These are the operators of such a step for models over
  * categorical data with many classes: rows of a table looked up by token, layer norm, the softmax loss over all classes,
- * and the clipping of the step's gradients by their common norm, each with its gradients.
+ * and the clipping of the step's gradients by their common norm, each with its gradients; and, where the rows come in sequences, of
+ * layers between lookup and loss: a root-mean-square norm on a residual stream, a gated recurrence, and rows kept in 8 bits until
+ * the backward pass.
  *
  * Conventions
  *   - every function returns CHICLE_OK (0) or a negative chicle_status (chicle_round.h); nothing throws or aborts;
@@ -21,7 +23,7 @@
  *     type are rounded once, where they are stored;
  *   - label and token arrays hold 32-bit integers, or 64-bit ones where `wide` is not 0.  A negative one means "none": no loss, a row
  *     of zeros, no gradient.  One past the end is treated like that too, and sets a bit of *flags (1: label, 2: token), an
- *     int32 of the caller's, or NULL;
+ *     int32 of the caller's, or NULL (4: offsets of sequences that are no rows of the call);
  *   - results do not depend on timing: the same call on the same inputs gives the same bits.
  */
 #ifndef CHICLE_TRAIN_H
@@ -77,6 +79,54 @@ size_t chicle_layer_norm_grad_bytes(int64_t n, int64_t d, int32_t type);
 int chicle_layer_norm_grad(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *gamma, const float *mean, const float *rstd,
                            int64_t n, int64_t d, int32_t type, void *dx, int64_t lddx, void *dgamma, void *dbeta, void *workspace,
                            size_t workspace_bytes, void *hip_stream);
+
+/* Rows kept in 8 bits (packed rows): whole numbers q from -127 to 127, 32 neighbouring columns with one scale 2^e, the least power of two from
+ * 2^-126 on with max |x| <= 127 2^e; q = x 2^-e, rounded to nearest even.  A value is off by at most half of 2^e; by less than 2^e where x
+ * is near the largest number of its type (q stops at 63 there, so that what is finite stays finite).  A group with an infinity or NaN unpacks to NaN.
+ * q: n rows of d bytes, ldq apart, a multiple of 32 that has room for d in whole groups, 16-byte aligned; the bytes behind the last column, up to a whole
+ * group, are written as zeros.  scales: a byte e + 127 for a group (255: NaN, 0: zeros), rows ldq / 32 apart.  Limits: n and d below 2^31. */
+int chicle_pack8(const void *x, int64_t ldx, int64_t n, int64_t d, int32_t type, void *q, void *scales, int64_t ldq, void *hip_stream);
+int chicle_unpack8(const void *q, const void *scales, int64_t ldq, int64_t n, int64_t d, int32_t type, void *out, int64_t ldo, void *hip_stream);
+
+/* Root-mean-square norm of rows on a residual stream: r = x + residual (residual may be NULL: r = x), rounded to the type;
+ * rstd = 1 / sqrt(sum_c r_c^2 / d + eps), y = r rstd gamma.  sum (or NULL) gets r; sum8 (or NULL) gets r as packed rows, ldsum8 bytes apart.  y is of the
+ * type where y_scales is NULL, else packed rows, ldy bytes apart, made from the 32-bit values.  rstd: n floats, which the gradient takes.
+ * Limits: n and d below 2^31. */
+int chicle_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *gamma, int64_t n, int64_t d, int32_t type, float eps,
+                    void *sum, int64_t ldsum, void *y, int64_t ldy, void *y_scales, void *sum8, void *sum8_scales, int64_t ldsum8, float *rstd,
+                    void *hip_stream);
+
+/* Its gradients: dx, that of x as of the residual, with dsum added, which reaches r on the other way (or NULL), and dgamma, from r: of the type
+ * where sum_scales is NULL, else packed rows, ldsum bytes apart. */
+size_t chicle_rms_norm_grad_bytes(int64_t n, int64_t d, int32_t type);
+int chicle_rms_norm_grad(const void *dy, int64_t lddy, const void *sum, int64_t ldsum, const void *sum_scales, const void *gamma, const float *rstd,
+                         const void *dsum, int64_t lddsum, int64_t n, int64_t d, int32_t type, void *dx, int64_t lddx, void *dgamma, void *workspace,
+                         size_t workspace_bytes, void *hip_stream);
+
+/* Gated linear recurrence over the rows of sequences, column by column: a = 1 / (1 + exp(-f)), h_t = a_t h_{t-1} + (1 - a_t) u_t, y_t = h_t.
+ * Sequence j has the rows offsets[j] to offsets[j + 1] - 1 (sequences + 1 integers, ascending, 32-bit ones, or 64-bit ones where wide is not 0); none where
+ * they are equal.  offsets NULL: one sequence of all rows.  Rows of no sequence (before the first offset, from the last one on) get zeros, whatever
+ * they hold.  Offsets that descend or are no rows of the call set a bit of *flags, and results are then not defined; nothing is read or
+ * written outside of the tensors.  h0 (or NULL: zeros) and last (or NULL): sequences x d floats, the state before a sequence's first row and
+ * after its last.  u is of the type where u_scales is NULL, else packed rows, ldu bytes apart.  states (or NULL): n / 32, rounded up, x d floats, the state
+ * that enters every 32nd row, which the gradient takes.  Of a gate beyond +-87, +-infinity too, nothing comes through on the side that it closes, whatever
+ * is there: f = +infinity masks a row.  An infinity or NaN that does come in stays in its column to the sequence's end, as one or the other.
+ * Limits: n, d and sequences below 2^31. */
+size_t chicle_gated_scan_bytes(int64_t n, int64_t d, int32_t type);
+int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,
+                      const float *h0, int64_t n, int64_t d, int32_t type, void *y, int64_t ldy, float *last, float *states, void *workspace,
+                      size_t workspace_bytes, int32_t *flags, void *hip_stream);
+
+/* Its gradients by f, u and, where dh0 is not NULL, h0, from dy and, where it is not NULL, dlast, the gradient of `last`; the other arguments are
+ * those of the forward call, and what it left in states.  Rows of no sequence get zeros. */
+int chicle_gated_scan_grad(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide,
+                           int64_t sequences, const float *h0, const float *states, const void *dy, int64_t lddy, const float *dlast, int64_t n, int64_t d,
+                           int32_t type, void *df, int64_t lddf, void *du, int64_t lddu, float *dh0, void *workspace, size_t workspace_bytes,
+                           int32_t *flags, void *hip_stream);
+
+/* One row of each of n sequences: state = a state + (1 - a) u, in place, y = state.  state: n x d floats, rows ldstate apart. */
+int chicle_gated_step(const void *f, int64_t ldf, const void *u, int64_t ldu, float *state, int64_t ldstate, int64_t n, int64_t d, int32_t type, void *y,
+                      int64_t ldy, void *hip_stream);
 
 /* The 2-norm of `count` tensors together (norm: one float), and, where out is not NULL, out_k = in_k * min(1, max_norm / (norm + 1e-6)).
  * in, out, sizes and types are host arrays of count entries: device pointers of contiguous tensors, numbers of values and

@@ -9,4 +9,4 @@ step for models over categorical data.
 """
 from .binding import (ChicleError, ChicleRound, balance, library_path, load_library,  # noqa: F401
                       next_solver_count, projected_iteration_time, rebalance, scale_in, scale_out)
-from .train import TrainOps, load_train_library, train_library_path  # noqa: F401
+from .train import Packed8, TrainOps, load_train_library, train_library_path  # noqa: F401

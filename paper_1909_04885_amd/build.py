@@ -22,7 +22,7 @@ def sources():
 
 
 def train_sources():
-    return [os.path.join(CSRC_TRAIN, "chicle_train.hip")]
+    return [os.path.join(CSRC_TRAIN, name) for name in ("chicle_train.hip", "sequence.hip")]
 
 
 def _compile(path: str, files, verbose: bool) -> str:

@@ -1,0 +1,312 @@
+// Entry points of include/chicle_train.h for layers over sequences: rows in 8 bits, root-mean-square norm, gated recurrence.
+#include <algorithm>
+#include "entry.hpp"
+#include "gated_scan.hpp"
+#include "packed.hpp"
+#include "rms_norm.hpp"
+
+using namespace chicle_train;
+
+namespace {
+
+// Packed rows of d columns: both pointers, rows a multiple of 32 bytes apart.
+bool packed_ok(const void *q, const void *scales, int64_t ld, int64_t d)
+{
+    return placed(q, 16) && scales && ld >= round_up(d, PACK_GROUP) && ld % PACK_GROUP == 0;
+}
+
+Packed packed_rows(void *q, void *scales, int64_t ld) { return Packed{(int8_t *)q, (uint8_t *)scales, ld}; }
+Packed packed_from(const Packed &p, int64_t row) { return p.q ? Packed{p.q + row * p.ld, p.scales + row * (p.ld / PACK_GROUP), p.ld} : p; }
+
+bool sizes_ok(int64_t n, int64_t d) { return n >= 0 && d >= 1 && n <= INT32_MAX && d <= INT32_MAX; }
+
+// f(first row, rows, workgroups) for all n rows of `per_row` vectors.
+template <typename F>
+int with_vectors_of_rows(int64_t n, int64_t per_row, F f)
+{
+    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 31) / per_row);
+    for (int64_t first = 0; first < n; first += most) {
+        const int64_t many = std::min(most, n - first);
+        TRY(f(first, many, (unsigned)ceil_div(many * per_row, PACK_THREADS * PACK_EACH)));
+    }
+    return CHICLE_OK;
+}
+
+// ---- root-mean-square norm --------------------------------------------------------------------------------------------
+
+constexpr int RMS_FORWARD_VALUES = 32, RMS_GRAD_VALUES = 16;
+constexpr int RMS_GRAD_GRID = 1024;
+
+RowShape rms_shape(int64_t d, int32_t type, int first_values, int most_values)
+{
+    const int vec = 16 / size_of(type);
+    RowShape s = row_shape(d, vec, first_values, most_values);
+    if (s.lanes < PACK_GROUP / vec) s.lanes = PACK_GROUP / vec;            // (whole groups of columns)
+    return s;
+}
+
+int64_t rms_norm_parts(int64_t n, int64_t d, int32_t type)
+{
+    const RowShape s = rms_shape(d, type, RMS_GRAD_VALUES, RMS_GRAD_VALUES);
+    return std::min<int64_t>(ceil_div(n, s.threads / s.lanes), RMS_GRAD_GRID);
+}
+
+template <typename T, bool PACKED>
+int run_rms_norm_grad(RmsGrad<T, PACKED> a, const RowShape &r, int64_t parts, T *dgamma, hipStream_t stream)
+{
+    if (parts > 0)
+        TRY(with_vectors(r.vectors, [&](auto v) {
+            constexpr int NV = decltype(v)::value;
+            if constexpr (NV * Elem<T>::VEC <= RMS_GRAD_VALUES) {
+                auto kernel = r.threads > 256 ? rms_norm_grad_rows<T, NV, LN_MOST_THREADS, PACKED> : rms_norm_grad_rows<T, NV, 256, PACKED>;
+                const size_t lds = (size_t)r.threads * Elem<T>::VEC * sizeof(float);
+                int resident = 0;
+                if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, r.threads, lds) != hipSuccess || resident < 1) resident = 1;
+                const int64_t round = std::min<int64_t>((int64_t)resident * CUS, RMS_GRAD_GRID);
+                parts = std::min(parts, RMS_GRAD_GRID / round * round);
+                kernel<<<(unsigned)parts, r.threads, lds, stream>>>(a);
+            }
+            return launched("rms_norm_grad_rows");
+        }));
+    return with_rows(a.d, LN_SUM_COLUMNS, [&](int64_t first, int64_t, unsigned grid) {
+        rms_norm_grad_sums<T><<<grid, 1024, 0, stream>>>(a.part, (int)parts, a.d, first, dgamma);
+        return launched("rms_norm_grad_sums");
+    });
+}
+
+// ---- gated recurrence -------------------------------------------------------------------------------------------------
+
+// f(whether u is packed)
+template <typename F>
+int with_packed(bool packed, F f)
+{
+    return packed ? f(std::true_type()) : f(std::false_type());
+}
+
+template <typename T, bool PACKED> ScanInput<T, PACKED> scan_input(const void *u, int64_t ldu, const void *scales)
+{
+    if constexpr (PACKED) return {(const int8_t *)u, (const uint8_t *)scales, ldu};
+    else return {(const T *)u, ldu};
+}
+
+int scan_check(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,
+               const void *h0, const void *states, int64_t n, int64_t d, int32_t type)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (!sizes_ok(n, d) || ldf < d || ldu < d || sequences < 0 || sequences > INT32_MAX || (!offsets && sequences != 1))
+        return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, sequences %lld, or a row distance", (long long)n, (long long)d, (long long)sequences);
+    const int s = size_of(type);
+    if ((offsets && !placed(offsets, wide ? 8 : 4)) || (h0 && !placed(h0, 4)) || (states && !placed(states, 4)))
+        return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    if (n > 0 && (!placed(f, s) || (u_scales ? !packed_ok(u, u_scales, ldu, d) : !placed(u, s)))) return fail(CHICLE_EINVAL, "a null or misplaced input");
+    return CHICLE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int chicle_pack8(const void *x, int64_t ldx, int64_t n, int64_t d, int32_t type, void *q, void *scales, int64_t ldq, void *hip_stream)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (!sizes_ok(n, d) || ldx < d) return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, or a row distance", (long long)n, (long long)d);
+    if (n == 0) return CHICLE_OK;
+    if (!placed(x, size_of(type)) || !packed_ok(q, scales, ldq, d)) return fail(CHICLE_EINVAL, "a null or misplaced pointer, or packed rows too near");
+    const Packed p = packed_rows(q, scales, ldq);
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        const int per_row = (int)(round_up(d, PACK_GROUP) / Elem<T>::VEC);
+        return with_vectors_of_rows(n, per_row, [&](int64_t first, int64_t many, unsigned grid) {
+            pack_rows<T><<<grid, PACK_THREADS, 0, (hipStream_t)hip_stream>>>((const T *)x + first * ldx, ldx, many, d, per_row, packed_from(p, first));
+            return launched("pack_rows");
+        });
+    });
+}
+
+int chicle_unpack8(const void *q, const void *scales, int64_t ldq, int64_t n, int64_t d, int32_t type, void *out, int64_t ldo, void *hip_stream)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (!sizes_ok(n, d) || ldo < d) return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, or a row distance", (long long)n, (long long)d);
+    if (n == 0) return CHICLE_OK;
+    if (!placed(out, size_of(type)) || !packed_ok(q, scales, ldq, d)) return fail(CHICLE_EINVAL, "a null or misplaced pointer, or packed rows too near");
+    const Packed p = packed_rows((void *)q, (void *)scales, ldq);
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        const int per_row = (int)(round_up(d, PACK_GROUP) / Elem<T>::VEC);
+        return with_vectors_of_rows(n, per_row, [&](int64_t first, int64_t many, unsigned grid) {
+            unpack_rows<T><<<grid, PACK_THREADS, 0, (hipStream_t)hip_stream>>>(packed_from(p, first), many, d, per_row, (T *)out + first * ldo, ldo);
+            return launched("unpack_rows");
+        });
+    });
+}
+
+int chicle_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *gamma, int64_t n, int64_t d, int32_t type, float eps,
+                    void *sum, int64_t ldsum, void *y, int64_t ldy, void *y_scales, void *sum8, void *sum8_scales, int64_t ldsum8, float *rstd,
+                    void *hip_stream)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (!sizes_ok(n, d) || ldx < d || (residual && ldres < d) || (sum && ldsum < d) || ldy < d || !(eps >= 0.f))
+        return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, a row distance or eps", (long long)n, (long long)d);
+    if (n == 0) return CHICLE_OK;
+    const int s = size_of(type);
+    if (!placed(x, s) || (residual && !placed(residual, s)) || !placed(gamma, s) || (sum && !placed(sum, s)) || !placed(rstd, 4) ||
+        (y_scales ? !packed_ok(y, y_scales, ldy, d) : !placed(y, s)) || (sum8 && !packed_ok(sum8, sum8_scales, ldsum8, d)))
+        return fail(CHICLE_EINVAL, "a null or misplaced pointer, or packed rows too near");
+    const RowShape r = rms_shape(d, type, RMS_FORWARD_VALUES / 2, RMS_FORWARD_VALUES);
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        return with_vectors(r.vectors, [&](auto v) {
+            constexpr int NV = decltype(v)::value;
+            if constexpr (NV * Elem<T>::VEC <= RMS_FORWARD_VALUES) {
+                auto kernel = r.threads > 256 ? rms_norm_rows<T, NV, LN_MOST_THREADS> : rms_norm_rows<T, NV, 256>;
+                return with_rows(n, r.threads / r.lanes, [&](int64_t first, int64_t many, unsigned grid) {
+                    RmsRows<T> a;
+                    a.x = (const T *)x + first * ldx;
+                    a.residual = residual ? (const T *)residual + first * ldres : nullptr;
+                    a.gamma = (const T *)gamma;
+                    a.sum = sum ? (T *)sum + first * ldsum : nullptr;
+                    a.y = y_scales ? nullptr : (T *)y + first * ldy;
+                    a.rstd = rstd + first;
+                    a.y8 = packed_from(packed_rows(y_scales ? y : nullptr, y_scales, ldy), first);
+                    a.sum8 = packed_from(packed_rows(sum8, sum8_scales, ldsum8), first);
+                    a.ldx = ldx; a.ldres = ldres; a.ldsum = ldsum; a.ldy = ldy;
+                    a.n = many; a.d = d;
+                    a.lanes = r.lanes;
+                    a.eps = eps;
+                    kernel<<<grid, r.threads, 0, (hipStream_t)hip_stream>>>(a);
+                    return launched("rms_norm_rows");
+                });
+            }
+            return (int)CHICLE_OK;
+        });
+    });
+}
+
+size_t chicle_rms_norm_grad_bytes(int64_t n, int64_t d, int32_t type)
+{
+    if (!type_ok(type) || !sizes_ok(n, d)) return 0;
+    Carver c(nullptr);
+    c.take<float>(rms_norm_parts(n, d, type) * d);
+    return c.total();
+}
+
+int chicle_rms_norm_grad(const void *dy, int64_t lddy, const void *sum, int64_t ldsum, const void *sum_scales, const void *gamma, const float *rstd,
+                         const void *dsum, int64_t lddsum, int64_t n, int64_t d, int32_t type, void *dx, int64_t lddx, void *dgamma, void *workspace,
+                         size_t workspace_bytes, void *hip_stream)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (!sizes_ok(n, d) || ldsum < d || lddy < d || lddx < d || (dsum && lddsum < d))
+        return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, or a row distance", (long long)n, (long long)d);
+    const int s = size_of(type);
+    if (!placed(gamma, s) || !placed(dgamma, s) ||
+        (n > 0 && (!placed(dy, s) || !placed(dx, s) || !placed(rstd, 4) || (dsum && !placed(dsum, s)) ||
+                   (sum_scales ? !packed_ok(sum, sum_scales, ldsum, d) : !placed(sum, s)))))
+        return fail(CHICLE_EINVAL, "a null or misplaced pointer, or packed rows too near");
+    TRY(check_workspace(workspace, workspace_bytes, chicle_rms_norm_grad_bytes(n, d, type)));
+    const RowShape r = rms_shape(d, type, RMS_GRAD_VALUES, RMS_GRAD_VALUES);
+    const int64_t parts = rms_norm_parts(n, d, type);
+    Carver c(workspace);
+    float *part = c.take<float>(parts * d);
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        return with_packed(sum_scales != nullptr, [&](auto packed) {
+            constexpr bool PACKED = decltype(packed)::value;
+            RmsGrad<T, PACKED> a;
+            if constexpr (PACKED) a.r = {(const int8_t *)sum, (const uint8_t *)sum_scales, ldsum};
+            else a.r = {(const T *)sum, ldsum};
+            a.dy = (const T *)dy; a.dr = (const T *)dsum; a.gamma = (const T *)gamma;
+            a.rstd = rstd;
+            a.dx = (T *)dx;
+            a.part = part;
+            a.lddy = lddy; a.lddr = lddsum; a.lddx = lddx;
+            a.n = n; a.d = d;
+            a.lanes = r.lanes;
+            return run_rms_norm_grad<T, PACKED>(a, r, parts, (T *)dgamma, (hipStream_t)hip_stream);
+        });
+    });
+}
+
+size_t chicle_gated_scan_bytes(int64_t n, int64_t d, int32_t type)
+{
+    if (!type_ok(type) || !sizes_ok(n, d)) return 0;
+    Carver c(nullptr);
+    return c.total();
+}
+
+int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,
+                      const float *h0, int64_t n, int64_t d, int32_t type, void *y, int64_t ldy, float *last, float *states, void *workspace,
+                      size_t workspace_bytes, int32_t *flags, void *hip_stream)
+{
+    TRY(scan_check(f, ldf, u, ldu, u_scales, offsets, wide, sequences, h0, states, n, d, type));
+    if (ldy < d) return fail(CHICLE_EINVAL, "a row distance is shorter than a row");
+    if ((n > 0 && !placed(y, size_of(type))) || (last && !placed(last, 4))) return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    TRY(check_workspace(workspace, workspace_bytes, chicle_gated_scan_bytes(n, d, type)));
+    if (sequences == 0 && n == 0) return CHICLE_OK;
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        return with_packed(u_scales != nullptr, [&](auto packed) {
+            constexpr bool PACKED = decltype(packed)::value;
+            Scan<T, PACKED> a = {};
+            a.u = scan_input<T, PACKED>(u, ldu, u_scales);
+            a.order = {offsets, wide, sequences, n};
+            a.f = (const T *)f; a.h0 = h0; a.states = states; a.last = last; a.y = (T *)y;
+            a.ldf = ldf; a.ldy = ldy; a.d = d;
+            a.flags = flags;
+            const dim3 grid((unsigned)ceil_div(d, 64), (unsigned)std::min<int64_t>(std::max<int64_t>(sequences, 1), 4096));
+            scan_forward<T, PACKED><<<grid, 64, 0, (hipStream_t)hip_stream>>>(a);
+            return launched("scan_forward");
+        });
+    });
+}
+
+int chicle_gated_scan_grad(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide,
+                           int64_t sequences, const float *h0, const float *states, const void *dy, int64_t lddy, const float *dlast, int64_t n, int64_t d,
+                           int32_t type, void *df, int64_t lddf, void *du, int64_t lddu, float *dh0, void *workspace, size_t workspace_bytes,
+                           int32_t *flags, void *hip_stream)
+{
+    TRY(scan_check(f, ldf, u, ldu, u_scales, offsets, wide, sequences, h0, states, n, d, type));
+    if (lddy < d || lddf < d || lddu < d) return fail(CHICLE_EINVAL, "a row distance is shorter than a row");
+    const int s = size_of(type);
+    if ((n > 0 && (!placed(dy, s) || !placed(df, s) || !placed(du, s) || !states)) || (dlast && !placed(dlast, 4)) || (dh0 && !placed(dh0, 4)))
+        return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    TRY(check_workspace(workspace, workspace_bytes, chicle_gated_scan_bytes(n, d, type)));
+    if (sequences == 0 && n == 0) return CHICLE_OK;
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        return with_packed(u_scales != nullptr, [&](auto packed) {
+            constexpr bool PACKED = decltype(packed)::value;
+            Scan<T, PACKED> a = {};
+            a.u = scan_input<T, PACKED>(u, ldu, u_scales);
+            a.order = {offsets, wide, sequences, n};
+            a.f = (const T *)f; a.dy = (const T *)dy; a.h0 = h0; a.dlast = dlast; a.states = (float *)states; a.dh0 = dh0;
+            a.df = (T *)df; a.du = (T *)du;
+            a.ldf = ldf; a.lddy = lddy; a.lddf = lddf; a.lddu = lddu; a.d = d;
+            a.flags = flags;
+            const dim3 grid((unsigned)ceil_div(d, 64), (unsigned)std::min<int64_t>(std::max<int64_t>(sequences, 1), 4096));
+            scan_backward<T, PACKED><<<grid, 64, 0, (hipStream_t)hip_stream>>>(a);
+            return launched("scan_backward");
+        });
+    });
+}
+
+int chicle_gated_step(const void *f, int64_t ldf, const void *u, int64_t ldu, float *state, int64_t ldstate, int64_t n, int64_t d, int32_t type, void *y,
+                      int64_t ldy, void *hip_stream)
+{
+    if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
+    if (!sizes_ok(n, d) || ldf < d || ldu < d || ldstate < d || ldy < d)
+        return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, or a row distance", (long long)n, (long long)d);
+    if (n == 0) return CHICLE_OK;
+    const int s = size_of(type);
+    if (!placed(f, s) || !placed(u, s) || !placed(y, s) || !placed(state, 4)) return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    const int lanes = pow2_at_least(ceil_div(d, 16 / s), STEP_THREADS);
+    return with_type(type, [&](auto t) {
+        typedef decltype(t) T;
+        return with_rows(n, STEP_THREADS / lanes, [&](int64_t first, int64_t many, unsigned grid) {
+            scan_step<T><<<grid, STEP_THREADS, 0, (hipStream_t)hip_stream>>>((const T *)f + first * ldf, ldf, (const T *)u + first * ldu, ldu,
+                                                                             state + first * ldstate, ldstate, (T *)y + first * ldy, ldy, many, d, lanes);
+            return launched("scan_step");
+        });
+    });
+}
+
+}  // extern "C"

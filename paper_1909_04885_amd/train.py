@@ -12,7 +12,7 @@ from __future__ import annotations
 import ctypes
 import os
 from array import array
-from typing import Optional, Sequence
+from typing import Any, NamedTuple, Optional, Sequence
 
 from .binding import EDEVICE, EINVAL, OK, ChicleError
 
@@ -23,7 +23,8 @@ _lib = None
 TRAIN_EXPORTS = [
     "chicle_softmax_loss_bytes", "chicle_softmax_loss", "chicle_softmax_loss_grad", "chicle_embed",
     "chicle_embed_grad_bytes", "chicle_embed_grad", "chicle_layer_norm", "chicle_layer_norm_grad_bytes",
-    "chicle_layer_norm_grad", "chicle_clip_grads_bytes", "chicle_clip_grads", "chicle_train_take_flags",
+    "chicle_layer_norm_grad", "chicle_pack8", "chicle_unpack8", "chicle_rms_norm", "chicle_rms_norm_grad_bytes", "chicle_rms_norm_grad",
+    "chicle_gated_scan_bytes", "chicle_gated_scan", "chicle_gated_scan_grad", "chicle_gated_step", "chicle_clip_grads_bytes", "chicle_clip_grads", "chicle_train_take_flags",
     "chicle_train_last_error",
 ]
 
@@ -53,6 +54,15 @@ def load_train_library():
         "chicle_layer_norm": (i32, [vp, i64, vp, vp, i64, i64, i32, f32, vp, i64, vp, vp, vp]),
         "chicle_layer_norm_grad_bytes": (sz, [i64, i64, i32]),
         "chicle_layer_norm_grad": (i32, [vp, i64, vp, i64, vp, vp, vp, i64, i64, i32, vp, i64, vp, vp, vp, sz, vp]),
+        "chicle_pack8": (i32, [vp, i64, i64, i64, i32, vp, vp, i64, vp]),
+        "chicle_unpack8": (i32, [vp, vp, i64, i64, i64, i32, vp, i64, vp]),
+        "chicle_rms_norm": (i32, [vp, i64, vp, i64, vp, i64, i64, i32, f32, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp]),
+        "chicle_rms_norm_grad_bytes": (sz, [i64, i64, i32]),
+        "chicle_rms_norm_grad": (i32, [vp, i64, vp, i64, vp, vp, vp, vp, i64, i64, i64, i32, vp, i64, vp, vp, sz, vp]),
+        "chicle_gated_scan_bytes": (sz, [i64, i64, i32]),
+        "chicle_gated_scan": (i32, [vp, i64, vp, i64, vp, vp, i32, i64, vp, i64, i64, i32, vp, i64, vp, vp, vp, sz, vp, vp]),
+        "chicle_gated_scan_grad": (i32, [vp, i64, vp, i64, vp, vp, i32, i64, vp, vp, vp, i64, vp, i64, i64, i32, vp, i64, vp, i64, vp, vp, sz, vp, vp]),
+        "chicle_gated_step": (i32, [vp, i64, vp, i64, vp, i64, i64, i64, i32, vp, i64, vp]),
         "chicle_clip_grads_bytes": (sz, [i32]),
         "chicle_clip_grads": (i32, [vp, vp, vp, vp, i32, f32, vp, vp, sz, vp]),
         "chicle_train_take_flags": (i32, [vp, vp, vp]),
@@ -69,6 +79,17 @@ def load_train_library():
 def _at(a: array) -> int:
     """The address of a host array, which stays where it is while it is not changed."""
     return a.buffer_info()[0] if len(a) else 0
+
+
+GROUP = 32                              # columns of a packed row with one scale
+SCAN_KEPT = 32                          # rows from one state that a scan keeps to the next
+
+
+class Packed8(NamedTuple):
+    """Rows kept in 8 bits: values, int8 [n, d in whole groups of 32], their scales, uint8 [n, groups], a byte e + 127 for 2^e, and d."""
+    values: Any
+    scales: Any
+    d: int
 
 
 class TrainOps:
@@ -246,6 +267,167 @@ class TrainOps:
                    dbeta.data_ptr(), ws.data_ptr(), nbytes)
         return dx, dgamma, dbeta
 
+    # -- rows kept in 8 bits
+    def _packed(self, p: Packed8, name: str, n: Optional[int] = None, cols: Optional[int] = None):
+        """The addresses of packed rows and their distance."""
+        q, scales, d = p
+        whole = -(-d // GROUP) * GROUP
+        if (q.device != self.device or q.dtype != self._torch.int8 or tuple(q.shape) != (q.shape[0], whole) or not q.is_contiguous() or d < 1 or
+                scales.device != self.device or scales.dtype != self._torch.uint8 or tuple(scales.shape) != (q.shape[0], whole // GROUP) or
+                not scales.is_contiguous() or (n is not None and q.shape[0] != n) or (cols is not None and d != cols)):
+            raise ChicleError(EINVAL, "%s must be contiguous packed rows on %s, of the other inputs' size" % (name, self.device))
+        return q.data_ptr(), scales.data_ptr(), whole
+
+    def _new_packed(self, n: int, d: int) -> Packed8:
+        groups = -(-d // GROUP)
+        return Packed8(self._empty((n, groups * GROUP), self._torch.int8), self._empty((n, groups), self._torch.uint8), d)
+
+    def pack8(self, x) -> Packed8:
+        """Rows x [n, d] in 8 bits, 32 columns to a scale that is a power of two."""
+        t, ldx = self._matrix(x, "x")
+        n, d = x.shape
+        out = self._new_packed(n, d)
+        qp, sp, ldq = self._packed(out, "out")
+        self._call(self._L.chicle_pack8, x.data_ptr(), ldx, n, d, t, qp, sp, ldq)
+        return out
+
+    def unpack8(self, p: Packed8, dtype):
+        """The values that packed rows stand for, [n, d] of a type."""
+        qp, sp, ldq = self._packed(p, "p")
+        if dtype not in self._types:
+            raise ChicleError(EINVAL, "rows unpack to float32, bfloat16 or float16")
+        n, d = p.values.shape[0], p.d
+        out = self._empty((n, d), dtype)
+        self._call(self._L.chicle_unpack8, qp, sp, ldq, n, d, self._types[dtype], out.data_ptr(), d)
+        return out
+
+    # -- root-mean-square norm
+    def rms_norm(self, x, gamma, residual=None, eps: float = 1e-5, y8: bool = False, keep8: bool = False):
+        """(y, r, rstd, kept): r = x + residual (x itself without one), y = r rstd gamma, rows packed where y8 is set; kept: r as packed
+        rows where keep8 is set, which rms_norm_grad takes in its place, else None."""
+        t, ldx = self._matrix(x, "x")
+        n, d = x.shape
+        gp = self._vector(gamma, "gamma", d, x.dtype)
+        resp = ldres = None
+        r, rp, f32 = x, None, self._torch.float32
+        if residual is not None:
+            _, ldres = self._matrix(residual, "residual", x, d)
+            if residual.shape[0] != n:
+                raise ChicleError(EINVAL, "residual needs a row per row of x")
+            resp, r = residual.data_ptr(), self._empty((n, d), x.dtype)
+            rp = r.data_ptr()
+        rstd = self._empty(n, f32)
+        if y8:
+            y = self._new_packed(n, d)
+            yp, ysp, ldy = self._packed(y, "y")
+        else:
+            y = self._empty((n, d), x.dtype)
+            yp, ysp, ldy = y.data_ptr(), None, d
+        kept, kp, ksp, ldk = None, None, None, 0
+        if keep8:
+            kept = self._new_packed(n, d)
+            kp, ksp, ldk = self._packed(kept, "kept")
+        self._call(self._L.chicle_rms_norm, x.data_ptr(), ldx, resp, ldres or 0, gp, n, d, t, eps, rp, d, yp, ldy, ysp, kp, ksp, ldk, rstd.data_ptr())
+        return y, r, rstd, kept
+
+    def rms_norm_grad(self, dy, r, gamma, rstd, dr=None):
+        """(dx, dgamma) from dy and what rms_norm returned: r, or what it kept of r in 8 bits; dx is the gradient of x and of the residual, with dr
+        added, the gradient that reaches r on the other way."""
+        t, lddy = self._matrix(dy, "dy")
+        n, d = dy.shape
+        if isinstance(r, Packed8):
+            rp, rsp, ldr = self._packed(r, "r", n, d)
+        else:
+            _, ldr = self._matrix(r, "r", dy, d)
+            rp, rsp = r.data_ptr(), None
+            if r.shape[0] != n:
+                raise ChicleError(EINVAL, "r needs a row per row of dy")
+        gp, sp = self._vector(gamma, "gamma", d, dy.dtype), self._vector(rstd, "rstd", n, self._torch.float32)
+        drp = lddr = None
+        if dr is not None:
+            _, lddr = self._matrix(dr, "dr", dy, d)
+            if dr.shape[0] != n:
+                raise ChicleError(EINVAL, "dr needs a row per row of dy")
+            drp = dr.data_ptr()
+        dx, dgamma = self._empty((n, d), dy.dtype), self._empty(d, dy.dtype)
+        nbytes = self._L.chicle_rms_norm_grad_bytes(n, d, t)
+        ws = self._workspace(nbytes)
+        self._call(self._L.chicle_rms_norm_grad, dy.data_ptr(), lddy, rp, ldr, rsp, gp, sp, drp, lddr or 0, n, d, t, dx.data_ptr(), d,
+                   dgamma.data_ptr(), ws.data_ptr(), nbytes)
+        return dx, dgamma
+
+    # -- gated recurrence
+    def _scan_inputs(self, f, u, offsets, h0):
+        """What the scan and its gradient take alike: (arguments, sequences, n, d, type)."""
+        t, ldf = self._matrix(f, "f")
+        n, d = f.shape
+        if isinstance(u, Packed8):
+            up, usp, ldu = self._packed(u, "u", n, d)
+        else:
+            _, ldu = self._matrix(u, "u", f, d)
+            up, usp = u.data_ptr(), None
+            if u.shape[0] != n:
+                raise ChicleError(EINVAL, "u needs a row per row of f")
+        op, wide, k = None, 0, 1
+        if offsets is not None:
+            op, wide = self._indices(offsets, "offsets")
+            k = offsets.shape[0] - 1
+            if k < 0:
+                raise ChicleError(EINVAL, "offsets need a value more than there are sequences")
+        hp = None if h0 is None else self._states(h0, "h0", k, d)
+        return (f.data_ptr(), ldf, up, ldu, usp, op, wide, k, hp), k, n, d, t
+
+    def _states(self, a, name: str, rows: int, d: int):
+        if a.device != self.device or a.dtype != self._torch.float32 or tuple(a.shape) != (rows, d) or not a.is_contiguous():
+            raise ChicleError(EINVAL, "%s must be a contiguous float32 tensor of %d x %d values on %s" % (name, rows, d, self.device))
+        if a.requires_grad and self._torch.is_grad_enabled():
+            self._no_graph(name)
+        return a.data_ptr()
+
+    def gated_scan(self, f, u, offsets=None, h0=None, last: bool = False, states: bool = False):
+        """(y, last, states): h_t = a_t h_{t-1} + (1 - a_t) u_t with a = sigmoid(f) over the rows offsets[j] to offsets[j + 1] - 1 of every sequence (without
+        offsets one sequence of all rows), from h0 [sequences, d] float32 or zeros.  u: rows of f's type, or packed ones.  last: the states after the
+        sequences, and states: those that enter every 32nd row, which gated_scan_grad takes, where they are asked for, else None."""
+        args, k, n, d, t = self._scan_inputs(f, u, offsets, h0)
+        f32 = self._torch.float32
+        y = self._empty((n, d), f.dtype)
+        end = self._empty((k, d), f32) if last else None
+        kept = self._empty((-(-n // SCAN_KEPT), d), f32) if states else None
+        nbytes = self._L.chicle_gated_scan_bytes(n, d, t)
+        ws = self._workspace(nbytes)
+        self._call(self._L.chicle_gated_scan, *args, n, d, t, y.data_ptr(), d, end.data_ptr() if last else None, kept.data_ptr() if states else None,
+                   ws.data_ptr(), nbytes, self._flags())
+        return y, end, kept
+
+    def gated_scan_grad(self, f, u, states, dy, offsets=None, h0=None, dlast=None):
+        """(df, du, dh0) from dy, dlast, the gradient of the last states (or None: zeros), and what gated_scan took and returned; dh0 is None without h0."""
+        args, k, n, d, t = self._scan_inputs(f, u, offsets, h0)
+        _, lddy = self._matrix(dy, "dy", f, d)
+        if dy.shape[0] != n:
+            raise ChicleError(EINVAL, "dy needs a row per row of f")
+        sp = self._states(states, "states", -(-n // SCAN_KEPT), d)
+        dlp = None if dlast is None else self._states(dlast, "dlast", k, d)
+        df, du = self._empty((n, d), f.dtype), self._empty((n, d), f.dtype)
+        dh0 = None if h0 is None else self._empty((k, d), self._torch.float32)
+        nbytes = self._L.chicle_gated_scan_bytes(n, d, t)
+        ws = self._workspace(nbytes)
+        self._call(self._L.chicle_gated_scan_grad, *args, sp, dy.data_ptr(), lddy, dlp, n, d, t, df.data_ptr(), d, du.data_ptr(), d,
+                   None if dh0 is None else dh0.data_ptr(), ws.data_ptr(), nbytes, self._flags())
+        return df, du, dh0
+
+    def gated_step(self, f, u, state):
+        """y: one row of every sequence, whose states [n, d] float32 become a state + (1 - a) u in place."""
+        t, ldf = self._matrix(f, "f")
+        n, d = f.shape
+        _, ldu = self._matrix(u, "u", f, d)
+        ts, lds = self._matrix(state, "state", None, d)
+        if ts != 0 or u.shape[0] != n or state.shape[0] != n:
+            raise ChicleError(EINVAL, "u and state need a row per row of f, and state the type float32")
+        y = self._empty((n, d), f.dtype)
+        self._call(self._L.chicle_gated_step, f.data_ptr(), ldf, u.data_ptr(), ldu, state.data_ptr(), lds, n, d, t, y.data_ptr(), d)
+        self._new_version(state)
+        return y
+
     # -- clipping
     def _pointers(self, tensors, name: str):
         """Addresses, numbers of values and types of contiguous tensors on this GPU (a list at a time: there are many)."""
@@ -282,10 +464,10 @@ class TrainOps:
         return self._clip(grads, grads if out is None else out, max_norm)
 
     def sync(self):
-        """Wait for the current stream; raise if a label or token was past the end that no sync has raised yet.  What another stream
+        """Wait for the current stream; raise if a label or token was past the end, or an offset no row, that no sync has raised yet.  What another stream
         reports meanwhile is raised by this sync or by a later one."""
         taken = self._empty(1, self._torch.int32)
         self._call(self._L.chicle_train_take_flags, self._flags(), taken.data_ptr())
         bits = int(taken.item())
         if bits:
-            raise ChicleError(EDEVICE, "%s out of range" % " and ".join(s for b, s in ((1, "a label"), (2, "a token")) if bits & b))
+            raise ChicleError(EDEVICE, "%s out of range" % " and ".join(s for b, s in ((1, "a label"), (2, "a token"), (4, "an offset")) if bits & b))
