@@ -89,12 +89,60 @@ template <typename T, bool PACKED> ScanInput<T, PACKED> scan_input(const void *u
     else return {(const T *)u, ldu};
 }
 
+// Tiles, and what workgroups hand on in the workspace: a ticket, then words.
+struct ScanPlan {
+    int64_t tiles, blocks, words;
+    unsigned *ticket;
+    unsigned long long *products, *handed;
+    size_t bytes;
+};
+
+ScanPlan scan_plan(int64_t n, int64_t d, int32_t type, void *workspace)
+{
+    ScanPlan p = {};
+    const int64_t columns = type == CHICLE_F32 ? SCAN_COLS<float> : SCAN_COLS<bf16>;
+    p.tiles = n > 0 ? ceil_div(n, SCAN_TILE) : 1;
+    p.blocks = ceil_div(d, columns);
+    Carver c(workspace);
+    if (p.tiles > 1) {
+        const int64_t line = p.blocks * columns, runs = ceil_div(p.tiles, SCAN_RUN);
+        p.words = (p.tiles + runs) * line;
+        p.ticket = c.take<unsigned>(1);
+        p.products = c.take<unsigned long long>(p.words);
+        p.handed = p.products + p.tiles * line;
+    }
+    p.bytes = c.total();
+    return p;
+}
+
+// Clears what is handed on, and launches the kernel.
+template <typename T, bool PACKED>
+int run_scan(Scan<T, PACKED> a, int32_t type, bool backward, void *workspace, hipStream_t stream)
+{
+    const ScanPlan p = scan_plan(a.order.n, a.d, type, workspace);
+    a.tiles = (unsigned)p.tiles;
+    a.blocks = (unsigned)p.blocks;
+    if (p.tiles > 1) {
+        a.ticket = p.ticket;
+        a.products = p.products;
+        a.handed = p.handed;
+        scan_begin<<<(unsigned)std::min<int64_t>(ceil_div(p.words, 256), 2048), 256, 0, stream>>>(p.ticket, p.products, p.words);
+        TRY(launched("scan_begin"));
+    }
+    const unsigned grid = (unsigned)(p.tiles * p.blocks);
+    if (backward) scan_backward<T, PACKED><<<grid, SCAN_THREADS, 0, stream>>>(a);
+    else scan_forward<T, PACKED><<<grid, SCAN_THREADS, 0, stream>>>(a);
+    return launched(backward ? "scan_backward" : "scan_forward");
+}
+
 int scan_check(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,
                const void *h0, const void *states, int64_t n, int64_t d, int32_t type)
 {
     if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
     if (!sizes_ok(n, d) || ldf < d || ldu < d || sequences < 0 || sequences > INT32_MAX || (!offsets && sequences != 1))
         return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, sequences %lld, or a row distance", (long long)n, (long long)d, (long long)sequences);
+    const ScanPlan p = scan_plan(n, d, type, nullptr);
+    if (p.tiles * p.blocks >= (int64_t)1 << 24) return fail(CHICLE_EINVAL, "too many values");              // (a launch has fewer than 2^32 threads)
     const int s = size_of(type);
     if ((offsets && !placed(offsets, wide ? 8 : 4)) || (h0 && !placed(h0, 4)) || (states && !placed(states, 4)))
         return fail(CHICLE_EINVAL, "a null or misplaced pointer");
@@ -229,8 +277,7 @@ int chicle_rms_norm_grad(const void *dy, int64_t lddy, const void *sum, int64_t 
 size_t chicle_gated_scan_bytes(int64_t n, int64_t d, int32_t type)
 {
     if (!type_ok(type) || !sizes_ok(n, d)) return 0;
-    Carver c(nullptr);
-    return c.total();
+    return scan_plan(n, d, type, nullptr).bytes;
 }
 
 int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,
@@ -252,9 +299,7 @@ int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, co
             a.f = (const T *)f; a.h0 = h0; a.states = states; a.last = last; a.y = (T *)y;
             a.ldf = ldf; a.ldy = ldy; a.d = d;
             a.flags = flags;
-            const dim3 grid((unsigned)ceil_div(d, 64), (unsigned)std::min<int64_t>(std::max<int64_t>(sequences, 1), 4096));
-            scan_forward<T, PACKED><<<grid, 64, 0, (hipStream_t)hip_stream>>>(a);
-            return launched("scan_forward");
+            return run_scan(a, type, false, workspace, (hipStream_t)hip_stream);
         });
     });
 }
@@ -282,9 +327,7 @@ int chicle_gated_scan_grad(const void *f, int64_t ldf, const void *u, int64_t ld
             a.df = (T *)df; a.du = (T *)du;
             a.ldf = ldf; a.lddy = lddy; a.lddf = lddf; a.lddu = lddu; a.d = d;
             a.flags = flags;
-            const dim3 grid((unsigned)ceil_div(d, 64), (unsigned)std::min<int64_t>(std::max<int64_t>(sequences, 1), 4096));
-            scan_backward<T, PACKED><<<grid, 64, 0, (hipStream_t)hip_stream>>>(a);
-            return launched("scan_backward");
+            return run_scan(a, type, true, workspace, (hipStream_t)hip_stream);
         });
     });
 }
