@@ -109,7 +109,7 @@ int chicle_rms_norm_grad(const void *dy, int64_t lddy, const void *sum, int64_t 
  * they hold.  Offsets that descend or are no rows of the call set a bit of *flags, and results are then not defined; nothing is read or
  * written outside of the tensors.  h0 (or NULL: zeros) and last (or NULL): sequences x d floats, the state before a sequence's first row and
  * after its last.  u is of the type where u_scales is NULL, else packed rows, ldu bytes apart.  states (or NULL): n / 32, rounded up, x d floats, the state
- * that enters every 32nd row, which the gradient takes.  Of a gate beyond +-87, +-infinity too, nothing comes through on the side that it closes, whatever
+ * that enters every 32nd row, which the gradient takes.  Of a gate beyond +-104, +-infinity too, nothing comes through on the side that it closes, whatever
  * is there: f = +infinity masks a row.  An infinity or NaN that does come in stays in its column to the sequence's end, as one or the other.
  * Limits: n, d and sequences below 2^31. */
 size_t chicle_gated_scan_bytes(int64_t n, int64_t d, int32_t type);

@@ -1,14 +1,16 @@
 // A gated linear recurrence over the rows of sequences, its gradients, and its form for one row of every sequence.
 //
-//   a_t = 1 / (1 + exp(-f_t)),  h_t = a_t h_{t-1} + (1 - a_t) u_t,  y_t = h_t, from the sequence's first state or from 0
+//   a_t = 1 / (1 + exp(-f_t)),  c_t = 1 - a_t,  h_t = a_t h_{t-1} + c_t u_t,  y_t = h_t, from the sequence's first state or from 0
 //   G_t = dy_t + a_{t+1} G_{t+1}, the last row's with the gradient of the last state:
-//   du_t = (1 - a_t) G_t,  df_t = G_t (h_{t-1} - u_t) a_t (1 - a_t),  dh0 = a_first G_first
+//   du_t = c_t G_t,  df_t = G_t (h_{t-1} - u_t) a_t c_t,  dh0 = a_first G_first
 //
-// Of a gate, s = min(a, 1 - a) = e / (1 + e) with e = exp(-|f|) is what is held, with the sign of f: both a and 1 - a come from it without
-// losing what is small, h_t = (1 - s) x + s z with x the one of h_{t-1} and u_t that keeps more.  Gates beyond +-87 are closed: s = 0, and what they
-// keep out counts nowhere, whatever it holds.
+// Of a gate, the smaller share is worked out, s = e / (1 + e) with e = exp(-|f|), the other one is 1 - s: neither loses what is small.  Where
+// e is no 32-bit number (beyond +-104) a gate is closed, s = 0, and what it keeps out counts nowhere, whatever it holds.
 //
-// States are 32-bit floats.  The forward pass leaves the state that enters every SCAN_KEPT-th row; the gradient works out those between again.
+// States are 32-bit floats.  A workgroup has a tile of SCAN_TILE rows, a wavefront SCAN_ROWS of them, a lane SCAN_V columns, held in registers and
+// read once.  What the rows of a wavefront do to the state that comes into them is a product and a sum; those of the tile are joined in LDS, and tiles
+// hand on what comes out of them (scan_hand).  The forward pass leaves the state that enters every SCAN_KEPT-th row; the gradient works out those
+// between again from the tile's first, and goes through the tiles from the last one.
 #pragma once
 #include <type_traits>
 #include "elements.hpp"
@@ -21,71 +23,60 @@ constexpr int SCAN_KEPT = 32;
 // s with the sign of f.
 __device__ __forceinline__ float gate_of(float f)
 {
-    constexpr float LOG2E = 1.44269502162933349609375f, LOG2E_REST = 1.92596299e-8f, LN2 = 0.693147182f;
-    const float x = fabsf(f), p = -x * LOG2E;
-    const float rest = fmaf(-x, LOG2E_REST, fmaf(-x, LOG2E, -p));         // what rounding took from the power of two
-    float e = __builtin_amdgcn_exp2f(p);
-    e = fmaf(e, rest * LN2, e);
-    const float s = e * __builtin_amdgcn_rcpf(1.f + e);
-    return copysignf(x > 87.f ? 0.f : s, f);
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(f));
+    return copysignf(e * __builtin_amdgcn_rcpf(1.f + e), f);
 }
 
-// (1 - s) x, and s x; nothing of x where its share is none.
-__device__ __forceinline__ float gate_more(float s, float x) { return s == 0.f ? x : fmaf(-s, x, x); }
-__device__ __forceinline__ float gate_less(float s, float x) { return s == 0.f ? 0.f : s * x; }
+struct GateShares { float a, c; };
+__device__ __forceinline__ GateShares gate_shares(float g)
+{
+    const float s = fabsf(g), more = 1.f - s;
+    return signbit(g) ? GateShares{s, more} : GateShares{more, s};
+}
 
-__device__ __forceinline__ float gate_step(float g, float h, float u)
-{
-    const bool keep = !signbit(g);
-    const float s = fabsf(g), x = keep ? h : u, z = keep ? u : h;
-    return s == 0.f ? x : fmaf(s, z, fmaf(-s, x, x));
-}
-__device__ __forceinline__ float gate_through(float g, float x) { return signbit(g) ? gate_less(fabsf(g), x) : gate_more(fabsf(g), x); }     // a x
-__device__ __forceinline__ float gate_into(float g, float x) { return signbit(g) ? gate_more(fabsf(g), x) : gate_less(fabsf(g), x); }        // (1 - a) x
-__device__ __forceinline__ float gate_slope(float g, float x)             // a (1 - a) x
-{
-    const float s = fabsf(g);
-    return s == 0.f ? 0.f : fmaf(-s, s, s) * x;
-}
+// A share of x.  CLOSED: none of it where the share is none, whatever x is.
+template <bool CLOSED> __device__ __forceinline__ float share_of(float share, float x) { return CLOSED && share == 0.f ? 0.f : share * x; }
+// a h + b
+template <bool CLOSED> __device__ __forceinline__ float gate_step(float a, float h, float b) { return CLOSED && a == 0.f ? b : fmaf(a, h, b); }
 
 constexpr int SCAN_ROWS = SCAN_KEPT, SCAN_WAVES = 4, SCAN_THREADS = 64 * SCAN_WAVES;
 constexpr int SCAN_TILE = SCAN_ROWS * SCAN_WAVES;        // rows of a workgroup's tile
-constexpr int SCAN_RUN = 16;                             // tiles of one column block whose products are added up before a state is handed on
-template <typename T> constexpr int SCAN_V = 4 / (int)sizeof(T);          // columns of a lane
-template <typename T> constexpr int SCAN_COLS = 64 * SCAN_V<T>;           // columns of a tile
+constexpr int SCAN_GROUP = 8, SCAN_RUN = 64;             // tiles whose products are joined, and tiles from one state that is handed on to the next
+// Columns of a lane: forward two of 16 bits; backward, where a row takes four registers a column, one.
+template <typename T, bool BACKWARD> constexpr int SCAN_V = 1;
 
 typedef unsigned u32_at_2 __attribute__((aligned(2)));
 
 // A lane's columns of a tile, counted from the tile's first: rows are given by uniform pointers to that one.  Lanes past the last column read
 // some column that is there and store nothing.
-template <typename T> struct ScanLane {
+template <typename T, int V> struct ScanLane {
+    static constexpr int COLS = 64 * V;
+    typedef typename std::conditional<V * sizeof(T) == 4, unsigned, uint16_t>::type word;
     int64_t first;                           // the tile's first column
     int e, left;                             // the lane's first column; columns from the tile's first to the last one, or the tile's
     bool full, odd;                          // all columns are there; the last one has no neighbour (16 bits)
-    __device__ __forceinline__ ScanLane(int64_t block, int64_t d) : first(block * SCAN_COLS<T>), e((threadIdx.x & 63) * SCAN_V<T>)
+    __device__ __forceinline__ ScanLane(int64_t block, int64_t d) : first(block * COLS), e((threadIdx.x & 63) * V)
     {
-        left = d - first < SCAN_COLS<T> ? (int)(d - first) : SCAN_COLS<T>;
-        full = left == SCAN_COLS<T>;
-        odd = SCAN_V<T> == 2 && (left & 1);
+        left = d - first < COLS ? (int)(d - first) : COLS;
+        full = left == COLS;
+        odd = V == 2 && (left & 1);
     }
     // The lane's values of SCAN_ROWS rows: the last of `many` again in place of those that are not there.
     template <typename L> static __device__ __forceinline__ void each_row(int many, L load)
     {
-        if (many == SCAN_ROWS) {
 #pragma unroll
-            for (int r = 0; r < SCAN_ROWS; ++r) load(r, 1);
-        } else {
-#pragma unroll
-            for (int r = 0; r < SCAN_ROWS; ++r) load(r, r + 1 < many);
+        for (int r = 0; r < SCAN_ROWS; ++r) {
+            asm volatile("" : "+s"(many));               // (one row's pointer after the other: all of them at once are too many scalars)
+            load(r, r + 1 < many);
         }
     }
     __device__ __forceinline__ void load(const T *row, int64_t ld, int many, unsigned (&out)[SCAN_ROWS]) const
     {
         const T *p = row + first;
-        if constexpr (SCAN_V<T> == 1) {
+        if constexpr (V == 1) {
             const unsigned off = e < left ? e : left - 1;
             each_row(many, [&](int r, bool further) {
-                out[r] = __builtin_nontemporal_load((const unsigned *)p + off);
+                out[r] = __builtin_nontemporal_load((const word *)p + off);
                 p += further ? ld : 0;
             });
         } else if (odd) {
@@ -105,19 +96,21 @@ template <typename T> struct ScanLane {
     static __device__ __forceinline__ void values(unsigned x, float *out)
     {
         if constexpr (sizeof(T) == 4) out[0] = __uint_as_float(x);
-        else if constexpr (__is_same(T, bf16)) { out[0] = __uint_as_float(x << 16); out[1] = __uint_as_float(x & 0xffff0000u); }
-        else {
+        else if constexpr (__is_same(T, bf16)) {
+            out[0] = __uint_as_float(x << 16);
+            if constexpr (V == 2) out[1] = __uint_as_float(x & 0xffff0000u);
+        } else {
             f16 v[2];
             __builtin_memcpy(v, &x, 4);
-            out[0] = (float)v[0];
-            out[1] = (float)v[1];
+#pragma unroll
+            for (int i = 0; i < V; ++i) out[i] = (float)v[i];
         }
     }
     // `row`: the tile's first column
     template <bool FULL> __device__ __forceinline__ void store(T *row, const float *in) const
     {
-        if constexpr (SCAN_V<T> == 1) {
-            if (FULL || e < left) __builtin_nontemporal_store((float)in[0], (float *)row + (unsigned)e);
+        if constexpr (V == 1) {
+            if (FULL || e < left) __builtin_nontemporal_store((T)in[0], row + (unsigned)e);
         } else {
             T v[2] = {(T)in[0], (T)in[1]};
             unsigned x;
@@ -131,13 +124,13 @@ template <typename T> struct ScanLane {
     {
         const float *row = p + j * d + first;
 #pragma unroll
-        for (int v = 0; v < SCAN_V<T>; ++v) out[v] = p ? row[(unsigned)(e + v < left ? e + v : left - 1)] : 0.f;
+        for (int v = 0; v < V; ++v) out[v] = p ? row[(unsigned)(e + v < left ? e + v : left - 1)] : 0.f;
     }
     __device__ __forceinline__ void store_floats(float *p, int64_t j, int64_t d, const float *in) const
     {
         float *row = p + j * d + first;
 #pragma unroll
-        for (int v = 0; v < SCAN_V<T>; ++v)
+        for (int v = 0; v < V; ++v)
             if (e + v < left) row[(unsigned)(e + v)] = in[v];
     }
 };
@@ -147,21 +140,20 @@ template <typename T, bool PACKED> struct ScanInput;
 template <typename T> struct ScanInput<T, false> {
     const T *p;
     int64_t ld;
-    __device__ __forceinline__ void load(int64_t row, int64_t, int many, const ScanLane<T> &at, unsigned (&out)[SCAN_ROWS]) const
+    template <int V> __device__ __forceinline__ void load(int64_t row, int64_t, int many, const ScanLane<T, V> &at, unsigned (&out)[SCAN_ROWS]) const
     {
         at.load(p + row * ld, ld, many, out);
     }
-    static __device__ __forceinline__ void values(unsigned x, float *out) { ScanLane<T>::values(x, out); }
+    template <int V> static __device__ __forceinline__ void values(unsigned x, float (&out)[V]) { ScanLane<T, V>::values(x, out); }
 };
 template <typename T> struct ScanInput<T, true> {
     const int8_t *q;
     const uint8_t *scales;
     int64_t ld;
-    __device__ __forceinline__ void load(int64_t row, int64_t d, int many, const ScanLane<T> &at, unsigned (&out)[SCAN_ROWS]) const
+    template <int V> __device__ __forceinline__ void load(int64_t row, int64_t d, int many, const ScanLane<T, V> &at, unsigned (&out)[SCAN_ROWS]) const
     {
-        constexpr int V = SCAN_V<T>;
         const int64_t whole = (d + PACK_GROUP - 1) / PACK_GROUP * PACK_GROUP - at.first;
-        const int left = whole < SCAN_COLS<T> ? (int)whole : SCAN_COLS<T>;
+        const int left = whole < at.COLS ? (int)whole : at.COLS;
         const unsigned off = at.e < left ? at.e : left - V;
         const int8_t *p = q + row * ld + at.first;
         const uint8_t *scale = scales + row * (ld / PACK_GROUP) + at.first / PACK_GROUP;
@@ -173,11 +165,11 @@ template <typename T> struct ScanInput<T, true> {
             scale += further ? ld / PACK_GROUP : 0;
         });
     }
-    static __device__ __forceinline__ void values(unsigned x, float *out)
+    template <int V> static __device__ __forceinline__ void values(unsigned x, float (&out)[V])
     {
         const float step = pack_step(x >> 16);
 #pragma unroll
-        for (int v = 0; v < SCAN_V<T>; ++v) out[v] = (float)(int8_t)(x >> (8 * v)) * step;
+        for (int v = 0; v < V; ++v) out[v] = (float)(int8_t)(x >> (8 * v)) * step;
     }
 };
 
@@ -201,7 +193,7 @@ template <typename T, bool PACKED> struct Scan {
     int *flags;
     // what workgroups hand on; null where there is one tile in a column block
     unsigned *ticket;
-    unsigned long long *products, *handed;
+    unsigned long long *products, *groups, *handed;
     unsigned tiles, blocks;                  // tiles of a column block, column blocks
 };
 
@@ -213,10 +205,12 @@ __global__ __launch_bounds__(256) static void scan_begin(unsigned *ticket, unsig
     if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
 }
 
-// What rows do to what comes into them: x becomes a x + b; a = 0 where it does not get through, whatever it is.
+// What rows do to what comes into them: x becomes a x + b; where a = 0 it does not get through, whatever it is.
 struct ScanProduct {
     float a, b;
-    __device__ __forceinline__ float of(float x) const { return a == 0.f ? b : fmaf(a, x, b); }
+    __device__ __forceinline__ float of(float x) const { return gate_step<true>(a, x, b); }
+    // What the rows do after `before`.
+    __device__ __forceinline__ ScanProduct after(const ScanProduct &before) const { return {share_of<true>(a, before.a), of(before.b)}; }
     __device__ __forceinline__ unsigned long long word() const
     {
         const unsigned lo = a == a ? __float_as_uint(a) : 0x7fc00000u;
@@ -310,48 +304,66 @@ struct ScanRows {
     }
 };
 
-// What comes into the q-th tile of a column block, in the order in which tiles are taken, from tile `from` on, whose product lets nothing through; hands
-// on what comes out.  By one wavefront.
+// What comes into the q-th tile of a column block, in the order in which tiles are taken, from tile `from` on, whose product lets nothing through
+// (from = q: nothing comes in, the tile's own lets nothing through); tells what others need.  By one wavefront.
 //
-// Tiles are taken in the order of tickets, those of all column blocks in turn: whoever waits does so for tiles with earlier tickets, whose
-// workgroups have begun and, first of all, tell their products without waiting.  So every wait ends.  What is added up, and in which order, follows
-// from the offsets alone.  A word is told whole, and says by itself whether it has been.
-template <typename T, bool PACKED>
-__device__ __forceinline__ void scan_hand(const Scan<T, PACKED> &a, unsigned q, unsigned block, unsigned from, const ScanProduct (&own)[SCAN_V<T>], float (&x)[SCAN_V<T>])
+// A tile tells its product; the last one of SCAN_GROUP tiles tells theirs, joined; the last one of SCAN_RUN tiles hands on the state that comes out.  So a
+// tile reads at most SCAN_GROUP - 1 products, those of as many groups and a state, and a state goes through a long sequence in steps of SCAN_RUN
+// tiles, everything else of which has been joined by then.
+//
+// Tiles are taken in the order of tickets, those of all column blocks in turn: whoever waits does so for tiles with earlier tickets, whose workgroups have
+// begun.  These tell their products without waiting, groups once the products of the group are told, and states after all that is before them.
+// So every wait ends.  What is joined, and in which order, follows from the offsets alone.  A word is told whole, and says by itself whether it
+// has been.
+template <int V>
+__device__ __forceinline__ void scan_join(const unsigned long long *words, int64_t line, unsigned from, unsigned to, ScanProduct (&x)[V])
 {
-    constexpr int V = SCAN_V<T>, AHEAD = 8;
-    const int lane = threadIdx.x & 63;
-    const int64_t line = (int64_t)a.blocks * SCAN_COLS<T>, at = (int64_t)block * SCAN_COLS<T> + lane;
+    constexpr int AHEAD = SCAN_GROUP - 1;
+    for (unsigned i = from; i < to; i += AHEAD) {
+        const unsigned long long *p = words + i * line;
+        unsigned long long w[AHEAD][V];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int v = 0; v < V; ++v) w[k][v] = i + k < to ? scan_look(p + k * line + v * 64) : 0;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (i + k < to)
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[v] = ScanProduct::from(scan_wait(p + k * line + v * 64, w[k][v])).after(x[v]);
+    }
+}
+
+template <typename T, bool PACKED, int V>
+__device__ __forceinline__ void scan_hand(const Scan<T, PACKED> &a, unsigned q, unsigned block, unsigned from, const ScanProduct (&own)[V], float (&x)[V])
+{
+    const int64_t line = (int64_t)a.blocks * 64 * V, at = (int64_t)block * 64 * V + (threadIdx.x & 63);
+    const unsigned group = q / SCAN_GROUP, run = q / SCAN_RUN;
+    ScanProduct near[V], far[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         scan_tell(a.products + q * line + at + v * 64, own[v].word());
+        near[v] = far[v] = {1.f, 0.f};
         x[v] = 0.f;
     }
-    const unsigned run = q / SCAN_RUN;
-    if (from < q) {
+    scan_join<V>(a.products + at, line, from > group * SCAN_GROUP ? from : group * SCAN_GROUP, q, near);
+    if (q % SCAN_GROUP == SCAN_GROUP - 1)
+#pragma unroll
+        for (int v = 0; v < V; ++v) scan_tell(a.groups + group * line + at + v * 64, own[v].after(near[v]).word());
+    if (from < group * SCAN_GROUP) {
+        const unsigned first = run * (SCAN_RUN / SCAN_GROUP);
+        scan_join<V>(a.groups + at, line, from / SCAN_GROUP > first ? from / SCAN_GROUP : first, group, far);
         if (from < run * SCAN_RUN) {
-            from = run * SCAN_RUN;
             const unsigned long long *p = a.handed + (int64_t)(run - 1) * line + at;
 #pragma unroll
             for (int v = 0; v < V; ++v) x[v] = __uint_as_float((unsigned)scan_wait(p + v * 64, scan_look(p + v * 64)));
         }
-        for (unsigned i = from; i < q; i += AHEAD) {
-            const unsigned long long *p = a.products + i * line + at;
-            unsigned long long w[AHEAD][V];
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-                for (int v = 0; v < V; ++v) w[k][v] = i + k < q ? scan_look(p + k * line + v * 64) : 0;
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k)
-                if (i + k < q)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) x[v] = ScanProduct::from(scan_wait(p + k * line + v * 64, w[k][v])).of(x[v]);
-        }
     }
-    if (q % SCAN_RUN == SCAN_RUN - 1)
 #pragma unroll
-        for (int v = 0; v < V; ++v) scan_tell(a.handed + (int64_t)run * line + at + v * 64, __float_as_uint(own[v].of(x[v])));
+    for (int v = 0; v < V; ++v) {
+        x[v] = near[v].after(far[v]).of(x[v]);
+        if (q % SCAN_RUN == SCAN_RUN - 1) scan_tell(a.handed + (int64_t)run * line + at + v * 64, __float_as_uint(own[v].of(x[v])));
+    }
 }
 
 // A sequence's number, the same in all lanes.
@@ -373,34 +385,44 @@ __device__ __forceinline__ void scan_unit(const Scan<T, PACKED> &a, unsigned &q,
     }
 }
 
-// Rows are worked on four at a time: without an end to it the compiler begins all of them, more than there are registers for.
-__device__ __forceinline__ void scan_four(int r)
-{
-    if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-}
-
-// The same value, of which the compiler does not know that it is: what an earlier pass worked out of it is worked out again instead of being kept.
-template <typename X> __device__ __forceinline__ void scan_anew(X &x) { asm volatile("" : "+v"(x)); }
-
-// f(whether sequences begin or end among the rows, or rows belong to none)
+// f(whether there is something that makes rows special)
 template <typename F>
-__device__ __forceinline__ void scan_rows(unsigned special, F f)
+__device__ __forceinline__ void scan_rows(bool special, F f)
 {
     if (special) f(std::true_type());
     else f(std::false_type());
 }
 
-template <typename T, bool PACKED>
-__global__ __launch_bounds__(SCAN_THREADS, 2) void scan_forward(const Scan<T, PACKED> a)
+// The gates of the wavefront's rows, and whether one of them is closed.
+template <typename T, int V>
+__device__ __forceinline__ bool scan_gates(const unsigned (&fs)[SCAN_ROWS], float (&g)[SCAN_ROWS][V])
 {
-    constexpr int V = SCAN_V<T>;
+    float least = 1.f;
+#pragma unroll
+    for (int r = 0; r < SCAN_ROWS; ++r) {
+        float f[V];
+        ScanLane<T, V>::values(fs[r], f);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            g[r][v] = gate_of(f[v]);
+            least = fminf(least, fabsf(g[r][v]));
+        }
+        if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);               // (not all rows at once: there are no registers for that)
+    }
+    return __any(least == 0.f);
+}
+
+template <typename T, bool PACKED>
+__global__ __launch_bounds__(SCAN_THREADS, 4) void scan_forward(const Scan<T, PACKED> a)
+{
+    constexpr int V = SCAN_V<T, false>;
     __shared__ ScanMarks marks;
     __shared__ ScanProduct products[SCAN_WAVES][V][64];
     __shared__ float into[V][64];
     unsigned q, block;
     scan_unit(a, q, block);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const ScanLane<T> at(block, a.d);
+    const ScanLane<T, V> at(block, a.d);
     const int64_t n = a.order.n, t0 = (int64_t)q * SCAN_TILE + wave * SCAN_ROWS;
     const int many = (int)(n - t0 < SCAN_ROWS ? n - t0 < 0 ? 0 : n - t0 : SCAN_ROWS);
     unsigned fs[SCAN_ROWS], us[SCAN_ROWS];
@@ -416,45 +438,50 @@ __global__ __launch_bounds__(SCAN_THREADS, 2) void scan_forward(const Scan<T, PA
     });
     __syncthreads();
     const ScanRows rows(a.order, marks, t0, wave * SCAN_ROWS);
-    auto first_state = [&](int r, float *h) {
-        at.load_floats(a.h0, scan_number(marks.start[wave * SCAN_ROWS + r]), a.d, h);
-    };
-    float g[SCAN_ROWS][V];
-    if (many > 0)
-#pragma unroll
-        for (int r = 0; r < SCAN_ROWS; ++r) {
-            float f[V];
-            at.values(fs[r], f);
-#pragma unroll
-            for (int v = 0; v < V; ++v) g[r][v] = gate_of(f[v]);
-            scan_four(r);
-        }
+    // every row as h = A h + B, the first one of a sequence with A = 0, and with it those of none
+    float A[SCAN_ROWS][V], B[SCAN_ROWS][V];
     ScanProduct p[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = {1.f, 0.f};
-    if (many > 0)
-        scan_rows(rows.starts | rows.none, [&](auto special) {
+    bool closed = false;
+    if (many > 0) {
+        closed = scan_gates<T, V>(fs, A);
+#pragma unroll
+        for (int r = 0; r < SCAN_ROWS; ++r) {
+            float u[V];
+            a.u.values(us[r], u);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const GateShares g = gate_shares(A[r][v]);
+                A[r][v] = g.a;
+                B[r][v] = share_of<true>(g.c, u[v]);
+            }
+            if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        if (rows.starts | rows.none) {
+            closed = true;
 #pragma unroll
             for (int r = 0; r < SCAN_ROWS; ++r) {
-                if constexpr (decltype(special)::value) {
-                    if (rows.none >> r & 1) {
+                if (rows.starts >> r & 1) {
+                    float h[V];
+                    at.load_floats(a.h0, scan_number(marks.start[wave * SCAN_ROWS + r]), a.d, h);
 #pragma unroll
-                        for (int v = 0; v < V; ++v) p[v] = {0.f, 0.f};
-                        continue;
-                    }
-                    if (rows.starts >> r & 1) {
-                        float h[V];
-                        first_state(r, h);
-#pragma unroll
-                        for (int v = 0; v < V; ++v) p[v] = {0.f, h[v]};
-                    }
+                    for (int v = 0; v < V; ++v) B[r][v] = gate_step<true>(A[r][v], h[v], B[r][v]);
                 }
-                float u[V];
-                a.u.values(us[r], u);
 #pragma unroll
-                for (int v = 0; v < V; ++v) p[v] = {gate_through(g[r][v], p[v].a), gate_step(g[r][v], p[v].b, u[v])};
+                for (int v = 0; v < V; ++v) {
+                    if ((rows.starts | rows.none) >> r & 1) A[r][v] = 0.f;
+                    if (rows.none >> r & 1) B[r][v] = 0.f;
+                }
             }
+        }
+        scan_rows(closed, [&](auto special) {
+#pragma unroll
+            for (int r = 0; r < SCAN_ROWS; ++r)
+#pragma unroll
+                for (int v = 0; v < V; ++v) p[v] = {p[v].a * A[r][v], gate_step<decltype(special)::value>(A[r][v], p[v].b, B[r][v])};
         });
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) products[wave][v][lane] = p[v];
     __syncthreads();
@@ -466,49 +493,37 @@ __global__ __launch_bounds__(SCAN_THREADS, 2) void scan_forward(const Scan<T, PA
             for (int v = 0; v < V; ++v) {
                 own[v] = p[v];
 #pragma unroll
-                for (int w = 1; w < SCAN_WAVES; ++w) {
-                    const ScanProduct next = products[w][v][lane];
-                    own[v] = {next.a == 0.f ? 0.f : own[v].a * next.a, next.of(own[v].b)};
-                }
+                for (int w = 1; w < SCAN_WAVES; ++w) own[v] = products[w][v][lane].after(own[v]);
             }
-            scan_hand(a, q, block, marks.from, own, x);
+            scan_hand<T, PACKED, V>(a, q, block, marks.from, own, x);
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) into[v][lane] = x[v];
     }
     __syncthreads();
     if (many == 0) return;
-#pragma unroll
-    for (int r = 0; r < SCAN_ROWS; ++r) {
-        scan_anew(us[r]);
-#pragma unroll
-        for (int v = 0; v < V; ++v) scan_anew(g[r][v]);
-    }
     float h[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = into[v][lane];
     for (int w = 0; w < wave; ++w)
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = products[w][v][lane].of(h[v]);
+    if (a.states) {
+        float enters[V];
+        if (rows.starts & 1) at.load_floats(a.h0, scan_number(marks.start[wave * SCAN_ROWS]), a.d, enters);
+        else
+#pragma unroll
+            for (int v = 0; v < V; ++v) enters[v] = rows.none & 1 ? 0.f : h[v];
+        at.store_floats(a.states, t0 / SCAN_KEPT, a.d, enters);
+    }
     T *y = a.y + t0 * a.ldy + at.first;
-    scan_rows(rows.starts | rows.ends | rows.none | !at.full, [&](auto special) {
+    scan_rows(closed || (rows.ends && a.last) || !at.full, [&](auto special) {
         constexpr bool SPECIAL = decltype(special)::value;
 #pragma unroll
         for (int r = 0; r < SCAN_ROWS; ++r) {
-            const bool none = SPECIAL && (rows.none >> r & 1);
             if (SPECIAL && r >= many) break;
-            if (SPECIAL && none) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) h[v] = 0.f;
-            }
-            if (SPECIAL && (rows.starts >> r & 1)) first_state(r, h);
-            if (r == 0 && a.states) at.store_floats(a.states, t0 / SCAN_KEPT, a.d, h);
-            if (!none) {
-                float u[V];
-                a.u.values(us[r], u);
-#pragma unroll
-                for (int v = 0; v < V; ++v) h[v] = gate_step(g[r][v], h[v], u[v]);
-            }
+            for (int v = 0; v < V; ++v) h[v] = gate_step<SPECIAL>(A[r][v], h[v], B[r][v]);
             at.template store<!SPECIAL>(y, h);
             y += a.ldy;
             if (SPECIAL && (rows.ends >> r & 1) && a.last) at.store_floats(a.last, scan_number(marks.end[wave * SCAN_ROWS + r]), a.d, h);
@@ -517,16 +532,16 @@ __global__ __launch_bounds__(SCAN_THREADS, 2) void scan_forward(const Scan<T, PA
 }
 
 template <typename T, bool PACKED>
-__global__ __launch_bounds__(SCAN_THREADS, 2) void scan_backward(const Scan<T, PACKED> a)
+__global__ __launch_bounds__(SCAN_THREADS, 3) void scan_backward(const Scan<T, PACKED> a)
 {
-    constexpr int V = SCAN_V<T>;
+    constexpr int V = SCAN_V<T, true>;
     __shared__ ScanMarks marks;
     __shared__ ScanProduct products[SCAN_WAVES][V][64];
     __shared__ float into[V][64];
     unsigned q, block;
     scan_unit(a, q, block);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const ScanLane<T> at(block, a.d);
+    const ScanLane<T, V> at(block, a.d);
     const unsigned tile = a.tiles - 1 - q;
     const int64_t n = a.order.n, t0 = (int64_t)tile * SCAN_TILE + wave * SCAN_ROWS;
     const int many = (int)(n - t0 < SCAN_ROWS ? n - t0 < 0 ? 0 : n - t0 : SCAN_ROWS);
@@ -546,61 +561,54 @@ __global__ __launch_bounds__(SCAN_THREADS, 2) void scan_backward(const Scan<T, P
     });
     __syncthreads();
     const ScanRows rows(a.order, marks, t0, wave * SCAN_ROWS);
-    auto last_gradient = [&](int r, float *x) {
-        at.load_floats(a.dlast, scan_number(marks.end[wave * SCAN_ROWS + r]), a.d, x);
-    };
-    float g[SCAN_ROWS][V], wide[SCAN_ROWS][V];           // gates, and h_{t-1} - u_t
-    if (many > 0)
-        scan_rows(rows.starts, [&](auto special) {
-#pragma unroll
-            for (int r = 0; r < SCAN_ROWS; ++r) {
-                float f[V], u[V];
-                if constexpr (decltype(special)::value)
-                    if (rows.starts >> r & 1) at.load_floats(a.h0, scan_number(marks.start[wave * SCAN_ROWS + r]), a.d, h);
-                at.values(fs[r], f);
-                a.u.values(us[r], u);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    g[r][v] = gate_of(f[v]);
-                    wide[r][v] = h[v] - u[v];
-                    h[v] = gate_step(g[r][v], h[v], u[v]);
-                }
-                scan_four(r);
-            }
-        });
-    if (many > 0)
-#pragma unroll
-        for (int r = 0; r < SCAN_ROWS; ++r)
-#pragma unroll
-            for (int v = 0; v < V; ++v) scan_anew(g[r][v]);
+    auto last_gradient = [&](int r, float (&x)[V]) { at.load_floats(a.dlast, scan_number(marks.end[wave * SCAN_ROWS + r]), a.d, x); };
+    float A[SCAN_ROWS][V], C[SCAN_ROWS][V], wide[SCAN_ROWS][V];          // shares, and h_{t-1} - u_t; rows of no sequence have none
     // x: what goes from a row to the one before, a G
     ScanProduct p[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = {1.f, 0.f};
-    if (many > 0)
-        scan_rows(rows.ends | rows.none, [&](auto special) {
+    bool closed = false;
+    if (many > 0) {
+        closed = scan_gates<T, V>(fs, A) || rows.none;
+#pragma unroll
+        for (int r = 0; r < SCAN_ROWS; ++r) {
+            float u[V];
+            if (rows.starts >> r & 1) at.load_floats(a.h0, scan_number(marks.start[wave * SCAN_ROWS + r]), a.d, h);
+            a.u.values(us[r], u);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const GateShares g = gate_shares(A[r][v]);
+                A[r][v] = g.a;
+                C[r][v] = g.c;
+                wide[r][v] = h[v] - u[v];
+                h[v] = gate_step<true>(g.a, h[v], share_of<true>(g.c, u[v]));
+            }
+            if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        if (rows.none) {
+#pragma unroll
+            for (int r = 0; r < SCAN_ROWS; ++r)
+                if (rows.none >> r & 1)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) A[r][v] = C[r][v] = 0.f;
+        }
+        scan_rows(closed || rows.ends, [&](auto special) {
+            constexpr bool SPECIAL = decltype(special)::value;
 #pragma unroll
             for (int r = SCAN_ROWS - 1; r >= 0; --r) {
-                if constexpr (decltype(special)::value) {
-                    if (rows.none >> r & 1) {
+                if (SPECIAL && (rows.ends >> r & 1)) {
+                    float x[V];
+                    last_gradient(r, x);
 #pragma unroll
-                        for (int v = 0; v < V; ++v) p[v] = {0.f, 0.f};
-                        continue;
-                    }
-                    if (rows.ends >> r & 1) {
-                        float x[V];
-                        last_gradient(r, x);
-#pragma unroll
-                        for (int v = 0; v < V; ++v) p[v] = {0.f, x[v]};
-                    }
+                    for (int v = 0; v < V; ++v) p[v] = {0.f, x[v]};
                 }
                 float dy[V];
                 at.values(dys[r], dy);
 #pragma unroll
-                for (int v = 0; v < V; ++v) p[v] = {gate_through(g[r][v], p[v].a), gate_through(g[r][v], p[v].b + dy[v])};
-                scan_four(r + 3);
+                for (int v = 0; v < V; ++v) p[v] = {p[v].a * A[r][v], share_of<SPECIAL>(A[r][v], p[v].b + dy[v])};
             }
         });
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) products[wave][v][lane] = p[v];
     __syncthreads();
@@ -612,24 +620,15 @@ __global__ __launch_bounds__(SCAN_THREADS, 2) void scan_backward(const Scan<T, P
             for (int v = 0; v < V; ++v) {
                 own[v] = p[v];
 #pragma unroll
-                for (int w = SCAN_WAVES - 2; w >= 0; --w) {
-                    const ScanProduct next = products[w][v][lane];
-                    own[v] = {next.a == 0.f ? 0.f : own[v].a * next.a, next.of(own[v].b)};
-                }
+                for (int w = SCAN_WAVES - 2; w >= 0; --w) own[v] = products[w][v][lane].after(own[v]);
             }
-            scan_hand(a, q, block, a.tiles - 1 - marks.to, own, x);
+            scan_hand<T, PACKED, V>(a, q, block, a.tiles - 1 - marks.to, own, x);
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) into[v][lane] = x[v];
     }
     __syncthreads();
     if (many == 0) return;
-#pragma unroll
-    for (int r = 0; r < SCAN_ROWS; ++r) {
-        scan_anew(dys[r]);
-#pragma unroll
-        for (int v = 0; v < V; ++v) scan_anew(g[r][v]);
-    }
     float x[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] = into[v][lane];
@@ -637,32 +636,25 @@ __global__ __launch_bounds__(SCAN_THREADS, 2) void scan_backward(const Scan<T, P
 #pragma unroll
         for (int v = 0; v < V; ++v) x[v] = products[w][v][lane].of(x[v]);
     T *df_row = a.df + (t0 + many - 1) * a.lddf + at.first, *du_row = a.du + (t0 + many - 1) * a.lddu + at.first;
-    scan_rows(rows.starts | rows.ends | rows.none | !at.full, [&](auto special) {
+    scan_rows(closed || rows.starts || rows.ends || !at.full, [&](auto special) {
         constexpr bool SPECIAL = decltype(special)::value;
 #pragma unroll
         for (int r = SCAN_ROWS - 1; r >= 0; --r) {
             if (SPECIAL && r >= many) continue;
-            float df[V] = {}, du[V] = {};
-            if (SPECIAL && (rows.none >> r & 1)) {
+            if (SPECIAL && (rows.ends >> r & 1)) last_gradient(r, x);
+            float dy[V], df[V], du[V];
+            at.values(dys[r], dy);
 #pragma unroll
-                for (int v = 0; v < V; ++v) x[v] = 0.f;
-            } else {
-                if (SPECIAL && (rows.ends >> r & 1)) last_gradient(r, x);
-                float dy[V];
-                at.values(dys[r], dy);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float y = x[v] + dy[v];
-                    df[v] = gate_slope(g[r][v], y * wide[r][v]);
-                    du[v] = gate_into(g[r][v], y);
-                    x[v] = gate_through(g[r][v], y);
-                }
+            for (int v = 0; v < V; ++v) {
+                const float G = x[v] + dy[v];
+                df[v] = share_of<SPECIAL>(A[r][v] * C[r][v], G * wide[r][v]);
+                du[v] = share_of<SPECIAL>(C[r][v], G);
+                x[v] = share_of<SPECIAL>(A[r][v], G);
             }
             at.template store<!SPECIAL>(df_row, df);
             at.template store<!SPECIAL>(du_row, du);
             df_row -= a.lddf;
             du_row -= a.lddu;
-            scan_four(r + 3);
             if (SPECIAL && (rows.starts >> r & 1) && a.dh0) at.store_floats(a.dh0, scan_number(marks.start[wave * SCAN_ROWS + r]), a.d, x);
         }
     });
@@ -686,7 +678,10 @@ __global__ __launch_bounds__(STEP_THREADS) void scan_step(const T *__restrict__ 
         unpack<T>(settle<T>(fs, c, d), fv);
         unpack<T>(settle<T>(us, c, d), uv);
 #pragma unroll
-        for (int i = 0; i < V; ++i) hs[i] = gate_step(gate_of(fv[i]), hs[i], uv[i]);
+        for (int i = 0; i < V; ++i) {
+            const GateShares g = gate_shares(gate_of(fv[i]));
+            hs[i] = gate_step<true>(g.a, hs[i], share_of<true>(g.c, uv[i]));
+        }
 #pragma unroll
         for (int k = 0; k < V; k += 4)
             if (c + k < d) store_vec(state + row * lds, c + k, d, hs + k);

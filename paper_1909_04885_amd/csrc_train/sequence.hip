@@ -93,23 +93,24 @@ template <typename T, bool PACKED> ScanInput<T, PACKED> scan_input(const void *u
 struct ScanPlan {
     int64_t tiles, blocks, words;
     unsigned *ticket;
-    unsigned long long *products, *handed;
+    unsigned long long *products, *groups, *handed;
     size_t bytes;
 };
 
-ScanPlan scan_plan(int64_t n, int64_t d, int32_t type, void *workspace)
+ScanPlan scan_plan(int64_t n, int64_t d, int32_t type, bool backward, void *workspace)
 {
     ScanPlan p = {};
-    const int64_t columns = type == CHICLE_F32 ? SCAN_COLS<float> : SCAN_COLS<bf16>;
+    const int64_t columns = 64 * (type == CHICLE_F32 ? 1 : backward ? SCAN_V<bf16, true> : SCAN_V<bf16, false>);
     p.tiles = n > 0 ? ceil_div(n, SCAN_TILE) : 1;
     p.blocks = ceil_div(d, columns);
     Carver c(workspace);
     if (p.tiles > 1) {
-        const int64_t line = p.blocks * columns, runs = ceil_div(p.tiles, SCAN_RUN);
-        p.words = (p.tiles + runs) * line;
+        const int64_t line = p.blocks * columns, groups = ceil_div(p.tiles, SCAN_GROUP), runs = ceil_div(p.tiles, SCAN_RUN);
+        p.words = (p.tiles + groups + runs) * line;
         p.ticket = c.take<unsigned>(1);
         p.products = c.take<unsigned long long>(p.words);
-        p.handed = p.products + p.tiles * line;
+        p.groups = p.products + p.tiles * line;
+        p.handed = p.groups + groups * line;
     }
     p.bytes = c.total();
     return p;
@@ -119,12 +120,13 @@ ScanPlan scan_plan(int64_t n, int64_t d, int32_t type, void *workspace)
 template <typename T, bool PACKED>
 int run_scan(Scan<T, PACKED> a, int32_t type, bool backward, void *workspace, hipStream_t stream)
 {
-    const ScanPlan p = scan_plan(a.order.n, a.d, type, workspace);
+    const ScanPlan p = scan_plan(a.order.n, a.d, type, backward, workspace);
     a.tiles = (unsigned)p.tiles;
     a.blocks = (unsigned)p.blocks;
     if (p.tiles > 1) {
         a.ticket = p.ticket;
         a.products = p.products;
+        a.groups = p.groups;
         a.handed = p.handed;
         scan_begin<<<(unsigned)std::min<int64_t>(ceil_div(p.words, 256), 2048), 256, 0, stream>>>(p.ticket, p.products, p.words);
         TRY(launched("scan_begin"));
@@ -141,7 +143,7 @@ int scan_check(const void *f, int64_t ldf, const void *u, int64_t ldu, const voi
     if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
     if (!sizes_ok(n, d) || ldf < d || ldu < d || sequences < 0 || sequences > INT32_MAX || (!offsets && sequences != 1))
         return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, sequences %lld, or a row distance", (long long)n, (long long)d, (long long)sequences);
-    const ScanPlan p = scan_plan(n, d, type, nullptr);
+    const ScanPlan p = scan_plan(n, d, type, true, nullptr);
     if (p.tiles * p.blocks >= (int64_t)1 << 24) return fail(CHICLE_EINVAL, "too many values");              // (a launch has fewer than 2^32 threads)
     const int s = size_of(type);
     if ((offsets && !placed(offsets, wide ? 8 : 4)) || (h0 && !placed(h0, 4)) || (states && !placed(states, 4)))
@@ -277,7 +279,7 @@ int chicle_rms_norm_grad(const void *dy, int64_t lddy, const void *sum, int64_t 
 size_t chicle_gated_scan_bytes(int64_t n, int64_t d, int32_t type)
 {
     if (!type_ok(type) || !sizes_ok(n, d)) return 0;
-    return scan_plan(n, d, type, nullptr).bytes;
+    return std::max(scan_plan(n, d, type, false, nullptr).bytes, scan_plan(n, d, type, true, nullptr).bytes);
 }
 
 int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,

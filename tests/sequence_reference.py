@@ -1,14 +1,18 @@
 """The operators of layers over sequences in 64 bits, on whatever device the inputs are, and the bounds the tests hold results to.
 
-Bounds are worst cases of rounding, U32 = 2^-24 a rounding to 32 bits.  A gate's smaller share s is off by at most 10 U32 of itself: a power of two, a
-reciprocal, each to a unit in the last place (two roundings), the correction of the first, 1 + e and a product.
+Bounds are worst cases of rounding, U32 = 2^-24 a rounding to 32 bits.  A gate's smaller share s is off by at most (10 + 2 |f|) U32 of itself: a power of two, a
+reciprocal, each to a unit in the last place (two roundings), 1 + e and a product, each once, and what the exponent |f| log2(e) is off, which is rounded
+once, as the factor is: (|f| log2(e)) 2 U32 ln(2) = 2 |f| U32.
 """
 import torch
 
 from train_reference import TINY, U, U32
 
 GROUP, KEPT = 32, 32
-GATE = 10 * U32
+
+
+def gate_off(f):
+    return (10 + 2 * f.double().abs().clamp(max=104)) * U32
 
 
 def pack(x):
@@ -66,10 +70,10 @@ def rms_norm_grad(dy, r, gamma, rstd, dr):
 
 
 def gates(f):
-    """(a, 1 - a, the smaller one), closed beyond +-87, in 64 bits."""
+    """(a, 1 - a, the smaller one), closed beyond +-104, in 64 bits."""
     f = f.double()
     a, c = torch.sigmoid(f), torch.sigmoid(-f)
-    a, c = torch.where(f > 87, 1.0, torch.where(f < -87, 0.0, a)), torch.where(f > 87, 0.0, torch.where(f < -87, 1.0, c))
+    a, c = torch.where(f > 104, 1.0, torch.where(f < -104, 0.0, a)), torch.where(f > 104, 0.0, torch.where(f < -104, 1.0, c))
     return a, c, torch.minimum(a, c)
 
 
@@ -82,6 +86,7 @@ def scan(f, u, offsets, h0):
     """f, u [n, d] in any type, offsets a list: h, the states that enter rows, those after the sequences, and how far h may be off before it is rounded."""
     n, d = f.shape
     a, c, s = gates(f)
+    gate = gate_off(f)
     u = u.double()
     h, before, off = torch.zeros_like(a), torch.zeros_like(a), torch.zeros_like(a)
     k = len(offsets) - 1
@@ -94,7 +99,7 @@ def scan(f, u, offsets, h0):
             before[t], off_before[t] = x, e
             parts = share(a[t], x).abs() + share(c[t], u[t]).abs()
             seen = share(s[t], x).abs() + share(s[t], u[t]).abs()
-            e = share(a[t], e) + 2 * (GATE * seen + 2 * U32 * parts)       # twice: rows are also carried as a product of shares and a sum
+            e = share(a[t], e) + 2 * (gate[t] * seen + 2 * U32 * parts)       # twice: rows are also carried as a product of shares and a sum
             x = share(a[t], x) + share(c[t], u[t])
             h[t], off[t] = x, e
         last[j], off_last[j] = x, e
@@ -105,6 +110,7 @@ def scan_grad(f, u, offsets, h0, dy, dlast):
     dtype = f.dtype
     r = scan(f, u, offsets, h0)
     a, c, s = gates(f)
+    gate = gate_off(f)
     u, dy = u.double(), dy.double()
     k, d = len(offsets) - 1, f.shape[1]
     g, off = torch.zeros_like(a), torch.zeros_like(a)
@@ -115,13 +121,13 @@ def scan_grad(f, u, offsets, h0, dy, dlast):
         for t in range(offsets[j + 1] - 1, offsets[j] - 1, -1):
             x, e = x + dy[t], e + 2 * U32 * (x + dy[t]).abs() + 2 * U32 * x.abs()
             g[t], off[t] = x, e
-            e = share(a[t], e) + 2 * (GATE * share(s[t], x).abs() + 2 * U32 * share(a[t], x).abs())
+            e = share(a[t], e) + 2 * (gate[t] * share(s[t], x).abs() + 2 * U32 * share(a[t], x).abs())
             x = share(a[t], x)
         dh0[j], off_dh0[j] = x, e
     wide = r["before"] - u
     slope = a * c
     df, du = share(slope, g * wide), share(c, g)
-    off_df = share(slope, off * wide.abs() + g.abs() * (r["off_before"] + 2 * U32 * wide.abs())) + (2 * GATE + 8 * U32) * df.abs()
-    off_du = share(c, off) + 2 * GATE * share(s, g).abs() + 2 * U32 * du.abs()
+    off_df = share(slope, off * wide.abs() + g.abs() * (r["off_before"] + 2 * U32 * wide.abs())) + (2 * gate + 8 * U32) * df.abs()
+    off_du = share(c, off) + 2 * gate * share(s, g).abs() + 2 * U32 * du.abs()
     return {"df": df, "du": du, "dh0": dh0, "off_df": off_df + U[dtype] * df.abs() + TINY[dtype], "off_du": off_du + U[dtype] * du.abs() + TINY[dtype],
             "off_dh0": off_dh0 + 2 * U32 * dh0.abs() + TINY[torch.float32]}

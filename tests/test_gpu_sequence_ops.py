@@ -354,7 +354,7 @@ def test_gated_step_is_the_scan_of_one_row(ops, dtype, n, d, extra, shift):
     assert bool((wide[:, :2] == 3.0).all()) and bool((wide[:, 2 + d:] == 3.0).all())
     a, c, s = ref.gates(f)
     exact = a * before.double() + c * u.double()
-    within(state, exact, 2 * (ref.GATE * s * (before.double().abs() + u.double().abs()) + 2 * U32 * (a * before.double().abs() + c * u.double().abs())))
+    within(state, exact, 2 * (ref.gate_off(f) * s * (before.double().abs() + u.double().abs()) + 2 * U32 * (a * before.double().abs() + c * u.double().abs())))
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=NAME.get)
