@@ -41,9 +41,12 @@ template <bool CLOSED> __device__ __forceinline__ float gate_step(float a, float
 
 constexpr int SCAN_ROWS = SCAN_KEPT, SCAN_WAVES = 4, SCAN_THREADS = 64 * SCAN_WAVES;
 constexpr int SCAN_TILE = SCAN_ROWS * SCAN_WAVES;        // rows of a workgroup's tile
+constexpr int SCAN_FORWARD_HELD = 4, SCAN_BACKWARD_HELD = 3;            // workgroups of a compute unit, as registers allow
 constexpr int SCAN_GROUP = 8, SCAN_RUN = 64;             // tiles whose products are joined, and tiles from one state that is handed on to the next
 // Columns of a lane: forward two of 16 bits; backward, where a row takes four registers a column, one.
 template <typename T, bool BACKWARD> constexpr int SCAN_V = 1;
+
+constexpr int SCAN_TICKET = 32;                          // places from one column block's ticket to the next: lines of their own
 
 typedef unsigned u32_at_2 __attribute__((aligned(2)));
 
@@ -106,19 +109,9 @@ template <typename T, int V> struct ScanLane {
             for (int i = 0; i < V; ++i) out[i] = (float)v[i];
         }
     }
-    // `row`: the tile's first column
-    template <bool FULL> __device__ __forceinline__ void store(T *row, const float *in) const
-    {
-        if constexpr (V == 1) {
-            if (FULL || e < left) __builtin_nontemporal_store((T)in[0], row + (unsigned)e);
-        } else {
-            T v[2] = {(T)in[0], (T)in[1]};
-            unsigned x;
-            __builtin_memcpy(&x, v, 4);
-            if (FULL || e + 1 < left) __builtin_nontemporal_store(x, (u32_at_2 *)(row + (unsigned)e));
-            else if (e < left) row[e] = v[0];
-        }
-    }
+    __device__ __forceinline__ bool here() const { return e < left; }
+    // `row`: the tile's first column; only lanes that have one
+    __device__ __forceinline__ void store(T *row, const float *in) const { __builtin_nontemporal_store((T)in[0], row + (unsigned)e); }
     // Row j of floats (of a null pointer: zeros).
     __device__ __forceinline__ void load_floats(const float *p, int64_t j, int64_t d, float *out) const
     {
@@ -135,41 +128,41 @@ template <typename T, int V> struct ScanLane {
     }
 };
 
-// Rows of T, or packed ones: what is asked for of a row, in one register, and its values.
+// The second input's rows, of T or packed: what a lane asks for of SCAN_ROWS of them, and its values.
 template <typename T, bool PACKED> struct ScanInput;
 template <typename T> struct ScanInput<T, false> {
+    struct Raw { unsigned x[SCAN_ROWS]; };
     const T *p;
     int64_t ld;
-    template <int V> __device__ __forceinline__ void load(int64_t row, int64_t, int many, const ScanLane<T, V> &at, unsigned (&out)[SCAN_ROWS]) const
+    template <int V> __device__ __forceinline__ void load(int64_t row, int64_t, int many, const ScanLane<T, V> &at, Raw &out) const
     {
-        at.load(p + row * ld, ld, many, out);
+        at.load(p + row * ld, ld, many, out.x);
     }
-    template <int V> static __device__ __forceinline__ void values(unsigned x, float (&out)[V]) { ScanLane<T, V>::values(x, out); }
+    template <int V> static __device__ __forceinline__ void values(const Raw &raw, int r, float (&out)[V]) { ScanLane<T, V>::values(raw.x[r], out); }
 };
 template <typename T> struct ScanInput<T, true> {
+    struct Raw { unsigned x[SCAN_ROWS], step; };         // step: of row lane / 2 and, of the tile's two groups, lane % 2
     const int8_t *q;
     const uint8_t *scales;
     int64_t ld;
-    template <int V> __device__ __forceinline__ void load(int64_t row, int64_t d, int many, const ScanLane<T, V> &at, unsigned (&out)[SCAN_ROWS]) const
+    template <int V> __device__ __forceinline__ void load(int64_t row, int64_t d, int many, const ScanLane<T, V> &at, Raw &out) const
     {
+        static_assert(V == 1 && SCAN_ROWS == 32 && PACK_GROUP == 32, "a lane for every scale");
         const int64_t whole = (d + PACK_GROUP - 1) / PACK_GROUP * PACK_GROUP - at.first;
-        const int left = whole < at.COLS ? (int)whole : at.COLS;
-        const unsigned off = at.e < left ? at.e : left - V;
-        const int8_t *p = q + row * ld + at.first;
-        const uint8_t *scale = scales + row * (ld / PACK_GROUP) + at.first / PACK_GROUP;
+        const int left = whole < at.COLS ? (int)whole : at.COLS, lane = threadIdx.x & 63;
+        const unsigned off = at.e < left ? at.e : left - 1;
+        const int which = lane >> 1 < many ? lane >> 1 : many > 0 ? many - 1 : 0;
+        out.step = scales[(row + which) * (ld / PACK_GROUP) + at.first / PACK_GROUP + ((lane & 1) * PACK_GROUP < left ? lane & 1 : 0)];
+        const uint8_t *p = (const uint8_t *)q + row * ld + at.first;
         at.each_row(many, [&](int r, bool further) {
-            if constexpr (V == 1) out[r] = ((const uint8_t *)p)[off];
-            else out[r] = *(const uint16_t *)(p + off);
-            out[r] |= (unsigned)scale[off / PACK_GROUP] << 16;
+            out.x[r] = __builtin_nontemporal_load(p + off);
             p += further ? ld : 0;
-            scale += further ? ld / PACK_GROUP : 0;
         });
     }
-    template <int V> static __device__ __forceinline__ void values(unsigned x, float (&out)[V])
+    template <int V> static __device__ __forceinline__ void values(const Raw &raw, int r, float (&out)[V])
     {
-        const float step = pack_step(x >> 16);
-#pragma unroll
-        for (int v = 0; v < V; ++v) out[v] = (float)(int8_t)(x >> (8 * v)) * step;
+        const int from = 2 * r + ((threadIdx.x & 63) >> 5);
+        out[0] = (float)(int8_t)raw.x[r] * pack_step((unsigned)__builtin_amdgcn_ds_bpermute(from * 4, (int)raw.step));
     }
 };
 
@@ -179,6 +172,13 @@ struct ScanOrder {
     int wide;
     int64_t count, n;
     __device__ __forceinline__ int64_t at(int64_t j) const { return offsets ? index_at(offsets, wide, j) : j == 0 ? 0 : n; }
+    // The same for a j that all lanes have in common: scalar loads, which do not wait behind the rows' loads.
+    __device__ __forceinline__ int64_t common(int64_t j) const
+    {
+        if (!offsets) return j == 0 ? 0 : n;
+        if (wide) return ((const __attribute__((address_space(4))) int64_t *)offsets)[j];
+        return ((const __attribute__((address_space(4))) int32_t *)offsets)[j];
+    }
 };
 
 template <typename T, bool PACKED> struct Scan {
@@ -192,17 +192,19 @@ template <typename T, bool PACKED> struct Scan {
     int64_t ldf, lddy, ldy, lddf, lddu, d;
     int *flags;
     // what workgroups hand on; null where there is one tile in a column block
-    unsigned *ticket;
+    unsigned *tickets;
     unsigned long long *products, *groups, *handed;
     unsigned tiles, blocks;                  // tiles of a column block, column blocks
 };
 
 constexpr unsigned long long SCAN_NOTHING = ~0ull;       // what no product is: its lower half is no NaN of these bits
 
-__global__ __launch_bounds__(256) static void scan_begin(unsigned *ticket, unsigned long long *words, int64_t count)
+__global__ __launch_bounds__(256) static void scan_begin(unsigned *tickets, unsigned blocks, unsigned long long *words, int64_t count)
 {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) words[i] = SCAN_NOTHING;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
+        words[i] = SCAN_NOTHING;
+        if (i < blocks) tickets[i * SCAN_TICKET] = 0;    // (there are more words than column blocks)
+    }
 }
 
 // What rows do to what comes into them: x becomes a x + b; where a = 0 it does not get through, whatever it is.
@@ -237,18 +239,22 @@ struct ScanMarks {
     unsigned from, to;
 };
 
-// How many of the offsets are at most t, by the whole wavefront.
-__device__ __forceinline__ int64_t scan_count(const ScanOrder &o, int64_t t)
+// How many of the offsets are at most t.  (In 32 bits, which is enough: hipcc 7.2 has been seen to take the condition of one choice between uniform
+// 64-bit numbers for that of the next.)
+__device__ __forceinline__ unsigned scan_count(const ScanOrder &o, int64_t t)
 {
-    const int lane = threadIdx.x & 63;
-    int64_t lo = 0, hi = o.count + 1;
+    unsigned lo = 0, hi = (unsigned)o.count + 1;
     while (lo < hi) {                                    // (the distance shrinks, whatever the offsets are)
-        const int64_t step = (hi - lo + 63) >> 6, j = lo + (lane + 1) * step - 1;
-        const int many = __popcll(__ballot(j < hi && o.at(j < hi ? j : lo) <= t));
-        const int64_t next = lo + (many + 1) * step - 1;
-        lo += many * step;
-        hi = next < hi ? next : hi;
-        lo = lo < hi ? lo : hi;
+        const unsigned step = (hi - lo + 3) >> 2;
+        unsigned many = 0;
+#pragma unroll
+        for (int k = 1; k <= 4; ++k) {
+            const unsigned j = lo + k * step - 1;
+            if (j < hi && o.common(j) <= t) ++many;
+        }
+        const unsigned next = lo + (many + 1) * step - 1;
+        lo = min(lo + many * step, hi);
+        hi = min(next, hi);
     }
     return lo;
 }
@@ -261,7 +267,7 @@ __device__ __forceinline__ void scan_mark(const ScanOrder &o, ScanMarks &m, unsi
     const bool last = tile + 1 == tiles;
     for (int i = threadIdx.x; i < SCAN_TILE; i += SCAN_THREADS) m.start[i] = m.end[i] = -1;
     if (threadIdx.x == 0) m.from = m.to = tile;
-    const int64_t first = scan_count(o, t0 - 1);         // offsets below the tile's first row
+    const unsigned first = scan_count(o, t0 - 1);        // offsets below the tile's first row
     __syncthreads();
     bool wrong = false, more = true;
     for (int64_t j0 = first > 0 ? first - 1 : 0; more && j0 < o.count; j0 += SCAN_THREADS) {
@@ -297,7 +303,7 @@ struct ScanRows {
     __device__ __forceinline__ ScanRows(const ScanOrder &o, const ScanMarks &m, int64_t t, int row0)
     {
         const int lane = threadIdx.x & 63, r = row0 + (lane & 31);
-        const int64_t lo = o.at(0), hi = o.at(o.count), row = t + (lane & 31);
+        const int64_t lo = o.common(0), hi = o.common(o.count), row = t + (lane & 31);
         starts = (unsigned)__ballot(m.start[r] >= 0);
         ends = (unsigned)__ballot(m.end[r] >= 0);
         none = (unsigned)__ballot(row < lo || row >= hi || row >= o.n);
@@ -311,8 +317,7 @@ struct ScanRows {
 // tile reads at most SCAN_GROUP - 1 products, those of as many groups and a state, and a state goes through a long sequence in steps of SCAN_RUN
 // tiles, everything else of which has been joined by then.
 //
-// Tiles are taken in the order of tickets, those of all column blocks in turn: whoever waits does so for tiles with earlier tickets, whose workgroups have
-// begun.  These tell their products without waiting, groups once the products of the group are told, and states after all that is before them.
+// Tiles are taken in the order of their column block's tickets: whoever waits does so for tiles with earlier tickets, whose workgroups have begun.  These tell their products without waiting, groups once the products of the group are told, and states after all that is before them.
 // So every wait ends.  What is joined, and in which order, follows from the offsets alone.  A word is told whole, and says by itself whether it
 // has been.
 template <int V>
@@ -369,21 +374,69 @@ __device__ __forceinline__ void scan_hand(const Scan<T, PACKED> &a, unsigned q, 
 // A sequence's number, the same in all lanes.
 __device__ __forceinline__ int64_t scan_number(int j) { return __builtin_amdgcn_readfirstlane(j); }
 
-// What the workgroup's tile is: tickets give tiles in the order in which workgroups begin.
-template <typename T, bool PACKED>
-__device__ __forceinline__ void scan_unit(const Scan<T, PACKED> &a, unsigned &q, unsigned &block)
+// What the workgroup's tile is: tickets, those of each column block for themselves, give tiles in the order in which workgroups begin.
+template <typename S> __device__ __forceinline__ unsigned scan_tile(const S &a, unsigned block)
 {
-    __shared__ unsigned unit;
-    if (a.ticket) {
-        if (threadIdx.x == 0) unit = atomicAdd(a.ticket, 1u);
-        __syncthreads();
-        q = __builtin_amdgcn_readfirstlane(unit) / a.blocks;
-        block = __builtin_amdgcn_readfirstlane(unit) - q * a.blocks;
-    } else {
-        q = 0;
-        block = blockIdx.x;
-    }
+    __shared__ unsigned tile;
+    if (!a.tickets) return 0;
+    if (threadIdx.x == 0) tile = atomicAdd(a.tickets + block * SCAN_TICKET, 1u);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(tile);
 }
+
+// What the wavefronts of a workgroup tell one another.
+template <int V> struct ScanShared {
+    ScanMarks marks;
+    ScanProduct products[SCAN_WAVES][V][64];
+    float into[V][64];
+};
+
+// States or gradients of sequences that begin or end among the wavefront's rows, each in the place of its row: a lane's own, read and written by no other.
+template <int V> struct ScanEdges {
+    float place[SCAN_ROWS][V][64];
+    __device__ __forceinline__ void get(int r, float (&x)[V]) const
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = place[r][v][threadIdx.x & 63];
+    }
+    __device__ __forceinline__ void put(int r, const float (&x)[V])
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) place[r][v][threadIdx.x & 63] = x[v];
+    }
+    // Fetches them for the rows of `which`, whose sequences `numbers` has; zeros of a null pointer.
+    template <typename L> __device__ __forceinline__ void fetch(unsigned which, const int *numbers, const float *from, int64_t d, const L &at)
+    {
+        constexpr int AHEAD = 4;
+        while (which) {
+            float x[AHEAD][V];
+            unsigned left = which;
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int r = left ? __builtin_ctz(left) : 0;
+                if (left) at.load_floats(from, scan_number(numbers[r]), d, x[k]);
+                left &= left - 1;
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (which) put(__builtin_ctz(which), x[k]);
+                which &= which - 1;
+            }
+        }
+    }
+    template <typename L> __device__ __forceinline__ void store(unsigned which, const int *numbers, float *to, int64_t d, const L &at) const
+    {
+        for (; which; which &= which - 1) {
+            const int r = __builtin_ctz(which);
+            float x[V];
+            get(r, x);
+            at.store_floats(to, scan_number(numbers[r]), d, x);
+        }
+    }
+};
+
+// The same value, of which the compiler does not know that it is: what an earlier pass worked out of it is worked out again instead of being kept.
+template <typename X> __device__ __forceinline__ void scan_anew(X &x) { asm volatile("" : "+v"(x)); }
 
 // f(whether there is something that makes rows special)
 template <typename F>
@@ -412,252 +465,270 @@ __device__ __forceinline__ bool scan_gates(const unsigned (&fs)[SCAN_ROWS], floa
     return __any(least == 0.f);
 }
 
+// Where there are no rows: what goes into the sequences comes out.
+static __global__ __launch_bounds__(256) void scan_nothing(const ScanOrder o, const float *in, float *out, int64_t d, int *flags)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < o.count * d; i += (int64_t)gridDim.x * 256) {
+        if (out) out[i] = in ? in[i] : 0.f;
+        if (flags && i % d == 0 && (o.at(i / d) != 0 || o.at(i / d + 1) != 0)) atomicOr(flags, FLAG_OFFSETS);
+    }
+}
+
 template <typename T, bool PACKED>
-__global__ __launch_bounds__(SCAN_THREADS, 4) void scan_forward(const Scan<T, PACKED> a)
+__global__ __launch_bounds__(SCAN_THREADS, SCAN_FORWARD_HELD) void scan_forward(const Scan<T, PACKED> a)
 {
     constexpr int V = SCAN_V<T, false>;
-    __shared__ ScanMarks marks;
-    __shared__ ScanProduct products[SCAN_WAVES][V][64];
-    __shared__ float into[V][64];
-    unsigned q, block;
-    scan_unit(a, q, block);
+    __shared__ ScanShared<V> told;
+    __shared__ ScanEdges<V> all_edges[SCAN_WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    ScanEdges<V> &edges = all_edges[wave];
+    const unsigned block = blockIdx.x % a.blocks, q = scan_tile(a, block);
     const ScanLane<T, V> at(block, a.d);
     const int64_t n = a.order.n, t0 = (int64_t)q * SCAN_TILE + wave * SCAN_ROWS;
+    // (wavefronts behind the last row have that one, as rows of no sequence, and store nothing)
     const int many = (int)(n - t0 < SCAN_ROWS ? n - t0 < 0 ? 0 : n - t0 : SCAN_ROWS);
-    unsigned fs[SCAN_ROWS], us[SCAN_ROWS];
-    if (many > 0) {
-        at.load(a.f + t0 * a.ldf, a.ldf, many, fs);
-        a.u.load(t0, a.d, many, at, us);
-    }
-    scan_mark(a.order, marks, q, a.tiles, block, a.flags, [&](int64_t j) {
+    const int64_t from = many > 0 ? t0 : n - 1;
+    unsigned fs[SCAN_ROWS];
+    typename ScanInput<T, PACKED>::Raw us;
+    at.load(a.f + from * a.ldf, a.ldf, many, fs);
+    a.u.load(from, a.d, many, at, us);
+    scan_mark(a.order, told.marks, q, a.tiles, block, a.flags, [&](int64_t j) {
         float h[V];
         if (!a.last) return;
         at.load_floats(a.h0, j, a.d, h);
         at.store_floats(a.last, j, a.d, h);
     });
     __syncthreads();
-    const ScanRows rows(a.order, marks, t0, wave * SCAN_ROWS);
+    const ScanRows rows(a.order, told.marks, t0, wave * SCAN_ROWS);
+    edges.fetch(rows.starts, told.marks.start + wave * SCAN_ROWS, a.h0, a.d, at);
     // every row as h = A h + B, the first one of a sequence with A = 0, and with it those of none
     float A[SCAN_ROWS][V], B[SCAN_ROWS][V];
+    const bool closed = scan_gates<T, V>(fs, A) || rows.none;
+#pragma unroll
+    for (int r = 0; r < SCAN_ROWS; ++r) {
+        float u[V];
+        a.u.values(us, r, u);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const GateShares g = gate_shares(A[r][v]);
+            A[r][v] = g.a;
+            B[r][v] = share_of<true>(g.c, u[v]);
+        }
+        if (rows.starts >> r & 1) {
+            float h[V];
+            edges.get(r, h);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                B[r][v] = gate_step<true>(A[r][v], h[v], B[r][v]);
+                A[r][v] = 0.f;
+            }
+        }
+    }
+    if (rows.none)
+#pragma unroll
+        for (int r = 0; r < SCAN_ROWS; ++r)
+            if (rows.none >> r & 1)
+#pragma unroll
+                for (int v = 0; v < V; ++v) A[r][v] = B[r][v] = 0.f;
     ScanProduct p[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = {1.f, 0.f};
-    bool closed = false;
-    if (many > 0) {
-        closed = scan_gates<T, V>(fs, A);
+    scan_rows(closed, [&](auto special) {
 #pragma unroll
         for (int r = 0; r < SCAN_ROWS; ++r) {
-            float u[V];
-            a.u.values(us[r], u);
+            if (rows.starts >> r & 1)
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const GateShares g = gate_shares(A[r][v]);
-                A[r][v] = g.a;
-                B[r][v] = share_of<true>(g.c, u[v]);
-            }
-            if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                for (int v = 0; v < V; ++v) p[v] = {0.f, 0.f};
+#pragma unroll
+            for (int v = 0; v < V; ++v) p[v] = {p[v].a * A[r][v], gate_step<decltype(special)::value>(A[r][v], p[v].b, B[r][v])};
         }
-        if (rows.starts | rows.none) {
-            closed = true;
+    });
 #pragma unroll
-            for (int r = 0; r < SCAN_ROWS; ++r) {
-                if (rows.starts >> r & 1) {
-                    float h[V];
-                    at.load_floats(a.h0, scan_number(marks.start[wave * SCAN_ROWS + r]), a.d, h);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) B[r][v] = gate_step<true>(A[r][v], h[v], B[r][v]);
-                }
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    if ((rows.starts | rows.none) >> r & 1) A[r][v] = 0.f;
-                    if (rows.none >> r & 1) B[r][v] = 0.f;
-                }
-            }
-        }
-        scan_rows(closed, [&](auto special) {
-#pragma unroll
-            for (int r = 0; r < SCAN_ROWS; ++r)
-#pragma unroll
-                for (int v = 0; v < V; ++v) p[v] = {p[v].a * A[r][v], gate_step<decltype(special)::value>(A[r][v], p[v].b, B[r][v])};
-        });
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) products[wave][v][lane] = p[v];
+    for (int v = 0; v < V; ++v) told.products[wave][v][lane] = p[v];
     __syncthreads();
     if (wave == 0) {
         float x[V] = {};
-        if (a.ticket) {
+        if (a.tickets) {
             ScanProduct own[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 own[v] = p[v];
 #pragma unroll
-                for (int w = 1; w < SCAN_WAVES; ++w) own[v] = products[w][v][lane].after(own[v]);
+                for (int w = 1; w < SCAN_WAVES; ++w) own[v] = told.products[w][v][lane].after(own[v]);
             }
-            scan_hand<T, PACKED, V>(a, q, block, marks.from, own, x);
+            scan_hand<T, PACKED, V>(a, q, block, told.marks.from, own, x);
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) into[v][lane] = x[v];
+        for (int v = 0; v < V; ++v) told.into[v][lane] = x[v];
     }
     __syncthreads();
     if (many == 0) return;
     float h[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = into[v][lane];
+    for (int v = 0; v < V; ++v) h[v] = told.into[v][lane];
     for (int w = 0; w < wave; ++w)
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = products[w][v][lane].of(h[v]);
+        for (int v = 0; v < V; ++v) h[v] = told.products[w][v][lane].of(h[v]);
     if (a.states) {
         float enters[V];
-        if (rows.starts & 1) at.load_floats(a.h0, scan_number(marks.start[wave * SCAN_ROWS]), a.d, enters);
-        else
 #pragma unroll
-            for (int v = 0; v < V; ++v) enters[v] = rows.none & 1 ? 0.f : h[v];
+        for (int v = 0; v < V; ++v) enters[v] = rows.none & 1 ? 0.f : h[v];
+        if (rows.starts & 1) edges.get(0, enters);
         at.store_floats(a.states, t0 / SCAN_KEPT, a.d, enters);
     }
+    const unsigned ends = a.last ? rows.ends : 0;
     T *y = a.y + t0 * a.ldy + at.first;
-    scan_rows(closed || (rows.ends && a.last) || !at.full, [&](auto special) {
-        constexpr bool SPECIAL = decltype(special)::value;
+    if (at.here())
+        scan_rows(closed || many < SCAN_ROWS, [&](auto special) {
+            constexpr bool SPECIAL = decltype(special)::value;
 #pragma unroll
-        for (int r = 0; r < SCAN_ROWS; ++r) {
-            if (SPECIAL && r >= many) break;
+            for (int r = 0; r < SCAN_ROWS; ++r) {
+                if (SPECIAL && r >= many) break;
+                if (rows.starts >> r & 1)
 #pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = gate_step<SPECIAL>(A[r][v], h[v], B[r][v]);
-            at.template store<!SPECIAL>(y, h);
-            y += a.ldy;
-            if (SPECIAL && (rows.ends >> r & 1) && a.last) at.store_floats(a.last, scan_number(marks.end[wave * SCAN_ROWS + r]), a.d, h);
-        }
-    });
+                    for (int v = 0; v < V; ++v) h[v] = 0.f;
+#pragma unroll
+                for (int v = 0; v < V; ++v) h[v] = gate_step<SPECIAL>(A[r][v], h[v], B[r][v]);
+                at.store(y, h);
+                y += a.ldy;
+                if (ends >> r & 1) edges.put(r, h);
+            }
+        });
+    edges.store(ends, told.marks.end + wave * SCAN_ROWS, a.last, a.d, at);
 }
 
 template <typename T, bool PACKED>
-__global__ __launch_bounds__(SCAN_THREADS, 3) void scan_backward(const Scan<T, PACKED> a)
+__global__ __launch_bounds__(SCAN_THREADS, SCAN_BACKWARD_HELD) void scan_backward(const Scan<T, PACKED> a)
 {
     constexpr int V = SCAN_V<T, true>;
-    __shared__ ScanMarks marks;
-    __shared__ ScanProduct products[SCAN_WAVES][V][64];
-    __shared__ float into[V][64];
-    unsigned q, block;
-    scan_unit(a, q, block);
+    __shared__ ScanShared<V> told;
+    __shared__ ScanEdges<V> all_edges[SCAN_WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    ScanEdges<V> &edges = all_edges[wave];
+    const unsigned block = blockIdx.x % a.blocks, q = scan_tile(a, block), tile = a.tiles - 1 - q;
     const ScanLane<T, V> at(block, a.d);
-    const unsigned tile = a.tiles - 1 - q;
     const int64_t n = a.order.n, t0 = (int64_t)tile * SCAN_TILE + wave * SCAN_ROWS;
     const int many = (int)(n - t0 < SCAN_ROWS ? n - t0 < 0 ? 0 : n - t0 : SCAN_ROWS);
-    unsigned fs[SCAN_ROWS], us[SCAN_ROWS], dys[SCAN_ROWS];
-    float h[V] = {};
-    if (many > 0) {
-        at.load(a.f + t0 * a.ldf, a.ldf, many, fs);
-        a.u.load(t0, a.d, many, at, us);
-        at.load_floats(a.states, t0 / SCAN_KEPT, a.d, h);
-        at.load(a.dy + t0 * a.lddy, a.lddy, many, dys);
-    }
-    scan_mark(a.order, marks, tile, a.tiles, block, a.flags, [&](int64_t j) {
+    const int64_t from = many > 0 ? t0 : n - 1;
+    unsigned fs[SCAN_ROWS], dys[SCAN_ROWS];
+    typename ScanInput<T, PACKED>::Raw us;
+    float h[V];
+    at.load(a.f + from * a.ldf, a.ldf, many, fs);
+    a.u.load(from, a.d, many, at, us);
+    at.load_floats(a.states, from / SCAN_KEPT, a.d, h);
+    at.load(a.dy + from * a.lddy, a.lddy, many, dys);
+    scan_mark(a.order, told.marks, tile, a.tiles, block, a.flags, [&](int64_t j) {
         float x[V];
         if (!a.dh0) return;
         at.load_floats(a.dlast, j, a.d, x);
         at.store_floats(a.dh0, j, a.d, x);
     });
     __syncthreads();
-    const ScanRows rows(a.order, marks, t0, wave * SCAN_ROWS);
-    auto last_gradient = [&](int r, float (&x)[V]) { at.load_floats(a.dlast, scan_number(marks.end[wave * SCAN_ROWS + r]), a.d, x); };
-    float A[SCAN_ROWS][V], C[SCAN_ROWS][V], wide[SCAN_ROWS][V];          // shares, and h_{t-1} - u_t; rows of no sequence have none
+    const ScanRows rows(a.order, told.marks, t0, wave * SCAN_ROWS);
+    edges.fetch(rows.starts, told.marks.start + wave * SCAN_ROWS, a.h0, a.d, at);
+    float g[SCAN_ROWS][V], wide[SCAN_ROWS][V];       // gates, and h_{t-1} - u_t
+    const bool closed = scan_gates<T, V>(fs, g) || rows.none;
+#pragma unroll
+    for (int r = 0; r < SCAN_ROWS; ++r) {
+        float u[V];
+        if (rows.starts >> r & 1) edges.get(r, h);
+        a.u.values(us, r, u);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const GateShares shares = gate_shares(g[r][v]);
+            wide[r][v] = h[v] - u[v];
+            h[v] = gate_step<true>(shares.a, h[v], share_of<true>(shares.c, u[v]));
+        }
+    }
+    edges.fetch(rows.ends, told.marks.end + wave * SCAN_ROWS, a.dlast, a.d, at);
+#pragma unroll
+    for (int r = 0; r < SCAN_ROWS; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v) scan_anew(g[r][v]);
     // x: what goes from a row to the one before, a G
     ScanProduct p[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = {1.f, 0.f};
-    bool closed = false;
-    if (many > 0) {
-        closed = scan_gates<T, V>(fs, A) || rows.none;
+    scan_rows(closed, [&](auto special) {
+        constexpr bool SPECIAL = decltype(special)::value;
 #pragma unroll
-        for (int r = 0; r < SCAN_ROWS; ++r) {
-            float u[V];
-            if (rows.starts >> r & 1) at.load_floats(a.h0, scan_number(marks.start[wave * SCAN_ROWS + r]), a.d, h);
-            a.u.values(us[r], u);
+        for (int r = SCAN_ROWS - 1; r >= 0; --r) {
+            float dy[V];
+            if (rows.ends >> r & 1) {
+                float x[V];
+                edges.get(r, x);
+#pragma unroll
+                for (int v = 0; v < V; ++v) p[v] = {0.f, x[v]};
+            }
+            at.values(dys[r], dy);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const GateShares g = gate_shares(A[r][v]);
-                A[r][v] = g.a;
-                C[r][v] = g.c;
-                wide[r][v] = h[v] - u[v];
-                h[v] = gate_step<true>(g.a, h[v], share_of<true>(g.c, u[v]));
+                const float share = gate_shares(g[r][v]).a;
+                p[v] = {p[v].a * share, share_of<SPECIAL>(share, p[v].b + dy[v])};
+                if (SPECIAL && (rows.none >> r & 1)) p[v] = {0.f, 0.f};
             }
-            if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
-        if (rows.none) {
+    });
 #pragma unroll
-            for (int r = 0; r < SCAN_ROWS; ++r)
-                if (rows.none >> r & 1)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) A[r][v] = C[r][v] = 0.f;
-        }
-        scan_rows(closed || rows.ends, [&](auto special) {
-            constexpr bool SPECIAL = decltype(special)::value;
-#pragma unroll
-            for (int r = SCAN_ROWS - 1; r >= 0; --r) {
-                if (SPECIAL && (rows.ends >> r & 1)) {
-                    float x[V];
-                    last_gradient(r, x);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) p[v] = {0.f, x[v]};
-                }
-                float dy[V];
-                at.values(dys[r], dy);
-#pragma unroll
-                for (int v = 0; v < V; ++v) p[v] = {p[v].a * A[r][v], share_of<SPECIAL>(A[r][v], p[v].b + dy[v])};
-            }
-        });
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) products[wave][v][lane] = p[v];
+    for (int v = 0; v < V; ++v) told.products[wave][v][lane] = p[v];
     __syncthreads();
     if (wave == SCAN_WAVES - 1) {
         float x[V] = {};
-        if (a.ticket) {
+        if (a.tickets) {
             ScanProduct own[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 own[v] = p[v];
 #pragma unroll
-                for (int w = SCAN_WAVES - 2; w >= 0; --w) own[v] = products[w][v][lane].after(own[v]);
+                for (int w = SCAN_WAVES - 2; w >= 0; --w) own[v] = told.products[w][v][lane].after(own[v]);
             }
-            scan_hand<T, PACKED, V>(a, q, block, a.tiles - 1 - marks.to, own, x);
+            scan_hand<T, PACKED, V>(a, q, block, a.tiles - 1 - told.marks.to, own, x);
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) into[v][lane] = x[v];
+        for (int v = 0; v < V; ++v) told.into[v][lane] = x[v];
     }
     __syncthreads();
     if (many == 0) return;
+#pragma unroll
+    for (int r = 0; r < SCAN_ROWS; ++r) {            // (not kept from the pass above)
+        scan_anew(dys[r]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) scan_anew(g[r][v]);
+    }
     float x[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) x[v] = into[v][lane];
+    for (int v = 0; v < V; ++v) x[v] = told.into[v][lane];
     for (int w = SCAN_WAVES - 1; w > wave; --w)
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = products[w][v][lane].of(x[v]);
+        for (int v = 0; v < V; ++v) x[v] = told.products[w][v][lane].of(x[v]);
+    const unsigned starts = a.dh0 ? rows.starts : 0;
     T *df_row = a.df + (t0 + many - 1) * a.lddf + at.first, *du_row = a.du + (t0 + many - 1) * a.lddu + at.first;
-    scan_rows(closed || rows.starts || rows.ends || !at.full, [&](auto special) {
-        constexpr bool SPECIAL = decltype(special)::value;
+    if (at.here())
+        scan_rows(closed || many < SCAN_ROWS, [&](auto special) {
+            constexpr bool SPECIAL = decltype(special)::value;
 #pragma unroll
-        for (int r = SCAN_ROWS - 1; r >= 0; --r) {
-            if (SPECIAL && r >= many) continue;
-            if (SPECIAL && (rows.ends >> r & 1)) last_gradient(r, x);
-            float dy[V], df[V], du[V];
-            at.values(dys[r], dy);
+            for (int r = SCAN_ROWS - 1; r >= 0; --r) {
+                if (SPECIAL && r >= many) continue;
+                if (rows.ends >> r & 1) edges.get(r, x);
+                float dy[V], df[V], du[V];
+                at.values(dys[r], dy);
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float G = x[v] + dy[v];
-                df[v] = share_of<SPECIAL>(A[r][v] * C[r][v], G * wide[r][v]);
-                du[v] = share_of<SPECIAL>(C[r][v], G);
-                x[v] = share_of<SPECIAL>(A[r][v], G);
+                for (int v = 0; v < V; ++v) {
+                    const float G = x[v] + dy[v];
+                    const GateShares shares = gate_shares(g[r][v]);
+                    df[v] = share_of<SPECIAL>(shares.a * shares.c, G * wide[r][v]);
+                    du[v] = share_of<SPECIAL>(shares.c, G);
+                    x[v] = share_of<SPECIAL>(shares.a, G);
+                    if (SPECIAL && (rows.none >> r & 1)) df[v] = du[v] = x[v] = 0.f;
+                }
+                at.store(df_row, df);
+                at.store(du_row, du);
+                df_row -= a.lddf;
+                du_row -= a.lddu;
+                if (starts >> r & 1) edges.put(r, x);
             }
-            at.template store<!SPECIAL>(df_row, df);
-            at.template store<!SPECIAL>(du_row, du);
-            df_row -= a.lddf;
-            du_row -= a.lddu;
-            if (SPECIAL && (rows.starts >> r & 1) && a.dh0) at.store_floats(a.dh0, scan_number(marks.start[wave * SCAN_ROWS + r]), a.d, x);
-        }
-    });
+        });
+    edges.store(starts, told.marks.start + wave * SCAN_ROWS, a.dh0, a.d, at);
 }
 
 // state = a state + (1 - a) u, y = state, one row of every sequence.  A thread has one vector of a row.

@@ -89,10 +89,10 @@ template <typename T, bool PACKED> ScanInput<T, PACKED> scan_input(const void *u
     else return {(const T *)u, ldu};
 }
 
-// Tiles, and what workgroups hand on in the workspace: a ticket, then words.
+// Tiles, and what workgroups hand on in the workspace: tickets, then words.
 struct ScanPlan {
     int64_t tiles, blocks, words;
-    unsigned *ticket;
+    unsigned *tickets;
     unsigned long long *products, *groups, *handed;
     size_t bytes;
 };
@@ -107,7 +107,7 @@ ScanPlan scan_plan(int64_t n, int64_t d, int32_t type, bool backward, void *work
     if (p.tiles > 1) {
         const int64_t line = p.blocks * columns, groups = ceil_div(p.tiles, SCAN_GROUP), runs = ceil_div(p.tiles, SCAN_RUN);
         p.words = (p.tiles + groups + runs) * line;
-        p.ticket = c.take<unsigned>(1);
+        p.tickets = c.take<unsigned>(p.blocks * SCAN_TICKET);
         p.products = c.take<unsigned long long>(p.words);
         p.groups = p.products + p.tiles * line;
         p.handed = p.groups + groups * line;
@@ -120,15 +120,21 @@ ScanPlan scan_plan(int64_t n, int64_t d, int32_t type, bool backward, void *work
 template <typename T, bool PACKED>
 int run_scan(Scan<T, PACKED> a, int32_t type, bool backward, void *workspace, hipStream_t stream)
 {
+    if (a.order.n == 0) {
+        if (a.order.count == 0) return CHICLE_OK;
+        scan_nothing<<<(unsigned)std::min<int64_t>(ceil_div(a.order.count * a.d, 256), 16384), 256, 0, stream>>>(a.order, backward ? a.dlast : a.h0,
+                                                                                                               backward ? a.dh0 : a.last, a.d, a.flags);
+        return launched("scan_nothing");
+    }
     const ScanPlan p = scan_plan(a.order.n, a.d, type, backward, workspace);
     a.tiles = (unsigned)p.tiles;
     a.blocks = (unsigned)p.blocks;
     if (p.tiles > 1) {
-        a.ticket = p.ticket;
+        a.tickets = p.tickets;
         a.products = p.products;
         a.groups = p.groups;
         a.handed = p.handed;
-        scan_begin<<<(unsigned)std::min<int64_t>(ceil_div(p.words, 256), 2048), 256, 0, stream>>>(p.ticket, p.products, p.words);
+        scan_begin<<<(unsigned)std::min<int64_t>(ceil_div(p.words, 256), 2048), 256, 0, stream>>>(p.tickets, a.blocks, p.products, p.words);
         TRY(launched("scan_begin"));
     }
     const unsigned grid = (unsigned)(p.tiles * p.blocks);
@@ -290,7 +296,6 @@ int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, co
     if (ldy < d) return fail(CHICLE_EINVAL, "a row distance is shorter than a row");
     if ((n > 0 && !placed(y, size_of(type))) || (last && !placed(last, 4))) return fail(CHICLE_EINVAL, "a null or misplaced pointer");
     TRY(check_workspace(workspace, workspace_bytes, chicle_gated_scan_bytes(n, d, type)));
-    if (sequences == 0 && n == 0) return CHICLE_OK;
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
         return with_packed(u_scales != nullptr, [&](auto packed) {
@@ -317,7 +322,6 @@ int chicle_gated_scan_grad(const void *f, int64_t ldf, const void *u, int64_t ld
     if ((n > 0 && (!placed(dy, s) || !placed(df, s) || !placed(du, s) || !states)) || (dlast && !placed(dlast, 4)) || (dh0 && !placed(dh0, 4)))
         return fail(CHICLE_EINVAL, "a null or misplaced pointer");
     TRY(check_workspace(workspace, workspace_bytes, chicle_gated_scan_bytes(n, d, type)));
-    if (sequences == 0 && n == 0) return CHICLE_OK;
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
         return with_packed(u_scales != nullptr, [&](auto packed) {
