@@ -39,64 +39,67 @@ template <bool CLOSED> __device__ __forceinline__ float share_of(float share, fl
 // a h + b
 template <bool CLOSED> __device__ __forceinline__ float gate_step(float a, float h, float b) { return CLOSED && a == 0.f ? b : fmaf(a, h, b); }
 
-constexpr int SCAN_ROWS = SCAN_KEPT, SCAN_WAVES = 4, SCAN_THREADS = 64 * SCAN_WAVES;
-constexpr int SCAN_TILE = SCAN_ROWS * SCAN_WAVES;        // rows of a workgroup's tile
-constexpr int SCAN_FORWARD_HELD = 4, SCAN_BACKWARD_HELD = 3;            // workgroups of a compute unit, as registers allow
+// A lane has 32 values of every input: of 16 bits two columns, so that it reads four bytes of a row, and half as many rows.
+template <typename T, bool BACKWARD> struct ScanShape {
+    static constexpr int V = BACKWARD ? 1 : 4 / (int)sizeof(T), COLS = 64 * V, ROWS = SCAN_KEPT / V;
+    static constexpr int WAVES = 4 * V, THREADS = 64 * WAVES, TILE = ROWS * WAVES;
+    static constexpr int HELD = V == 1 ? 3 : 4;          // wavefronts of a SIMD, as registers allow
+};
 constexpr int SCAN_GROUP = 8, SCAN_RUN = 64;             // tiles whose products are joined, and tiles from one state that is handed on to the next
-// Columns of a lane: forward two of 16 bits; backward, where a row takes four registers a column, one.
-template <typename T, bool BACKWARD> constexpr int SCAN_V = 1;
-
 constexpr int SCAN_TICKET = 32;                          // places from one column block's ticket to the next: lines of their own
 
 typedef unsigned u32_at_2 __attribute__((aligned(2)));
 
 // A lane's columns of a tile, counted from the tile's first: rows are given by uniform pointers to that one.  Lanes past the last column read
 // some column that is there and store nothing.
-template <typename T, int V> struct ScanLane {
-    static constexpr int COLS = 64 * V;
-    typedef typename std::conditional<V * sizeof(T) == 4, unsigned, uint16_t>::type word;
+template <typename T, typename S> struct ScanLane {
+    static constexpr int V = S::V, ROWS = S::ROWS;
     int64_t first;                           // the tile's first column
     int e, left;                             // the lane's first column; columns from the tile's first to the last one, or the tile's
-    bool full, odd;                          // all columns are there; the last one has no neighbour (16 bits)
-    __device__ __forceinline__ ScanLane(int64_t block, int64_t d) : first(block * COLS), e((threadIdx.x & 63) * V)
+    __device__ __forceinline__ ScanLane(int64_t block, int64_t d) : first(block * S::COLS), e((threadIdx.x & 63) * V)
     {
-        left = d - first < COLS ? (int)(d - first) : COLS;
-        full = left == COLS;
-        odd = V == 2 && (left & 1);
+        left = d - first < S::COLS ? (int)(d - first) : S::COLS;
     }
-    // The lane's values of SCAN_ROWS rows: the last of `many` again in place of those that are not there.
+    __device__ __forceinline__ bool here() const { return e < left; }
+    __device__ __forceinline__ bool odd() const { return V == 2 && (left & 1); }          // the last column has no neighbour
+    // The lane's values of a wavefront's rows: the last of `many` again in place of those that are not there.
     template <typename L> static __device__ __forceinline__ void each_row(int many, L load)
     {
 #pragma unroll
-        for (int r = 0; r < SCAN_ROWS; ++r) {
+        for (int r = 0; r < ROWS; ++r) {
             asm volatile("" : "+s"(many));               // (one row's pointer after the other: all of them at once are too many scalars)
             load(r, r + 1 < many);
         }
     }
-    __device__ __forceinline__ void load(const T *row, int64_t ld, int many, unsigned (&out)[SCAN_ROWS]) const
+    __device__ __forceinline__ void load(const T *row, int64_t ld, int many, unsigned (&out)[ROWS]) const
     {
         const T *p = row + first;
         if constexpr (V == 1) {
+            typedef typename std::conditional<sizeof(T) == 4, unsigned, uint16_t>::type word;
             const unsigned off = e < left ? e : left - 1;
             each_row(many, [&](int r, bool further) {
                 out[r] = __builtin_nontemporal_load((const word *)p + off);
                 p += further ? ld : 0;
             });
-        } else if (odd) {
-            const unsigned off = e < left ? e : left - 1, next = e + 1 < left ? e + 1 : left - 1;
-            each_row(many, [&](int r, bool further) {
-                out[r] = ((const uint16_t *)p)[off] | (unsigned)((const uint16_t *)p)[next] << 16;
-                p += further ? ld : 0;
-            });
-        } else {
-            const unsigned off = e < left ? e : left - 2;
+        } else if (left > 1) {
+            // (a column that has no neighbour comes with the one before it)
+            const unsigned off = e + 1 < left ? e : left - 2;
             each_row(many, [&](int r, bool further) {
                 out[r] = __builtin_nontemporal_load((const u32_at_2 *)(p + off));
                 p += further ? ld : 0;
             });
-        }
+            if (odd()) {
+                const int bits = e + 1 == left ? 16 : 0;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) out[r] >>= bits;
+            }
+        } else
+            each_row(many, [&](int r, bool further) {
+                out[r] = *(const uint16_t *)p;
+                p += further ? ld : 0;
+            });
     }
-    static __device__ __forceinline__ void values(unsigned x, float *out)
+    static __device__ __forceinline__ void values(unsigned x, float (&out)[V])
     {
         if constexpr (sizeof(T) == 4) out[0] = __uint_as_float(x);
         else if constexpr (__is_same(T, bf16)) {
@@ -109,17 +112,26 @@ template <typename T, int V> struct ScanLane {
             for (int i = 0; i < V; ++i) out[i] = (float)v[i];
         }
     }
-    __device__ __forceinline__ bool here() const { return e < left; }
-    // `row`: the tile's first column; only lanes that have one
-    __device__ __forceinline__ void store(T *row, const float *in) const { __builtin_nontemporal_store((T)in[0], row + (unsigned)e); }
+    // `row`: the tile's first column; only lanes that have one.  EDGE: the last column may have no neighbour.
+    template <bool EDGE> __device__ __forceinline__ void store(T *row, const float (&in)[V]) const
+    {
+        if constexpr (V == 1) __builtin_nontemporal_store((T)in[0], row + (unsigned)e);
+        else {
+            T v[2] = {(T)in[0], (T)in[1]};
+            unsigned x;
+            __builtin_memcpy(&x, v, 4);
+            if (EDGE && e + 1 == left) row[(unsigned)e] = v[0];
+            else __builtin_nontemporal_store(x, (u32_at_2 *)(row + (unsigned)e));
+        }
+    }
     // Row j of floats (of a null pointer: zeros).
-    __device__ __forceinline__ void load_floats(const float *p, int64_t j, int64_t d, float *out) const
+    __device__ __forceinline__ void load_floats(const float *p, int64_t j, int64_t d, float (&out)[V]) const
     {
         const float *row = p + j * d + first;
 #pragma unroll
         for (int v = 0; v < V; ++v) out[v] = p ? row[(unsigned)(e + v < left ? e + v : left - 1)] : 0.f;
     }
-    __device__ __forceinline__ void store_floats(float *p, int64_t j, int64_t d, const float *in) const
+    __device__ __forceinline__ void store_floats(float *p, int64_t j, int64_t d, const float (&in)[V]) const
     {
         float *row = p + j * d + first;
 #pragma unroll
@@ -128,41 +140,47 @@ template <typename T, int V> struct ScanLane {
     }
 };
 
-// The second input's rows, of T or packed: what a lane asks for of SCAN_ROWS of them, and its values.
+// The second input's rows, of T or packed: what a lane asks for of a wavefront's rows, and its values.
 template <typename T, bool PACKED> struct ScanInput;
 template <typename T> struct ScanInput<T, false> {
-    struct Raw { unsigned x[SCAN_ROWS]; };
+    template <typename S> struct Raw { unsigned x[S::ROWS]; };
     const T *p;
     int64_t ld;
-    template <int V> __device__ __forceinline__ void load(int64_t row, int64_t, int many, const ScanLane<T, V> &at, Raw &out) const
+    template <typename S> __device__ __forceinline__ void load(int64_t row, int64_t, int many, const ScanLane<T, S> &at, Raw<S> &out) const
     {
         at.load(p + row * ld, ld, many, out.x);
     }
-    template <int V> static __device__ __forceinline__ void values(const Raw &raw, int r, float (&out)[V]) { ScanLane<T, V>::values(raw.x[r], out); }
+    template <typename S> static __device__ __forceinline__ void values(const Raw<S> &raw, int r, float (&out)[S::V]) { ScanLane<T, S>::values(raw.x[r], out); }
 };
 template <typename T> struct ScanInput<T, true> {
-    struct Raw { unsigned x[SCAN_ROWS], step; };         // step: of row lane / 2 and, of the tile's two groups, lane % 2
+    // step: a lane has the scale of one row and one of the tile's groups, row by row
+    template <typename S> struct Raw { unsigned x[S::ROWS], step; };
     const int8_t *q;
     const uint8_t *scales;
     int64_t ld;
-    template <int V> __device__ __forceinline__ void load(int64_t row, int64_t d, int many, const ScanLane<T, V> &at, Raw &out) const
+    template <typename S> __device__ __forceinline__ void load(int64_t row, int64_t d, int many, const ScanLane<T, S> &at, Raw<S> &out) const
     {
-        static_assert(V == 1 && SCAN_ROWS == 32 && PACK_GROUP == 32, "a lane for every scale");
+        constexpr int V = S::V, GROUPS = S::COLS / PACK_GROUP;
+        static_assert(GROUPS * S::ROWS == 64, "a lane for every scale");
         const int64_t whole = (d + PACK_GROUP - 1) / PACK_GROUP * PACK_GROUP - at.first;
-        const int left = whole < at.COLS ? (int)whole : at.COLS, lane = threadIdx.x & 63;
-        const unsigned off = at.e < left ? at.e : left - 1;
-        const int which = lane >> 1 < many ? lane >> 1 : many > 0 ? many - 1 : 0;
-        out.step = scales[(row + which) * (ld / PACK_GROUP) + at.first / PACK_GROUP + ((lane & 1) * PACK_GROUP < left ? lane & 1 : 0)];
+        const int left = whole < S::COLS ? (int)whole : S::COLS, lane = threadIdx.x & 63;
+        const unsigned off = at.e < left ? at.e : left - V;
+        const int r = lane / GROUPS, which = r < many ? r : many > 0 ? many - 1 : 0, group = lane % GROUPS;
+        out.step = scales[(row + which) * (ld / PACK_GROUP) + at.first / PACK_GROUP + (group * PACK_GROUP < left ? group : 0)];
         const uint8_t *p = (const uint8_t *)q + row * ld + at.first;
-        at.each_row(many, [&](int r, bool further) {
-            out.x[r] = __builtin_nontemporal_load(p + off);
+        at.each_row(many, [&](int i, bool further) {
+            if constexpr (V == 1) out.x[i] = __builtin_nontemporal_load(p + off);
+            else out.x[i] = __builtin_nontemporal_load((const uint16_t *)(p + off));
             p += further ? ld : 0;
         });
     }
-    template <int V> static __device__ __forceinline__ void values(const Raw &raw, int r, float (&out)[V])
+    template <typename S> static __device__ __forceinline__ void values(const Raw<S> &raw, int r, float (&out)[S::V])
     {
-        const int from = 2 * r + ((threadIdx.x & 63) >> 5);
-        out[0] = (float)(int8_t)raw.x[r] * pack_step((unsigned)__builtin_amdgcn_ds_bpermute(from * 4, (int)raw.step));
+        constexpr int GROUPS = S::COLS / PACK_GROUP;
+        const int from = GROUPS * r + (threadIdx.x & 63) / (64 / GROUPS);
+        const float step = pack_step((unsigned)__builtin_amdgcn_ds_bpermute(from * 4, (int)raw.step));
+#pragma unroll
+        for (int v = 0; v < S::V; ++v) out[v] = (float)(int8_t)(raw.x[r] >> (8 * v)) * step;
     }
 };
 
@@ -172,12 +190,29 @@ struct ScanOrder {
     int wide;
     int64_t count, n;
     __device__ __forceinline__ int64_t at(int64_t j) const { return offsets ? index_at(offsets, wide, j) : j == 0 ? 0 : n; }
-    // The same for a j that all lanes have in common: scalar loads, which do not wait behind the rows' loads.
-    __device__ __forceinline__ int64_t common(int64_t j) const
+    // The same for a j that all lanes have in common, the lower 32 bits: scalar loads, which do not wait behind the rows' loads.
+    __device__ __forceinline__ unsigned common(unsigned j) const
     {
-        if (!offsets) return j == 0 ? 0 : n;
-        if (wide) return ((const __attribute__((address_space(4))) int64_t *)offsets)[j];
-        return ((const __attribute__((address_space(4))) int32_t *)offsets)[j];
+        if (!offsets) return j == 0 ? 0u : (unsigned)n;
+        return ((const __attribute__((address_space(4))) unsigned *)offsets)[wide ? 2 * (int64_t)j : (int64_t)j];
+    }
+    // How many of the offsets are at most t.
+    __device__ __forceinline__ unsigned up_to(unsigned t) const
+    {
+        unsigned lo = 0, hi = (unsigned)count + 1;
+        while (lo < hi) {                                // (the distance shrinks, whatever the offsets are)
+            const unsigned step = (hi - lo + 7) >> 3;
+            unsigned many = 0;
+#pragma unroll
+            for (int k = 1; k <= 8; ++k) {
+                const unsigned j = lo + k * step - 1;
+                if (j < hi && common(j) <= t) ++many;
+            }
+            const unsigned next = lo + (many + 1) * step - 1;
+            lo = min(lo + many * step, hi);
+            hi = min(next, hi);
+        }
+        return lo;
     }
 };
 
@@ -232,92 +267,75 @@ __device__ __forceinline__ unsigned long long scan_wait(const unsigned long long
     return w;
 }
 
-// What the workgroup knows of its rows: where sequences begin and end among them (a sequence's number, or -1), which rows belong to none, and the
-// tile that the sequence of the first row (backwards: of the last one) begins (ends) in.
-struct ScanMarks {
-    int start[SCAN_TILE], end[SCAN_TILE];
-    unsigned from, to;
-};
-
-// How many of the offsets are at most t.  (In 32 bits, which is enough: hipcc 7.2 has been seen to take the condition of one choice between uniform
-// 64-bit numbers for that of the next.)
-__device__ __forceinline__ unsigned scan_count(const ScanOrder &o, int64_t t)
-{
-    unsigned lo = 0, hi = (unsigned)o.count + 1;
-    while (lo < hi) {                                    // (the distance shrinks, whatever the offsets are)
-        const unsigned step = (hi - lo + 3) >> 2;
-        unsigned many = 0;
-#pragma unroll
-        for (int k = 1; k <= 4; ++k) {
-            const unsigned j = lo + k * step - 1;
-            if (j < hi && o.common(j) <= t) ++many;
-        }
-        const unsigned next = lo + (many + 1) * step - 1;
-        lo = min(lo + many * step, hi);
-        hi = min(next, hi);
-    }
-    return lo;
-}
-
-// Marks the tile's rows.  `empty(j)` is called by whole wavefronts for the sequences without rows that lie in the tile.
-template <typename F>
-__device__ __forceinline__ void scan_mark(const ScanOrder &o, ScanMarks &m, unsigned tile, unsigned tiles, unsigned block, int *flags, F empty)
-{
-    const int64_t t0 = (int64_t)tile * SCAN_TILE, t1 = t0 + SCAN_TILE;
-    const bool last = tile + 1 == tiles;
-    for (int i = threadIdx.x; i < SCAN_TILE; i += SCAN_THREADS) m.start[i] = m.end[i] = -1;
-    if (threadIdx.x == 0) m.from = m.to = tile;
-    const unsigned first = scan_count(o, t0 - 1);        // offsets below the tile's first row
-    __syncthreads();
-    bool wrong = false, more = true;
-    for (int64_t j0 = first > 0 ? first - 1 : 0; more && j0 < o.count; j0 += SCAN_THREADS) {
-        const int64_t j = j0 + threadIdx.x;
-        bool none = false;
-        more = false;
-        if (j < o.count) {
-            const int64_t lo = o.at(j), hi = o.at(j + 1);
-            more = lo < t1 || last;
-            if (lo < 0 || hi < lo || hi > o.n) wrong = true;
-            else if (lo == hi) none = lo >= t0 && more;
-            else {
-                if (lo >= t0 && lo < t1) m.start[lo - t0] = (int)j;
-                if (hi > t0 && hi <= t1) m.end[hi - 1 - t0] = (int)j;
-                if (lo < t0 && hi > t0) m.from = (unsigned)(lo / SCAN_TILE);
-                if (lo < t1 && hi > t1) m.to = (unsigned)((hi - 1) / SCAN_TILE);
-            }
-        }
-        more = __any(more);                              // (offsets ascend: the lanes in front decide)
-        for (unsigned long long left = __ballot(none); left; left &= left - 1) empty(j0 + (threadIdx.x & ~63) + __builtin_ctzll(left));
-    }
-    if (block == 0)                                      // every offset is looked at by some tile
-        for (int64_t j = (int64_t)tile * SCAN_THREADS + threadIdx.x; j < o.count; j += (int64_t)tiles * SCAN_THREADS) {
-            const int64_t lo = o.at(j), hi = o.at(j + 1);
-            wrong |= lo < 0 || hi < lo || hi > o.n;
-        }
-    if (wrong && flags) atomicOr(flags, FLAG_OFFSETS);
-}
-
-// The wavefront's 32 rows in three masks.
+// What a wavefront knows of its rows: which of them are a sequence's first, a sequence's last, or of none, and in lane r the numbers of the sequences
+// that begin and end with row r.  Worked out with scalars while the rows are on their way; offsets that are no rows lead to wrong marks, but to
+// no place outside of the rows and the sequences.
 struct ScanRows {
     unsigned starts, ends, none;
-    __device__ __forceinline__ ScanRows(const ScanOrder &o, const ScanMarks &m, int64_t t, int row0)
+    int start, end;                          // of this lane's row
+    unsigned before, behind;                 // where the sequence of the first row begins, and that of the last one ends, if not with it; else ~0
+    template <typename S> __device__ __forceinline__ ScanRows(const ScanOrder &o, unsigned t0, S)
     {
-        const int lane = threadIdx.x & 63, r = row0 + (lane & 31);
-        const int64_t lo = o.common(0), hi = o.common(o.count), row = t + (lane & 31);
-        starts = (unsigned)__ballot(m.start[r] >= 0);
-        ends = (unsigned)__ballot(m.end[r] >= 0);
-        none = (unsigned)__ballot(row < lo || row >= hi || row >= o.n);
+        const unsigned t1 = t0 + S::ROWS, lane = threadIdx.x & 63, count = (unsigned)o.count;
+        starts = ends = 0;
+        start = end = 0;
+        before = behind = ~0u;
+        unsigned j = t0 > 0 ? o.up_to(t0 - 1) : 0;
+        if (j > 0 && j <= count && o.common(j) > t0) before = o.common(j - 1);
+        while (j <= count) {                             // (at most S::ROWS + 2 times, where offsets ascend)
+            const unsigned at = o.common(j);
+            if (at > t1) break;
+            // sequence j - 1 ends in front of row `at`, sequence k - 1 begins with it; those between have no rows
+            if (j > 0 && at - 1 - t0 < S::ROWS) {
+                ends |= 1u << (at - 1 - t0);
+                end = lane == at - 1 - t0 ? (int)j - 1 : end;
+            }
+            unsigned k = j + 1;
+            if (k <= count && o.common(k) <= at) k = max(k, o.up_to(at));
+            if (k <= count && at - t0 < S::ROWS) {
+                starts |= 1u << (at - t0);
+                start = lane == at - t0 ? (int)k - 1 : start;
+            }
+            j = k;
+        }
+        if (j > 0 && j <= count && o.common(j - 1) < t1) behind = o.common(j);
+        const unsigned lo = o.common(0), hi = min(o.common(count), (unsigned)o.n);
+        const unsigned all = S::ROWS == 32 ? ~0u : (1u << S::ROWS % 32) - 1;
+        const unsigned row = t0 + (lane & (S::ROWS - 1));
+        none = (unsigned)__ballot(row < lo || row >= hi) & all;
+        starts &= ~none;
+        ends &= ~none;
     }
 };
 
-// What comes into the q-th tile of a column block, in the order in which tiles are taken, from tile `from` on, whose product lets nothing through
-// (from = q: nothing comes in, the tile's own lets nothing through); tells what others need.  By one wavefront.
+// What sequences without rows get, each from one tile, and a look at all offsets.
+template <typename S, typename F>
+__device__ __forceinline__ void scan_empty(const ScanOrder &o, unsigned tile, unsigned tiles, bool check, int *flags, F empty)
+{
+    bool wrong = false;
+    for (int64_t j0 = (int64_t)tile * S::THREADS; j0 < o.count; j0 += (int64_t)tiles * S::THREADS) {
+        const int64_t j = j0 + threadIdx.x;
+        bool none = false;
+        if (j < o.count) {
+            const int64_t lo = o.at(j), hi = o.at(j + 1);
+            none = lo == hi;
+            wrong |= lo < 0 || hi < lo || hi > o.n;
+        }
+        for (unsigned long long left = __ballot(none); left; left &= left - 1) empty(j0 + (threadIdx.x & ~63) + __builtin_ctzll(left));
+    }
+    if (check && wrong && flags) atomicOr(flags, FLAG_OFFSETS);
+}
+
+// How states go from tile to tile of a column block, q being a tile's number in the order in which tiles are taken, and `from` the one whose product
+// lets nothing through that is needed (from >= q: nothing comes in, the tile's own product lets nothing through).
 //
-// A tile tells its product; the last one of SCAN_GROUP tiles tells theirs, joined; the last one of SCAN_RUN tiles hands on the state that comes out.  So a
-// tile reads at most SCAN_GROUP - 1 products, those of as many groups and a state, and a state goes through a long sequence in steps of SCAN_RUN
-// tiles, everything else of which has been joined by then.
+// A tile tells its product; the last one of SCAN_GROUP tiles tells theirs, joined; the last one of SCAN_RUN tiles hands on the state that comes out.  What
+// comes into a tile is, in this order, the state handed on from the run before, the products of the run's groups before its own (`far`), and those of
+// the tiles before it in its own (`near`): a state goes through a long sequence in steps of SCAN_RUN tiles, everything else of which has been joined
+// by then.  Three wavefronts look for the three.
 //
-// Tiles are taken in the order of their column block's tickets: whoever waits does so for tiles with earlier tickets, whose workgroups have begun.  These tell their products without waiting, groups once the products of the group are told, and states after all that is before them.
+// Tiles are taken in the order of their column block's tickets: whoever waits does so for tiles with earlier tickets, whose workgroups have begun.
+// These tell their products without waiting, groups once the products of the group are told, and states after all that is before them.
 // So every wait ends.  What is joined, and in which order, follows from the offsets alone.  A word is told whole, and says by itself whether it
 // has been.
 template <int V>
@@ -339,40 +357,37 @@ __device__ __forceinline__ void scan_join(const unsigned long long *words, int64
     }
 }
 
+// By the first wavefront: tells the tile's product and, with the last of the group, the group's.
 template <typename T, bool PACKED, int V>
-__device__ __forceinline__ void scan_hand(const Scan<T, PACKED> &a, unsigned q, unsigned block, unsigned from, const ScanProduct (&own)[V], float (&x)[V])
+__device__ __forceinline__ void scan_near(const Scan<T, PACKED> &a, unsigned q, unsigned block, unsigned from, const ScanProduct (&own)[V], ScanProduct (&near)[V])
 {
     const int64_t line = (int64_t)a.blocks * 64 * V, at = (int64_t)block * 64 * V + (threadIdx.x & 63);
-    const unsigned group = q / SCAN_GROUP, run = q / SCAN_RUN;
-    ScanProduct near[V], far[V];
+    const unsigned group = q / SCAN_GROUP;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        scan_tell(a.products + q * line + at + v * 64, own[v].word());
-        near[v] = far[v] = {1.f, 0.f};
-        x[v] = 0.f;
-    }
-    scan_join<V>(a.products + at, line, from > group * SCAN_GROUP ? from : group * SCAN_GROUP, q, near);
+    for (int v = 0; v < V; ++v) scan_tell(a.products + q * line + at + v * 64, own[v].word());
+    scan_join<V>(a.products + at, line, max(from, group * SCAN_GROUP), q, near);
     if (q % SCAN_GROUP == SCAN_GROUP - 1)
 #pragma unroll
         for (int v = 0; v < V; ++v) scan_tell(a.groups + group * line + at + v * 64, own[v].after(near[v]).word());
-    if (from < group * SCAN_GROUP) {
-        const unsigned first = run * (SCAN_RUN / SCAN_GROUP);
-        scan_join<V>(a.groups + at, line, from / SCAN_GROUP > first ? from / SCAN_GROUP : first, group, far);
-        if (from < run * SCAN_RUN) {
-            const unsigned long long *p = a.handed + (int64_t)(run - 1) * line + at;
-#pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = __uint_as_float((unsigned)scan_wait(p + v * 64, scan_look(p + v * 64)));
-        }
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        x[v] = near[v].after(far[v]).of(x[v]);
-        if (q % SCAN_RUN == SCAN_RUN - 1) scan_tell(a.handed + (int64_t)run * line + at + v * 64, __float_as_uint(own[v].of(x[v])));
-    }
 }
 
-// A sequence's number, the same in all lanes.
-__device__ __forceinline__ int64_t scan_number(int j) { return __builtin_amdgcn_readfirstlane(j); }
+template <typename T, bool PACKED, int V>
+__device__ __forceinline__ void scan_far(const Scan<T, PACKED> &a, unsigned q, unsigned block, unsigned from, ScanProduct (&far)[V])
+{
+    const int64_t line = (int64_t)a.blocks * 64 * V, at = (int64_t)block * 64 * V + (threadIdx.x & 63);
+    scan_join<V>(a.groups + at, line, max(from / SCAN_GROUP, q / SCAN_RUN * (SCAN_RUN / SCAN_GROUP)), q / SCAN_GROUP, far);
+}
+
+template <typename T, bool PACKED, int V>
+__device__ __forceinline__ void scan_handed(const Scan<T, PACKED> &a, unsigned q, unsigned block, unsigned from, float (&x)[V])
+{
+    const int64_t line = (int64_t)a.blocks * 64 * V;
+    const unsigned run = q / SCAN_RUN;
+    if (from >= run * SCAN_RUN) return;
+    const unsigned long long *p = a.handed + (int64_t)(run - 1) * line + (int64_t)block * 64 * V + (threadIdx.x & 63);
+#pragma unroll
+    for (int v = 0; v < V; ++v) x[v] = __uint_as_float((unsigned)scan_wait(p + v * 64, scan_look(p + v * 64)));
+}
 
 // What the workgroup's tile is: tickets, those of each column block for themselves, give tiles in the order in which workgroups begin.
 template <typename S> __device__ __forceinline__ unsigned scan_tile(const S &a, unsigned block)
@@ -385,15 +400,74 @@ template <typename S> __device__ __forceinline__ unsigned scan_tile(const S &a, 
 }
 
 // What the wavefronts of a workgroup tell one another.
-template <int V> struct ScanShared {
-    ScanMarks marks;
-    ScanProduct products[SCAN_WAVES][V][64];
-    float into[V][64];
+template <typename S> struct ScanShared {
+    static constexpr int V = S::V;
+    ScanProduct products[S::WAVES][V][64], own[V][64], near[V][64], far[V][64];
+    float handed[V][64], between[S::WAVES / 2][V][64];
+    unsigned from;
+    // What comes into the wavefront's rows.  p: its product; mine: `from` of the wavefront whose rows come first, backwards the last one's.  All
+    // wavefronts together.
+    template <bool BACKWARD, typename T, bool PACKED>
+    __device__ __forceinline__ void join(const Scan<T, PACKED> &a, unsigned q, unsigned block, unsigned mine, int wave, const ScanProduct (&p)[V], float (&x)[V])
+    {
+        const int lane = threadIdx.x & 63;
+        if (wave == (BACKWARD ? S::WAVES - 1 : 0)) from = mine;
+#pragma unroll
+        for (int v = 0; v < V; ++v) products[wave][v][lane] = p[v];
+        __syncthreads();
+        if (a.tickets) {
+            const unsigned first = __builtin_amdgcn_readfirstlane(from);
+            if (wave == 0) {
+                ScanProduct all[V], k[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    all[v] = products[BACKWARD ? S::WAVES - 1 : 0][v][lane];
+                    k[v] = {1.f, 0.f};
+#pragma unroll
+                    for (int w = 1; w < S::WAVES; ++w) all[v] = products[BACKWARD ? S::WAVES - 1 - w : w][v][lane].after(all[v]);
+                    own[v][lane] = all[v];
+                }
+                scan_near<T, PACKED, V>(a, q, block, first, all, k);
+#pragma unroll
+                for (int v = 0; v < V; ++v) near[v][lane] = k[v];
+            } else if (wave == 1) {
+                ScanProduct k[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) k[v] = {1.f, 0.f};
+                scan_far<T, PACKED, V>(a, q, block, first, k);
+#pragma unroll
+                for (int v = 0; v < V; ++v) far[v][lane] = k[v];
+            } else if (wave == 2) {
+                float k[V] = {};
+                scan_handed<T, PACKED, V>(a, q, block, first, k);
+#pragma unroll
+                for (int v = 0; v < V; ++v) handed[v][lane] = k[v];
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            x[v] = a.tickets ? near[v][lane].after(far[v][lane]).of(handed[v][lane]) : 0.f;
+            if (a.tickets && wave == S::WAVES - 1 && q % SCAN_RUN == SCAN_RUN - 1)
+                scan_tell(a.handed + ((int64_t)(q / SCAN_RUN) * a.blocks + block) * 64 * V + lane + v * 64, __float_as_uint(own[v][lane].of(x[v])));
+        }
+        // and what the wavefronts in front of this one do to it
+        if constexpr (BACKWARD) {
+            for (int w = S::WAVES - 1; w > wave; --w)
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[v] = products[w][v][lane].of(x[v]);
+        } else {
+            for (int w = 0; w < wave; ++w)
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[v] = products[w][v][lane].of(x[v]);
+        }
+    }
 };
 
 // States or gradients of sequences that begin or end among the wavefront's rows, each in the place of its row: a lane's own, read and written by no other.
-template <int V> struct ScanEdges {
-    float place[SCAN_ROWS][V][64];
+template <typename S> struct ScanEdges {
+    static constexpr int V = S::V;
+    float place[S::ROWS][V][64];
     __device__ __forceinline__ void get(int r, float (&x)[V]) const
     {
 #pragma unroll
@@ -404,8 +478,8 @@ template <int V> struct ScanEdges {
 #pragma unroll
         for (int v = 0; v < V; ++v) place[r][v][threadIdx.x & 63] = x[v];
     }
-    // Fetches them for the rows of `which`, whose sequences `numbers` has; zeros of a null pointer.
-    template <typename L> __device__ __forceinline__ void fetch(unsigned which, const int *numbers, const float *from, int64_t d, const L &at)
+    // Fetches them for the rows of `which`, whose sequences the lanes' numbers are; zeros of a null pointer.
+    template <typename L> __device__ __forceinline__ void fetch(unsigned which, int number, const float *from, int64_t d, const L &at)
     {
         constexpr int AHEAD = 4;
         while (which) {
@@ -413,8 +487,7 @@ template <int V> struct ScanEdges {
             unsigned left = which;
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
-                const int r = left ? __builtin_ctz(left) : 0;
-                if (left) at.load_floats(from, scan_number(numbers[r]), d, x[k]);
+                if (left) at.load_floats(from, __builtin_amdgcn_readlane(number, __builtin_ctz(left)), d, x[k]);
                 left &= left - 1;
             }
 #pragma unroll
@@ -424,13 +497,13 @@ template <int V> struct ScanEdges {
             }
         }
     }
-    template <typename L> __device__ __forceinline__ void store(unsigned which, const int *numbers, float *to, int64_t d, const L &at) const
+    template <typename L> __device__ __forceinline__ void store(unsigned which, int number, float *to, int64_t d, const L &at) const
     {
         for (; which; which &= which - 1) {
             const int r = __builtin_ctz(which);
             float x[V];
             get(r, x);
-            at.store_floats(to, scan_number(numbers[r]), d, x);
+            at.store_floats(to, __builtin_amdgcn_readlane(number, r), d, x);
         }
     }
 };
@@ -447,20 +520,20 @@ __device__ __forceinline__ void scan_rows(bool special, F f)
 }
 
 // The gates of the wavefront's rows, and whether one of them is closed.
-template <typename T, int V>
-__device__ __forceinline__ bool scan_gates(const unsigned (&fs)[SCAN_ROWS], float (&g)[SCAN_ROWS][V])
+template <typename T, typename S>
+__device__ __forceinline__ bool scan_gates(const unsigned (&fs)[S::ROWS], float (&g)[S::ROWS][S::V])
 {
     float least = 1.f;
 #pragma unroll
-    for (int r = 0; r < SCAN_ROWS; ++r) {
-        float f[V];
-        ScanLane<T, V>::values(fs[r], f);
+    for (int r = 0; r < S::ROWS; ++r) {
+        float f[S::V];
+        ScanLane<T, S>::values(fs[r], f);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
+        for (int v = 0; v < S::V; ++v) {
             g[r][v] = gate_of(f[v]);
             least = fminf(least, fabsf(g[r][v]));
         }
-        if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);               // (not all rows at once: there are no registers for that)
+        if (r % (4 / S::V) == 4 / S::V - 1) __builtin_amdgcn_sched_barrier(0);             // (not all rows at once: there are no registers for that)
     }
     return __any(least == 0.f);
 }
@@ -475,164 +548,146 @@ static __global__ __launch_bounds__(256) void scan_nothing(const ScanOrder o, co
 }
 
 template <typename T, bool PACKED>
-__global__ __launch_bounds__(SCAN_THREADS, SCAN_FORWARD_HELD) void scan_forward(const Scan<T, PACKED> a)
+__global__ __launch_bounds__((ScanShape<T, false>::THREADS), (ScanShape<T, false>::HELD)) void scan_forward(const Scan<T, PACKED> a)
 {
-    constexpr int V = SCAN_V<T, false>;
-    __shared__ ScanShared<V> told;
-    __shared__ ScanEdges<V> all_edges[SCAN_WAVES];
+    typedef ScanShape<T, false> S;
+    constexpr int V = S::V, ROWS = S::ROWS;
+    __shared__ ScanShared<S> told;
+    __shared__ ScanEdges<S> all_edges[S::WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    ScanEdges<V> &edges = all_edges[wave];
+    ScanEdges<S> &edges = all_edges[wave];
     const unsigned block = blockIdx.x % a.blocks, q = scan_tile(a, block);
-    const ScanLane<T, V> at(block, a.d);
-    const int64_t n = a.order.n, t0 = (int64_t)q * SCAN_TILE + wave * SCAN_ROWS;
+    const ScanLane<T, S> at(block, a.d);
+    const int64_t n = a.order.n, t0 = (int64_t)q * S::TILE + wave * ROWS;
     // (wavefronts behind the last row have that one, as rows of no sequence, and store nothing)
-    const int many = (int)(n - t0 < SCAN_ROWS ? n - t0 < 0 ? 0 : n - t0 : SCAN_ROWS);
+    const int many = (int)(n - t0 < ROWS ? n - t0 < 0 ? 0 : n - t0 : ROWS);
     const int64_t from = many > 0 ? t0 : n - 1;
-    unsigned fs[SCAN_ROWS];
-    typename ScanInput<T, PACKED>::Raw us;
+    unsigned fs[ROWS];
+    typename ScanInput<T, PACKED>::template Raw<S> us;
     at.load(a.f + from * a.ldf, a.ldf, many, fs);
     a.u.load(from, a.d, many, at, us);
-    scan_mark(a.order, told.marks, q, a.tiles, block, a.flags, [&](int64_t j) {
-        float h[V];
-        if (!a.last) return;
-        at.load_floats(a.h0, j, a.d, h);
-        at.store_floats(a.last, j, a.d, h);
-    });
-    __syncthreads();
-    const ScanRows rows(a.order, told.marks, t0, wave * SCAN_ROWS);
-    edges.fetch(rows.starts, told.marks.start + wave * SCAN_ROWS, a.h0, a.d, at);
+    const ScanRows rows(a.order, (unsigned)t0, S());
+    edges.fetch(rows.starts, rows.start, a.h0, a.d, at);
     // every row as h = A h + B, the first one of a sequence with A = 0, and with it those of none
-    float A[SCAN_ROWS][V], B[SCAN_ROWS][V];
-    const bool closed = scan_gates<T, V>(fs, A) || rows.none;
+    float A[ROWS][V], B[ROWS][V];
+    const bool closed = scan_gates<T, S>(fs, A), special = closed || (rows.starts | rows.none);
 #pragma unroll
-    for (int r = 0; r < SCAN_ROWS; ++r) {
+    for (int r = 0; r < ROWS; ++r) {
         float u[V];
-        a.u.values(us, r, u);
+        a.u.template values<S>(us, r, u);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const GateShares g = gate_shares(A[r][v]);
             A[r][v] = g.a;
             B[r][v] = share_of<true>(g.c, u[v]);
         }
-        if (rows.starts >> r & 1) {
-            float h[V];
-            edges.get(r, h);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                B[r][v] = gate_step<true>(A[r][v], h[v], B[r][v]);
-                A[r][v] = 0.f;
-            }
-        }
     }
-    if (rows.none)
+    if (rows.starts | rows.none)
 #pragma unroll
-        for (int r = 0; r < SCAN_ROWS; ++r)
+        for (int r = 0; r < ROWS; ++r) {
+            if (rows.starts >> r & 1) {
+                float h[V];
+                edges.get(r, h);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    B[r][v] = gate_step<true>(A[r][v], h[v], B[r][v]);
+                    A[r][v] = 0.f;
+                }
+            }
             if (rows.none >> r & 1)
 #pragma unroll
                 for (int v = 0; v < V; ++v) A[r][v] = B[r][v] = 0.f;
+        }
     ScanProduct p[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = {1.f, 0.f};
-    scan_rows(closed, [&](auto special) {
+    scan_rows(special, [&](auto is_special) {
+        constexpr bool SPECIAL = decltype(is_special)::value;
 #pragma unroll
-        for (int r = 0; r < SCAN_ROWS; ++r) {
-            if (rows.starts >> r & 1)
+        for (int r = 0; r < ROWS; ++r) {
+            if (SPECIAL && (rows.starts >> r & 1))
 #pragma unroll
                 for (int v = 0; v < V; ++v) p[v] = {0.f, 0.f};
 #pragma unroll
-            for (int v = 0; v < V; ++v) p[v] = {p[v].a * A[r][v], gate_step<decltype(special)::value>(A[r][v], p[v].b, B[r][v])};
+            for (int v = 0; v < V; ++v) p[v] = {p[v].a * A[r][v], gate_step<SPECIAL>(A[r][v], p[v].b, B[r][v])};
         }
     });
-#pragma unroll
-    for (int v = 0; v < V; ++v) told.products[wave][v][lane] = p[v];
-    __syncthreads();
-    if (wave == 0) {
-        float x[V] = {};
-        if (a.tickets) {
-            ScanProduct own[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                own[v] = p[v];
-#pragma unroll
-                for (int w = 1; w < SCAN_WAVES; ++w) own[v] = told.products[w][v][lane].after(own[v]);
-            }
-            scan_hand<T, PACKED, V>(a, q, block, told.marks.from, own, x);
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) told.into[v][lane] = x[v];
-    }
-    __syncthreads();
-    if (many == 0) return;
     float h[V];
+    told.template join<false>(a, q, block, rows.before / S::TILE, wave, p, h);
+    if (many > 0) {
+        if (a.states && t0 % SCAN_KEPT == 0) {
+            float enters[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = told.into[v][lane];
-    for (int w = 0; w < wave; ++w)
+            for (int v = 0; v < V; ++v) enters[v] = rows.none & 1 ? 0.f : h[v];
+            if (rows.starts & 1) edges.get(0, enters);
+            at.store_floats(a.states, t0 / SCAN_KEPT, a.d, enters);
+        }
+        const unsigned ends = a.last ? rows.ends : 0;
+        T *y = a.y + t0 * a.ldy + at.first;
+        if (at.here())
+            scan_rows(special || ends || many < ROWS || at.odd(), [&](auto is_special) {
+                constexpr bool SPECIAL = decltype(is_special)::value;
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = told.products[w][v][lane].of(h[v]);
-    if (a.states) {
-        float enters[V];
+                for (int r = 0; r < ROWS; ++r) {
+                    if (SPECIAL && r >= many) break;
+                    if (SPECIAL && (rows.starts >> r & 1))
 #pragma unroll
-        for (int v = 0; v < V; ++v) enters[v] = rows.none & 1 ? 0.f : h[v];
-        if (rows.starts & 1) edges.get(0, enters);
-        at.store_floats(a.states, t0 / SCAN_KEPT, a.d, enters);
+                        for (int v = 0; v < V; ++v) h[v] = 0.f;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) h[v] = gate_step<SPECIAL>(A[r][v], h[v], B[r][v]);
+                    at.template store<SPECIAL>(y, h);
+                    y += a.ldy;
+                    if (SPECIAL && (ends >> r & 1)) edges.put(r, h);
+                }
+            });
+        edges.store(ends, rows.end, a.last, a.d, at);
     }
-    const unsigned ends = a.last ? rows.ends : 0;
-    T *y = a.y + t0 * a.ldy + at.first;
-    if (at.here())
-        scan_rows(closed || many < SCAN_ROWS, [&](auto special) {
-            constexpr bool SPECIAL = decltype(special)::value;
-#pragma unroll
-            for (int r = 0; r < SCAN_ROWS; ++r) {
-                if (SPECIAL && r >= many) break;
-                if (rows.starts >> r & 1)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) h[v] = 0.f;
-#pragma unroll
-                for (int v = 0; v < V; ++v) h[v] = gate_step<SPECIAL>(A[r][v], h[v], B[r][v]);
-                at.store(y, h);
-                y += a.ldy;
-                if (ends >> r & 1) edges.put(r, h);
-            }
-        });
-    edges.store(ends, told.marks.end + wave * SCAN_ROWS, a.last, a.d, at);
+    scan_empty<S>(a.order, q, a.tiles, block == 0, a.flags, [&](int64_t j) {
+        float h[V];
+        if (!a.last) return;
+        at.load_floats(a.h0, j, a.d, h);
+        at.store_floats(a.last, j, a.d, h);
+    });
 }
 
 template <typename T, bool PACKED>
-__global__ __launch_bounds__(SCAN_THREADS, SCAN_BACKWARD_HELD) void scan_backward(const Scan<T, PACKED> a)
+__global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>::HELD)) void scan_backward(const Scan<T, PACKED> a)
 {
-    constexpr int V = SCAN_V<T, true>;
-    __shared__ ScanShared<V> told;
-    __shared__ ScanEdges<V> all_edges[SCAN_WAVES];
+    typedef ScanShape<T, true> S;
+    constexpr int V = S::V, ROWS = S::ROWS;
+    __shared__ ScanShared<S> told;
+    __shared__ ScanEdges<S> all_edges[S::WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    ScanEdges<V> &edges = all_edges[wave];
+    ScanEdges<S> &edges = all_edges[wave];
     const unsigned block = blockIdx.x % a.blocks, q = scan_tile(a, block), tile = a.tiles - 1 - q;
-    const ScanLane<T, V> at(block, a.d);
-    const int64_t n = a.order.n, t0 = (int64_t)tile * SCAN_TILE + wave * SCAN_ROWS;
-    const int many = (int)(n - t0 < SCAN_ROWS ? n - t0 < 0 ? 0 : n - t0 : SCAN_ROWS);
+    const ScanLane<T, S> at(block, a.d);
+    const int64_t n = a.order.n, t0 = (int64_t)tile * S::TILE + wave * ROWS;
+    const int many = (int)(n - t0 < ROWS ? n - t0 < 0 ? 0 : n - t0 : ROWS);
     const int64_t from = many > 0 ? t0 : n - 1;
-    unsigned fs[SCAN_ROWS], dys[SCAN_ROWS];
-    typename ScanInput<T, PACKED>::Raw us;
+    unsigned fs[ROWS], dys[ROWS];
+    typename ScanInput<T, PACKED>::template Raw<S> us;
     float h[V];
     at.load(a.f + from * a.ldf, a.ldf, many, fs);
     a.u.load(from, a.d, many, at, us);
     at.load_floats(a.states, from / SCAN_KEPT, a.d, h);
     at.load(a.dy + from * a.lddy, a.lddy, many, dys);
-    scan_mark(a.order, told.marks, tile, a.tiles, block, a.flags, [&](int64_t j) {
-        float x[V];
-        if (!a.dh0) return;
-        at.load_floats(a.dlast, j, a.d, x);
-        at.store_floats(a.dh0, j, a.d, x);
-    });
-    __syncthreads();
-    const ScanRows rows(a.order, told.marks, t0, wave * SCAN_ROWS);
-    edges.fetch(rows.starts, told.marks.start + wave * SCAN_ROWS, a.h0, a.d, at);
-    float g[SCAN_ROWS][V], wide[SCAN_ROWS][V];       // gates, and h_{t-1} - u_t
-    const bool closed = scan_gates<T, V>(fs, g) || rows.none;
+    const ScanRows rows(a.order, (unsigned)t0, S());
+    edges.fetch(rows.starts, rows.start, a.h0, a.d, at);
+    float g[ROWS][V], wide[ROWS][V];       // gates, and h_{t-1} - u_t
+    const bool closed = scan_gates<T, S>(fs, g) || rows.none;
+    // Where SCAN_KEPT rows have two wavefronts, the second one's state comes from the first.  (Each wavefront goes through one barrier, in front of its
+    // rows or behind them.)
+    const bool second = V == 2 && (wave & 1);
+    if (second) {
+        __syncthreads();
 #pragma unroll
-    for (int r = 0; r < SCAN_ROWS; ++r) {
+        for (int v = 0; v < V; ++v) h[v] = told.between[wave / 2][v][lane];
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
         float u[V];
         if (rows.starts >> r & 1) edges.get(r, h);
-        a.u.values(us, r, u);
+        a.u.template values<S>(us, r, u);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const GateShares shares = gate_shares(g[r][v]);
@@ -640,9 +695,14 @@ __global__ __launch_bounds__(SCAN_THREADS, SCAN_BACKWARD_HELD) void scan_backwar
             h[v] = gate_step<true>(shares.a, h[v], share_of<true>(shares.c, u[v]));
         }
     }
-    edges.fetch(rows.ends, told.marks.end + wave * SCAN_ROWS, a.dlast, a.d, at);
+    if (V == 2 && !second) {
 #pragma unroll
-    for (int r = 0; r < SCAN_ROWS; ++r)
+        for (int v = 0; v < V; ++v) told.between[wave / 2][v][lane] = h[v];
+        __syncthreads();
+    }
+    edges.fetch(rows.ends, rows.end, a.dlast, a.d, at);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v) scan_anew(g[r][v]);
     // x: what goes from a row to the one before, a G
@@ -652,7 +712,7 @@ __global__ __launch_bounds__(SCAN_THREADS, SCAN_BACKWARD_HELD) void scan_backwar
     scan_rows(closed, [&](auto special) {
         constexpr bool SPECIAL = decltype(special)::value;
 #pragma unroll
-        for (int r = SCAN_ROWS - 1; r >= 0; --r) {
+        for (int r = ROWS - 1; r >= 0; --r) {
             float dy[V];
             if (rows.ends >> r & 1) {
                 float x[V];
@@ -669,66 +729,50 @@ __global__ __launch_bounds__(SCAN_THREADS, SCAN_BACKWARD_HELD) void scan_backwar
             }
         }
     });
-#pragma unroll
-    for (int v = 0; v < V; ++v) told.products[wave][v][lane] = p[v];
-    __syncthreads();
-    if (wave == SCAN_WAVES - 1) {
-        float x[V] = {};
-        if (a.tickets) {
-            ScanProduct own[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                own[v] = p[v];
-#pragma unroll
-                for (int w = SCAN_WAVES - 2; w >= 0; --w) own[v] = told.products[w][v][lane].after(own[v]);
-            }
-            scan_hand<T, PACKED, V>(a, q, block, a.tiles - 1 - told.marks.to, own, x);
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) told.into[v][lane] = x[v];
-    }
-    __syncthreads();
-    if (many == 0) return;
-#pragma unroll
-    for (int r = 0; r < SCAN_ROWS; ++r) {            // (not kept from the pass above)
-        scan_anew(dys[r]);
-#pragma unroll
-        for (int v = 0; v < V; ++v) scan_anew(g[r][v]);
-    }
     float x[V];
+    told.template join<true>(a, q, block, rows.behind == ~0u ? q : a.tiles - 1 - (rows.behind - 1) / S::TILE, wave, p, x);
+    if (many > 0) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) x[v] = told.into[v][lane];
-    for (int w = SCAN_WAVES - 1; w > wave; --w)
+        for (int r = 0; r < ROWS; ++r) {                 // (not kept from the pass above)
+            scan_anew(dys[r]);
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = told.products[w][v][lane].of(x[v]);
-    const unsigned starts = a.dh0 ? rows.starts : 0;
-    T *df_row = a.df + (t0 + many - 1) * a.lddf + at.first, *du_row = a.du + (t0 + many - 1) * a.lddu + at.first;
-    if (at.here())
-        scan_rows(closed || many < SCAN_ROWS, [&](auto special) {
-            constexpr bool SPECIAL = decltype(special)::value;
+            for (int v = 0; v < V; ++v) scan_anew(g[r][v]);
+        }
+        const unsigned starts = a.dh0 ? rows.starts : 0;
+        T *df_row = a.df + (t0 + many - 1) * a.lddf + at.first, *du_row = a.du + (t0 + many - 1) * a.lddu + at.first;
+        if (at.here())
+            scan_rows(closed || many < ROWS || at.odd(), [&](auto special) {
+                constexpr bool SPECIAL = decltype(special)::value;
 #pragma unroll
-            for (int r = SCAN_ROWS - 1; r >= 0; --r) {
-                if (SPECIAL && r >= many) continue;
-                if (rows.ends >> r & 1) edges.get(r, x);
-                float dy[V], df[V], du[V];
-                at.values(dys[r], dy);
+                for (int r = ROWS - 1; r >= 0; --r) {
+                    if (SPECIAL && r >= many) continue;
+                    if (rows.ends >> r & 1) edges.get(r, x);
+                    float dy[V], df[V], du[V];
+                    at.values(dys[r], dy);
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float G = x[v] + dy[v];
-                    const GateShares shares = gate_shares(g[r][v]);
-                    df[v] = share_of<SPECIAL>(shares.a * shares.c, G * wide[r][v]);
-                    du[v] = share_of<SPECIAL>(shares.c, G);
-                    x[v] = share_of<SPECIAL>(shares.a, G);
-                    if (SPECIAL && (rows.none >> r & 1)) df[v] = du[v] = x[v] = 0.f;
+                    for (int v = 0; v < V; ++v) {
+                        const float G = x[v] + dy[v];
+                        const GateShares shares = gate_shares(g[r][v]);
+                        df[v] = share_of<SPECIAL>(shares.a * shares.c, G * wide[r][v]);
+                        du[v] = share_of<SPECIAL>(shares.c, G);
+                        x[v] = share_of<SPECIAL>(shares.a, G);
+                        if (SPECIAL && (rows.none >> r & 1)) df[v] = du[v] = x[v] = 0.f;
+                    }
+                    at.template store<SPECIAL>(df_row, df);
+                    at.template store<SPECIAL>(du_row, du);
+                    df_row -= a.lddf;
+                    du_row -= a.lddu;
+                    if (starts >> r & 1) edges.put(r, x);
                 }
-                at.store(df_row, df);
-                at.store(du_row, du);
-                df_row -= a.lddf;
-                du_row -= a.lddu;
-                if (starts >> r & 1) edges.put(r, x);
-            }
-        });
-    edges.store(starts, told.marks.start + wave * SCAN_ROWS, a.dh0, a.d, at);
+            });
+        edges.store(starts, rows.start, a.dh0, a.d, at);
+    }
+    scan_empty<S>(a.order, q, a.tiles, block == 0, a.flags, [&](int64_t j) {
+        float x[V];
+        if (!a.dh0) return;
+        at.load_floats(a.dlast, j, a.d, x);
+        at.store_floats(a.dh0, j, a.d, x);
+    });
 }
 
 // state = a state + (1 - a) u, y = state, one row of every sequence.  A thread has one vector of a row.

@@ -97,11 +97,12 @@ struct ScanPlan {
     size_t bytes;
 };
 
-ScanPlan scan_plan(int64_t n, int64_t d, int32_t type, bool backward, void *workspace)
+template <typename S>
+ScanPlan scan_plan(int64_t n, int64_t d, void *workspace)
 {
     ScanPlan p = {};
-    const int64_t columns = 64 * (type == CHICLE_F32 ? 1 : backward ? SCAN_V<bf16, true> : SCAN_V<bf16, false>);
-    p.tiles = n > 0 ? ceil_div(n, SCAN_TILE) : 1;
+    const int64_t columns = S::COLS;
+    p.tiles = n > 0 ? ceil_div(n, S::TILE) : 1;
     p.blocks = ceil_div(d, columns);
     Carver c(workspace);
     if (p.tiles > 1) {
@@ -116,17 +117,24 @@ ScanPlan scan_plan(int64_t n, int64_t d, int32_t type, bool backward, void *work
     return p;
 }
 
-// Clears what is handed on, and launches the kernel.
-template <typename T, bool PACKED>
-int run_scan(Scan<T, PACKED> a, int32_t type, bool backward, void *workspace, hipStream_t stream)
+ScanPlan scan_plan(int64_t n, int64_t d, int32_t type, bool backward)
 {
+    if (type == CHICLE_F32) return backward ? scan_plan<ScanShape<float, true>>(n, d, nullptr) : scan_plan<ScanShape<float, false>>(n, d, nullptr);
+    return backward ? scan_plan<ScanShape<bf16, true>>(n, d, nullptr) : scan_plan<ScanShape<bf16, false>>(n, d, nullptr);
+}
+
+// Clears what is handed on, and launches the kernel.
+template <bool BACKWARD, typename T, bool PACKED>
+int run_scan(Scan<T, PACKED> a, void *workspace, hipStream_t stream)
+{
+    typedef ScanShape<T, BACKWARD> S;
     if (a.order.n == 0) {
         if (a.order.count == 0) return CHICLE_OK;
-        scan_nothing<<<(unsigned)std::min<int64_t>(ceil_div(a.order.count * a.d, 256), 16384), 256, 0, stream>>>(a.order, backward ? a.dlast : a.h0,
-                                                                                                               backward ? a.dh0 : a.last, a.d, a.flags);
+        scan_nothing<<<(unsigned)std::min<int64_t>(ceil_div(a.order.count * a.d, 256), 16384), 256, 0, stream>>>(a.order, BACKWARD ? a.dlast : a.h0,
+                                                                                                               BACKWARD ? a.dh0 : a.last, a.d, a.flags);
         return launched("scan_nothing");
     }
-    const ScanPlan p = scan_plan(a.order.n, a.d, type, backward, workspace);
+    const ScanPlan p = scan_plan<S>(a.order.n, a.d, workspace);
     a.tiles = (unsigned)p.tiles;
     a.blocks = (unsigned)p.blocks;
     if (p.tiles > 1) {
@@ -138,9 +146,9 @@ int run_scan(Scan<T, PACKED> a, int32_t type, bool backward, void *workspace, hi
         TRY(launched("scan_begin"));
     }
     const unsigned grid = (unsigned)(p.tiles * p.blocks);
-    if (backward) scan_backward<T, PACKED><<<grid, SCAN_THREADS, 0, stream>>>(a);
-    else scan_forward<T, PACKED><<<grid, SCAN_THREADS, 0, stream>>>(a);
-    return launched(backward ? "scan_backward" : "scan_forward");
+    if constexpr (BACKWARD) scan_backward<T, PACKED><<<grid, S::THREADS, 0, stream>>>(a);
+    else scan_forward<T, PACKED><<<grid, S::THREADS, 0, stream>>>(a);
+    return launched(BACKWARD ? "scan_backward" : "scan_forward");
 }
 
 int scan_check(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,
@@ -149,8 +157,9 @@ int scan_check(const void *f, int64_t ldf, const void *u, int64_t ldu, const voi
     if (!type_ok(type)) return fail(CHICLE_EINVAL, "unknown type %d", type);
     if (!sizes_ok(n, d) || ldf < d || ldu < d || sequences < 0 || sequences > INT32_MAX || (!offsets && sequences != 1))
         return fail(CHICLE_EINVAL, "sizes n %lld, d %lld, sequences %lld, or a row distance", (long long)n, (long long)d, (long long)sequences);
-    const ScanPlan p = scan_plan(n, d, type, true, nullptr);
-    if (p.tiles * p.blocks >= (int64_t)1 << 24) return fail(CHICLE_EINVAL, "too many values");              // (a launch has fewer than 2^32 threads)
+    // (a launch has fewer than 2^32 threads)
+    const ScanPlan p = scan_plan(n, d, type, false), q = scan_plan(n, d, type, true);
+    if (p.tiles * p.blocks >= (int64_t)1 << 23 || q.tiles * q.blocks >= (int64_t)1 << 23) return fail(CHICLE_EINVAL, "too many values");
     const int s = size_of(type);
     if ((offsets && !placed(offsets, wide ? 8 : 4)) || (h0 && !placed(h0, 4)) || (states && !placed(states, 4)))
         return fail(CHICLE_EINVAL, "a null or misplaced pointer");
@@ -285,7 +294,7 @@ int chicle_rms_norm_grad(const void *dy, int64_t lddy, const void *sum, int64_t 
 size_t chicle_gated_scan_bytes(int64_t n, int64_t d, int32_t type)
 {
     if (!type_ok(type) || !sizes_ok(n, d)) return 0;
-    return std::max(scan_plan(n, d, type, false, nullptr).bytes, scan_plan(n, d, type, true, nullptr).bytes);
+    return std::max(scan_plan(n, d, type, false).bytes, scan_plan(n, d, type, true).bytes);
 }
 
 int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,
@@ -306,7 +315,7 @@ int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, co
             a.f = (const T *)f; a.h0 = h0; a.states = states; a.last = last; a.y = (T *)y;
             a.ldf = ldf; a.ldy = ldy; a.d = d;
             a.flags = flags;
-            return run_scan(a, type, false, workspace, (hipStream_t)hip_stream);
+            return run_scan<false>(a, workspace, (hipStream_t)hip_stream);
         });
     });
 }
@@ -333,7 +342,7 @@ int chicle_gated_scan_grad(const void *f, int64_t ldf, const void *u, int64_t ld
             a.df = (T *)df; a.du = (T *)du;
             a.ldf = ldf; a.lddy = lddy; a.lddf = lddf; a.lddu = lddu; a.d = d;
             a.flags = flags;
-            return run_scan(a, type, true, workspace, (hipStream_t)hip_stream);
+            return run_scan<true>(a, workspace, (hipStream_t)hip_stream);
         });
     });
 }
