@@ -44,6 +44,7 @@ template <typename T, bool BACKWARD> struct ScanShape {
     static constexpr int V = BACKWARD ? 1 : 4 / (int)sizeof(T), COLS = 64 * V, ROWS = SCAN_KEPT / V;
     static constexpr int WAVES = 4 * V, THREADS = 64 * WAVES, TILE = ROWS * WAVES;
     static constexpr int HELD = V == 1 ? 3 : 4;          // wavefronts of a SIMD, as registers allow
+    static constexpr bool LINES = !BACKWARD || sizeof(T) == 4;             // there are registers for both kinds of loads
 };
 constexpr int SCAN_GROUP = 8, SCAN_RUN = 64;             // tiles whose products are joined, and tiles from one state that is handed on to the next
 constexpr int SCAN_TICKET = 32;                          // places from one column block's ticket to the next: lines of their own
@@ -71,33 +72,35 @@ template <typename T, typename S> struct ScanLane {
             load(r, r + 1 < many);
         }
     }
-    __device__ __forceinline__ void load(const T *row, int64_t ld, int many, unsigned (&out)[ROWS]) const
+    // `lines`: rows are whole lines of the cache, which no other column block reads, and are not kept there.
+    __device__ __forceinline__ void load(const T *row, int64_t ld, int many, bool lines, unsigned (&out)[ROWS]) const
     {
         const T *p = row + first;
-        if constexpr (V == 1) {
-            typedef typename std::conditional<sizeof(T) == 4, unsigned, uint16_t>::type word;
-            const unsigned off = e < left ? e : left - 1;
-            each_row(many, [&](int r, bool further) {
-                out[r] = __builtin_nontemporal_load((const word *)p + off);
-                p += further ? ld : 0;
-            });
-        } else if (left > 1) {
-            // (a column that has no neighbour comes with the one before it)
-            const unsigned off = e + 1 < left ? e : left - 2;
-            each_row(many, [&](int r, bool further) {
-                out[r] = __builtin_nontemporal_load((const u32_at_2 *)(p + off));
-                p += further ? ld : 0;
-            });
-            if (odd()) {
-                const int bits = e + 1 == left ? 16 : 0;
-#pragma unroll
-                for (int r = 0; r < ROWS; ++r) out[r] >>= bits;
-            }
-        } else
+        if (V == 2 && left == 1) {
             each_row(many, [&](int r, bool further) {
                 out[r] = *(const uint16_t *)p;
                 p += further ? ld : 0;
             });
+            return;
+        }
+        typedef typename std::conditional<V * sizeof(T) == 4, u32_at_2, uint16_t>::type word;
+        // (a column that has no neighbour comes with the one before it)
+        const unsigned off = e + V <= left ? e : left - V;
+        if (S::LINES && lines)
+            each_row(many, [&](int r, bool further) {
+                out[r] = __builtin_nontemporal_load((const word *)(p + off));
+                p += further ? ld : 0;
+            });
+        else
+            each_row(many, [&](int r, bool further) {
+                out[r] = *(const word *)(p + off);
+                p += further ? ld : 0;
+            });
+        if (odd()) {
+            const int bits = e + 1 == left ? 16 : 0;
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) out[r] >>= bits;
+        }
     }
     static __device__ __forceinline__ void values(unsigned x, float (&out)[V])
     {
@@ -146,9 +149,9 @@ template <typename T> struct ScanInput<T, false> {
     template <typename S> struct Raw { unsigned x[S::ROWS]; };
     const T *p;
     int64_t ld;
-    template <typename S> __device__ __forceinline__ void load(int64_t row, int64_t, int many, const ScanLane<T, S> &at, Raw<S> &out) const
+    template <typename S> __device__ __forceinline__ void load(int64_t row, int64_t, int many, bool lines, const ScanLane<T, S> &at, Raw<S> &out) const
     {
-        at.load(p + row * ld, ld, many, out.x);
+        at.load(p + row * ld, ld, many, lines, out.x);
     }
     template <typename S> static __device__ __forceinline__ void values(const Raw<S> &raw, int r, float (&out)[S::V]) { ScanLane<T, S>::values(raw.x[r], out); }
 };
@@ -158,7 +161,7 @@ template <typename T> struct ScanInput<T, true> {
     const int8_t *q;
     const uint8_t *scales;
     int64_t ld;
-    template <typename S> __device__ __forceinline__ void load(int64_t row, int64_t d, int many, const ScanLane<T, S> &at, Raw<S> &out) const
+    template <typename S> __device__ __forceinline__ void load(int64_t row, int64_t d, int many, bool, const ScanLane<T, S> &at, Raw<S> &out) const
     {
         constexpr int V = S::V, GROUPS = S::COLS / PACK_GROUP;
         static_assert(GROUPS * S::ROWS == 64, "a lane for every scale");
@@ -169,8 +172,8 @@ template <typename T> struct ScanInput<T, true> {
         out.step = scales[(row + which) * (ld / PACK_GROUP) + at.first / PACK_GROUP + (group * PACK_GROUP < left ? group : 0)];
         const uint8_t *p = (const uint8_t *)q + row * ld + at.first;
         at.each_row(many, [&](int i, bool further) {
-            if constexpr (V == 1) out.x[i] = __builtin_nontemporal_load(p + off);
-            else out.x[i] = __builtin_nontemporal_load((const uint16_t *)(p + off));
+            if constexpr (V == 1) out.x[i] = p[off];
+            else out.x[i] = *(const uint16_t *)(p + off);
             p += further ? ld : 0;
         });
     }
@@ -230,6 +233,7 @@ template <typename T, bool PACKED> struct Scan {
     unsigned *tickets;
     unsigned long long *products, *groups, *handed;
     unsigned tiles, blocks;                  // tiles of a column block, column blocks
+    bool lines;                              // rows of T that are read are whole lines of the cache
 };
 
 constexpr unsigned long long SCAN_NOTHING = ~0ull;       // what no product is: its lower half is no NaN of these bits
@@ -389,14 +393,27 @@ __device__ __forceinline__ void scan_handed(const Scan<T, PACKED> &a, unsigned q
     for (int v = 0; v < V; ++v) x[v] = __uint_as_float((unsigned)scan_wait(p + v * 64, scan_look(p + v * 64)));
 }
 
-// What the workgroup's tile is: tickets, those of each column block for themselves, give tiles in the order in which workgroups begin.
-template <typename S> __device__ __forceinline__ unsigned scan_tile(const S &a, unsigned block)
+// The workgroup's column block and tile.  Tickets, those of each column block for themselves, give tiles in the order in which workgroups begin.
+// Workgroups go to the chip's eight L2 partitions in turn: those of one take neighbouring column blocks first, whose rows meet in lines of the cache, and
+// then whatever is left (there are as many workgroups as tiles, so that each finds one).
+template <typename S> __device__ __forceinline__ void scan_unit(const S &a, unsigned &block, unsigned &q)
 {
-    __shared__ unsigned tile;
-    if (!a.tickets) return 0;
-    if (threadIdx.x == 0) tile = atomicAdd(a.tickets + block * SCAN_TICKET, 1u);
+    __shared__ unsigned found[2];
+    if (!a.tickets) {
+        block = blockIdx.x;
+        q = 0;
+        return;
+    }
+    if (threadIdx.x == 0) {
+        const unsigned part = blockIdx.x & 7, begin = a.blocks * (uint64_t)part / 8, many = max(a.blocks * (uint64_t)(part + 1) / 8 - begin, (uint64_t)1);
+        unsigned b = begin + (blockIdx.x >> 3) % many, tile;
+        for (unsigned tried = 0; (tile = atomicAdd(a.tickets + b * SCAN_TICKET, 1u)) >= a.tiles && tried < a.blocks; ++tried) b = b + 1 < a.blocks ? b + 1 : 0;
+        found[0] = b;
+        found[1] = tile;
+    }
     __syncthreads();
-    return __builtin_amdgcn_readfirstlane(tile);
+    block = __builtin_amdgcn_readfirstlane(found[0]);
+    q = __builtin_amdgcn_readfirstlane(found[1]);
 }
 
 // What the wavefronts of a workgroup tell one another.
@@ -556,7 +573,8 @@ __global__ __launch_bounds__((ScanShape<T, false>::THREADS), (ScanShape<T, false
     __shared__ ScanEdges<S> all_edges[S::WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     ScanEdges<S> &edges = all_edges[wave];
-    const unsigned block = blockIdx.x % a.blocks, q = scan_tile(a, block);
+    unsigned block, q;
+    scan_unit(a, block, q);
     const ScanLane<T, S> at(block, a.d);
     const int64_t n = a.order.n, t0 = (int64_t)q * S::TILE + wave * ROWS;
     // (wavefronts behind the last row have that one, as rows of no sequence, and store nothing)
@@ -564,8 +582,8 @@ __global__ __launch_bounds__((ScanShape<T, false>::THREADS), (ScanShape<T, false
     const int64_t from = many > 0 ? t0 : n - 1;
     unsigned fs[ROWS];
     typename ScanInput<T, PACKED>::template Raw<S> us;
-    at.load(a.f + from * a.ldf, a.ldf, many, fs);
-    a.u.load(from, a.d, many, at, us);
+    at.load(a.f + from * a.ldf, a.ldf, many, a.lines, fs);
+    a.u.load(from, a.d, many, a.lines, at, us);
     const ScanRows rows(a.order, (unsigned)t0, S());
     edges.fetch(rows.starts, rows.start, a.h0, a.d, at);
     // every row as h = A h + B, the first one of a sequence with A = 0, and with it those of none
@@ -659,7 +677,9 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
     __shared__ ScanEdges<S> all_edges[S::WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     ScanEdges<S> &edges = all_edges[wave];
-    const unsigned block = blockIdx.x % a.blocks, q = scan_tile(a, block), tile = a.tiles - 1 - q;
+    unsigned block, q;
+    scan_unit(a, block, q);
+    const unsigned tile = a.tiles - 1 - q;
     const ScanLane<T, S> at(block, a.d);
     const int64_t n = a.order.n, t0 = (int64_t)tile * S::TILE + wave * ROWS;
     const int many = (int)(n - t0 < ROWS ? n - t0 < 0 ? 0 : n - t0 : ROWS);
@@ -667,10 +687,10 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
     unsigned fs[ROWS], dys[ROWS];
     typename ScanInput<T, PACKED>::template Raw<S> us;
     float h[V];
-    at.load(a.f + from * a.ldf, a.ldf, many, fs);
-    a.u.load(from, a.d, many, at, us);
+    at.load(a.f + from * a.ldf, a.ldf, many, a.lines, fs);
+    a.u.load(from, a.d, many, a.lines, at, us);
     at.load_floats(a.states, from / SCAN_KEPT, a.d, h);
-    at.load(a.dy + from * a.lddy, a.lddy, many, dys);
+    at.load(a.dy + from * a.lddy, a.lddy, many, a.lines, dys);
     const ScanRows rows(a.order, (unsigned)t0, S());
     edges.fetch(rows.starts, rows.start, a.h0, a.d, at);
     float g[ROWS][V], wide[ROWS][V];       // gates, and h_{t-1} - u_t
