@@ -91,13 +91,6 @@ int with_config(int c, F f)
     return c == MIDDLE ? f(MmMiddle()) : f(MmThin());
 }
 
-template <typename K>
-int allow_lds(K kernel, int bytes)
-{
-    const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    return e == hipSuccess ? CHICLE_OK : fail(CHICLE_EDEVICE, "shared memory: %s", hipGetErrorString(e));
-}
-
 // ---- softmax loss: where everything lies ------------------------------------------------------------------------------
 
 struct LossPlan {

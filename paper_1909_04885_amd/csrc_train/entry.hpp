@@ -123,4 +123,11 @@ inline int with_vectors(int vectors, F f)
     }
 }
 
+template <typename K>
+inline int allow_lds(K kernel, int bytes)
+{
+    const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e == hipSuccess ? CHICLE_OK : fail(CHICLE_EDEVICE, "shared memory: %s", hipGetErrorString(e));
+}
+
 }  // namespace chicle_train

@@ -70,20 +70,15 @@ __global__ __launch_bounds__(THREADS) void rms_norm_rows(const RmsRows<T> a)
         for (int i = 0; i < V; ++i) s += u[i] * u[i];
     };
     if constexpr (NV > 0) {
-        constexpr int RAW = NV * V <= 16 || THREADS <= 256 ? NV : 1;       // vectors that are asked for together, as registers allow
-        u32x4 xs[RAW], rs[RAW] = {};
+        u32x4 xs[NV], rs[NV] = {};
 #pragma unroll
-        for (int k = 0; k < RAW; ++k) {
+        for (int k = 0; k < NV; ++k) {
             xs[k] = ask_raw<T, true>(xr, first + k * step, d);
             if (resr) rs[k] = ask_raw<T, true>(resr, first + k * step, d);
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            if (RAW == 1 && k > 0) {
-                xs[0] = ask_raw<T, true>(xr, first + k * step, d);
-                if (resr) rs[0] = ask_raw<T, true>(resr, first + k * step, d);
-            }
-            add(xs[RAW == 1 ? 0 : k], rs[RAW == 1 ? 0 : k], first + k * step, v[k]);
+            add(xs[k], rs[k], first + k * step, v[k]);
             square(v[k]);
         }
     } else {
@@ -160,26 +155,30 @@ __global__ __launch_bounds__(THREADS) void rms_norm_grad_rows(const RmsGrad<T, P
     extern __shared__ __align__(16) float group_sums[];
     const int64_t d = a.d;
     const int lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = blockDim.x / a.lanes;
-    int64_t first = (int64_t)lane * V;
-    const int64_t step = (int64_t)a.lanes * V;
+    const int64_t first = (int64_t)lane * V, step = (int64_t)a.lanes * V;
     float *mine = a.part + (int64_t)blockIdx.x * d;
-    constexpr bool HELD = NV == 1 || (NV > 1 && THREADS <= 256);           // gamma, and the next row, in registers, where there are enough
+    // gamma, and the next row, in registers, where there are enough; else a thread's vectors of gamma lie in LDS, where they do not wait behind the next
+    // row (read from memory twice a row: 10,143 x 10,061 in bfloat16 280 us instead of 245)
+    constexpr bool HELD = NV > 0 && (NV * V <= 8 || THREADS <= 256), AHEAD = HELD || (NV > 0 && sizeof(T) == 2);
     float sg[N][V] = {}, ga[HELD ? N : 1][V];
+    u32x4 *own_gamma = (u32x4 *)group_sums + threadIdx.x;
     if constexpr (NV > 0) {
-        if constexpr (HELD)
 #pragma unroll
-            for (int k = 0; k < NV; ++k) load_vec(a.gamma, first + k * step, d, ga[k]);
+        for (int k = 0; k < NV; ++k) {
+            if constexpr (HELD) load_vec(a.gamma, first + k * step, d, ga[k]);
+            else own_gamma[k * blockDim.x] = load_raw(a.gamma, first + k * step, d);
+        }
     } else {
         for (int64_t c = first; c < d; c += step)
             for (int i = 0; i < V && c + i < d; ++i) mine[c + i] = 0.f;
     }
-    typename Kept::raw next_r[HELD ? N : 1];
-    u32x4 next_dy[HELD ? N : 1];
+    typename Kept::raw next_r[AHEAD ? N : 1];
+    u32x4 next_dy[AHEAD ? N : 1];
     float next_rstd;
     auto ask = [&](int64_t row) {
         row = min(row, a.n - 1);
         next_rstd = a.rstd[row];
-        if constexpr (HELD)
+        if constexpr (AHEAD)
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 next_r[k] = a.r.ask(row, first + k * step, d);
@@ -196,7 +195,7 @@ __global__ __launch_bounds__(THREADS) void rms_norm_grad_rows(const RmsGrad<T, P
         float h[N][V], g[N][V];                          // h and dy
         u32x4 drs[N] = {};
         float s = 0.f;
-        if constexpr (HELD) {
+        if constexpr (AHEAD) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 Kept::values(next_r[k], first + k * step, d, h[k]);
@@ -205,10 +204,9 @@ __global__ __launch_bounds__(THREADS) void rms_norm_grad_rows(const RmsGrad<T, P
             }
         }
         ask(row + (int64_t)gridDim.x * groups);
-        if constexpr (NV > 1 && !HELD) asm volatile("" : "+v"(first));     // (nor addresses from the row before: the registers are full)
         // Past the end of the row dy is zero, so what h has there counts nowhere.
         auto take = [&](int64_t c, float *hk, float *gk, const float *gak) {
-            if constexpr (!HELD) {
+            if constexpr (!AHEAD) {
                 Kept::values(a.r.ask(at, c, d), c, d, hk);
                 load_vec(dyr, c, d, gk);
             }
@@ -221,7 +219,7 @@ __global__ __launch_bounds__(THREADS) void rms_norm_grad_rows(const RmsGrad<T, P
         if constexpr (NV > 0) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                if constexpr (!HELD) load_vec(fresh(a.gamma), first + k * step, d, ga[0]);
+                if constexpr (!HELD) unpack<T>(own_gamma[k * blockDim.x], ga[0]);
                 take(first + k * step, h[k], g[k], ga[HELD ? k : 0]);
             }
         } else {
@@ -241,10 +239,9 @@ __global__ __launch_bounds__(THREADS) void rms_norm_grad_rows(const RmsGrad<T, P
             for (int k = 0; k < NV; ++k) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) sg[k][i] += g[k][i] * h[k][i];
-                if constexpr (!HELD) {
-                    load_vec(fresh(a.gamma), first + k * step, d, ga[0]);
+                if constexpr (!HELD) unpack<T>(own_gamma[k * blockDim.x], ga[0]);
+                if constexpr (!AHEAD)
                     if (drr) drs[k] = ask_raw<T, true>(drr, first + k * step, d);
-                }
                 give(first + k * step, h[k], g[k], ga[HELD ? k : 0], drs[k]);
             }
         } else {
@@ -259,6 +256,7 @@ __global__ __launch_bounds__(THREADS) void rms_norm_grad_rows(const RmsGrad<T, P
     }
     if constexpr (NV > 0) {
         // the groups of a workgroup by halves
+#pragma unroll
         for (int k = 0; k < NV; ++k) {
             __syncthreads();
 #pragma unroll

@@ -35,7 +35,10 @@ int with_vectors_of_rows(int64_t n, int64_t per_row, F f)
 // ---- root-mean-square norm --------------------------------------------------------------------------------------------
 
 constexpr int RMS_FORWARD_VALUES = 32, RMS_GRAD_VALUES = 16;
-constexpr int RMS_GRAD_GRID = 1024;
+// Workgroups of the gradient: whole rounds of what the compute units hold at once, up to RMS_GRAD_GRID, and with RMS_GRAD_ROWS rows each where there are more
+// than one round's, since each has a row of sums to write and to read again.  In us, 1 / 8 / 16 / 32 rows, 16 bits: 4000 x 16,000 177 / 127 / 126 / 127,
+// 1024 x 16,384 98 / 50 / 50 / 50, 10,143 x 10,061 313 / 311 / 289 / 280, 9000 x 5000 114 / 114 / 105 / 105; 32 bits: 30,000 x 4096 354 / 355 / 353 / 344.
+constexpr int RMS_GRAD_GRID = 1024, RMS_GRAD_ROWS = 32;
 
 RowShape rms_shape(int64_t d, int32_t type, int first_values, int most_values)
 {
@@ -59,11 +62,14 @@ int run_rms_norm_grad(RmsGrad<T, PACKED> a, const RowShape &r, int64_t parts, T 
             constexpr int NV = decltype(v)::value;
             if constexpr (NV * Elem<T>::VEC <= RMS_GRAD_VALUES) {
                 auto kernel = r.threads > 256 ? rms_norm_grad_rows<T, NV, LN_MOST_THREADS, PACKED> : rms_norm_grad_rows<T, NV, 256, PACKED>;
-                const size_t lds = (size_t)r.threads * Elem<T>::VEC * sizeof(float);
+                // (sums of the workgroup's groups, or gamma)
+                const size_t lds = std::max<size_t>((size_t)r.threads * Elem<T>::VEC * sizeof(float), (size_t)NV * r.threads * 16);
+                TRY(allow_lds(kernel, (int)lds));
                 int resident = 0;
                 if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, r.threads, lds) != hipSuccess || resident < 1) resident = 1;
                 const int64_t round = std::min<int64_t>((int64_t)resident * CUS, RMS_GRAD_GRID);
-                parts = std::min(parts, RMS_GRAD_GRID / round * round);
+                const int64_t most = std::min<int64_t>(RMS_GRAD_GRID, ceil_div(a.n, RMS_GRAD_ROWS * (r.threads / r.lanes)));
+                parts = std::min(parts, std::max<int64_t>(1, most / round) * round);
                 kernel<<<(unsigned)parts, r.threads, lds, stream>>>(a);
             }
             return launched("rms_norm_grad_rows");

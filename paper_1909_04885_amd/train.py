@@ -271,23 +271,24 @@ class TrainOps:
     def _packed(self, p: Packed8, name: str, n: Optional[int] = None, cols: Optional[int] = None):
         """The addresses of packed rows and their distance."""
         q, scales, d = p
-        whole = -(-d // GROUP) * GROUP
-        if (q.device != self.device or q.dtype != self._torch.int8 or tuple(q.shape) != (q.shape[0], whole) or not q.is_contiguous() or d < 1 or
-                scales.device != self.device or scales.dtype != self._torch.uint8 or tuple(scales.shape) != (q.shape[0], whole // GROUP) or
-                not scales.is_contiguous() or (n is not None and q.shape[0] != n) or (cols is not None and d != cols)):
+        rows, groups = q.shape[0] if q.dim() == 2 else -1, -(-d // GROUP)
+        if (d < 1 or q.shape != (rows, groups * GROUP) or scales.shape != (rows, groups) or q.dtype != self._torch.int8 or
+                scales.dtype != self._torch.uint8 or q.device != self.device or scales.device != self.device or not q.is_contiguous() or
+                not scales.is_contiguous() or (n is not None and rows != n) or (cols is not None and d != cols)):
             raise ChicleError(EINVAL, "%s must be contiguous packed rows on %s, of the other inputs' size" % (name, self.device))
-        return q.data_ptr(), scales.data_ptr(), whole
+        return q.data_ptr(), scales.data_ptr(), groups * GROUP
 
-    def _new_packed(self, n: int, d: int) -> Packed8:
+    def _new_packed(self, n: int, d: int):
+        """New packed rows, their addresses and distance."""
         groups = -(-d // GROUP)
-        return Packed8(self._empty((n, groups * GROUP), self._torch.int8), self._empty((n, groups), self._torch.uint8), d)
+        q, scales = self._empty((n, groups * GROUP), self._torch.int8), self._empty((n, groups), self._torch.uint8)
+        return Packed8(q, scales, d), q.data_ptr(), scales.data_ptr(), groups * GROUP
 
     def pack8(self, x) -> Packed8:
         """Rows x [n, d] in 8 bits, 32 columns to a scale that is a power of two."""
         t, ldx = self._matrix(x, "x")
         n, d = x.shape
-        out = self._new_packed(n, d)
-        qp, sp, ldq = self._packed(out, "out")
+        out, qp, sp, ldq = self._new_packed(n, d)
         self._call(self._L.chicle_pack8, x.data_ptr(), ldx, n, d, t, qp, sp, ldq)
         return out
 
@@ -318,15 +319,13 @@ class TrainOps:
             rp = r.data_ptr()
         rstd = self._empty(n, f32)
         if y8:
-            y = self._new_packed(n, d)
-            yp, ysp, ldy = self._packed(y, "y")
+            y, yp, ysp, ldy = self._new_packed(n, d)
         else:
             y = self._empty((n, d), x.dtype)
             yp, ysp, ldy = y.data_ptr(), None, d
         kept, kp, ksp, ldk = None, None, None, 0
         if keep8:
-            kept = self._new_packed(n, d)
-            kp, ksp, ldk = self._packed(kept, "kept")
+            kept, kp, ksp, ldk = self._new_packed(n, d)
         self._call(self._L.chicle_rms_norm, x.data_ptr(), ldx, resp, ldres or 0, gp, n, d, t, eps, rp, d, yp, ldy, ysp, kp, ksp, ldk, rstd.data_ptr())
         return y, r, rstd, kept
 
