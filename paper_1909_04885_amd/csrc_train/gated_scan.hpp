@@ -262,9 +262,11 @@ struct ScanProduct {
 
 __device__ __forceinline__ unsigned long long scan_look(const unsigned long long *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void scan_tell(unsigned long long *p, unsigned long long w) { __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// (Every wait ends by itself, see below.  Where a workspace is written by something else meanwhile, against its rules, this one ends too, after some
+// seconds, with what is no number.)
 __device__ __forceinline__ unsigned long long scan_wait(const unsigned long long *p, unsigned long long w)
 {
-    while (w == SCAN_NOTHING) {
+    for (int left = 1 << 22; w == SCAN_NOTHING && left > 0; --left) {
         __builtin_amdgcn_s_sleep(1);
         w = scan_look(p);
     }
@@ -395,7 +397,7 @@ __device__ __forceinline__ void scan_handed(const Scan<T, PACKED> &a, unsigned q
 
 // The workgroup's column block and tile.  Tickets, those of each column block for themselves, give tiles in the order in which workgroups begin.
 // Workgroups go to the chip's eight L2 partitions in turn: those of one take neighbouring column blocks first, whose rows meet in lines of the cache, and
-// then whatever is left (there are as many workgroups as tiles, so that each finds one).
+// then whatever is left (there are as many workgroups as tiles, so that each finds one: all blocks are used up only when every tile is taken).
 template <typename S> __device__ __forceinline__ void scan_unit(const S &a, unsigned &block, unsigned &q)
 {
     __shared__ unsigned found[2];
@@ -575,6 +577,7 @@ __global__ __launch_bounds__((ScanShape<T, false>::THREADS), (ScanShape<T, false
     ScanEdges<S> &edges = all_edges[wave];
     unsigned block, q;
     scan_unit(a, block, q);
+    if (q >= a.tiles) return;
     const ScanLane<T, S> at(block, a.d);
     const int64_t n = a.order.n, t0 = (int64_t)q * S::TILE + wave * ROWS;
     // (wavefronts behind the last row have that one, as rows of no sequence, and store nothing)
@@ -679,6 +682,7 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
     ScanEdges<S> &edges = all_edges[wave];
     unsigned block, q;
     scan_unit(a, block, q);
+    if (q >= a.tiles) return;
     const unsigned tile = a.tiles - 1 - q;
     const ScanLane<T, S> at(block, a.d);
     const int64_t n = a.order.n, t0 = (int64_t)tile * S::TILE + wave * ROWS;

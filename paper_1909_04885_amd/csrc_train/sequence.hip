@@ -64,7 +64,7 @@ int run_rms_norm_grad(RmsGrad<T, PACKED> a, const RowShape &r, int64_t parts, T 
                 auto kernel = r.threads > 256 ? rms_norm_grad_rows<T, NV, LN_MOST_THREADS, PACKED> : rms_norm_grad_rows<T, NV, 256, PACKED>;
                 // (sums of the workgroup's groups, or gamma)
                 const size_t lds = std::max<size_t>((size_t)r.threads * Elem<T>::VEC * sizeof(float), (size_t)NV * r.threads * 16);
-                TRY(allow_lds(kernel, (int)lds));
+                if (lds >= 64 * 1024 - LN_MOST_THREADS) TRY(allow_lds(kernel, (int)lds));
                 int resident = 0;
                 if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, r.threads, lds) != hipSuccess || resident < 1) resident = 1;
                 const int64_t round = std::min<int64_t>((int64_t)resident * CUS, RMS_GRAD_GRID);
