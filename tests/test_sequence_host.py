@@ -130,3 +130,39 @@ def test_reference_gradients_against_differences():
                 assert abs((moved(eps) - moved(-eps)) / (2 * eps) - float((got * what).sum())) < tol
     finally:
         del train_reference.U[f64], train_reference.TINY[f64]
+
+
+def test_no_kernel_keeps_registers_in_scratch_memory(lib):
+    """The kernels' metadata in the library that was built here, those of every source file."""
+    import struct
+
+    import msgpack
+
+    import paper_1909_04885_amd as m
+    data, at, kernels, bundles = open(m.train_library_path(), "rb").read(), -1, [], 0
+    while (at := data.find(b"__CLANG_OFFLOAD_BUNDLE__", at + 1)) >= 0:
+        count, pos = struct.unpack_from("<Q", data, at + 24)[0], at + 32
+        for _ in range(count):
+            offset, size, name = struct.unpack_from("<3Q", data, pos)
+            if b"gfx950" in data[pos + 24:pos + 24 + name]:
+                kernels += metadata(data[at + offset:at + offset + size], struct, msgpack)
+                bundles += 1
+            pos += 24 + name
+    assert bundles == 2 and len(kernels) > 100
+    assert any("scan_backward" in k[".name"] for k in kernels)
+    assert [k[".name"] for k in kernels if k[".private_segment_fixed_size"] > 0] == []
+
+
+def metadata(elf, struct, msgpack):
+    sections, entry, number = struct.unpack_from("<Q", elf, 40)[0], *struct.unpack_from("<2H", elf, 58)
+    kernels = []
+    for i in range(number):
+        kind, offset, size = struct.unpack_from("<I", elf, sections + i * entry + 4)[0], *struct.unpack_from("<2Q", elf, sections + i * entry + 24)
+        while kind == 7 and size > 0:
+            name, desc, what = struct.unpack_from("<3I", elf, offset)
+            start = offset + 12 + (name + 3) // 4 * 4
+            if what == 32 and elf[offset + 12:offset + 18] == b"AMDGPU":
+                kernels += msgpack.unpackb(elf[start:start + desc])["amdhsa.kernels"]
+            size -= start + (desc + 3) // 4 * 4 - offset
+            offset = start + (desc + 3) // 4 * 4
+    return kernels
