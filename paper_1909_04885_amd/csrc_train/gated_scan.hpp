@@ -422,7 +422,7 @@ template <typename S> __device__ __forceinline__ void scan_unit(const S &a, unsi
 template <typename S> struct ScanShared {
     static constexpr int V = S::V;
     ScanProduct products[S::WAVES][V][64], own[V][64], near[V][64], far[V][64];
-    float handed[V][64], between[S::WAVES / 2][V][64];
+    float handed[V][64];
     unsigned from;
     // What comes into the wavefront's rows.  p: its product; mine: `from` of the wavefront whose rows come first, backwards the last one's.  All
     // wavefronts together.
@@ -538,6 +538,26 @@ __device__ __forceinline__ void scan_rows(bool special, F f)
     else f(std::false_type());
 }
 
+// f(r, whether rows are special, whether there may be an edge) for all rows, BACKWARD from the last one on: eight at a time, without looks at each where
+// none of them is one of `edges`.  (Looked at one by one, gradients of 65,536 x 2048 in bfloat16 take 317 instead of 309 us; with one look for all, sequences
+// of 100 rows 345 instead of 315.)
+template <int ROWS, bool BACKWARD, typename F>
+__device__ __forceinline__ void scan_each(bool special, unsigned edges, F f)
+{
+    constexpr int EACH = 8;
+    if (special) {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) f(BACKWARD ? ROWS - 1 - k : k, std::true_type(), std::true_type());
+    } else {
+#pragma unroll
+        for (int k0 = 0; k0 < ROWS; k0 += EACH)
+            scan_rows(edges >> (BACKWARD ? ROWS - EACH - k0 : k0) & ((1u << EACH) - 1), [&](auto edge) __attribute__((always_inline)) {
+#pragma unroll
+                for (int k = k0; k < k0 + EACH; ++k) f(BACKWARD ? ROWS - 1 - k : k, std::false_type(), edge);
+            });
+    }
+}
+
 // The gates of the wavefront's rows, and whether one of them is closed.
 template <typename T, typename S>
 __device__ __forceinline__ bool scan_gates(const unsigned (&fs)[S::ROWS], float (&g)[S::ROWS][S::V])
@@ -591,7 +611,7 @@ __global__ __launch_bounds__((ScanShape<T, false>::THREADS), (ScanShape<T, false
     edges.fetch(rows.starts, rows.start, a.h0, a.d, at);
     // every row as h = A h + B, the first one of a sequence with A = 0, and with it those of none
     float A[ROWS][V], B[ROWS][V];
-    const bool closed = scan_gates<T, S>(fs, A), special = closed || (rows.starts | rows.none);
+    const bool closed = scan_gates<T, S>(fs, A) || rows.none;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         float u[V];
@@ -622,16 +642,12 @@ __global__ __launch_bounds__((ScanShape<T, false>::THREADS), (ScanShape<T, false
     ScanProduct p[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = {1.f, 0.f};
-    scan_rows(special, [&](auto is_special) {
-        constexpr bool SPECIAL = decltype(is_special)::value;
+    scan_each<ROWS, false>(closed, rows.starts, [&](int r, auto special, auto edge) __attribute__((always_inline)) {
+        if (decltype(edge)::value && (rows.starts >> r & 1))
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            if (SPECIAL && (rows.starts >> r & 1))
+            for (int v = 0; v < V; ++v) p[v] = {0.f, 0.f};
 #pragma unroll
-                for (int v = 0; v < V; ++v) p[v] = {0.f, 0.f};
-#pragma unroll
-            for (int v = 0; v < V; ++v) p[v] = {p[v].a * A[r][v], gate_step<SPECIAL>(A[r][v], p[v].b, B[r][v])};
-        }
+        for (int v = 0; v < V; ++v) p[v] = {p[v].a * A[r][v], gate_step<decltype(special)::value>(A[r][v], p[v].b, B[r][v])};
     });
     float h[V];
     told.template join<false>(a, q, block, rows.before / S::TILE, wave, p, h);
@@ -646,20 +662,17 @@ __global__ __launch_bounds__((ScanShape<T, false>::THREADS), (ScanShape<T, false
         const unsigned ends = a.last ? rows.ends : 0;
         T *y = a.y + t0 * a.ldy + at.first;
         if (at.here())
-            scan_rows(special || ends || many < ROWS || at.odd(), [&](auto is_special) {
-                constexpr bool SPECIAL = decltype(is_special)::value;
+            scan_each<ROWS, false>(closed || many < ROWS || at.odd(), rows.starts | ends, [&](int r, auto special, auto edge) __attribute__((always_inline)) {
+                constexpr bool SPECIAL = decltype(special)::value, EDGE = decltype(edge)::value;
+                if (SPECIAL && r >= many) return;
+                if (EDGE && (rows.starts >> r & 1))
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) {
-                    if (SPECIAL && r >= many) break;
-                    if (SPECIAL && (rows.starts >> r & 1))
+                    for (int v = 0; v < V; ++v) h[v] = 0.f;
 #pragma unroll
-                        for (int v = 0; v < V; ++v) h[v] = 0.f;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) h[v] = gate_step<SPECIAL>(A[r][v], h[v], B[r][v]);
-                    at.template store<SPECIAL>(y, h);
-                    y += a.ldy;
-                    if (SPECIAL && (ends >> r & 1)) edges.put(r, h);
-                }
+                for (int v = 0; v < V; ++v) h[v] = gate_step<SPECIAL>(A[r][v], h[v], B[r][v]);
+                at.template store<SPECIAL>(y, h);
+                y += a.ldy;
+                if (EDGE && (ends >> r & 1)) edges.put(r, h);
             });
         edges.store(ends, rows.end, a.last, a.d, at);
     }
@@ -699,14 +712,6 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
     edges.fetch(rows.starts, rows.start, a.h0, a.d, at);
     float g[ROWS][V], wide[ROWS][V];       // gates, and h_{t-1} - u_t
     const bool closed = scan_gates<T, S>(fs, g) || rows.none;
-    // Where SCAN_KEPT rows have two wavefronts, the second one's state comes from the first.  (Each wavefront goes through one barrier, in front of its
-    // rows or behind them.)
-    const bool second = V == 2 && (wave & 1);
-    if (second) {
-        __syncthreads();
-#pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = told.between[wave / 2][v][lane];
-    }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         float u[V];
@@ -719,11 +724,6 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
             h[v] = gate_step<true>(shares.a, h[v], share_of<true>(shares.c, u[v]));
         }
     }
-    if (V == 2 && !second) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) told.between[wave / 2][v][lane] = h[v];
-        __syncthreads();
-    }
     edges.fetch(rows.ends, rows.end, a.dlast, a.d, at);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
@@ -733,26 +733,24 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
     ScanProduct p[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = {1.f, 0.f};
-    scan_rows(closed, [&](auto special) {
+    auto back = [&](int r, auto special, auto edge) __attribute__((always_inline)) {
         constexpr bool SPECIAL = decltype(special)::value;
+        float dy[V];
+        if (decltype(edge)::value && (rows.ends >> r & 1)) {
+            float x[V];
+            edges.get(r, x);
 #pragma unroll
-        for (int r = ROWS - 1; r >= 0; --r) {
-            float dy[V];
-            if (rows.ends >> r & 1) {
-                float x[V];
-                edges.get(r, x);
-#pragma unroll
-                for (int v = 0; v < V; ++v) p[v] = {0.f, x[v]};
-            }
-            at.values(dys[r], dy);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float share = gate_shares(g[r][v]).a;
-                p[v] = {p[v].a * share, share_of<SPECIAL>(share, p[v].b + dy[v])};
-                if (SPECIAL && (rows.none >> r & 1)) p[v] = {0.f, 0.f};
-            }
+            for (int v = 0; v < V; ++v) p[v] = {0.f, x[v]};
         }
-    });
+        at.values(dys[r], dy);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float share = gate_shares(g[r][v]).a;
+            p[v] = {p[v].a * share, share_of<SPECIAL>(share, p[v].b + dy[v])};
+            if (SPECIAL && (rows.none >> r & 1)) p[v] = {0.f, 0.f};
+        }
+    };
+    scan_each<ROWS, true>(closed, rows.ends, back);
     float x[V];
     told.template join<true>(a, q, block, rows.behind == ~0u ? q : a.tiles - 1 - (rows.behind - 1) / S::TILE, wave, p, x);
     if (many > 0) {
@@ -764,31 +762,28 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
         }
         const unsigned starts = a.dh0 ? rows.starts : 0;
         T *df_row = a.df + (t0 + many - 1) * a.lddf + at.first, *du_row = a.du + (t0 + many - 1) * a.lddu + at.first;
-        if (at.here())
-            scan_rows(closed || many < ROWS || at.odd(), [&](auto special) {
-                constexpr bool SPECIAL = decltype(special)::value;
+        auto give = [&](int r, auto special, auto edge) __attribute__((always_inline)) {
+            constexpr bool SPECIAL = decltype(special)::value, EDGE = decltype(edge)::value;
+            if (SPECIAL && r >= many) return;
+            if (EDGE && (rows.ends >> r & 1)) edges.get(r, x);
+            float dy[V], df[V], du[V];
+            at.values(dys[r], dy);
 #pragma unroll
-                for (int r = ROWS - 1; r >= 0; --r) {
-                    if (SPECIAL && r >= many) continue;
-                    if (rows.ends >> r & 1) edges.get(r, x);
-                    float dy[V], df[V], du[V];
-                    at.values(dys[r], dy);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        const float G = x[v] + dy[v];
-                        const GateShares shares = gate_shares(g[r][v]);
-                        df[v] = share_of<SPECIAL>(shares.a * shares.c, G * wide[r][v]);
-                        du[v] = share_of<SPECIAL>(shares.c, G);
-                        x[v] = share_of<SPECIAL>(shares.a, G);
-                        if (SPECIAL && (rows.none >> r & 1)) df[v] = du[v] = x[v] = 0.f;
-                    }
-                    at.template store<SPECIAL>(df_row, df);
-                    at.template store<SPECIAL>(du_row, du);
-                    df_row -= a.lddf;
-                    du_row -= a.lddu;
-                    if (starts >> r & 1) edges.put(r, x);
-                }
-            });
+            for (int v = 0; v < V; ++v) {
+                const float G = x[v] + dy[v];
+                const GateShares shares = gate_shares(g[r][v]);
+                df[v] = share_of<SPECIAL>(shares.a * shares.c, G * wide[r][v]);
+                du[v] = share_of<SPECIAL>(shares.c, G);
+                x[v] = share_of<SPECIAL>(shares.a, G);
+                if (SPECIAL && (rows.none >> r & 1)) df[v] = du[v] = x[v] = 0.f;
+            }
+            at.template store<SPECIAL>(df_row, df);
+            at.template store<SPECIAL>(du_row, du);
+            df_row -= a.lddf;
+            du_row -= a.lddu;
+            if (EDGE && (starts >> r & 1)) edges.put(r, x);
+        };
+        if (at.here()) scan_each<ROWS, true>(closed || many < ROWS, rows.ends | starts, give);
         edges.store(starts, rows.start, a.dh0, a.d, at);
     }
     scan_empty<S>(a.order, q, a.tiles, block == 0, a.flags, [&](int64_t j) {

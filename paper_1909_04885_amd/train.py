@@ -418,6 +418,8 @@ class TrainOps:
         """y: one row of every sequence, whose states [n, d] float32 become a state + (1 - a) u in place."""
         t, ldf = self._matrix(f, "f")
         n, d = f.shape
+        if isinstance(u, Packed8):
+            raise ChicleError(EINVAL, "u must be rows of f's type here: unpack8 gives them")
         _, ldu = self._matrix(u, "u", f, d)
         ts, lds = self._matrix(state, "state", None, d)
         if ts != 0 or u.shape[0] != n or state.shape[0] != n:

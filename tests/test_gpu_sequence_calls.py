@@ -162,7 +162,7 @@ def test_refusals(ops):
         lambda: ops.gated_step(x, x, half), lambda: ops.gated_step(x, x, x[:39]), lambda: ops.gated_step(x, x[:39], x.clone()),
         lambda: ops.gated_step(x, x, torch.zeros(1, 64, device="cuda").expand(40, 64)), lambda: ops.gated_step(x, p, x.clone())]
     for k, call in enumerate(bad):
-        with pytest.raises((chicle.ChicleError, AttributeError)):
+        with pytest.raises(chicle.ChicleError):
             call()
             pytest.fail("call %d was not refused" % k)
     ops.sync()
