@@ -110,7 +110,8 @@ int chicle_rms_norm_grad(const void *dy, int64_t lddy, const void *sum, int64_t 
  * written outside of the tensors.  h0 (or NULL: zeros) and last (or NULL): sequences x d floats, the state before a sequence's first row and
  * after its last.  u is of the type where u_scales is NULL, else packed rows, ldu bytes apart.  states (or NULL): n / 32, rounded up, x d floats, the state
  * that enters every 32nd row, which the gradient takes.  Of a gate beyond +-104, +-infinity too, nothing comes through on the side that it closes, whatever
- * is there: f = +infinity masks a row.  An infinity or NaN that does come in stays in its column to the sequence's end, as one or the other.
+ * is there: f = +infinity masks a row.  An infinity or NaN that does come in stays in its column, as one or the other, until a gate closes or the
+ * sequence ends (the gradients', until it begins).
  * Limits: n, d and sequences below 2^31. */
 size_t chicle_gated_scan_bytes(int64_t n, int64_t d, int32_t type);
 int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,
@@ -124,7 +125,8 @@ int chicle_gated_scan_grad(const void *f, int64_t ldf, const void *u, int64_t ld
                            int32_t type, void *df, int64_t lddf, void *du, int64_t lddu, float *dh0, void *workspace, size_t workspace_bytes,
                            int32_t *flags, void *hip_stream);
 
-/* One row of each of n sequences: state = a state + (1 - a) u, in place, y = state.  state: n x d floats, rows ldstate apart. */
+/* One row of each of n sequences: state = a state + (1 - a) u, in place, y = state.  state: n x d floats, rows ldstate apart (a state
+ * that overlaps another tensor of the call is refused). */
 int chicle_gated_step(const void *f, int64_t ldf, const void *u, int64_t ldu, float *state, int64_t ldstate, int64_t n, int64_t d, int32_t type, void *y,
                       int64_t ldy, void *hip_stream);
 

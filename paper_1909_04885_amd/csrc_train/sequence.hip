@@ -20,6 +20,17 @@ Packed packed_from(const Packed &p, int64_t row) { return p.q ? Packed{p.q + row
 
 bool sizes_ok(int64_t n, int64_t d) { return n >= 0 && d >= 1 && n <= INT32_MAX && d <= INT32_MAX; }
 
+// Whether n rows of two tensors share no memory, given where they begin, their distance and their length in bytes: one ends before the other begins, or each
+// row of one lies between two rows of the other.
+bool rows_apart(const void *a, int64_t lda, int64_t la, const void *b, int64_t ldb, int64_t lb, int64_t n)
+{
+    const uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
+    if (pa + (n - 1) * lda + la <= pb || pb + (n - 1) * ldb + lb <= pa) return true;
+    if (lda != ldb) return false;
+    const int64_t shift = pb >= pa ? (int64_t)((pb - pa) % lda) : lda - 1 - (int64_t)((pa - pb - 1) % lda);
+    return shift >= la && shift + lb <= lda;
+}
+
 // f(first row, rows, workgroups) for all n rows of `per_row` vectors.
 template <typename F>
 int with_vectors_of_rows(int64_t n, int64_t per_row, F f)
@@ -368,6 +379,9 @@ int chicle_gated_step(const void *f, int64_t ldf, const void *u, int64_t ldu, fl
     if (n == 0) return CHICLE_OK;
     const int s = size_of(type);
     if (!placed(f, s) || !placed(u, s) || !placed(y, s) || !placed(state, 4)) return fail(CHICLE_EINVAL, "a null or misplaced pointer");
+    // (another thread may have written there what this one still has to read)
+    auto apart = [&](const void *p, int64_t ld) { return rows_apart(state, ldstate * 4, d * 4, p, ld * s, d * s, n); };
+    if (!apart(f, ldf) || !apart(u, ldu) || !apart(y, ldy)) return fail(CHICLE_EINVAL, "state overlaps another tensor");
     const int lanes = pow2_at_least(ceil_div(d, 16 / s), STEP_THREADS);
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;

@@ -415,7 +415,7 @@ class TrainOps:
         return df, du, dh0
 
     def gated_step(self, f, u, state):
-        """y: one row of every sequence, whose states [n, d] float32 become a state + (1 - a) u in place."""
+        """y: one row of every sequence, whose states [n, d] float32 become a state + (1 - a) u in place (a state that shares memory with f or u is refused)."""
         t, ldf = self._matrix(f, "f")
         n, d = f.shape
         if isinstance(u, Packed8):

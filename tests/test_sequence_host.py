@@ -66,6 +66,18 @@ def test_refusals(lib, name, good, bad, code):
     assert lib.chicle_train_last_error()
 
 
+# (four rows of 64 columns: 128 bytes of f, u and y, 256 of the state)
+@pytest.mark.parametrize("name", ["f", "u", "y"])
+@pytest.mark.parametrize("place", [
+    dict(), dict(at=4096 + 896), dict(at=4096 - 510), dict(at=4096 + 128, ld=128), dict(at=4096 + 254, ld=192, lds=96), dict(at=4096 + 258, ld=192, lds=96),
+    dict(at=4096 - 130, ld=192, lds=96, n=2), dict(at=4096 - 126 - 384, ld=192, lds=96), dict(at=4096, ld=64, n=1), dict(at=4096 + 256, ld=256, lds=96)])
+def test_a_state_that_another_tensor_overlaps_is_refused(lib, name, place):
+    ld, state = place.get("ld", 64), 4096
+    args = dict(STEP, f=ctypes.c_void_p(1 << 20), u=ctypes.c_void_p(1 << 21), y=ctypes.c_void_p(1 << 22), state=P, n=place.get("n", 4), lds=place.get("lds", 64))
+    args.update({name: ctypes.c_void_p(place.get("at", state)), "ld" + name: ld})
+    assert lib.chicle_gated_step(*args.values()) == EINVAL and b"overlap" in lib.chicle_train_last_error()
+
+
 def test_workspace_sizes(lib):
     assert lib.chicle_rms_norm_grad_bytes(-1, 4, 0) == 0 and lib.chicle_rms_norm_grad_bytes(4, 0, 0) == 0 and lib.chicle_rms_norm_grad_bytes(4, 4, 7) == 0
     assert lib.chicle_gated_scan_bytes(-1, 4, 0) == 0 and lib.chicle_gated_scan_bytes(4, 0, 0) == 0 and lib.chicle_gated_scan_bytes(4, 4, 3) == 0
