@@ -7,10 +7,15 @@
 // Of a gate, the smaller share is worked out, s = e / (1 + e) with e = exp(-|f|), the other one is 1 - s: neither loses what is small.  Where
 // e is no 32-bit number (beyond +-104) a gate is closed, s = 0, and what it keeps out counts nowhere, whatever it holds.
 //
-// States are 32-bit floats.  A workgroup has a tile of SCAN_TILE rows, a wavefront SCAN_ROWS of them, a lane SCAN_V columns, held in registers and
-// read once.  What the rows of a wavefront do to the state that comes into them is a product and a sum; those of the tile are joined in LDS, and tiles
-// hand on what comes out of them (scan_hand).  The forward pass leaves the state that enters every SCAN_KEPT-th row; the gradient works out those
-// between again from the tile's first, and goes through the tiles from the last one.
+// States are 32-bit floats.  A workgroup has a tile of rows and columns (ScanShape), a wavefront some of its rows, a lane one or two columns of them, held in
+// registers and read once.  What the rows of a wavefront do to the state that comes into them is a product and a sum (ScanProduct); those of the tile are
+// joined in LDS, and tiles tell one another theirs (ScanShared::join), so that one long sequence fills the chip as well as many short ones.  The forward
+// pass leaves the state that enters every SCAN_KEPT-th row; the gradient works out those between again, and goes through the tiles from the last one.
+//
+// What bounds it is memory: every value is read and written once, a large copy goes at 4.95 TB/s.  65,536 rows of 2048 columns in bfloat16, forward
+// and its gradients: sequences of 128 rows 166 and 293 us (5.0 and 4.6 TB/s), one sequence 206 and 308 us (4.0 and 4.4): there tiles wait for what comes
+// into them; rows of 1024 in float32 141 and 240 us (5.8 and 5.6), one sequence 162 and 252 (5.0 and 5.3).  A thread that goes through its column alone takes
+// 29,950 us for 65,536 rows in one sequence.  Small calls are launches: 333 x 250 in float32 11.0 and 13.1 us, of which 4 are a state's way through the three tiles.
 #pragma once
 #include <type_traits>
 #include "elements.hpp"
@@ -39,13 +44,17 @@ template <bool CLOSED> __device__ __forceinline__ float share_of(float share, fl
 // a h + b
 template <bool CLOSED> __device__ __forceinline__ float gate_step(float a, float h, float b) { return CLOSED && a == 0.f ? b : fmaf(a, h, b); }
 
-// A lane has 32 values of every input: of 16 bits two columns, so that it reads four bytes of a row, and half as many rows.
+// A lane has 32 values of every input: of 16 bits two columns, so that it reads four bytes of a row, and half as many rows.  (Forward, 65,536 x 2048 in bfloat16,
+// one sequence: one column and 32 rows 225 us, two and 16 rows 184 when first measured.  The gradient has three inputs and a pass more: with two
+// columns, its wavefronts in pairs that share a tile's rows, it takes 330 to 550 us instead of 315.  Two wavefronts to a workgroup are slower in both.)
 template <typename T, bool BACKWARD> struct ScanShape {
     static constexpr int V = BACKWARD ? 1 : 4 / (int)sizeof(T), COLS = 64 * V, ROWS = SCAN_KEPT / V;
     static constexpr int WAVES = 4 * V, THREADS = 64 * WAVES, TILE = ROWS * WAVES;
     static constexpr int HELD = V == 1 ? 3 : 4;          // wavefronts of a SIMD, as registers allow
     static constexpr bool LINES = !BACKWARD || sizeof(T) == 4;             // there are registers for both kinds of loads
 };
+// (200,000 x 16 in float32, 1563 tiles in one column block: 8 and 64 take 41 us, 8 and 16 or 16 and 16 take 84 to 88, 8 and 128 the same 41; with 16 and 64,
+// 65,536 x 2048 in bfloat16 takes 231 and 343 us instead of 206 and 308, for registers.)
 constexpr int SCAN_GROUP = 8, SCAN_RUN = 64;             // tiles whose products are joined, and tiles from one state that is handed on to the next
 constexpr int SCAN_TICKET = 32;                          // places from one column block's ticket to the next: lines of their own
 
@@ -55,12 +64,9 @@ typedef unsigned u32_at_2 __attribute__((aligned(2)));
 // some column that is there and store nothing.
 template <typename T, typename S> struct ScanLane {
     static constexpr int V = S::V, ROWS = S::ROWS;
-    int64_t first;                           // the tile's first column
+    unsigned first;                          // the tile's first column
     int e, left;                             // the lane's first column; columns from the tile's first to the last one, or the tile's
-    __device__ __forceinline__ ScanLane(int64_t block, int64_t d) : first(block * S::COLS), e((threadIdx.x & 63) * V)
-    {
-        left = d - first < S::COLS ? (int)(d - first) : S::COLS;
-    }
+    __device__ __forceinline__ ScanLane(unsigned block, unsigned d) : first(block * S::COLS), e((threadIdx.x & 63) * V) { left = min(d - first, (unsigned)S::COLS); }
     __device__ __forceinline__ bool here() const { return e < left; }
     __device__ __forceinline__ bool odd() const { return V == 2 && (left & 1); }          // the last column has no neighbour
     // The lane's values of a wavefront's rows: the last of `many` again in place of those that are not there.
@@ -165,8 +171,8 @@ template <typename T> struct ScanInput<T, true> {
     {
         constexpr int V = S::V, GROUPS = S::COLS / PACK_GROUP;
         static_assert(GROUPS * S::ROWS == 64, "a lane for every scale");
-        const int64_t whole = (d + PACK_GROUP - 1) / PACK_GROUP * PACK_GROUP - at.first;
-        const int left = whole < S::COLS ? (int)whole : S::COLS, lane = threadIdx.x & 63;
+        const unsigned whole = ((unsigned)d + PACK_GROUP - 1) / PACK_GROUP * PACK_GROUP;
+        const int left = min(whole - at.first, (unsigned)S::COLS), lane = threadIdx.x & 63;
         const unsigned off = at.e < left ? at.e : left - V;
         const int r = lane / GROUPS, which = r < many ? r : many > 0 ? many - 1 : 0, group = lane % GROUPS;
         out.step = scales[(row + which) * (ld / PACK_GROUP) + at.first / PACK_GROUP + (group * PACK_GROUP < left ? group : 0)];
@@ -199,7 +205,8 @@ struct ScanOrder {
         if (!offsets) return j == 0 ? 0u : (unsigned)n;
         return ((const __attribute__((address_space(4))) unsigned *)offsets)[wide ? 2 * (int64_t)j : (int64_t)j];
     }
-    // How many of the offsets are at most t.
+    // How many of the offsets are at most t.  (Rows, columns and sequences are 32-bit numbers here, also because hipcc 7.2 has been seen to take the condition
+    // of one choice between uniform 64-bit numbers for that of the next.)
     __device__ __forceinline__ unsigned up_to(unsigned t) const
     {
         unsigned lo = 0, hi = (unsigned)count + 1;
@@ -246,12 +253,15 @@ __global__ __launch_bounds__(256) static void scan_begin(unsigned *tickets, unsi
     }
 }
 
-// What rows do to what comes into them: x becomes a x + b; where a = 0 it does not get through, whatever it is.
+// What rows do to what comes into them: x becomes a x + b.  Where it does not get through, whatever it is, since a sequence begins or a gate is closed, a is
+// -0: a product of shares that is too small for a number is +0, and lets what is no number through.
+constexpr float SCAN_STOP = -0.f;
+
 struct ScanProduct {
     float a, b;
-    __device__ __forceinline__ float of(float x) const { return gate_step<true>(a, x, b); }
+    __device__ __forceinline__ float of(float x) const { return signbit(a) ? b : fmaf(a, x, b); }
     // What the rows do after `before`.
-    __device__ __forceinline__ ScanProduct after(const ScanProduct &before) const { return {share_of<true>(a, before.a), of(before.b)}; }
+    __device__ __forceinline__ ScanProduct after(const ScanProduct &before) const { return {signbit(a) ? SCAN_STOP : a * before.a, of(before.b)}; }
     __device__ __forceinline__ unsigned long long word() const
     {
         const unsigned lo = a == a ? __float_as_uint(a) : 0x7fc00000u;
@@ -288,7 +298,7 @@ struct ScanRows {
         before = behind = ~0u;
         unsigned j = t0 > 0 ? o.up_to(t0 - 1) : 0;
         if (j > 0 && j <= count && o.common(j) > t0) before = o.common(j - 1);
-        while (j <= count) {                             // (at most S::ROWS + 2 times, where offsets ascend)
+        for (int left = S::ROWS + 1; j <= count && left > 0; --left) {     // (rows t0 to t1, where offsets ascend)
             const unsigned at = o.common(j);
             if (at > t1) break;
             // sequence j - 1 ends in front of row `at`, sequence k - 1 begins with it; those between have no rows
@@ -598,16 +608,16 @@ __global__ __launch_bounds__((ScanShape<T, false>::THREADS), (ScanShape<T, false
     unsigned block, q;
     scan_unit(a, block, q);
     if (q >= a.tiles) return;
-    const ScanLane<T, S> at(block, a.d);
-    const int64_t n = a.order.n, t0 = (int64_t)q * S::TILE + wave * ROWS;
-    // (wavefronts behind the last row have that one, as rows of no sequence, and store nothing)
-    const int many = (int)(n - t0 < ROWS ? n - t0 < 0 ? 0 : n - t0 : ROWS);
-    const int64_t from = many > 0 ? t0 : n - 1;
+    const ScanLane<T, S> at(block, (unsigned)a.d);
+    // (rows and columns are fewer than 2^31; wavefronts behind the last row have that one, as rows of no sequence, and store nothing)
+    const unsigned n = (unsigned)a.order.n, t = q * S::TILE + wave * ROWS;
+    const int many = t < n ? min(n - t, (unsigned)ROWS) : 0;
+    const int64_t t0 = t, from = many > 0 ? t : n - 1;
     unsigned fs[ROWS];
     typename ScanInput<T, PACKED>::template Raw<S> us;
     at.load(a.f + from * a.ldf, a.ldf, many, a.lines, fs);
     a.u.load(from, a.d, many, a.lines, at, us);
-    const ScanRows rows(a.order, (unsigned)t0, S());
+    const ScanRows rows(a.order, t, S());
     edges.fetch(rows.starts, rows.start, a.h0, a.d, at);
     // every row as h = A h + B, the first one of a sequence with A = 0, and with it those of none
     float A[ROWS][V], B[ROWS][V];
@@ -643,11 +653,13 @@ __global__ __launch_bounds__((ScanShape<T, false>::THREADS), (ScanShape<T, false
 #pragma unroll
     for (int v = 0; v < V; ++v) p[v] = {1.f, 0.f};
     scan_each<ROWS, false>(closed, rows.starts, [&](int r, auto special, auto edge) __attribute__((always_inline)) {
-        if (decltype(edge)::value && (rows.starts >> r & 1))
+        constexpr bool SPECIAL = decltype(special)::value;
+        const bool starts = decltype(edge)::value && (rows.starts >> r & 1);
 #pragma unroll
-            for (int v = 0; v < V; ++v) p[v] = {0.f, 0.f};
-#pragma unroll
-        for (int v = 0; v < V; ++v) p[v] = {p[v].a * A[r][v], gate_step<decltype(special)::value>(A[r][v], p[v].b, B[r][v])};
+        for (int v = 0; v < V; ++v) {
+            if (starts || (SPECIAL && A[r][v] == 0.f)) p[v] = {SCAN_STOP, B[r][v]};
+            else p[v] = {p[v].a * A[r][v], fmaf(A[r][v], p[v].b, B[r][v])};
+        }
     });
     float h[V];
     told.template join<false>(a, q, block, rows.before / S::TILE, wave, p, h);
@@ -697,10 +709,10 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
     scan_unit(a, block, q);
     if (q >= a.tiles) return;
     const unsigned tile = a.tiles - 1 - q;
-    const ScanLane<T, S> at(block, a.d);
-    const int64_t n = a.order.n, t0 = (int64_t)tile * S::TILE + wave * ROWS;
-    const int many = (int)(n - t0 < ROWS ? n - t0 < 0 ? 0 : n - t0 : ROWS);
-    const int64_t from = many > 0 ? t0 : n - 1;
+    const ScanLane<T, S> at(block, (unsigned)a.d);
+    const unsigned n = (unsigned)a.order.n, t = tile * S::TILE + wave * ROWS;
+    const int many = t < n ? min(n - t, (unsigned)ROWS) : 0;
+    const int64_t t0 = t, from = many > 0 ? t : n - 1;
     unsigned fs[ROWS], dys[ROWS];
     typename ScanInput<T, PACKED>::template Raw<S> us;
     float h[V];
@@ -708,7 +720,7 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
     a.u.load(from, a.d, many, a.lines, at, us);
     at.load_floats(a.states, from / SCAN_KEPT, a.d, h);
     at.load(a.dy + from * a.lddy, a.lddy, many, a.lines, dys);
-    const ScanRows rows(a.order, (unsigned)t0, S());
+    const ScanRows rows(a.order, t, S());
     edges.fetch(rows.starts, rows.start, a.h0, a.d, at);
     float g[ROWS][V], wide[ROWS][V];       // gates, and h_{t-1} - u_t
     const bool closed = scan_gates<T, S>(fs, g) || rows.none;
@@ -740,14 +752,14 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
             float x[V];
             edges.get(r, x);
 #pragma unroll
-            for (int v = 0; v < V; ++v) p[v] = {0.f, x[v]};
+            for (int v = 0; v < V; ++v) p[v] = {SCAN_STOP, x[v]};
         }
         at.values(dys[r], dy);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float share = gate_shares(g[r][v]).a;
-            p[v] = {p[v].a * share, share_of<SPECIAL>(share, p[v].b + dy[v])};
-            if (SPECIAL && (rows.none >> r & 1)) p[v] = {0.f, 0.f};
+            if (SPECIAL && (share == 0.f || (rows.none >> r & 1))) p[v] = {SCAN_STOP, 0.f};
+            else p[v] = {p[v].a * share, share * (p[v].b + dy[v])};
         }
     };
     scan_each<ROWS, true>(closed, rows.ends, back);

@@ -140,6 +140,28 @@ def test_a_state_that_is_written_has_a_new_version(ops):
         product.backward()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_states_that_lie_between_the_rows_of_other_tensors(ops, dtype):
+    """One buffer has the rows of f, u and the states beside each other, the states first or last; what is between stays as it was."""
+    g, n, d = gen(9), 5, 24
+    f, u, state = torch.randn(n, d, generator=g, device="cuda").to(dtype), torch.randn(n, d, generator=g, device="cuda").to(dtype), torch.randn(n, d, generator=g, device="cuda")
+    want_state = state.clone()
+    want = ops.gated_step(f, u, want_state)
+    narrow = d * f.element_size() // 4                   # floats that a row of f takes
+    for first in (0, 2 * narrow):
+        buffer = torch.zeros(n, 2 * narrow + d, device="cuda")
+        at = d if first == 0 else 0
+        s = buffer[:, first:first + d]
+        rows = [buffer[:, at + k * narrow:at + (k + 1) * narrow].view(dtype) for k in range(2)]
+        s.copy_(state), rows[0].copy_(f), rows[1].copy_(u)
+        assert torch.equal(ops.gated_step(*rows, s), want) and torch.equal(s, want_state) and torch.equal(rows[0], f) and torch.equal(rows[1], u)
+    wide = torch.zeros(n, d, device="cuda")
+    for bad in ((wide, f.float()), (f.float(), wide)):
+        with pytest.raises(Exception, match="overlap"):
+            ops.gated_step(*bad, wide)
+    ops.sync()
+
+
 def test_refusals(ops):
     import paper_1909_04885_amd as chicle
     x, v, ones = torch.randn(40, 64, device="cuda"), torch.ones(64, device="cuda"), torch.ones(40, device="cuda")
@@ -201,6 +223,28 @@ def test_nothing_of_a_sequence_reaches_another(ops, dtype):
         if a is not None:
             assert torch.equal(grads2[2][others], grads[2][others])
     ops.sync()
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("share", [0.0, -9.0])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_what_is_no_number_goes_on_until_a_gate_is_closed(ops, dtype, share, bad):
+    """Also where the product of the shares between is too small for a number: a half or 1.2e-4 a row."""
+    n, d, first, shut = 900, 70, 3, 700
+    f, u = torch.full((n, d), share, dtype=dtype, device="cuda"), torch.ones(n, d, dtype=dtype, device="cuda")
+    u[first, ::2] = bad
+    f[shut, ::4] = -INF
+    offsets = torch.tensor([0, 850, n], device="cuda")
+    y, last, states = ops.gated_scan(f, u, offsets, last=True, states=True)
+    assert not y[first:shut, ::2].isfinite().any() and not y[shut:850, 2::4].isfinite().any() and not last[0, 2::4].isfinite().any()
+    assert y[:first].isfinite().all() and y[:, 1::2].isfinite().all() and y[shut:, ::4].isfinite().all() and y[850:].isfinite().all()
+    dy = torch.ones(n, d, dtype=dtype, device="cuda")
+    u[first, ::2] = 1
+    dy[845, ::2] = bad
+    _, _, states = ops.gated_scan(f, u, offsets, states=True)
+    df, du, dh0 = ops.gated_scan_grad(f, u, states, dy, offsets, h0=torch.zeros(2, d, device="cuda"))
+    assert not du[shut:846, ::2].isfinite().any() and not du[:shut, 2::4].isfinite().any() and not dh0[0, 2::4].isfinite().any()
+    assert du[846:].isfinite().all() and du[:, 1::2].isfinite().all() and du[:shut, ::4].isfinite().all() and dh0[1].isfinite().all()
 
 
 def test_one_state_and_no_gradient_of_the_last_and_the_other_way_round(ops):
