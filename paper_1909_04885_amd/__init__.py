@@ -5,7 +5,7 @@
 used only to allocate device memory and to supply the HIP stream.
 
 `train.TrainOps` is the same over `libchicle_train.so` (`include/chicle_train.h`): the operators of a local SGD
-step for models over categorical data.
+step for models over categorical data, also in sequences.
 """
 from .binding import (ChicleError, ChicleRound, balance, library_path, load_library,  # noqa: F401
                       next_solver_count, projected_iteration_time, rebalance, scale_in, scale_out)
