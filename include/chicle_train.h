@@ -112,7 +112,7 @@ int chicle_rms_norm_grad(const void *dy, int64_t lddy, const void *sum, int64_t 
  * that enters every 32nd row, which the gradient takes.  Of a gate beyond +-104, +-infinity too, nothing comes through on the side that it closes, whatever
  * is there: f = +infinity masks a row.  An infinity or NaN that does come in stays in its column, as one or the other, until a gate closes or the
  * sequence ends (the gradients', until it begins).
- * Limits: n, d and sequences below 2^31. */
+ * Limits: n, d and sequences below 2^31, and n / 128 times d / 64, each rounded up, below 2^23. */
 size_t chicle_gated_scan_bytes(int64_t n, int64_t d, int32_t type);
 int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,
                       const float *h0, int64_t n, int64_t d, int32_t type, void *y, int64_t ldy, float *last, float *states, void *workspace,

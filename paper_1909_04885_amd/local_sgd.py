@@ -70,6 +70,8 @@ class SequenceModel:
 
     def offsets(self, rows: int, device):
         import torch
+        if rows % self.length:
+            raise ValueError("%d rows are no whole sequences of %d rows" % (rows, self.length))
         return torch.arange(0, rows + 1, self.length, dtype=torch.int32, device=device)
 
     def forward(self, ops: TrainOps, params: Sequence, tokens, states: bool = False):

@@ -85,6 +85,25 @@ def test_workspace_sizes(lib):
     assert lib.chicle_gated_scan_bytes(65536, 2048, 1) < 65536 * 2048              # less than a byte for a value
 
 
+@pytest.mark.parametrize("rows, whole", [(0, True), (6, True), (7, False), (5, False)])
+def test_rows_that_are_no_whole_sequences_are_refused(rows, whole):
+    from paper_1909_04885_amd.local_sgd import SequenceModel
+    model = SequenceModel(8, 4, 16, 1, 3, torch.float32, "cpu")
+    if whole:
+        assert model.offsets(rows, "cpu").tolist() == list(range(0, rows + 1, 3))
+    else:
+        with pytest.raises(ValueError):
+            model.offsets(rows, "cpu")
+
+
+@pytest.mark.parametrize("n, d", [(1 << 30, 64), ((1 << 30) - 127, 1), (129, (1 << 28) - 63), (1 << 20, 1 << 16)])
+def test_scans_of_more_workgroups_than_a_launch_has_are_refused(lib, n, d):
+    big = dict(n=n, d=d, ldf=d, ldu=d, ldy=d)
+    assert lib.chicle_gated_scan(*dict(SCAN, **big).values()) == EINVAL and b"too many" in lib.chicle_train_last_error()
+    big = dict(n=n, d=d, ldf=d, ldu=d, lddy=d, lddf=d, lddu=d)
+    assert lib.chicle_gated_scan_grad(*dict(SCAN_GRAD, **big).values()) == EINVAL and b"too many" in lib.chicle_train_last_error()
+
+
 def test_reference_of_the_8_bits():
     """The scale is the least power of two that is enough, and values come back to half of it."""
     g = torch.Generator().manual_seed(3)
