@@ -13,7 +13,7 @@
 // pass leaves the state that enters every SCAN_KEPT-th row; the gradient works out those between again, and goes through the tiles from the last one.
 //
 // What bounds it is memory: every value is read and written once, a large copy goes at 4.95 TB/s.  65,536 rows of 2048 columns in bfloat16, forward
-// and its gradients: sequences of 128 rows 166 and 293 us (5.0 and 4.6 TB/s), one sequence 206 and 308 us (4.0 and 4.4): there tiles wait for what comes
+// and its gradients: sequences of 128 rows 166 and 268 us (5.0 and 5.1 TB/s), one sequence 202 and 302 us (4.1 and 4.5): there tiles wait for what comes
 // into them; rows of 1024 in float32 141 and 240 us (5.8 and 5.6), one sequence 162 and 252 (5.0 and 5.3).  A thread that goes through its column alone takes
 // 29,950 us for 65,536 rows in one sequence.  Small calls are launches: 333 x 250 in float32 11.0 and 13.1 us, of which 4 are a state's way through the three tiles.
 #pragma once
@@ -50,11 +50,13 @@ template <bool CLOSED> __device__ __forceinline__ float gate_step(float a, float
 template <typename T, bool BACKWARD> struct ScanShape {
     static constexpr int V = BACKWARD ? 1 : 4 / (int)sizeof(T), COLS = 64 * V, ROWS = SCAN_KEPT / V;
     static constexpr int WAVES = 4 * V, THREADS = 64 * WAVES, TILE = ROWS * WAVES;
-    static constexpr int HELD = V == 1 ? 3 : 4;          // wavefronts of a SIMD, as registers allow
+    // wavefronts of a SIMD, as registers allow (gradients in 16 bits, 65,536 x 2048 in sequences of 128 rows: three 293 us, four 268)
+    static constexpr int HELD = BACKWARD && sizeof(T) == 4 ? 3 : 4;
+    static constexpr int MORE_LDS = V == 1 ? 16384 : 0;  // LDS besides with which there are three workgroups to a compute unit
     static constexpr bool LINES = !BACKWARD || sizeof(T) == 4;             // there are registers for both kinds of loads
 };
 // (200,000 x 16 in float32, 1563 tiles in one column block: 8 and 64 take 41 us, 8 and 16 or 16 and 16 take 84 to 88, 8 and 128 the same 41; with 16 and 64,
-// 65,536 x 2048 in bfloat16 takes 231 and 343 us instead of 206 and 308, for registers.)
+// 65,536 x 2048 in bfloat16 takes 231 and 343 us instead of 206 and 308, for registers, when measured.)
 constexpr int SCAN_GROUP = 8, SCAN_RUN = 64;             // tiles whose products are joined, and tiles from one state that is handed on to the next
 constexpr int SCAN_TICKET = 32;                          // places from one column block's ticket to the next: lines of their own
 
@@ -537,7 +539,8 @@ template <typename S> struct ScanEdges {
     }
 };
 
-// The same value, of which the compiler does not know that it is: what an earlier pass worked out of it is worked out again instead of being kept.
+// The same value, of which the compiler does not know that it is: it is worked out here, and not where it is used from what it is made of, and what an
+// earlier pass worked out of it is worked out again, instead of all of that being kept (the gradients: 161 registers, with these 120).
 template <typename X> __device__ __forceinline__ void scan_anew(X &x) { asm volatile("" : "+v"(x)); }
 
 // f(whether there is something that makes rows special)
@@ -550,7 +553,7 @@ __device__ __forceinline__ void scan_rows(bool special, F f)
 
 // f(r, whether rows are special, whether there may be an edge) for all rows, BACKWARD from the last one on: eight at a time, without looks at each where
 // none of them is one of `edges`.  (Looked at one by one, gradients of 65,536 x 2048 in bfloat16 take 317 instead of 309 us; with one look for all, sequences
-// of 100 rows 345 instead of 315.)
+// of 100 rows 345 instead of 315, when measured.)
 template <int ROWS, bool BACKWARD, typename F>
 __device__ __forceinline__ void scan_each(bool special, unsigned edges, F f)
 {
@@ -580,6 +583,7 @@ __device__ __forceinline__ bool scan_gates(const unsigned (&fs)[S::ROWS], float 
 #pragma unroll
         for (int v = 0; v < S::V; ++v) {
             g[r][v] = gate_of(f[v]);
+            scan_anew(g[r][v]);
             least = fminf(least, fabsf(g[r][v]));
         }
         if (r % (4 / S::V) == 4 / S::V - 1) __builtin_amdgcn_sched_barrier(0);             // (not all rows at once: there are no registers for that)
@@ -733,6 +737,7 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
         for (int v = 0; v < V; ++v) {
             const GateShares shares = gate_shares(g[r][v]);
             wide[r][v] = h[v] - u[v];
+            scan_anew(wide[r][v]);
             h[v] = gate_step<true>(shares.a, h[v], share_of<true>(shares.c, u[v]));
         }
     }
@@ -741,6 +746,23 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
     for (int r = 0; r < ROWS; ++r)
 #pragma unroll
         for (int v = 0; v < V; ++v) scan_anew(g[r][v]);
+    // (dy of two rows in one register, where it is of 16 bits)
+    constexpr int PER = sizeof(T) == 2 ? 2 : 1;
+    unsigned two[ROWS / PER];
+#pragma unroll
+    for (int i = 0; i < ROWS / PER; ++i) {
+        two[i] = PER == 2 ? dys[i * PER] | dys[i * PER + PER - 1] << 16 : dys[i];
+        scan_anew(two[i]);
+    }
+    auto dy_of = [&](int r, float (&dy)[V]) __attribute__((always_inline)) {
+        if constexpr (PER == 1) at.values(two[r], dy);
+        else if constexpr (__is_same(T, bf16)) dy[0] = __uint_as_float(r % 2 ? two[r / 2] & 0xffff0000u : two[r / 2] << 16);
+        else {
+            f16 v[2];
+            __builtin_memcpy(v, &two[r / 2], 4);
+            dy[0] = (float)v[r % 2];
+        }
+    };
     // x: what goes from a row to the one before, a G
     ScanProduct p[V];
 #pragma unroll
@@ -754,7 +776,7 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
 #pragma unroll
             for (int v = 0; v < V; ++v) p[v] = {SCAN_STOP, x[v]};
         }
-        at.values(dys[r], dy);
+        dy_of(r, dy);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float share = gate_shares(g[r][v]).a;
@@ -768,7 +790,7 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
     if (many > 0) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {                 // (not kept from the pass above)
-            scan_anew(dys[r]);
+            if (r % PER == 0) scan_anew(two[r / PER]);
 #pragma unroll
             for (int v = 0; v < V; ++v) scan_anew(g[r][v]);
         }
@@ -779,7 +801,7 @@ __global__ __launch_bounds__((ScanShape<T, true>::THREADS), (ScanShape<T, true>:
             if (SPECIAL && r >= many) return;
             if (EDGE && (rows.ends >> r & 1)) edges.get(r, x);
             float dy[V], df[V], du[V];
-            at.values(dys[r], dy);
+            dy_of(r, dy);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float G = x[v] + dy[v];

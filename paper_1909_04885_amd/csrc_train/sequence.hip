@@ -169,8 +169,11 @@ int run_scan(Scan<T, PACKED> a, void *workspace, hipStream_t stream)
         TRY(launched("scan_begin"));
     }
     const unsigned grid = (unsigned)(p.tiles * p.blocks);
-    if constexpr (BACKWARD) scan_backward<T, PACKED><<<grid, S::THREADS, 0, stream>>>(a);
-    else scan_forward<T, PACKED><<<grid, S::THREADS, 0, stream>>>(a);
+    // Rows that meet in lines: three workgroups to a compute unit, so that a line is still there when the next column block comes for its part.  Gradients, three /
+    // four, 16 bits: 30,011 x 1000 83 / 90 us, 90,000 x 300 98 / 104, 5000 x 4099 73 / 83; forward, 32 bits: 200,000 x 16 41 / 43.5.
+    const size_t lds = a.lines ? 0 : S::MORE_LDS;
+    if constexpr (BACKWARD) scan_backward<T, PACKED><<<grid, S::THREADS, lds, stream>>>(a);
+    else scan_forward<T, PACKED><<<grid, S::THREADS, lds, stream>>>(a);
     return launched(BACKWARD ? "scan_backward" : "scan_forward");
 }
 
