@@ -109,9 +109,9 @@ int chicle_rms_norm_grad(const void *dy, int64_t lddy, const void *sum, int64_t 
  * they hold.  Offsets that descend or are no rows of the call set a bit of *flags, and results are then not defined; nothing is read or
  * written outside of the tensors.  h0 (or NULL: zeros) and last (or NULL): sequences x d floats, the state before a sequence's first row and
  * after its last.  u is of the type where u_scales is NULL, else packed rows, ldu bytes apart.  states (or NULL): n / 32, rounded up, x d floats, the state
- * that enters every 32nd row, which the gradient takes.  Of a gate beyond +-104, +-infinity too, nothing comes through on the side that it closes, whatever
- * is there: f = +infinity masks a row.  An infinity or NaN that does come in stays in its column, as one or the other, until a gate closes or the
- * sequence ends (the gradients', until it begins).
+ * that enters every 32nd row, which the gradient takes.  Of a gate beyond +-103.97 (150 ln 2, where its smaller share, down to 2^-149 before, is rounded
+ * to 0), +-infinity too, nothing comes through on the side that it closes, whatever is there: f = +infinity masks a row.  An infinity or NaN that
+ * does come in stays in its column, as one or the other, until a gate closes or the sequence ends (the gradients', until it begins).
  * Limits: n, d and sequences below 2^31, and n / 128 times d / 64, each rounded up, below 2^23. */
 size_t chicle_gated_scan_bytes(int64_t n, int64_t d, int32_t type);
 int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide, int64_t sequences,

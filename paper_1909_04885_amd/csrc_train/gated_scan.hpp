@@ -4,8 +4,8 @@
 //   G_t = dy_t + a_{t+1} G_{t+1}, the last row's with the gradient of the last state:
 //   du_t = c_t G_t,  df_t = G_t (h_{t-1} - u_t) a_t c_t,  dh0 = a_first G_first
 //
-// Of a gate, the smaller share is worked out, s = e / (1 + e) with e = exp(-|f|), the other one is 1 - s: neither loses what is small.  Where
-// e is no 32-bit number (beyond +-104) a gate is closed, s = 0, and what it keeps out counts nowhere, whatever it holds.
+// Of a gate, the smaller share is worked out, s = e / (1 + e) with e = exp(-|f|), the other one is 1 - s: neither loses what is small, down to the last 32-bit
+// number, 2^-149.  Where e is rounded to nothing, from 150 ln 2 = 103.97 on, a gate is closed, s = 0, and what it keeps out counts nowhere, whatever it holds.
 //
 // States are 32-bit floats.  A workgroup has a tile of rows and columns (ScanShape), a wavefront some of its rows, a lane one or two columns of them, held in
 // registers and read once.  What the rows of a wavefront do to the state that comes into them is a product and a sum (ScanProduct); those of the tile are
@@ -25,11 +25,13 @@ namespace chicle_train {
 
 constexpr int SCAN_KEPT = 32;
 
-// s with the sign of f.
+// s with the sign of f.  The exponential of the hardware gives no numbers below 2^-126: there it is that of 64 more, which the quotient brings down by
+// 2^64 (where 1 + e is 1), with its one rounding.
 __device__ __forceinline__ float gate_of(float f)
 {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(f));
-    return copysignf(e * __builtin_amdgcn_rcpf(1.f + e), f);
+    const bool small = fabsf(f) > 87.33f;                // (126 ln 2 = 87.337)
+    const float e = __builtin_amdgcn_exp2f(fmaf(-1.44269504f, fabsf(f), small ? 64.f : 0.f));
+    return copysignf(e * __builtin_amdgcn_rcpf((small ? 0x1p64f : 1.f) + e), f);
 }
 
 struct GateShares { float a, c; };
