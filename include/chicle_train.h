@@ -91,6 +91,7 @@ int chicle_unpack8(const void *q, const void *scales, int64_t ldq, int64_t n, in
 /* Root-mean-square norm of rows on a residual stream: r = x + residual (residual may be NULL: r = x), rounded to the type;
  * rstd = 1 / sqrt(sum_c r_c^2 / d + eps), y = r rstd gamma.  sum (or NULL) gets r; sum8 (or NULL) gets r as packed rows, ldsum8 bytes apart.  y is of the
  * type where y_scales is NULL, else packed rows, ldy bytes apart, made from the 32-bit values.  rstd: n floats, which the gradient takes.
+ * Values may be as large as the type's largest, and, where eps is 0, as small as 2^-126; a row of zeros without eps has no norm (rstd infinite, y NaN).
  * Limits: n and d below 2^31. */
 int chicle_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *gamma, int64_t n, int64_t d, int32_t type, float eps,
                     void *sum, int64_t ldsum, void *y, int64_t ldy, void *y_scales, void *sum8, void *sum8_scales, int64_t ldsum8, float *rstd,
