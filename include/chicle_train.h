@@ -23,7 +23,8 @@
  *     type are rounded once, where they are stored;
  *   - label and token arrays hold 32-bit integers, or 64-bit ones where `wide` is not 0.  A negative one means "none": no loss, a row
  *     of zeros, no gradient.  One past the end is treated like that too, and sets a bit of *flags (1: label, 2: token), an
- *     int32 of the caller's, or NULL (4: offsets of sequences that are no rows of the call);
+ *     int32 of the caller's, or NULL (4: offsets of sequences that are no rows of the call; 8: a scan whose workgroups gave up waiting for one another, after seconds, as
+ *     where something else writes into its workspace: its results are not defined);
  *   - results do not depend on timing: the same call on the same inputs gives the same bits.
  */
 #ifndef CHICLE_TRAIN_H

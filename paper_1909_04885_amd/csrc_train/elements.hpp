@@ -126,7 +126,7 @@ __device__ __forceinline__ int64_t index_at(const void *p, int wide, int64_t i)
     return wide ? ((const int64_t *)p)[i] : (int64_t)((const int32_t *)p)[i];
 }
 
-constexpr int FLAG_LABEL_RANGE = 1, FLAG_ID_RANGE = 2, FLAG_OFFSETS = 4;
+constexpr int FLAG_LABEL_RANGE = 1, FLAG_ID_RANGE = 2, FLAG_OFFSETS = 4, FLAG_WAIT = 8;
 
 static __global__ void take_flags(int *flags, int *out) { *out = atomicExch(flags, 0); }
 

@@ -239,7 +239,7 @@ template <typename T, bool PACKED> struct Scan {
     float *last, *dh0;                       // or null
     T *y, *df, *du;
     int64_t ldf, lddy, ldy, lddf, lddu, d;
-    int *flags;
+    int *flags, looks;                       // looks: before a wait is given up
     // what workgroups hand on; null where there is one tile in a column block
     unsigned *tickets;
     unsigned long long *products, *groups, *handed;
@@ -276,14 +276,18 @@ struct ScanProduct {
 
 __device__ __forceinline__ unsigned long long scan_look(const unsigned long long *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void scan_tell(unsigned long long *p, unsigned long long w) { __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-// (Every wait ends by itself, see below.  Where a workspace is written by something else meanwhile, against its rules, this one ends too, after some
-// seconds, with what is no number.)
-__device__ __forceinline__ unsigned long long scan_wait(const unsigned long long *p, unsigned long long w)
+// (Every wait ends by itself, see below.  Where a workspace is written by something else meanwhile, against its rules, this one ends too, after so many looks,
+// some seconds, with what is no number, and says so.)
+struct ScanPatience { int looks, *flags; };
+__device__ __forceinline__ unsigned long long scan_wait(const unsigned long long *p, unsigned long long w, const ScanPatience &most)
 {
-    for (int left = 1 << 22; w == SCAN_NOTHING && left > 0; --left) {
+    bool missing = __any(w == SCAN_NOTHING);
+    for (int left = most.looks; missing && left > 0; --left) {
         __builtin_amdgcn_s_sleep(1);
         w = scan_look(p);
+        missing = __any(w == SCAN_NOTHING);
     }
+    if (missing && most.flags) atomicOr(most.flags, FLAG_WAIT);
     return w;
 }
 
@@ -359,7 +363,7 @@ __device__ __forceinline__ void scan_empty(const ScanOrder &o, unsigned tile, un
 // So every wait ends.  What is joined, and in which order, follows from the offsets alone.  A word is told whole, and says by itself whether it
 // has been.
 template <int V>
-__device__ __forceinline__ void scan_join(const unsigned long long *words, int64_t line, unsigned from, unsigned to, ScanProduct (&x)[V])
+__device__ __forceinline__ void scan_join(const unsigned long long *words, int64_t line, unsigned from, unsigned to, const ScanPatience &most, ScanProduct (&x)[V])
 {
     constexpr int AHEAD = SCAN_GROUP - 1;
     for (unsigned i = from; i < to; i += AHEAD) {
@@ -373,7 +377,7 @@ __device__ __forceinline__ void scan_join(const unsigned long long *words, int64
         for (int k = 0; k < AHEAD; ++k)
             if (i + k < to)
 #pragma unroll
-                for (int v = 0; v < V; ++v) x[v] = ScanProduct::from(scan_wait(p + k * line + v * 64, w[k][v])).after(x[v]);
+                for (int v = 0; v < V; ++v) x[v] = ScanProduct::from(scan_wait(p + k * line + v * 64, w[k][v], most)).after(x[v]);
     }
 }
 
@@ -385,7 +389,7 @@ __device__ __forceinline__ void scan_near(const Scan<T, PACKED> &a, unsigned q, 
     const unsigned group = q / SCAN_GROUP;
 #pragma unroll
     for (int v = 0; v < V; ++v) scan_tell(a.products + q * line + at + v * 64, own[v].word());
-    scan_join<V>(a.products + at, line, max(from, group * SCAN_GROUP), q, near);
+    scan_join<V>(a.products + at, line, max(from, group * SCAN_GROUP), q, {a.looks, a.flags}, near);
     if (q % SCAN_GROUP == SCAN_GROUP - 1)
 #pragma unroll
         for (int v = 0; v < V; ++v) scan_tell(a.groups + group * line + at + v * 64, own[v].after(near[v]).word());
@@ -395,7 +399,7 @@ template <typename T, bool PACKED, int V>
 __device__ __forceinline__ void scan_far(const Scan<T, PACKED> &a, unsigned q, unsigned block, unsigned from, ScanProduct (&far)[V])
 {
     const int64_t line = (int64_t)a.blocks * 64 * V, at = (int64_t)block * 64 * V + (threadIdx.x & 63);
-    scan_join<V>(a.groups + at, line, max(from / SCAN_GROUP, q / SCAN_RUN * (SCAN_RUN / SCAN_GROUP)), q / SCAN_GROUP, far);
+    scan_join<V>(a.groups + at, line, max(from / SCAN_GROUP, q / SCAN_RUN * (SCAN_RUN / SCAN_GROUP)), q / SCAN_GROUP, {a.looks, a.flags}, far);
 }
 
 template <typename T, bool PACKED, int V>
@@ -406,7 +410,7 @@ __device__ __forceinline__ void scan_handed(const Scan<T, PACKED> &a, unsigned q
     if (from >= run * SCAN_RUN) return;
     const unsigned long long *p = a.handed + (int64_t)(run - 1) * line + (int64_t)block * 64 * V + (threadIdx.x & 63);
 #pragma unroll
-    for (int v = 0; v < V; ++v) x[v] = __uint_as_float((unsigned)scan_wait(p + v * 64, scan_look(p + v * 64)));
+    for (int v = 0; v < V; ++v) x[v] = __uint_as_float((unsigned)scan_wait(p + v * 64, scan_look(p + v * 64), {a.looks, a.flags}));
 }
 
 // The workgroup's column block and tile.  Tickets, those of each column block for themselves, give tiles in the order in which workgroups begin.

@@ -7,6 +7,9 @@
 
 using namespace chicle_train;
 
+// How often a scan's tile looks for what another one tells it before it gives up; less than this only where that is tested.
+extern "C" int32_t chicle_scan_looks = 1 << 22;
+
 namespace {
 
 // Packed rows of d columns: both pointers, rows a multiple of 32 bytes apart.
@@ -165,6 +168,7 @@ int run_scan(Scan<T, PACKED> a, void *workspace, hipStream_t stream)
         a.products = p.products;
         a.groups = p.groups;
         a.handed = p.handed;
+        a.looks = chicle_scan_looks;
         scan_begin<<<(unsigned)std::min<int64_t>(ceil_div(p.words, 256), 2048), 256, 0, stream>>>(p.tickets, a.blocks, p.products, p.words);
         TRY(launched("scan_begin"));
     }

@@ -465,10 +465,12 @@ class TrainOps:
         return self._clip(grads, grads if out is None else out, max_norm)
 
     def sync(self):
-        """Wait for the current stream; raise if a label or token was past the end, or an offset no row, that no sync has raised yet.  What another stream
-        reports meanwhile is raised by this sync or by a later one."""
+        """Wait for the current stream; raise if a label or token was past the end, an offset no row, or a scan gave up waiting for its own tiles, that no sync has
+        raised yet.  What another stream reports meanwhile is raised by this sync or by a later one."""
         taken = self._empty(1, self._torch.int32)
         self._call(self._L.chicle_train_take_flags, self._flags(), taken.data_ptr())
         bits = int(taken.item())
         if bits:
-            raise ChicleError(EDEVICE, "%s out of range" % " and ".join(s for b, s in ((1, "a label"), (2, "a token"), (4, "an offset")) if bits & b))
+            outside = " and ".join(s for b, s in ((1, "a label"), (2, "a token"), (4, "an offset")) if bits & b)
+            raise ChicleError(EDEVICE, "; ".join(([outside + " out of range"] if outside else []) +
+                                                 (["a scan's tiles waited too long for one another"] if bits & 8 else [])))
