@@ -277,17 +277,22 @@ struct ScanProduct {
 __device__ __forceinline__ unsigned long long scan_look(const unsigned long long *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void scan_tell(unsigned long long *p, unsigned long long w) { __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 // (Every wait ends by itself, see below.  Where a workspace is written by something else meanwhile, against its rules, this one ends too, after so many looks,
-// some seconds, with what is no number, and says so.)
-struct ScanPatience { int looks, *flags; };
-__device__ __forceinline__ unsigned long long scan_wait(const unsigned long long *p, unsigned long long w, const ScanPatience &most)
+// some seconds, with what is no number, and says so.)  A: the kernel's arguments, which are read anew where there is a wait: kept for it in scalar registers they
+// cost all rows 2 per cent.
+template <typename A>
+__device__ __forceinline__ unsigned long long scan_wait(const unsigned long long *p, unsigned long long w)
 {
-    bool missing = __any(w == SCAN_NOTHING);
-    for (int left = most.looks; missing && left > 0; --left) {
-        __builtin_amdgcn_s_sleep(1);
-        w = scan_look(p);
-        missing = __any(w == SCAN_NOTHING);
+    if (__any(w == SCAN_NOTHING)) {
+        auto args = (const __attribute__((address_space(4))) A *)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(args));
+        bool missing = true;
+        for (int left = args->looks; missing && left > 0; --left) {
+            __builtin_amdgcn_s_sleep(1);
+            w = scan_look(p);
+            missing = __any(w == SCAN_NOTHING);
+        }
+        if (missing && args->flags) atomicOr(args->flags, FLAG_WAIT);
     }
-    if (missing && most.flags) atomicOr(most.flags, FLAG_WAIT);
     return w;
 }
 
@@ -362,8 +367,8 @@ __device__ __forceinline__ void scan_empty(const ScanOrder &o, unsigned tile, un
 // These tell their products without waiting, groups once the products of the group are told, and states after all that is before them.
 // So every wait ends.  What is joined, and in which order, follows from the offsets alone.  A word is told whole, and says by itself whether it
 // has been.
-template <int V>
-__device__ __forceinline__ void scan_join(const unsigned long long *words, int64_t line, unsigned from, unsigned to, const ScanPatience &most, ScanProduct (&x)[V])
+template <typename A, int V>
+__device__ __forceinline__ void scan_join(const unsigned long long *words, int64_t line, unsigned from, unsigned to, ScanProduct (&x)[V])
 {
     constexpr int AHEAD = SCAN_GROUP - 1;
     for (unsigned i = from; i < to; i += AHEAD) {
@@ -377,7 +382,7 @@ __device__ __forceinline__ void scan_join(const unsigned long long *words, int64
         for (int k = 0; k < AHEAD; ++k)
             if (i + k < to)
 #pragma unroll
-                for (int v = 0; v < V; ++v) x[v] = ScanProduct::from(scan_wait(p + k * line + v * 64, w[k][v], most)).after(x[v]);
+                for (int v = 0; v < V; ++v) x[v] = ScanProduct::from(scan_wait<A>(p + k * line + v * 64, w[k][v])).after(x[v]);
     }
 }
 
@@ -389,7 +394,7 @@ __device__ __forceinline__ void scan_near(const Scan<T, PACKED> &a, unsigned q, 
     const unsigned group = q / SCAN_GROUP;
 #pragma unroll
     for (int v = 0; v < V; ++v) scan_tell(a.products + q * line + at + v * 64, own[v].word());
-    scan_join<V>(a.products + at, line, max(from, group * SCAN_GROUP), q, {a.looks, a.flags}, near);
+    scan_join<Scan<T, PACKED>, V>(a.products + at, line, max(from, group * SCAN_GROUP), q, near);
     if (q % SCAN_GROUP == SCAN_GROUP - 1)
 #pragma unroll
         for (int v = 0; v < V; ++v) scan_tell(a.groups + group * line + at + v * 64, own[v].after(near[v]).word());
@@ -399,7 +404,7 @@ template <typename T, bool PACKED, int V>
 __device__ __forceinline__ void scan_far(const Scan<T, PACKED> &a, unsigned q, unsigned block, unsigned from, ScanProduct (&far)[V])
 {
     const int64_t line = (int64_t)a.blocks * 64 * V, at = (int64_t)block * 64 * V + (threadIdx.x & 63);
-    scan_join<V>(a.groups + at, line, max(from / SCAN_GROUP, q / SCAN_RUN * (SCAN_RUN / SCAN_GROUP)), q / SCAN_GROUP, {a.looks, a.flags}, far);
+    scan_join<Scan<T, PACKED>, V>(a.groups + at, line, max(from / SCAN_GROUP, q / SCAN_RUN * (SCAN_RUN / SCAN_GROUP)), q / SCAN_GROUP, far);
 }
 
 template <typename T, bool PACKED, int V>
@@ -410,7 +415,7 @@ __device__ __forceinline__ void scan_handed(const Scan<T, PACKED> &a, unsigned q
     if (from >= run * SCAN_RUN) return;
     const unsigned long long *p = a.handed + (int64_t)(run - 1) * line + (int64_t)block * 64 * V + (threadIdx.x & 63);
 #pragma unroll
-    for (int v = 0; v < V; ++v) x[v] = __uint_as_float((unsigned)scan_wait(p + v * 64, scan_look(p + v * 64), {a.looks, a.flags}));
+    for (int v = 0; v < V; ++v) x[v] = __uint_as_float((unsigned)scan_wait<Scan<T, PACKED>>(p + v * 64, scan_look(p + v * 64)));
 }
 
 // The workgroup's column block and tile.  Tickets, those of each column block for themselves, give tiles in the order in which workgroups begin.
