@@ -26,7 +26,8 @@ namespace chicle_train {
 constexpr int SCAN_KEPT = 32;
 
 // s with the sign of f.  The exponential of the hardware gives no numbers below 2^-126: there it is that of 64 more, which the quotient brings down by
-// 2^64 (where 1 + e is 1), with its one rounding.
+// 2^64 (where 1 + e is 1), with its one rounding.  (65,536 x 2048 in bfloat16, sequences of 128 rows, forward: 195 us a call, and 191 without the small shares; one
+// sequence and the gradients the same.)
 __device__ __forceinline__ float gate_of(float f)
 {
     const bool small = fabsf(f) > 87.33f;                // (126 ln 2 = 87.337)
@@ -239,12 +240,14 @@ template <typename T, bool PACKED> struct Scan {
     float *last, *dh0;                       // or null
     T *y, *df, *du;
     int64_t ldf, lddy, ldy, lddf, lddu, d;
-    int *flags, looks;                       // looks: before a wait is given up
+    int *flags;
     // what workgroups hand on; null where there is one tile in a column block
     unsigned *tickets;
     unsigned long long *products, *groups, *handed;
     unsigned tiles, blocks;                  // tiles of a column block, column blocks
     bool lines;                              // rows of T that are read are whole lines of the cache
+    int looks;                               // before a wait is given up (the last: with `tickets` eight bytes further on, which a workgroup asks for first,
+                                             // gradients of 30,011 x 1000 in half precision, one sequence, take 92 us instead of 86)
 };
 
 constexpr unsigned long long SCAN_NOTHING = ~0ull;       // what no product is: its lower half is no NaN of these bits
@@ -277,8 +280,8 @@ struct ScanProduct {
 __device__ __forceinline__ unsigned long long scan_look(const unsigned long long *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void scan_tell(unsigned long long *p, unsigned long long w) { __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 // (Every wait ends by itself, see below.  Where a workspace is written by something else meanwhile, against its rules, this one ends too, after so many looks,
-// some seconds, with what is no number, and says so.)  A: the kernel's arguments, which are read anew where there is a wait: kept for it in scalar registers they
-// cost all rows 2 per cent.
+// some seconds, with what is no number, and says so.)  A: the kernel's arguments, of which those for this are read where there is a
+// wait, and not kept in scalar registers all along.
 template <typename A>
 __device__ __forceinline__ unsigned long long scan_wait(const unsigned long long *p, unsigned long long w)
 {
