@@ -72,7 +72,7 @@ int chicle_embed_grad(const void *ids, int32_t wide, const void *dout, int64_t l
                       int32_t accumulate, void *dtable, int64_t ldo, void *workspace, size_t workspace_bytes, int32_t *flags, void *hip_stream);
 
 /* Layer norm over rows of d values: y = (x - mean) rstd gamma + beta, rstd = 1 / sqrt(var + eps); mean and rstd (n floats each) are
- * what the gradient takes.  Limits: n and d below 2^31. */
+ * what the gradient takes.  The sum of (x - mean)^2 is a 32-bit number: values below 2^63 / sqrt(d) have it.  Limits: n and d below 2^31. */
 int chicle_layer_norm(const void *x, int64_t ldx, const void *gamma, const void *beta, int64_t n, int64_t d, int32_t type, float eps,
                       void *y, int64_t ldy, float *mean, float *rstd, void *hip_stream);
 
@@ -92,7 +92,8 @@ int chicle_unpack8(const void *q, const void *scales, int64_t ldq, int64_t n, in
 /* Root-mean-square norm of rows on a residual stream: r = x + residual (residual may be NULL: r = x), rounded to the type;
  * rstd = 1 / sqrt(sum_c r_c^2 / d + eps), y = r rstd gamma.  sum (or NULL) gets r; sum8 (or NULL) gets r as packed rows, ldsum8 bytes apart.  y is of the
  * type where y_scales is NULL, else packed rows, ldy bytes apart, made from the 32-bit values.  rstd: n floats, which the gradient takes.
- * Values may be as large as the type's largest, and, where eps is 0, as small as 2^-126; a row of zeros without eps has no norm (rstd infinite, y NaN).
+ * Values may be as large as the type's largest; where eps is 0, the root of a row's mean square is 2^-127 or more, since rstd is one over it (a row of zeros
+ * has no norm then: rstd infinite, y NaN).
  * Limits: n and d below 2^31. */
 int chicle_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldres, const void *gamma, int64_t n, int64_t d, int32_t type, float eps,
                     void *sum, int64_t ldsum, void *y, int64_t ldy, void *y_scales, void *sum8, void *sum8_scales, int64_t ldsum8, float *rstd,
@@ -121,7 +122,7 @@ int chicle_gated_scan(const void *f, int64_t ldf, const void *u, int64_t ldu, co
                       size_t workspace_bytes, int32_t *flags, void *hip_stream);
 
 /* Its gradients by f, u and, where dh0 is not NULL, h0, from dy and, where it is not NULL, dlast, the gradient of `last`; the other arguments are
- * those of the forward call, and what it left in states.  Rows of no sequence get zeros. */
+ * those of the forward call, and what it left in states.  Rows of no sequence get zeros.  h - u, and its product with h's gradient, are 32-bit numbers. */
 int chicle_gated_scan_grad(const void *f, int64_t ldf, const void *u, int64_t ldu, const void *u_scales, const void *offsets, int32_t wide,
                            int64_t sequences, const float *h0, const float *states, const void *dy, int64_t lddy, const float *dlast, int64_t n, int64_t d,
                            int32_t type, void *df, int64_t lddf, void *du, int64_t lddu, float *dh0, void *workspace, size_t workspace_bytes,

@@ -13,9 +13,9 @@
 // pass leaves the state that enters every SCAN_KEPT-th row; the gradient works out those between again, and goes through the tiles from the last one.
 //
 // What bounds it is memory: every value is read and written once, a large copy goes at 4.95 TB/s.  65,536 rows of 2048 columns in bfloat16, forward
-// and its gradients: sequences of 128 rows 166 and 268 us (5.0 and 5.1 TB/s), one sequence 202 and 302 us (4.1 and 4.5): there tiles wait for what comes
-// into them; rows of 1024 in float32 141 and 240 us (5.8 and 5.6), one sequence 162 and 252 (5.0 and 5.3).  A thread that goes through its column alone takes
-// 29,950 us for 65,536 rows in one sequence.  Small calls are launches: 333 x 250 in float32 11.0 and 13.1 us, of which 4 are a state's way through the three tiles.
+// and its gradients: sequences of 128 rows 176 and 270 us (4.7 and 5.0 TB/s), one sequence 210 and 303 us (3.9 and 4.5): there tiles wait for what comes
+// into them; rows of 1024 in float32 140 and 241 us (5.8 and 5.6), one sequence 159 and 252 (5.1 and 5.4).  A thread that goes through its column alone takes
+// 29,950 us for 65,536 rows in one sequence.  Small calls are launches: 333 x 250 in float32 9.2 and 12.0 us, of which 4 are a state's way through the three tiles.
 #pragma once
 #include <type_traits>
 #include "elements.hpp"

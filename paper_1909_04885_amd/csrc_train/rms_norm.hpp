@@ -9,9 +9,9 @@
 //
 // A row is held in registers by `lanes` neighbouring threads, NV vectors of sixteen bytes each, and read once: NV is two for rows of up to 4096 columns
 // of 16 bits, where a workgroup of 256 threads has one, and short rows share a workgroup.  Rows that no workgroup holds (NV = 0) are read again.
-// The bound is the memory (a large copy: 4.95 TB/s).  Forward, 32,768 x 4096 in bfloat16 with a residual, y and r in 8 bits: 178 us, 6.1 TB/s; one row of
-// 4096: 3.8 us, a launch.  Gradients, 65,536 x 4096 in bfloat16 from r in 8 bits with dr: 330 us, 5.7 TB/s, and 6 for the sums over workgroups;
-// 9001 x 1537 in float32, 1540 apart: 46 and 5, 4.9 TB/s.  Gradients of rows that no workgroup holds read twice: 3000 x 20,000 in bfloat16 410 us, 1.2 TB/s.
+// The bound is the memory (a large copy: 4.95 TB/s).  Forward, 32,768 x 4096 in bfloat16 with a residual, y and r in 8 bits: 181 us, 6.0 TB/s; one row of
+// 4096: 4.0 us, a launch.  Gradients, 65,536 x 4096 in bfloat16 from r in 8 bits with dr: 330 us, 5.7 TB/s, and 6 for the sums over workgroups;
+// 9001 x 1537 in float32, 1540 apart: 46 and 5, 4.9 TB/s.  Gradients of rows that no workgroup holds read twice: 3000 x 20,000 in bfloat16 369 us, 1.3 TB/s.
 #pragma once
 #include "elements.hpp"
 #include "layer_norm.hpp"

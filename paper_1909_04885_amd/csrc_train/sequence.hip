@@ -173,8 +173,9 @@ int run_scan(Scan<T, PACKED> a, void *workspace, hipStream_t stream)
         TRY(launched("scan_begin"));
     }
     const unsigned grid = (unsigned)(p.tiles * p.blocks);
-    // Rows that meet in lines: three workgroups to a compute unit, so that a line is still there when the next column block comes for its part.  Gradients, three /
-    // four, 16 bits: 30,011 x 1000 83 / 90 us, 90,000 x 300 98 / 104, 5000 x 4099 73 / 83; forward, 32 bits: 200,000 x 16 41 / 43.5.
+    // Rows that meet in lines: three workgroups to a compute unit, so that a line is still there when the next column block comes for its part.  Calls of
+    // gradients, three / four, 16 bits: 30,011 x 1000 in sequences of 100 rows 90 / 93 us, in one 87 / 92, 90,000 x 300 in sequences of 300 98 / 106, 5000 x 4099 in
+    // one 77 / 88, 20,000 x 700 in sequences of 50 63 / 60; forward, 32 bits: 200,000 x 16 in one 43 / 46, 30,011 x 1000 in sequences of 100 80 / 75.
     const size_t lds = a.lines ? 0 : S::MORE_LDS;
     if constexpr (BACKWARD) scan_backward<T, PACKED><<<grid, S::THREADS, lds, stream>>>(a);
     else scan_forward<T, PACKED><<<grid, S::THREADS, lds, stream>>>(a);
